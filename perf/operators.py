@@ -1,0 +1,382 @@
+"""The operators of a multi-class head as cases that can be timed: the root-mean-square norm that makes its features (with the residual's
+addition, and an output in 8 bits), the matrix product with bias, activation and residual that makes its logits, and the loss against a
+teacher's top logits that it is trained by, with the gradients and the Hessian-vector product.
+
+`run` computes them with elementary torch operations in 32 bits, or, where `own` is true, with this library's calls on the same
+state.  Inputs are drawn on the GPU from the seed: hidden states with a few large features, weights of variance 1 / k, logits of
+standard deviation 3 whose teacher is the same plus noise; some rows have no weight, some teacher entries are missing."""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "e4m3": torch.float8_e4m3fn}
+BYTES = {"f32": 4, "bf16": 2, "f16": 2, "e4m3": 1}
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+EPS = 1e-6
+E4M3_MAX = 448.0
+
+
+def listed():
+    return [
+        # the features of one token, on their way to a product in 8 bits: the smallest call, where latency counts
+        {"name": "norm_token_e4m3", "op": "norm", "m": 1, "d": 4096, "type": "bf16", "out": "e4m3", "residual": True},
+        # those of a batch of prompts
+        {"name": "norm_prompts_e4m3", "op": "norm", "m": 16384, "d": 8192, "type": "bf16", "out": "e4m3", "residual": True},
+        # the backward pass of the norm in training, an odd width
+        {"name": "norm_grad_odd", "op": "norm_grad", "m": 20011, "d": 2047, "type": "f16", "residual": True},
+        # logits of one token: the weights are read once, nothing else counts
+        {"name": "linear_token", "op": "linear", "m": 1, "n": 32000, "k": 4096, "type": "bf16", "out": "bf16", "act": "none", "bias": True, "residual": False, "pre": False},
+        # a hidden layer of the head in 8 bits over a batch of prompts
+        {"name": "linear_e4m3", "op": "linear", "m": 8192, "n": 8192, "k": 4096, "type": "e4m3", "out": "bf16", "act": "gelu", "bias": True, "residual": False, "pre": False},
+        # a thousand classes on a few hundred rows, every size odd, in training: the values before the activation are kept
+        {"name": "linear_odd", "op": "linear", "m": 777, "n": 1001, "k": 2049, "type": "f16", "out": "f16", "act": "silu", "bias": True, "residual": True, "pre": True},
+        # logits of a training batch over a vocabulary: the largest
+        {"name": "linear_logits", "op": "linear", "m": 8192, "n": 32000, "k": 4096, "type": "bf16", "out": "bf16", "act": "none", "bias": True, "residual": False, "pre": False},
+        # all gradients of a hidden layer
+        {"name": "linear_grad", "op": "linear_grad", "m": 8192, "n": 4096, "k": 4096, "type": "bf16", "act": "gelu", "dw": "bf16"},
+        # loss and gradient of a training batch over a large vocabulary
+        {"name": "distill_step", "op": "distill", "m": 4096, "v": 128000, "top": 64, "type": "bf16", "ids": "i64", "temperature": 2.0, "grad": True},
+        # the loss of a few rows, as an evaluation takes it: one row is split over many compute units
+        {"name": "distill_few", "op": "distill", "m": 13, "v": 32000, "top": 32, "type": "f32", "ids": "i64", "temperature": 1.0, "grad": False},
+        # the gradient alone, from the stored sums of the forward pass; odd sizes
+        {"name": "distill_grad_odd", "op": "distill_grad", "m": 2011, "v": 50021, "top": 20, "type": "f16", "ids": "i32", "temperature": 1.5},
+        # the Hessian-vector product of an inner solve
+        {"name": "distill_hv", "op": "distill_hv", "m": 8192, "v": 32000, "top": 32, "type": "bf16", "ids": "i64", "temperature": 1.0},
+    ]
+
+
+def _log(rng, lo, hi):
+    size = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    return size + 1 if size == 3072 else size
+
+
+def draw(rng):
+    op = rng.choice(["norm", "norm", "norm_grad", "linear", "linear", "linear", "linear_grad", "distill", "distill", "distill_grad", "distill_hv"])
+    if op in ("norm", "norm_grad"):
+        d = _log(rng, 64, 16384)
+        m = _log(rng, 1, min(65536, (16384 * 8192) // d))
+        kind = rng.choice(["bf16", "bf16", "f16", "f32"])
+        case = {"op": op, "m": m, "d": d, "type": kind, "residual": rng.random() < 0.7}
+        return case | ({"out": rng.choice(["e4m3", kind])} if op == "norm" else {})
+    if op in ("linear", "linear_grad"):
+        most = 8192 * 32000 * 4096 // (2 if op == "linear_grad" else 1)
+        while True:
+            m, n, k = _log(rng, 1, 16384), _log(rng, 16, 32768), _log(rng, 32, 8192)
+            if rng.random() < 0.5:  # what programs choose; the others are odd as often as even
+                n, k = max(64, n // 128 * 128), max(64, k // 128 * 128)
+            if 3072 in (n, k):
+                continue
+            if m * n * k <= most and m * n <= 8192 * 32000:
+                break
+        act = rng.choice(["none", "relu", "gelu", "silu"])
+        if op == "linear_grad":
+            return {"op": op, "m": m, "n": n, "k": k, "type": rng.choice(["bf16", "f16"]), "act": act, "dw": "bf16" if act != "none" else rng.choice(["bf16", "f32"])}
+        kind = rng.choice(["bf16", "bf16", "f16", "e4m3"])
+        return {"op": op, "m": m, "n": n, "k": k, "type": kind, "out": rng.choice(["bf16", "f32"]) if kind != "f16" else "f16", "act": act,
+                "bias": rng.random() < 0.7, "residual": rng.random() < 0.4, "pre": rng.random() < 0.3}
+    v = _log(rng, 100, 200_000)
+    case = {"op": op, "m": _log(rng, 1, min(16384, 4096 * 128000 // v)), "v": v, "type": rng.choice(["bf16", "bf16", "f16", "f32"]), "temperature": rng.choice([1.0, 1.0, 2.0, 0.7])}
+    if case["type"] == "f32":
+        case["m"] = max(1, case["m"] // 2)
+    case |= {"top": _log(rng, 1, min(v, 256)), "ids": rng.choice(["i64", "i32"])}
+    return case | ({"grad": rng.random() < 0.6} if op == "distill" else {})
+
+
+def _normal(g, shape, dtype, std=1.0):
+    return torch.empty(shape, dtype=torch.float32, device="cuda").normal_(0.0, std, generator=g).to(dtype)
+
+
+def _hidden(g, m, d, dtype):
+    """Hidden states: about one feature in a hundred is ten times as large as the others."""
+    size = torch.where(torch.rand(d, generator=g, device="cuda") < 0.01, 10.0, 1.0)
+    return (torch.empty((m, d), device="cuda").normal_(generator=g) * size).to(dtype)
+
+
+def _in_8_bits(a):
+    scale = a.abs().amax(1) / E4M3_MAX
+    return (a / scale[:, None]).to(torch.float8_e4m3fn), scale
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(int(seed))
+    op, m, dt = case["op"], case["m"], DTYPES[case["type"]]
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
+    s = {"case": case}
+    if op == "norm":
+        d, out = case["d"], DTYPES[case["out"]]
+        s["x"] = _hidden(g, m, d, dt)
+        s["residual"] = _normal(g, (m, d), dt) if case["residual"] else None
+        s["gain"] = 1.0 + _normal(g, (d,), torch.float32, 0.1)
+        s["y"], s["rstd"] = new(m, d, dtype=out), new(m)
+        s["total"] = new(m, d, dtype=dt) if case["residual"] else None
+        s["scale"] = new(m) if case["out"] == "e4m3" else None
+    elif op == "norm_grad":
+        d = case["d"]
+        s["total"] = _hidden(g, m, d, dt)
+        s["rstd"] = (s["total"].float().square().mean(1) + EPS).rsqrt()
+        s["gain"] = 1.0 + _normal(g, (d,), torch.float32, 0.1)
+        s["dy"] = _normal(g, (m, d), dt)
+        s["dtotal"] = _normal(g, (m, d), dt) if case["residual"] else None
+        s["dx"], s["dgain"] = new(m, d, dtype=dt), new(d)
+    elif op == "linear":
+        n, k, out = case["n"], case["k"], DTYPES[case["out"]]
+        x, w = _hidden(g, m, k, torch.float32), _normal(g, (n, k), torch.float32, k ** -0.5)
+        s["x_scale"] = s["w_scale"] = None
+        if case["type"] == "e4m3":
+            s["x"], s["x_scale"] = _in_8_bits(x)
+            s["w"], s["w_scale"] = _in_8_bits(w)
+        else:
+            s["x"], s["w"] = x.to(dt), w.to(dt)
+        s["bias"] = _normal(g, (n,), torch.float32, 0.1) if case["bias"] else None
+        s["residual"] = _normal(g, (m, n), out) if case["residual"] else None
+        s["y"], s["pre"] = new(m, n, dtype=out), new(m, n, dtype=out) if case["pre"] else None
+    elif op == "linear_grad":
+        n, k = case["n"], case["k"]
+        s["x"], s["w"] = _hidden(g, m, k, dt), _normal(g, (n, k), dt, k ** -0.5)
+        s["dy"], s["pre"] = _normal(g, (m, n), dt), _normal(g, (m, n), dt)
+        s["dx"], s["dw"], s["dbias"] = new(m, k, dtype=dt), new(n, k, dtype=DTYPES[case["dw"]]), new(n)
+    else:
+        v = case["v"]
+        z = torch.empty((m, v), device="cuda").normal_(0.0, 3.0, generator=g)
+        # about one row in eight is a prompt's or padding: it has no weight.  The others' is that of a mean; 16-bit floats of five
+        # bits of exponent scale it up by the number of rows, as programs do that train in them
+        idle = torch.rand(m, generator=g, device="cuda") < 0.125
+        idle[0] = False
+        s["weight"] = torch.where(idle, 0.0, 1.0 if case["type"] == "f16" else 1.0 / m)
+        s["z"] = z.to(dt)
+        if op != "distill":
+            s["lse"] = torch.logsumexp(s["z"].float() / case["temperature"], 1)
+        if op == "distill_hv":
+            s["u"] = _normal(g, (m, v), dt)
+            s["hu"] = new(m, v, dtype=dt)
+        z += torch.empty_like(z).normal_(0.0, 1.0, generator=g)
+        t, ids = z.topk(case["top"], 1)
+        # one list in sixteen is shorter by an entry (a list of one: empty)
+        ids[torch.rand(m, generator=g, device="cuda") < 1 / 16, -1] = -1
+        s["t"], s["ids"] = t, ids if case["ids"] == "i64" else ids.to(torch.int32)
+        if op == "distill":
+            s["loss"], s["lse"] = new(m), new(m)
+        if op == "distill_grad" or case.get("grad"):
+            s["dz"] = new(m, v, dtype=dt)
+        elif op == "distill":
+            s["dz"] = None
+    return s
+
+
+# ------------------------------------------------------------------------------------------ the plain forms
+def _act(a, name):
+    if name == "relu":
+        return a.clamp(min=0.0)
+    if name == "gelu":
+        return 0.5 * a * (1.0 + torch.erf(a * math.sqrt(0.5)))
+    return a / (1.0 + torch.exp(-a)) if name == "silu" else a
+
+
+def _act_slope(a, name):
+    if name == "relu":
+        return (a > 0.0).to(a.dtype)
+    if name == "gelu":
+        return 0.5 * (1.0 + torch.erf(a * math.sqrt(0.5))) + a * torch.exp(-0.5 * a * a) * (1.0 / math.sqrt(2.0 * math.pi))
+    if name == "silu":
+        h = 1.0 / (1.0 + torch.exp(-a))
+        return h * (1.0 + a * (1.0 - h))
+    return torch.ones_like(a)
+
+
+def _teacher(s, v):
+    """Probabilities of the listed entries, their logarithms, and their columns; entries that are missing have probability 0."""
+    there = s["ids"] >= 0
+    t = torch.where(there, s["t"] / s["case"]["temperature"], -math.inf)
+    top = t.amax(1, keepdim=True)
+    top = torch.where(top > -math.inf, top, 0.0)
+    e = torch.exp(t - top)
+    total = e.sum(1, keepdim=True)
+    q = torch.where(total > 0, e / total, 0.0)
+    return q, torch.where(q > 0, t - top - torch.log(total), 0.0), torch.where(there, s["ids"], 0).long()
+
+
+def _row_weight(s):
+    """Rows without weight or without a teacher's entry have neither loss nor gradient."""
+    return torch.where((s["ids"] >= 0).any(1, keepdim=True), s["weight"][:, None], 0.0)
+
+
+def _plain(s):
+    case = s["case"]
+    op = case["op"]
+    f = lambda a: None if a is None else a.float()  # noqa: E731
+    if op == "norm":
+        total = f(s["x"]) if s["residual"] is None else f(s["x"]) + f(s["residual"])
+        rstd = 1.0 / torch.sqrt((total * total).mean(1) + EPS)
+        y = total * rstd[:, None] * s["gain"]
+        out = {"rstd": rstd}
+        if s["total"] is not None:
+            out["total"] = total.to(s["total"].dtype)
+        if s["scale"] is None:
+            return out | {"y": y.to(s["y"].dtype)}
+        top = y.abs().amax(1)
+        scale = torch.where(top > 0, top / E4M3_MAX, 1.0)
+        return out | {"y": (y / scale[:, None]).to(torch.float8_e4m3fn), "scale": scale}
+    if op == "norm_grad":
+        total, dy, rstd = f(s["total"]), f(s["dy"]), s["rstd"][:, None]
+        a = dy * s["gain"]
+        dx = rstd * (a - total * (rstd * rstd * (a * total).mean(1, keepdim=True)))
+        if s["dtotal"] is not None:
+            dx = dx + f(s["dtotal"])
+        return {"dx": dx.to(s["dx"].dtype), "dgain": (dy * total * rstd).sum(0)}
+    if op == "linear":
+        pre = f(s["x"]) @ f(s["w"]).T
+        if s["x_scale"] is not None:
+            pre = pre * s["x_scale"][:, None] * s["w_scale"]
+        if s["bias"] is not None:
+            pre = pre + s["bias"]
+        y = _act(pre, case["act"])
+        if s["residual"] is not None:
+            y = y + f(s["residual"])
+        out = {"y": y.to(s["y"].dtype)}
+        return out if s["pre"] is None else out | {"pre": pre.to(s["pre"].dtype)}
+    if op == "linear_grad":
+        dpre = f(s["dy"]) * _act_slope(f(s["pre"]), case["act"])
+        return {"dx": (dpre @ f(s["w"])).to(s["dx"].dtype), "dw": (dpre.T @ f(s["x"])).to(s["dw"].dtype), "dbias": dpre.sum(0)}
+    temperature, w = case["temperature"], _row_weight(s)
+    z = f(s["z"]) / temperature
+    if op == "distill_hv":
+        p = torch.exp(z - s["lse"][:, None])
+        pu = p * f(s["u"])
+        return {"hu": (w * (pu - p * pu.sum(1, keepdim=True))).to(s["hu"].dtype)}
+    q, log_q, at = _teacher(s, case["v"])
+    out = {}
+    if op == "distill":
+        top = z.amax(1, keepdim=True)
+        lse = top + torch.log(torch.exp(z - top).sum(1, keepdim=True))
+        loss = w * (temperature * temperature) * (q * (log_q - (z.gather(1, at) - lse))).sum(1, keepdim=True)
+        out = {"loss": loss[:, 0], "lse": lse[:, 0]}
+        if s["dz"] is None:
+            return out
+    else:
+        lse = s["lse"][:, None]
+    dz = torch.exp(z - lse).scatter_add_(1, at, -q) * (w * temperature)
+    return out | {"dz": dz.to(s["dz"].dtype)}
+
+
+def _own(s):
+    import paper_2008_03433_amd as tron
+
+    case = s["case"]
+    op = case["op"]
+    if op == "norm":
+        tron.tron_rms_norm(s["x"], s["y"], gain=s["gain"], eps=EPS, residual=s["residual"], total=s["total"], scale=s["scale"], rstd=s["rstd"])
+        return {k: s[k] for k in ("rstd", "total", "y", "scale") if s[k] is not None}
+    if op == "norm_grad":
+        tron.tron_rms_norm_grad(s["total"], s["rstd"], s["dy"], s["dx"], gain=s["gain"], dtotal=s["dtotal"], dgain=s["dgain"])
+        return {"dx": s["dx"], "dgain": s["dgain"]}
+    if op == "linear":
+        tron.tron_linear(s["x"], s["w"], s["y"], bias=s["bias"], act=ACTS[case["act"]], residual=s["residual"], pre=s["pre"], x_scale=s["x_scale"], w_scale=s["w_scale"])
+        return {"y": s["y"]} if s["pre"] is None else {"y": s["y"], "pre": s["pre"]}
+    if op == "linear_grad":
+        tron.tron_linear_grad(s["x"], s["w"], s["dy"], dx=s["dx"], dw=s["dw"], dbias=s["dbias"], act=ACTS[case["act"]], pre=s["pre"])
+        return {"dx": s["dx"], "dw": s["dw"], "dbias": s["dbias"]}
+    if op == "distill_hv":
+        tron.tron_distill_hv(s["z"], s["lse"], s["u"], s["hu"], ids=s["ids"], temperature=case["temperature"], weight=s["weight"])
+        return {"hu": s["hu"]}
+    if op == "distill_grad":
+        tron.tron_distill_grad(s["z"], s["lse"], s["ids"], s["t"], s["dz"], temperature=case["temperature"], weight=s["weight"])
+        return {"dz": s["dz"]}
+    tron.tron_distill(s["z"], s["ids"], s["t"], s["loss"], s["lse"], temperature=case["temperature"], weight=s["weight"], dz=s["dz"])
+    return {k: s[k] for k in ("loss", "lse", "dz") if s[k] is not None}
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+def work(case):
+    op, m, b = case["op"], case["m"], BYTES[case["type"]]
+    if op in ("norm", "norm_grad"):
+        d, extra = case["d"], 2 if case["residual"] else 0
+        if op == "norm":  # x, and the residual and the sum; y, its scales, rstd, gain
+            return {"bytes": m * d * (b * (1 + extra) + BYTES[case["out"]]) + m * (8 if case["out"] == "e4m3" else 4) + 4 * d, "flops": 5 * m * d}
+        return {"bytes": m * d * b * (3 + extra // 2) + 4 * m + 8 * d, "flops": 9 * m * d}
+    if op == "linear":
+        n, k, o = case["n"], case["k"], BYTES[case["out"]]
+        scales = 4 * (m + n) if case["type"] == "e4m3" else 0
+        return {"bytes": b * k * (m + n) + o * m * n * (1 + case["residual"] + case["pre"]) + scales + 4 * n * case["bias"], "flops": 2 * m * n * k}
+    if op == "linear_grad":
+        n, k = case["n"], case["k"]
+        pre = 1 if case["act"] != "none" else 0
+        return {"bytes": b * (2 * m * k + n * k + m * n * (1 + pre)) + BYTES[case["dw"]] * n * k + 4 * n, "flops": 4 * m * n * k}
+    mv = m * case["v"]
+    if op == "distill_hv":
+        return {"bytes": 3 * b * mv + m * case["top"] * (8 if case["ids"] == "i64" else 4) + 8 * m, "flops": 6 * mv}
+    lists = m * case["top"] * (4 + (8 if case["ids"] == "i64" else 4))
+    both = 2 if op == "distill_grad" or case["grad"] else 1
+    return {"bytes": both * b * mv + lists + 12 * m, "flops": (1 + 2 * both) * mv}
+
+
+# ------------------------------------------------------------------------------------------ the definitions in 64 bits
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = case["op"]
+    D = lambda name: s[name].double()  # noqa: E731
+    if op == "norm":
+        a = D("x")
+        if s["residual"] is not None:
+            a += D("residual")
+        r = (a.pow(2).sum(1) / case["d"] + EPS).pow(-0.5)
+        y = a.mul(r.unsqueeze(1)).mul(D("gain"))
+        out = {"rstd": r, "y": y}
+        if s["total"] is not None:
+            out["total"] = a
+        if s["scale"] is not None:
+            largest = torch.linalg.vector_norm(y, math.inf, 1)
+            out["scale"] = largest.div(E4M3_MAX).masked_fill(largest == 0, 1.0)
+            out["y"] = y.div(out["scale"].unsqueeze(1))
+        return out
+    if op == "norm_grad":
+        # through the normalised row h = total rstd: d h_j / d total_l = rstd (delta_jl - h_j h_l / d)
+        h = D("total").mul(D("rstd").unsqueeze(1))
+        a = D("dy").mul(D("gain"))
+        dot = a.mul(h).sum(1, True).div(case["d"])
+        dx = a.sub(h.mul(dot)).mul(D("rstd").unsqueeze(1))
+        return {"dx": dx if s["dtotal"] is None else dx.add(D("dtotal")), "dgain": D("dy").mul(h).sum(0)}
+    if op == "linear":
+        x, w = D("x"), D("w")
+        if s["x_scale"] is not None:
+            x.mul_(D("x_scale").unsqueeze(1)), w.mul_(D("w_scale").unsqueeze(1))
+        a = torch.mm(x, w.t())
+        if s["bias"] is not None:
+            a.add_(D("bias"))
+        y = {"none": lambda v: v, "relu": torch.relu, "gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu}[case["act"]](a)
+        if s["residual"] is not None:
+            y = y.add(D("residual"))
+        return {"y": y} if s["pre"] is None else {"y": y, "pre": a}
+    if op == "linear_grad":
+        a = D("pre").requires_grad_()
+        y = {"none": lambda v: v * 1.0, "relu": torch.relu, "gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu}[case["act"]](a)
+        (da,) = torch.autograd.grad(y, a, D("dy"))
+        return {"dx": torch.mm(da, D("w")), "dw": torch.mm(da.t().contiguous(), D("x")), "dbias": da.sum(0)}
+    T = case["temperature"]
+    listed_ = s["ids"].ge(0)
+    weight = D("weight").mul(listed_.any(1))
+    if op == "distill_hv":
+        p = D("z").div_(T).sub_(D("lse").unsqueeze(1)).exp_()
+        u = D("u")
+        return {"hu": u.sub_(p.mul(u).sum(1, True)).mul_(p).mul_(weight.unsqueeze(1))}
+    t = D("t").div(T).masked_fill(listed_.logical_not(), -math.inf)
+    log_q = torch.log_softmax(t, 1).nan_to_num(nan=-math.inf, neginf=-math.inf)
+    q = log_q.exp()
+    z = D("z").div_(T)
+    at = s["ids"].long().clamp(min=0)
+    out = {}
+    if op == "distill":
+        lse = torch.logsumexp(z, 1)
+        cross = q.mul(log_q.masked_fill(q == 0, 0.0).sub(z.gather(1, at)).add(lse.unsqueeze(1))).sum(1)
+        out = {"loss": cross.mul(weight).mul(T * T), "lse": lse}
+        if s["dz"] is None:
+            return out
+    else:
+        lse = D("lse")
+    p = z.sub_(lse.unsqueeze(1)).exp_()
+    p.scatter_add_(1, at, q.neg())
+    return out | {"dz": p.mul_(weight.mul(T).unsqueeze(1))}
