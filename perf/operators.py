@@ -278,7 +278,7 @@ def _own(s):
         tron.tron_linear_grad(s["x"], s["w"], s["dy"], dx=s["dx"], dw=s["dw"], dbias=s["dbias"], act=ACTS[case["act"]], pre=s["pre"])
         return {"dx": s["dx"], "dw": s["dw"], "dbias": s["dbias"]}
     if op == "distill_hv":
-        tron.tron_distill_hv(s["z"], s["lse"], s["u"], s["hu"], ids=s["ids"], temperature=case["temperature"], weight=s["weight"])
+        tron.tron_distill_hv(s["z"], s["lse"], s["u"], s["hu"], ids=s["ids"], t=s["t"], temperature=case["temperature"], weight=s["weight"])
         return {"hu": s["hu"]}
     if op == "distill_grad":
         tron.tron_distill_grad(s["z"], s["lse"], s["ids"], s["t"], s["dz"], temperature=case["temperature"], weight=s["weight"])
