@@ -393,6 +393,112 @@ TRON_API int tron_tuning_set(const char *name, int64_t value);
 TRON_API int tron_probe_copy_bandwidth(double *dst_dev, const double *src_dev, int64_t count, int reps,
                                        void *hip_stream, double *ms_per_launch);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of a multi-class softmax head: the norm that makes its features, the matrix product that makes its
+ * logits, and the loss against a teacher's top logits that it is trained by, with gradients and the
+ * Hessian-vector product.  For many classes, and features that a network made, they are what z = X w, zhat and D
+ * are for two.
+ *
+ * They have no handle: every array is a caller's device pointer on the current device, row-major, with a leading
+ * dimension in elements, and every call enqueues on `hip_stream` and returns (nothing synchronises or allocates, so
+ * calls may be captured into a graph).  Arrays need the alignment of their elements only; operands whose base is at a
+ * multiple of 16 bytes and whose rows are too are read faster.  Leading dimensions of arrays that are read may be
+ * anything from 0 on (0: one row for all; its gradient is the sum of the rows'); rows that are written may not
+ * overlap.  m = 0 is allowed: nothing is written but sums over rows, which are 0.  Where a call needs a work space,
+ * tron_..._work says its bytes; it lies at a multiple of 16, its contents are undefined before and after, and calls on
+ * different streams need different ones.  Outputs may not overlap inputs except where it is said.
+ * Sums, softmax statistics and activations are held in 32 bits or more; results are rounded once to the output's type, to nearest, ties to
+ * even.  No atomics: the same call gives the same bits.
+ * ------------------------------------------------------------------------------------------ */
+enum {
+    TRON_TYPE_F32 = 0,
+    TRON_TYPE_BF16 = 1,
+    TRON_TYPE_F16 = 2,
+    TRON_TYPE_E4M3 = 3 /* 8 bits: 4 of exponent, 3 of fraction, largest value 448, no infinities; held with a scale per row */
+};
+enum { TRON_ACT_NONE = 0, TRON_ACT_RELU = 1, TRON_ACT_GELU = 2 /* a/2 (1 + erf(a / sqrt 2)) */, TRON_ACT_SILU = 3 /* a / (1 + exp(-a)) */ };
+
+/*
+ * Root-mean-square norm with the residual's addition, rows of d elements:
+ *   s = x + residual;  rstd = (mean_j s_j^2 + eps)^-1/2;  y = s rstd gain.
+ * x, residual (or NULL), total (or NULL: s, rounded) are of `type` (f32, bf16, f16); gain: d floats, or NULL for 1.
+ * y is of `type`, or e4m3: then scale[i] = max_j |y_ij| / 448 (1 for a row of zeros) and what is stored is y / scale.
+ * rstd: m floats or NULL.  total may be x or residual (same leading dimension).
+ */
+TRON_API int tron_rms_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                           const float *gain, double eps, void *total, int64_t ldt, int out_type, void *y, int64_t ldy,
+                           float *scale, float *rstd, void *hip_stream);
+
+/*
+ * Its gradient: with a = dy gain,
+ *   dx = rstd (a - s rstd^2 mean_j(a_j s_j)) + dtotal   (the gradient of x and of the residual alike);
+ *   dgain_j = sum_i dy_ij s_ij rstd_i.
+ * `total`: the s of the forward call; dtotal (or NULL): the gradient that reaches s by another way; dgain: d floats or NULL.  An output in 8
+ * bits has the gradient of the values before rounding.  dx may be dy or dtotal (same leading dimension).  The work
+ * space is needed for dgain only.
+ */
+TRON_API int64_t tron_rms_norm_grad_work(int64_t m, int64_t d);
+TRON_API int tron_rms_norm_grad(int64_t m, int64_t d, int type, const void *total, int64_t lds, const float *rstd,
+                                const float *gain, const void *dy, int64_t lddy, const void *dtotal, int64_t lddt, void *dx,
+                                int64_t lddx, float *dgain, void *work, int64_t work_bytes, void *hip_stream);
+
+/*
+ * Matrix product with bias, activation and residual:
+ *   pre_ij = x_scale_i w_scale_j sum_l x_il w_jl + bias_j;   y = act(pre) + residual.
+ * x: m x k and w: n x k of `type`: bf16, f16, or e4m3 with m and n scales (no scales otherwise).  bias: n floats or NULL.  y,
+ * residual (or NULL) and pre (or NULL) are m x n of `out_type` (f32, bf16, f16).  y may be residual (same leading dimension).
+ */
+TRON_API int64_t tron_linear_work(int64_t m, int64_t n, int64_t k, int type);
+TRON_API int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const float *x_scale,
+                         const void *w, int64_t ldw, const float *w_scale, const float *bias, int act, const void *residual,
+                         int64_t ldr, int out_type, void *y, int64_t ldy, void *pre, int64_t ldpre, void *work,
+                         int64_t work_bytes, void *hip_stream);
+
+/*
+ * Its gradients, for operands of 16 bits: with dpre = dy act'(pre) (the slope of relu at 0 is 0),
+ *   dx = dpre w  (m x k, of `type`);   dw = dpre' x  (n x k, of dw_type);   dbias_j = sum_i dpre_ij  (n floats).
+ * Each may be NULL; the residual's gradient is dy.  With an activation the products take dpre rounded to `type`, as their operands
+ * are; dbias sums it unrounded.
+ */
+TRON_API int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias);
+TRON_API int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const void *w,
+                              int64_t ldw, const void *dy, int64_t lddy, int act, const void *pre, int64_t ldpre, void *dx,
+                              int64_t lddx, int dw_type, void *dw, int64_t lddw, float *dbias, void *work, int64_t work_bytes,
+                              void *hip_stream);
+
+/*
+ * Loss of a softmax head against a teacher that gives K <= 1024 entries a row.  Row i, with T = temperature (2^-20 .. 2^20):
+ *   q = softmax(t / T) over the entries that are there;  p = softmax(z / T) over all V columns;
+ *   loss_i = weight_i T^2 sum_j q_j (log q_j - log p_j)       (z of `type`: f32, bf16, f16; t: m x K floats)
+ *   lse_i  = log sum_j exp(z_ij / T)                          (or NULL)
+ *   dz     = weight T (p - q)                                 (of `type`, or NULL; may be z: same leading dimension)
+ * ids: m x K columns as int32 or int64 (id_bytes 4 or 8).  An id outside [0, V) is an entry that is missing, whatever its t; a
+ * column that is listed twice has both masses.  weight: m floats, or NULL for 1.  A row of weight 0, or without an
+ * entry of t > -inf, has loss 0 and gradient 0, whatever its z holds.  In the others -inf is a probability of 0 (and a loss of
+ * +inf where the teacher has mass; a row of nothing but -inf has p = 0), and NaN or +inf makes the row NaN; a NaN among the listed t makes the loss
+ * and the listed columns NaN.  With K = 1 it is
+ * the cross entropy of a label.  V < 2^31 - 64.
+ */
+TRON_API int64_t tron_distill_work(int64_t m, int64_t V);
+TRON_API int tron_distill(int64_t m, int64_t V, int type, const void *z, int64_t ldz, int64_t K, const void *ids,
+                          int id_bytes, int64_t ldi, const float *t, int64_t ldt, double temperature, const float *weight,
+                          float *loss, float *lse, void *dz, int64_t lddz, void *work, int64_t work_bytes, void *hip_stream);
+
+/* The gradient alone, from the lse of the forward call.  dz may be z (same leading dimension). */
+TRON_API int tron_distill_grad(int64_t m, int64_t V, int type, const void *z, int64_t ldz, const float *lse, int64_t K,
+                               const void *ids, int id_bytes, int64_t ldi, const float *t, int64_t ldt, double temperature,
+                               const float *weight, void *dz, int64_t lddz, void *hip_stream);
+
+/*
+ * The Hessian of the losses' sum with respect to z, times u (of `type`): hu = weight (p u - p (p.u)), p from z and lse.
+ * ids and t: as in the forward call, whose rows without an entry are 0 here too.  K = -1: no lists, every row counts.
+ * hu may be u (same leading dimension).  Work space: tron_distill_work.
+ */
+TRON_API int tron_distill_hv(int64_t m, int64_t V, int type, const void *z, int64_t ldz, const float *lse, const void *u,
+                             int64_t ldu, int64_t K, const void *ids, int id_bytes, int64_t ldi, const float *t, int64_t ldt,
+                             double temperature, const float *weight, void *hu, int64_t ldhu, void *work, int64_t work_bytes,
+                             void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,3 +14,7 @@ from .binding import (  # noqa: F401
     tron_probe_copy_bandwidth, tron_tuning_set, Batch, BATCH_MAX, BATCH_MAX_D, tron_batch_create, tron_batch_destroy,
     tron_batch_fun_grad, tron_batch_hv, tron_batch_solve,
 )
+from .heads import (  # noqa: F401
+    ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, SoftmaxHead, tron_rms_norm, tron_rms_norm_grad, tron_rms_norm_grad_work, tron_linear,
+    tron_linear_work, tron_linear_grad, tron_linear_grad_work, tron_distill, tron_distill_work, tron_distill_grad, tron_distill_hv,
+)

@@ -101,6 +101,18 @@ _SIGNATURES = {
     "tron_probe_read_bandwidth": (_int, [_vp, _i64, _int, _vp, ctypes.POINTER(_dbl), ctypes.POINTER(_dbl)]),
     "tron_tuning_set": (_int, [ctypes.c_char_p, _i64]),
     "tron_probe_copy_bandwidth": (_int, [_vp, _vp, _i64, _int, _vp, ctypes.POINTER(_dbl)]),
+    # operators of a multi-class head (heads.py)
+    "tron_rms_norm": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _dbl, _vp, _i64, _int, _vp, _i64, _vp, _vp, _vp]),
+    "tron_rms_norm_grad_work": (_i64, [_i64, _i64]),
+    "tron_rms_norm_grad": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "tron_linear_work": (_i64, [_i64, _i64, _i64, _int]),
+    "tron_linear": (_int, [_i64, _i64, _i64, _int, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _int, _vp, _i64, _int, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "tron_linear_grad_work": (_i64, [_i64, _i64, _i64, _int, _int, _int, _int]),
+    "tron_linear_grad": (_int, [_i64, _i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "tron_distill_work": (_i64, [_i64, _i64]),
+    "tron_distill": (_int, [_i64, _i64, _int, _vp, _i64, _i64, _vp, _int, _i64, _vp, _i64, _dbl, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "tron_distill_grad": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _int, _i64, _vp, _i64, _dbl, _vp, _vp, _i64, _vp]),
+    "tron_distill_hv": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _int, _i64, _vp, _i64, _dbl, _vp, _vp, _i64, _vp, _i64, _vp]),
 }
 
 _lib = None

@@ -81,7 +81,7 @@ void Profiler::destroy()
 }
 
 // ------------------------------------------------------------------ helpers
-static int check_device()
+int check_device()
 {
     int count = 0;
     hipError_t e = hipGetDeviceCount(&count);

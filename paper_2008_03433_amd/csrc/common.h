@@ -15,6 +15,7 @@ namespace tron {
 // ---------------------------------------------------------------- errors
 void set_error(const char *fmt, ...) __attribute__((format(printf, 1, 2)));
 int hip_fail(hipError_t e, const char *what, const char *file, int line);
+int check_device();   // TRON_EDEVICE where there is no usable device
 
 #define TRON_HIP(expr)                                                        \
     do {                                                                      \

@@ -1,0 +1,750 @@
+// Matrix product with bias, activation and residual in its epilogue, and its gradients.
+//
+//   y = act(x w' (x_scale_i w_scale_j) + b) + r;    dpre = dy act'(pre),  dx = dpre w,  dw = dpre' x,  db = sum_i dpre_i
+//
+// Both operands of a product lie with the inner index k contiguous.  A step of the inner loop takes 128 bytes of every row: 64
+// elements of 16 bits, or 128 of 8.  In LDS the sixteen-byte chunks of a row are exchanged among themselves by the row's number, so that
+// sixteen rows of one column of chunks lie in different banks, and a chunk is what a lane of a matrix instruction takes: the
+// order of k among chunks is the same for both operands and does not matter to the sum.
+//
+// Which kernel runs is a rule on the sizes (see linear_plan): tiles of 256 x 256 or 128 x 128 of the result for many rows, a kernel
+// that reads w once, straight into registers, for few rows; the inner index is cut where there are fewer tiles than
+// compute units, and the parts are added in a fixed order.
+#include "head_util.h"
+
+namespace tron {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------ operand types
+template <typename T>
+constexpr int kStepElems = 128 / (int)sizeof(T);   // elements of a row that a step takes
+template <typename T>
+constexpr int kChunkElems = 16 / (int)sizeof(T);
+
+// What a lane has of a chunk, as operands of matrix instructions.  e4m3 is made bf16 on the way, which holds each of its values: the
+// matrix instructions for 8 bits keep 13 bits below the largest product of a step (a product 2^14 times smaller than another adds
+// nothing), those for 16 bits sum in 32.
+template <typename T>
+struct Fragment {
+    static constexpr int kCount = 1;
+    i32x4 v[1];
+};
+template <>
+struct Fragment<e4m3> {
+    static constexpr int kCount = 2;
+    i32x4 v[2];
+};
+
+template <typename T>
+__device__ __forceinline__ Fragment<T> fragment(i32x4 chunk)
+{
+    Fragment<T> f;
+    if constexpr (sizeof(T) == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f.v[i / 2][i % 2 * 2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(chunk[i], 1.f, false));
+            f.v[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(chunk[i], 1.f, true));
+        }
+    } else {
+        f.v[0] = chunk;
+    }
+    return f;
+}
+
+template <typename T>
+__device__ __forceinline__ f32x4 mma(const Fragment<T> &a, const Fragment<T> &b, f32x4 c)
+{
+#pragma unroll
+    for (int i = 0; i < Fragment<T>::kCount; ++i) {
+        if constexpr (sizeof(T) == 2 && !__is_same(T, __bf16))
+            c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.v[i]), __builtin_bit_cast(f16x8, b.v[i]), c, 0, 0, 0);
+        else
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v[i]), __builtin_bit_cast(bf16x8, b.v[i]), c, 0, 0, 0);
+    }
+    return c;
+}
+
+// ------------------------------------------------------------------ epilogue
+struct Epilogue {
+    const float *x_scale, *w_scale, *bias;
+    const void *residual;
+    void *y, *pre;
+    int64_t m, n, ldr, ldy, ldpre;
+    int act, out;
+    float *part;   // [parts][m][n]: sums of a part of the inner index instead
+};
+
+__device__ __forceinline__ float act_of(float a, int act)
+{
+    switch (act) {
+    case TRON_ACT_RELU: return a > 0.f || a != a ? a : 0.f;
+    case TRON_ACT_GELU: return 0.5f * a * (1.f + erff(a * 0.70710678f));
+    case TRON_ACT_SILU: return a / (1.f + __expf(-a));
+    default: return a;
+    }
+}
+
+__device__ __forceinline__ float act_slope(float a, int act)
+{
+    switch (act) {
+    case TRON_ACT_RELU: return a > 0.f || a != a ? 1.f : 0.f;
+    case TRON_ACT_GELU: return 0.5f * (1.f + erff(a * 0.70710678f)) + a * 0.39894228f * __expf(-0.5f * a * a);
+    case TRON_ACT_SILU: {
+        const float h = 1.f / (1.f + __expf(-a));
+        return h * (1.f + a * (1.f - h));
+    }
+    default: return 1.f;
+    }
+}
+
+template <typename O>
+__device__ __forceinline__ void load_as(float *v, const void *base, int64_t at, int64_t n)
+{
+    const O *p = static_cast<const O *>(base) + at;
+    const Raw8<O> r = n >= kVec ? load8(p) : load_first(p, (int)n, static_cast<O>(0.f));
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = static_cast<float>(r.v[i]);
+}
+
+__device__ __forceinline__ void load_out(float *v, const void *base, int out, int64_t at, int64_t n)
+{
+    if (out == TRON_TYPE_F32) load_as<float>(v, base, at, n);
+    else if (out == TRON_TYPE_BF16) load_as<__bf16>(v, base, at, n);
+    else load_as<_Float16>(v, base, at, n);
+}
+
+__device__ __forceinline__ void store_out(void *base, int out, int64_t at, const float *v, int64_t n)
+{
+    if (out == TRON_TYPE_F32) store8_of<float>(static_cast<float *>(base) + at, v, n);
+    else if (out == TRON_TYPE_BF16) store8_of<__bf16>(static_cast<__bf16 *>(base) + at, v, n);
+    else store8_of<_Float16>(static_cast<_Float16 *>(base) + at, v, n);
+}
+
+// eight neighbouring sums of a row
+__device__ __forceinline__ void finish8(const Epilogue &E, float *v, int64_t i, int64_t j)
+{
+    const int64_t n = E.n - j;
+    float f[kVec];
+    if (E.x_scale) {
+        const float xs = E.x_scale[i];
+        load_as<float>(f, E.w_scale, j, n);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] *= xs * f[e];
+    }
+    if (E.bias) {
+        load_as<float>(f, E.bias, j, n);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] += f[e];
+    }
+    if (E.pre) store_out(E.pre, E.out, i * E.ldpre + j, v, n);
+    if (E.act != TRON_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = act_of(v[e], E.act);
+    }
+    if (E.residual) {
+        load_out(f, E.residual, E.out, i * E.ldr + j, n);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] += f[e];
+    }
+    store_out(E.y, E.out, i * E.ldy + j, v, n);
+}
+
+__device__ __forceinline__ void put8(const Epilogue &E, float *v, int64_t i, int64_t j, int part)
+{
+    if (E.part) store8_of<float>(E.part + ((int64_t)part * E.m + i) * E.n + j, v, E.n - j);
+    else finish8(E, v, i, j);
+}
+
+// behind a product whose inner index was cut, or is empty: eight sums a thread
+__global__ __launch_bounds__(kBlock) void k_linear_join(Epilogue E, int parts)
+{
+    const int64_t per_row = (E.n + kVec - 1) / kVec, at = block_number() * kBlock + threadIdx.x;
+    if (at >= per_row * E.m) return;
+    const int64_t i = at / per_row, j = at % per_row * kVec;
+    float v[kVec], f[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = 0.f;
+    for (int p = 0; p < parts; ++p) {
+        load_as<float>(f, E.part, ((int64_t)p * E.m + i) * E.n + j, E.n - j);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] += f[e];
+    }
+    finish8(E, v, i, j);
+}
+
+// ------------------------------------------------------------------ tiles
+struct Operand {
+    const void *p;
+    int64_t rows, ld;   // in elements
+};
+
+struct ProductArgs {
+    Operand x, w;
+    int64_t k;          // inner length
+    int64_t k_part;     // of a part; a multiple of a step
+    int64_t tiles_m, tiles_n;
+    Epilogue E;
+};
+
+// a chunk's place in LDS: rows of 128 bytes
+__device__ __forceinline__ int chunk_place(int row, int chunk) { return row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4); }
+
+// Sixteen bytes of a row from element k on; elements from `end` on are zeros.
+template <typename T>
+__device__ __forceinline__ i32x4 load_chunk(const T *row, int64_t k, int64_t end)
+{
+    i32x4 v = {0, 0, 0, 0};
+    if (k + kChunkElems<T> <= end) {
+        __builtin_memcpy(&v, row + k, 16);
+    } else if (k < end) {
+        T some[kChunkElems<T>];
+#pragma unroll
+        for (int i = 0; i < kChunkElems<T>; ++i) {
+            if (k + i < end) some[i] = row[k + i];
+            else __builtin_memset(&some[i], 0, sizeof(T));
+        }
+        __builtin_memcpy(&v, some, 16);
+    }
+    return v;
+}
+
+// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn; each XCD gets a contiguous range of tiles, walked in groups
+// of eight tiles of m, so that what its L2 holds is used by the tiles that run there together.
+__device__ __forceinline__ void tile_of(const ProductArgs &A, int64_t block, int64_t &tm, int64_t &tn)
+{
+    const int64_t count = A.tiles_m * A.tiles_n, xcd = block % 8, each = count / 8, more = count % 8;
+    const int64_t t = xcd * each + (xcd < more ? xcd : more) + block / 8;
+    constexpr int64_t kGroup = 8;
+    const int64_t group = t / (kGroup * A.tiles_n), first = group * kGroup, high = A.tiles_m - first < kGroup ? A.tiles_m - first : kGroup;
+    const int64_t in = t - group * kGroup * A.tiles_n;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+template <int BM, int BN>
+constexpr int kTileLds = 2 * (BM + BN) * 128 > 128 * (BN + 4) * 4 ? 2 * (BM + BN) * 128 : 128 * (BN + 4) * 4;
+
+// A tile of BM x BN, WM x WN wavefronts.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
+{
+    constexpr int kThreads = WM * WN * kWave, FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int kChunks = (BM + BN) * 8 / kThreads;   // that a thread moves in a step
+    constexpr int kRowsAtOnce = kThreads / 8;
+    extern __shared__ __align__(16) char lds[];
+    const int64_t count = A.tiles_m * A.tiles_n;
+    if (block_number() >= count) return;
+    int64_t tm, tn;
+    tile_of(A, block_number(), tm, tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN;
+    const int part = blockIdx.z;
+    const int64_t k_from = part * A.k_part, k_to = k_from + A.k_part < A.k ? k_from + A.k_part : A.k;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, wm = wave / WN, wn = wave % WN;
+
+    // rows of x first, rows of w behind them; rows past the end repeat the last one, and their results are not stored
+    const T *rows[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        const int r = c * kRowsAtOnce + threadIdx.x / 8;
+        if (r < BM) {
+            const int64_t i = m0 + r < A.x.rows ? m0 + r : A.x.rows - 1;
+            rows[c] = static_cast<const T *>(A.x.p) + i * A.x.ld;
+        } else {
+            const int64_t i = n0 + r - BM < A.w.rows ? n0 + r - BM : A.w.rows - 1;
+            rows[c] = static_cast<const T *>(A.w.p) + i * A.w.ld;
+        }
+    }
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    i32x4 next[kChunks];
+    auto fetch = [&](int64_t k) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) next[c] = load_chunk(rows[c], k + (threadIdx.x % 8) * kChunkElems<T>, k_to);
+    };
+    auto put = [&] {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+            *reinterpret_cast<i32x4 *>(lds + chunk_place(c * kRowsAtOnce + threadIdx.x / 8, threadIdx.x % 8)) = next[c];
+    };
+    fetch(k_from);
+    put();
+    __syncthreads();
+    for (int64_t k = k_from; k < k_to; k += kStepElems<T>) {
+        const bool more = k + kStepElems<T> < k_to;
+        if (more) fetch(k + kStepElems<T>);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Fragment<T> a[FM], b[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+                a[i] = fragment<T>(*reinterpret_cast<const i32x4 *>(lds + chunk_place(wm * FM * 16 + i * 16 + lane % 16, lane / 16 + 4 * h)));
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                b[j] = fragment<T>(*reinterpret_cast<const i32x4 *>(lds + chunk_place(BM + wn * FN * 16 + j * 16 + lane % 16, lane / 16 + 4 * h)));
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = mma<T>(b[j], a[i], acc[i][j]);
+        }
+        __syncthreads();
+        if (more) {
+            put();
+            __syncthreads();
+        }
+    }
+    // Lane l holds row l % 16 and columns l / 16 * 4 .. + 3 of a 16 x 16 piece.  Through LDS, 128 rows at a time, to stores of whole lines.
+    constexpr int kRows = BM < 128 ? BM : 128, kPitch = BN + 4;
+    float *out = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int half = 0; half < BM / kRows; ++half) {
+        if (half) __syncthreads();
+        constexpr int kWaveTall = FM * 16;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int r = wm * kWaveTall + i * 16 + lane % 16 - half * kRows;
+            if (r >= 0 && r < kRows) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + j * 16 + lane / 16 * 4) = acc[i][j];
+            }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int at = threadIdx.x; at < kRows * BN / kVec; at += kThreads) {
+            const int r = at / (BN / kVec), c = at % (BN / kVec) * kVec;
+            const int64_t i = m0 + half * kRows + r, j = n0 + c;
+            if (i >= A.E.m || j >= A.E.n) continue;
+            float v[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] = out[r * kPitch + c + e];
+            put8(A.E, v, i, j, part);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ few rows
+constexpr int kFewWaves = 4;
+
+// Up to 16 MT rows of x, 16 NT rows of w a workgroup.  Its wavefronts take the inner index in turns of two steps of 128 bytes; a lane
+// loads the chunks of its row straight into the registers of the matrix instruction, each row of w once.
+template <typename T, int MT, int NT>
+__global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
+{
+    __shared__ float room[kFewWaves][MT * 16][NT * 16 + 4];
+    const int64_t tn = block_number();
+    if (tn >= A.tiles_n) return;
+    const int part = blockIdx.z;
+    const int64_t n0 = tn * NT * 16, k_from = part * A.k_part, k_to = k_from + A.k_part < A.k ? k_from + A.k_part : A.k;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const T *x[MT], *w[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x[i] = static_cast<const T *>(A.x.p) + (i * 16 + lane % 16 < A.x.rows ? i * 16 + lane % 16 : 0) * A.x.ld;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int64_t r = n0 + j * 16 + lane % 16;
+        w[j] = static_cast<const T *>(A.w.p) + (r < A.w.rows ? r : A.w.rows - 1) * A.w.ld;
+    }
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int kSteps = 2;
+    constexpr int64_t kTurn = kSteps * kStepElems<T>;
+    for (int64_t k = k_from + wave * kTurn; k < k_to; k += kFewWaves * kTurn) {
+        i32x4 a[MT][kSteps][2], b[NT][kSteps][2];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t at = k + s * kStepElems<T> + (lane / 16 + 4 * h) * kChunkElems<T>;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[j][s][h] = load_chunk(w[j], at, k_to);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    a[i][s][h] = i32x4{0, 0, 0, 0};
+                    if (i * 16 + lane % 16 < A.x.rows) a[i][s][h] = load_chunk(x[i], at, k_to);
+                }
+            }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                Fragment<T> f[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) f[i] = fragment<T>(a[i][s][h]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const Fragment<T> g = fragment<T>(b[j][s][h]);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) acc[i][j] = mma<T>(g, f[i], acc[i][j]);
+                }
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&room[wave][i * 16 + lane % 16][j * 16 + lane / 16 * 4]) = acc[i][j];
+    __syncthreads();
+    for (int at = threadIdx.x; at < MT * 16 * NT * 2; at += kFewWaves * kWave) {
+        const int r = at / (NT * 2), c = at % (NT * 2) * kVec;
+        if (r >= A.E.m || n0 + c >= A.E.n) continue;
+        float v[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            v[e] = room[0][r][c + e];
+            for (int u = 1; u < kFewWaves; ++u) v[e] += room[u][r][c + e];
+        }
+        put8(A.E, v, r, n0 + c, part);
+    }
+}
+
+// ------------------------------------------------------------------ which kernel
+enum Shape { SHAPE_FEW = 0, SHAPE_128, SHAPE_256 };
+struct Plan {
+    Shape shape;
+    int64_t tiles_m, tiles_n;
+    int parts;
+    int64_t k_part;
+};
+
+constexpr int64_t kFewRows = 64;
+constexpr int64_t kUnits = 256;   // compute units
+
+Plan linear_plan(int64_t m, int64_t n, int64_t k, int type)
+{
+    Plan P;
+    const int64_t step = 128 / type_bytes(type), steps = std::max<int64_t>(1, ceil_div(k, step));
+    int64_t most;
+    if (m <= kFewRows) {
+        P.shape = SHAPE_FEW;
+        P.tiles_m = 1;
+        P.tiles_n = ceil_div(n, 64);
+        most = std::min<int64_t>(steps / (2 * kFewWaves), 2 * kUnits / P.tiles_n);
+    } else {
+        const int64_t large = ceil_div(m, 256) * ceil_div(n, 256);
+        P.shape = large >= kUnits ? SHAPE_256 : SHAPE_128;
+        const int64_t b = P.shape == SHAPE_256 ? 256 : 128;
+        P.tiles_m = ceil_div(m, b);
+        P.tiles_n = ceil_div(n, b);
+        most = std::min<int64_t>(steps / 8, 2 * kUnits / (P.tiles_m * P.tiles_n));
+    }
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(most, 64));
+    P.k_part = ceil_div(steps, parts) * step;
+    P.parts = (int)ceil_div(steps * step, P.k_part);
+    return P;
+}
+
+int64_t plan_bytes(const Plan &P, int64_t m, int64_t n) { return P.parts > 1 ? ceil_div(P.parts * m * n * 4, 16) * 16 : 0; }
+
+template <typename K>
+int allow_lds(K kernel, int bytes)
+{
+    TRON_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    return TRON_OK;
+}
+
+template <typename T, int MT>
+void launch_few(const ProductArgs &A, dim3 grid, hipStream_t st)
+{
+    k_linear_few<T, MT, 4><<<grid, kFewWaves * kWave, 0, st>>>(A);
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+int launch_tile(const ProductArgs &A, dim3 grid, hipStream_t st)
+{
+    TRON_TRY(allow_lds(k_linear_tile<T, BM, BN, WM, WN>, kTileLds<BM, BN>));
+    k_linear_tile<T, BM, BN, WM, WN><<<grid, WM * WN * kWave, kTileLds<BM, BN>, st>>>(A);
+    return TRON_OK;
+}
+
+template <typename T>
+int product(Operand x, Operand w, int64_t k, const Plan &P, Epilogue E, float *part, hipStream_t st)
+{
+    E.part = P.parts > 1 ? part : nullptr;
+    const ProductArgs A{x, w, k, P.k_part, P.tiles_m, P.tiles_n, E};
+    dim3 grid = block_grid(P.tiles_m * P.tiles_n);
+    grid.z = (unsigned)P.parts;
+    if (P.shape == SHAPE_FEW) {
+        if (x.rows <= 16) launch_few<T, 1>(A, grid, st);
+        else if (x.rows <= 32) launch_few<T, 2>(A, grid, st);
+        else launch_few<T, 4>(A, grid, st);
+    } else if (P.shape == SHAPE_128) {
+        TRON_TRY((launch_tile<T, 128, 128, 2, 2>(A, grid, st)));
+    } else {
+        TRON_TRY((launch_tile<T, 256, 256, 2, 4>(A, grid, st)));
+    }
+    TRON_HIP(hipGetLastError());
+    if (P.parts > 1) {
+        k_linear_join<<<block_grid(ceil_div(ceil_div(E.n, kVec) * E.m, kBlock)), kBlock, 0, st>>>(A.E, P.parts);
+        TRON_HIP(hipGetLastError());
+    }
+    return TRON_OK;
+}
+
+// ------------------------------------------------------------------ gradients
+constexpr int kPatch = 64;   // columns and rows of a patch that one workgroup turns
+
+struct TurnArgs {
+    const void *a, *pre;       // [rows][cols]; pre: a is multiplied by act'(pre)
+    int64_t rows, cols, lda, ldpre;
+    int act;
+    void *same, *turned;       // [rows][ldsame], [cols][ldturned], both zero up to their row's length; or NULL
+    int64_t ldsame, ldturned;
+    float *shares;             // [patches of rows][cols]: column sums of the products before rounding, or NULL
+};
+
+// A patch of 64 x 64 through LDS, eight elements a thread at a time: read by rows, written by rows and by columns.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_turn(TurnArgs A)
+{
+    __shared__ T patch[kPatch][kPatch + 2];
+    __shared__ float sums[kBlock / kVec][kPatch];
+    const int64_t across = (A.cols + kPatch - 1) / kPatch, down = (A.rows + kPatch - 1) / kPatch, number = block_number();
+    if (number >= across * down) return;
+    const int64_t r0 = number / across * kPatch, c0 = number % across * kPatch;
+    const int lane8 = threadIdx.x % kVec, group = threadIdx.x / kVec;   // 32 rows at once
+    float sum[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+#pragma unroll
+    for (int h = 0; h < kPatch / (kBlock / kVec); ++h) {
+        const int r = group + h * (kBlock / kVec);
+        const int64_t i = r0 + r, j = c0 + lane8 * kVec, n = A.cols - j;
+        float v[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = 0.f;
+        if (i < A.rows && n > 0) {
+            load_as<T>(v, A.a, i * A.lda + j, n);
+            if (A.act != TRON_ACT_NONE) {
+                float p[kVec];
+                load_as<T>(p, A.pre, i * A.ldpre + j, n);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) v[e] = e < n ? v[e] * act_slope(p[e], A.act) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[e] += v[e];
+        }
+        if (A.same && i < A.rows && j < A.ldsame) store8_of<T>(static_cast<T *>(A.same) + i * A.ldsame + j, v, A.ldsame - j);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) patch[r][lane8 * kVec + e] = static_cast<T>(v[e]);
+    }
+    if (A.shares) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sums[group][lane8 * kVec + e] = sum[e];
+    }
+    __syncthreads();
+    if (A.shares && threadIdx.x < kPatch && c0 + threadIdx.x < A.cols) {
+        float s = 0.f;
+        for (int g = 0; g < kBlock / kVec; ++g) s += sums[g][threadIdx.x];
+        A.shares[number / across * A.cols + c0 + threadIdx.x] = s;
+    }
+    if (!A.turned) return;
+#pragma unroll
+    for (int h = 0; h < kPatch / (kBlock / kVec); ++h) {
+        const int c = group + h * (kBlock / kVec);
+        const int64_t j = c0 + c, i = r0 + lane8 * kVec;
+        if (j >= A.cols || i >= A.ldturned) continue;
+        Raw8<T> v;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v.v[e] = patch[lane8 * kVec + e][c];
+        if (A.ldturned - i >= kVec) store8(static_cast<T *>(A.turned) + j * A.ldturned + i, v);
+        else store_first(static_cast<T *>(A.turned) + j * A.ldturned + i, (int)(A.ldturned - i), v);
+    }
+}
+
+template <typename T>
+int turn(const TurnArgs &A, hipStream_t st)
+{
+    k_turn<T><<<block_grid(ceil_div(A.rows, kPatch) * ceil_div(A.cols, kPatch)), kBlock, 0, st>>>(A);
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+inline int64_t padded(int64_t n) { return ceil_div(n, kVec) * kVec; }
+
+// the work space of the gradients, in the order of its parts
+struct GradSpace {
+    int64_t dpre, dpre_t, w_t, x_t, shares, part, total;
+};
+GradSpace grad_space(int64_t m, int64_t n, int64_t k, bool act, bool dx, bool dw, bool db)
+{
+    GradSpace S;
+    int64_t at = 0;
+    auto take = [&](bool want, int64_t bytes) {
+        const int64_t from = at;
+        if (want) at += ceil_div(bytes, 256) * 256;
+        return from;
+    };
+    S.dpre = take(dx && act, m * padded(n) * 2);
+    S.dpre_t = take(dw, n * padded(m) * 2);
+    S.w_t = take(dx, k * padded(n) * 2);
+    S.x_t = take(dw, k * padded(m) * 2);
+    S.shares = take(db, ceil_div(m, kPatch) * n * 4);
+    const int64_t for_dx = dx ? plan_bytes(linear_plan(m, k, padded(n), TRON_TYPE_BF16), m, k) : 0;
+    const int64_t for_dw = dw ? plan_bytes(linear_plan(n, k, padded(m), TRON_TYPE_BF16), n, k) : 0;
+    S.part = take(true, std::max(for_dx, for_dw));
+    S.total = at;
+    return S;
+}
+
+struct GradArgs {
+    int64_t m, n, k;
+    const void *x, *w, *dy, *pre;
+    int64_t ldx, ldw, lddy, ldpre;
+    int act, type;
+    void *dx, *dw;
+    int64_t lddx, lddw;
+    int dw_type;
+    float *dbias;
+    char *work;
+};
+
+template <typename T>
+int linear_grad_typed(const GradArgs &G, hipStream_t st)
+{
+    const int64_t m = G.m, n = G.n, k = G.k, np = padded(n), mp = padded(m);
+    const bool act = G.act != TRON_ACT_NONE;
+    const GradSpace S = grad_space(m, n, k, act, G.dx, G.dw, G.dbias);
+    float *shares = reinterpret_cast<float *>(G.work + S.shares), *part = reinterpret_cast<float *>(G.work + S.part);
+    void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
+    if (G.dbias || G.dw || (G.dx && act))
+        TRON_TRY(turn<T>(TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, G.dx && act ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr}, st));
+    if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
+    Epilogue E{};
+    if (G.dx) {
+        TRON_TRY(turn<T>(TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr}, st));
+        E.y = G.dx;
+        E.m = m;
+        E.n = k;
+        E.ldy = G.lddx;
+        E.out = G.type;
+        // without an activation dy itself, whose rows end at n
+        const Operand a = act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy};
+        TRON_TRY(product<T>(a, Operand{w_t, k, np}, act ? np : n, linear_plan(m, k, np, G.type), E, part, st));
+    }
+    if (G.dw) {
+        TRON_TRY(turn<T>(TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr}, st));
+        E.y = G.dw;
+        E.m = n;
+        E.n = k;
+        E.ldy = G.lddw;
+        E.out = G.dw_type;
+        TRON_TRY(product<T>(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mp, linear_plan(n, k, mp, G.type), E, part, st));
+    }
+    return TRON_OK;
+}
+
+bool sizes_ok(int64_t m, int64_t n, int64_t k)
+{
+    return m >= 0 && n >= 1 && k >= 1 && m <= INT32_MAX && n <= INT32_MAX && k <= INT32_MAX && extent_ok(m, n, n) && extent_ok(m, k, k) && extent_ok(n, k, k);
+}
+bool act_ok(int act) { return act >= TRON_ACT_NONE && act <= TRON_ACT_SILU; }
+
+}  // namespace
+}  // namespace tron
+
+using namespace tron;
+
+extern "C" {
+
+int64_t tron_linear_work(int64_t m, int64_t n, int64_t k, int type)
+{
+    return sizes_ok(m, n, k) && m > 0 && type >= TRON_TYPE_BF16 && type <= TRON_TYPE_E4M3 ? plan_bytes(linear_plan(m, n, k, type), m, n) : 0;
+}
+
+int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const float *x_scale, const void *w, int64_t ldw, const float *w_scale,
+                const float *bias, int act, const void *residual, int64_t ldr, int out_type, void *y, int64_t ldy, void *pre, int64_t ldpre, void *work,
+                int64_t work_bytes, void *hip_stream)
+{
+    const bool eight = type == TRON_TYPE_E4M3;
+    if (!sizes_ok(m, n, k) || type < TRON_TYPE_BF16 || type > TRON_TYPE_E4M3 || !type_is_float(out_type) || !act_ok(act)) {
+        set_error("tron_linear: bad argument (need 0 <= m < 2^31, 1 <= n, k < 2^31, operands bf16, f16 or e4m3, out_type f32, bf16 or f16, a known activation)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && (!x || !w || !y || (eight && (!x_scale || !w_scale)) || (!eight && (x_scale || w_scale)))) {
+        set_error("tron_linear: bad argument (x, w and y are needed; e4m3 operands, and they alone, have scales)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && (!rows_ok(m, k, ldx, false) || !rows_ok(n, k, ldw, false) || (residual && !rows_ok(m, n, ldr, false)) || !rows_ok(m, n, ldy, true) ||
+                  (pre && !rows_ok(m, n, ldpre, true)) || !extent_ok(m, ldx, k) || !extent_ok(n, ldw, k) || !extent_ok(m, residual ? ldr : 0, n) ||
+                  !extent_ok(m, ldy, n) || !extent_ok(m, pre ? ldpre : 0, n))) {
+        set_error("tron_linear: bad leading dimension (rows that are written may not overlap)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && !work_ok(work, work_bytes, tron_linear_work(m, n, k, type))) {
+        set_error("tron_linear: needs a work space of tron_linear_work(m, n, k, type) bytes at a multiple of 16");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    if (m == 0) return TRON_OK;
+    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr};
+    const Operand a{x, m, ldx}, b{w, n, ldw};
+    const Plan P = linear_plan(m, n, k, type);
+    float *part = static_cast<float *>(work);
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    return type == TRON_TYPE_BF16 ? product<__bf16>(a, b, k, P, E, part, st)
+           : type == TRON_TYPE_F16 ? product<_Float16>(a, b, k, P, E, part, st) : product<e4m3>(a, b, k, P, E, part, st);
+}
+
+int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias)
+{
+    return sizes_ok(m, n, k) && m > 0 && act_ok(act) ? grad_space(m, n, k, act != TRON_ACT_NONE, want_dx != 0, want_dw != 0, want_dbias != 0).total : 0;
+}
+
+int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const void *w, int64_t ldw, const void *dy, int64_t lddy, int act,
+                     const void *pre, int64_t ldpre, void *dx, int64_t lddx, int dw_type, void *dw, int64_t lddw, float *dbias, void *work, int64_t work_bytes,
+                     void *hip_stream)
+{
+    if (!sizes_ok(m, n, k) || (type != TRON_TYPE_BF16 && type != TRON_TYPE_F16) || !act_ok(act) || (dw && !type_is_float(dw_type))) {
+        set_error("tron_linear_grad: bad argument (need 0 <= m < 2^31, 1 <= n, k < 2^31, type bf16 or f16, dw_type f32, bf16 or f16, a known activation)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && ((dw && !x) || (dx && !w) || !dy || (act != TRON_ACT_NONE && !pre))) {
+        set_error("tron_linear_grad: bad argument (dy is needed, x for dw, w for dx, pre where there is an activation)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && ((dw && !rows_ok(m, k, ldx, false)) || (dx && !rows_ok(n, k, ldw, false)) || !rows_ok(m, n, lddy, false) ||
+                  (act != TRON_ACT_NONE && !rows_ok(m, n, ldpre, false)) || !extent_ok(m, dw ? ldx : 0, k) || !extent_ok(n, dx ? ldw : 0, k) ||
+                  !extent_ok(m, lddy, n) || !extent_ok(m, act != TRON_ACT_NONE ? ldpre : 0, n) || (dx && (!rows_ok(m, k, lddx, true) || !extent_ok(m, lddx, k))))) {
+        set_error("tron_linear_grad: bad leading dimension (rows that are written may not overlap)");
+        return TRON_EINVAL;
+    }
+    if (dw && (!rows_ok(n, k, lddw, true) || !extent_ok(n, lddw, k))) {
+        set_error("tron_linear_grad: bad leading dimension of dw");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && !work_ok(work, work_bytes, tron_linear_grad_work(m, n, k, act, dx != nullptr, dw != nullptr, dbias != nullptr))) {
+        set_error("tron_linear_grad: needs a work space of tron_linear_grad_work(...) bytes at a multiple of 16");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    if (m == 0) {
+        // sums over no rows
+        if (dbias) TRON_TRY(column_sums(nullptr, 0, n, dbias, st));
+        if (!dw) return TRON_OK;
+        Epilogue E{};
+        E.y = dw;
+        E.m = n;
+        E.n = k;
+        E.ldy = lddw;
+        E.out = dw_type;
+        k_linear_join<<<block_grid(ceil_div(ceil_div(k, kVec) * n, kBlock)), kBlock, 0, st>>>(E, 0);
+        TRON_HIP(hipGetLastError());
+        return TRON_OK;
+    }
+    const GradArgs G{m, n, k, x, w, dy, pre, ldx, ldw, lddy, ldpre, act, type, dx, dw, lddx, lddw, dw_type, dbias, static_cast<char *>(work)};
+    return type == TRON_TYPE_BF16 ? linear_grad_typed<__bf16>(G, st) : linear_grad_typed<_Float16>(G, st);
+}
+
+}  // extern "C"

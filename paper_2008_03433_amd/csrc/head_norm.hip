@@ -1,0 +1,491 @@
+// Root-mean-square norm of the sum of a row and its residual, with an output in the input's type or in 8 bits, and its gradient.
+//
+//   s = x + r,  rstd = (mean s^2 + eps)^-1/2,  y = s rstd gain          (e4m3: y / scale with scale = max |y| / 448)
+//   dx = rstd (a - s rstd^2 mean(a s)) + dtotal,  a = dy gain;          dgain_j = sum_i dy_ij s_ij rstd_i
+//
+// Both are bound by memory: every matrix is read or written once, and a row stays in registers between the sums over it and the
+// outputs that need them.  A row belongs to one wavefront (narrow rows: no barriers) or to one workgroup.  The sums are taken in
+// 32 bits over the unrounded s; `total` is s rounded to its type, and the gradient reads that.
+#include "head_util.h"
+
+namespace tron {
+namespace {
+
+constexpr int kWaveRows = 4;            // wavefronts, each with rows of its own, of a workgroup over narrow rows
+constexpr int64_t kNarrow = 2048;       // columns up to which a wavefront holds a row: four chunks of eight elements a lane
+constexpr int64_t kWide = 32768;        // above: rows are read twice
+
+struct NormArgs {
+    const void *x, *residual;
+    const float *gain;
+    void *total, *y;
+    float *scale, *rstd;
+    int64_t m, d, ldx, ldr, ldt, ldy;
+    float eps, inv_d;
+};
+
+constexpr float kE4m3Max = 448.f;
+
+template <typename T>
+struct Elements {
+    const T *p;
+    int64_t d;
+    __device__ __forceinline__ Raw8<T> at(int64_t j) const { return j + kVec <= d ? load8(p + j) : load_first(p + j, (int)(d - j), static_cast<T>(0.f)); }
+};
+
+__device__ __forceinline__ void gain8(float *g, const float *gain, int64_t j, int64_t d)
+{
+    if (!gain) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) g[i] = 1.f;
+        return;
+    }
+    const Raw8<float> r = Elements<float>{gain, d}.at(j);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) g[i] = r.v[i];
+}
+
+// What a row's sums give: its factors
+struct RowFactors {
+    float rstd, scale, per_scale;
+};
+__device__ __forceinline__ RowFactors row_factors(float sum2, float top, float eps, float inv_d)
+{
+    RowFactors f;
+    f.rstd = 1.f / sqrtf(sum2 * inv_d + eps);
+    // max |y| = rstd max |s gain|; a row of zeros (and one with a NaN, which every y then is) has scale 1.  The smallest normal
+    // number as the least scale has a finite reciprocal.
+    const float largest = top * f.rstd;
+    f.scale = largest > 0.f ? fmaxf(largest / kE4m3Max, 0x1p-126f) : 1.f;
+    f.per_scale = 1.f / f.scale;
+    return f;
+}
+
+// CH chunks of eight elements a thread; WAVE: a wavefront a row, otherwise a workgroup
+template <typename T, typename O, int CH, bool WAVE>
+__global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm(NormArgs A)
+{
+    constexpr bool kEight = sizeof(O) == 1;
+    __shared__ float room[2 * kMostWaves];
+    const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
+    const int64_t row = WAVE ? block_number() * kWaveRows + threadIdx.x / kWave : block_number();
+    if (row >= A.m) return;
+    const int64_t d = A.d;
+    const Elements<T> x{static_cast<const T *>(A.x) + row * A.ldx, d};
+    float s[CH][kVec];
+    float sum2 = 0.f, top = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t j = (int64_t)(me + c * team) * kVec;
+        if (j < d) {
+            const Raw8<T> v = x.at(j);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) s[c][i] = static_cast<float>(v.v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) s[c][i] = 0.f;
+        }
+    }
+    if (A.residual) {
+        const Elements<T> r{static_cast<const T *>(A.residual) + row * A.ldr, d};
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t j = (int64_t)(me + c * team) * kVec;
+            if (j < d) {
+                const Raw8<T> v = r.at(j);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) s[c][i] += static_cast<float>(v.v[i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum2 = fmaf(s[c][i], s[c][i], sum2);
+    if (A.total) {
+        T *t = static_cast<T *>(A.total) + row * A.ldt;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t j = (int64_t)(me + c * team) * kVec;
+            if (j < d) store8_of<T>(t + j, s[c], d - j);
+        }
+    }
+    // s gain from here on
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t j = (int64_t)(me + c * team) * kVec;
+        if (j < d) {
+            float g[kVec];
+            gain8(g, A.gain, j, d);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                s[c][i] *= g[i];
+                if (kEight) top = fmaxf(top, fabsf(s[c][i]));
+            }
+        }
+    }
+    if (WAVE) {
+        sum2 = wave_sumf(sum2);
+        if (kEight) top = wave_maxf(top);
+    } else if (kEight) {
+        block_sum_max(sum2, top, room);
+    } else {
+        sum2 = block_sumf(sum2, room);
+    }
+    const RowFactors f = row_factors(sum2, top, A.eps, A.inv_d);
+    if (me == 0) {
+        if (A.rstd) A.rstd[row] = f.rstd;
+        if (kEight) A.scale[row] = f.scale;
+    }
+    O *y = static_cast<O *>(A.y) + row * A.ldy;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t j = (int64_t)(me + c * team) * kVec;
+        if (j < d) {
+            float v[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = kEight ? s[c][i] * f.rstd * f.per_scale : s[c][i] * f.rstd;
+            store8_of<O>(y + j, v, d - j);
+        }
+    }
+}
+
+// Rows that registers do not hold: read twice.  What is written lies behind the thread's last read of it, so `total` may be x or r.
+template <typename T, typename O>
+__global__ __launch_bounds__(1024) void k_rms_norm_wide(NormArgs A)
+{
+    constexpr bool kEight = sizeof(O) == 1;
+    __shared__ float room[2 * kMostWaves];
+    const int64_t row = block_number(), d = A.d, step = (int64_t)blockDim.x * kVec;
+    if (row >= A.m) return;
+    const Elements<T> x{static_cast<const T *>(A.x) + row * A.ldx, d}, r{static_cast<const T *>(A.residual) + (A.residual ? row * A.ldr : 0), d};
+    auto sum8 = [&](float *s, int64_t j) {
+        const Raw8<T> v = x.at(j);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) s[i] = static_cast<float>(v.v[i]);
+        if (A.residual) {
+            const Raw8<T> u = r.at(j);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) s[i] += static_cast<float>(u.v[i]);
+        }
+    };
+    float sum2 = 0.f, top = 0.f;
+    for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
+        float s[kVec], g[kVec];
+        sum8(s, j);
+        if (kEight) gain8(g, A.gain, j, d);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            sum2 = fmaf(s[i], s[i], sum2);
+            if (kEight) top = fmaxf(top, fabsf(s[i] * g[i]));
+        }
+    }
+    block_sum_max(sum2, top, room);
+    const RowFactors f = row_factors(sum2, top, A.eps, A.inv_d);
+    if (threadIdx.x == 0) {
+        if (A.rstd) A.rstd[row] = f.rstd;
+        if (kEight) A.scale[row] = f.scale;
+    }
+    O *y = static_cast<O *>(A.y) + row * A.ldy;
+    T *t = static_cast<T *>(A.total) + (A.total ? row * A.ldt : 0);
+    for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
+        float s[kVec], g[kVec];
+        sum8(s, j);
+        if (A.total) store8_of<T>(t + j, s, d - j);
+        gain8(g, A.gain, j, d);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) s[i] = kEight ? s[i] * g[i] * f.rstd * f.per_scale : s[i] * g[i] * f.rstd;
+        store8_of<O>(y + j, s, d - j);
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+struct NormGradArgs {
+    const void *total, *dy, *dtotal;
+    const float *gain, *rstd;
+    void *dx;
+    float *partial;   // [teams][d]: each team's share of dgain, or NULL
+    int64_t m, d, lds, lddy, lddt, lddx;
+    float inv_d;
+};
+
+// Teams (wavefronts or workgroups) take rows in turn and keep their columns' shares of dgain in registers.
+template <typename T, int CH, bool WAVE>
+__global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm_grad(NormGradArgs A)
+{
+    __shared__ float room[2][kMostWaves];
+    const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
+    const int64_t teams = WAVE ? (int64_t)gridDim.x * kWaveRows : gridDim.x;
+    const int64_t first = WAVE ? (int64_t)blockIdx.x * kWaveRows + threadIdx.x / kWave : blockIdx.x;
+    const int64_t d = A.d;
+    float g[CH][kVec], dg[CH][kVec];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t j = (int64_t)(me + c * team) * kVec;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) g[c][i] = dg[c][i] = 0.f;
+        if (j < d) gain8(g[c], A.gain, j, d);
+    }
+    int turn = 0;
+    for (int64_t row = first; row < A.m; row += teams, turn ^= 1) {
+        const Elements<T> sv{static_cast<const T *>(A.total) + row * A.lds, d}, dyv{static_cast<const T *>(A.dy) + row * A.lddy, d};
+        const float rstd = A.rstd[row];
+        Raw8<T> s[CH], dy[CH], dt[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t j = (int64_t)(me + c * team) * kVec;
+            if (j < d) {
+                s[c] = sv.at(j);
+                dy[c] = dyv.at(j);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) s[c].v[i] = dy[c].v[i] = static_cast<T>(0.f);
+            }
+        }
+        if (A.dtotal) {
+            const Elements<T> v{static_cast<const T *>(A.dtotal) + row * A.lddt, d};
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int64_t j = (int64_t)(me + c * team) * kVec;
+                if (j < d) dt[c] = v.at(j);
+            }
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const float a = static_cast<float>(dy[c].v[i]), v = static_cast<float>(s[c].v[i]);
+                dot = fmaf(a * g[c][i], v, dot);
+                dg[c][i] = fmaf(a, v * rstd, dg[c][i]);
+            }
+        // two rooms in turn: who writes the next row's sums has passed the barrier behind which the last ones of this room were read
+        dot = WAVE ? wave_sumf(dot) : block_sumf(dot, room[turn]);
+        const float back = rstd * rstd * (dot * A.inv_d);
+        T *dx = static_cast<T *>(A.dx) + row * A.lddx;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t j = (int64_t)(me + c * team) * kVec;
+            if (j < d) {
+                float v[kVec];
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    v[i] = rstd * (static_cast<float>(dy[c].v[i]) * g[c][i] - static_cast<float>(s[c].v[i]) * back);
+                    if (A.dtotal) v[i] += static_cast<float>(dt[c].v[i]);
+                }
+                store8_of<T>(dx + j, v, d - j);
+            }
+        }
+    }
+    if (A.partial) {
+        float *p = A.partial + first * d;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t j = (int64_t)(me + c * team) * kVec;
+            if (j < d) store8_of<float>(p + j, dg[c], d - j);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_rms_norm_grad_wide(NormGradArgs A)
+{
+    __shared__ float room[kMostWaves];
+    const int64_t row = block_number(), d = A.d, step = (int64_t)blockDim.x * kVec;
+    if (row >= A.m) return;
+    const Elements<T> sv{static_cast<const T *>(A.total) + row * A.lds, d}, dyv{static_cast<const T *>(A.dy) + row * A.lddy, d};
+    const Elements<T> dtv{static_cast<const T *>(A.dtotal) + (A.dtotal ? row * A.lddt : 0), d};
+    float dot = 0.f;
+    for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
+        const Raw8<T> s = sv.at(j), dy = dyv.at(j);
+        float g[kVec];
+        gain8(g, A.gain, j, d);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dot = fmaf(static_cast<float>(dy.v[i]) * g[i], static_cast<float>(s.v[i]), dot);
+    }
+    dot = block_sumf(dot, room);
+    const float rstd = A.rstd[row], back = rstd * rstd * (dot * A.inv_d);
+    T *dx = static_cast<T *>(A.dx) + row * A.lddx;
+    for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
+        const Raw8<T> s = sv.at(j), dy = dyv.at(j);
+        float g[kVec], v[kVec];
+        gain8(g, A.gain, j, d);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = rstd * (static_cast<float>(dy.v[i]) * g[i] - static_cast<float>(s.v[i]) * back);
+        if (A.dtotal) {
+            const Raw8<T> dt = dtv.at(j);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] += static_cast<float>(dt.v[i]);
+        }
+        store8_of<T>(dx + j, v, d - j);
+    }
+}
+
+// shares of dgain of rows that registers do not hold: a thread a column, gridDim.y shares
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_gain_shares(NormGradArgs A)
+{
+    const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (j >= A.d) return;
+    float sum = 0.f;
+    for (int64_t row = blockIdx.y; row < A.m; row += gridDim.y)
+        sum = fmaf(static_cast<float>(static_cast<const T *>(A.dy)[row * A.lddy + j]),
+                   static_cast<float>(static_cast<const T *>(A.total)[row * A.lds + j]) * A.rstd[row], sum);
+    A.partial[blockIdx.y * A.d + j] = sum;
+}
+
+}  // namespace
+
+// out_j = sum over the rows of shares, in a fixed order: a wavefront a share modulo 16, 64 columns a workgroup
+__global__ __launch_bounds__(1024) void k_column_sums(const float *shares, int64_t count, int64_t d, float *out)
+{
+    __shared__ float room[kMostWaves][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t j = (int64_t)blockIdx.x * kWave + lane;
+    float sum = 0.f;
+    if (j < d)
+        for (int64_t i = wave; i < count; i += kMostWaves) sum += shares[i * d + j];
+    room[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && j < d) {
+        sum = 0.f;
+        for (int w = 0; w < kMostWaves; ++w) sum += room[w][lane];
+        out[j] = sum;
+    }
+}
+
+int column_sums(const float *shares, int64_t count, int64_t d, float *out, hipStream_t st)
+{
+    k_column_sums<<<(unsigned)ceil_div(d, kWave), 1024, 0, st>>>(shares, count, d, out);
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+namespace {
+
+// threads of a workgroup that holds a row in CH chunks a thread
+inline unsigned row_threads(int64_t d, int ch) { return (unsigned)(ceil_div(ceil_div(d, kVec), (int64_t)ch * kWave) * kWave); }
+
+template <typename T, typename O>
+int norm_launch(const NormArgs &A, hipStream_t st)
+{
+    const int64_t d = A.d;
+    if (d <= kNarrow) {
+        const dim3 grid = block_grid(ceil_div(A.m, kWaveRows));
+        if (d <= 512) k_rms_norm<T, O, 1, true><<<grid, kWaveRows * kWave, 0, st>>>(A);
+        else if (d <= 1024) k_rms_norm<T, O, 2, true><<<grid, kWaveRows * kWave, 0, st>>>(A);
+        else k_rms_norm<T, O, 4, true><<<grid, kWaveRows * kWave, 0, st>>>(A);
+    } else if (d <= 8192) {
+        k_rms_norm<T, O, 2, false><<<block_grid(A.m), row_threads(d, 2), 0, st>>>(A);
+    } else if (d <= kWide) {
+        k_rms_norm<T, O, 4, false><<<block_grid(A.m), row_threads(d, 4), 0, st>>>(A);
+    } else {
+        k_rms_norm_wide<T, O><<<block_grid(A.m), 1024, 0, st>>>(A);
+    }
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+template <typename T>
+int norm_typed(const NormArgs &A, bool eight, hipStream_t st)
+{
+    return eight ? norm_launch<T, e4m3>(A, st) : norm_launch<T, T>(A, st);
+}
+
+// how the gradient is cut: its teams, which are its shares of dgain too
+constexpr int64_t kGradWide = 16384;
+struct GradCut {
+    int64_t teams;
+    unsigned grid;
+};
+GradCut grad_cut(int64_t m, int64_t d)
+{
+    if (d <= kNarrow) {
+        const int64_t grid = std::min<int64_t>(ceil_div(m, kWaveRows), 1024);
+        return {grid * kWaveRows, (unsigned)grid};
+    }
+    const int64_t teams = std::min<int64_t>(m, d <= 8192 ? 1024 : d <= kGradWide ? 512 : 64);
+    return {teams, (unsigned)teams};
+}
+
+template <typename T>
+int norm_grad_typed(const NormGradArgs &A, float *dgain, hipStream_t st)
+{
+    const int64_t d = A.d;
+    const GradCut cut = grad_cut(A.m, d);
+    if (d <= kNarrow) {
+        if (d <= 512) k_rms_norm_grad<T, 1, true><<<cut.grid, kWaveRows * kWave, 0, st>>>(A);
+        else if (d <= 1024) k_rms_norm_grad<T, 2, true><<<cut.grid, kWaveRows * kWave, 0, st>>>(A);
+        else k_rms_norm_grad<T, 4, true><<<cut.grid, kWaveRows * kWave, 0, st>>>(A);
+    } else if (d <= 8192) {
+        k_rms_norm_grad<T, 1, false><<<cut.grid, row_threads(d, 1), 0, st>>>(A);
+    } else if (d <= kGradWide) {
+        k_rms_norm_grad<T, 2, false><<<cut.grid, row_threads(d, 2), 0, st>>>(A);
+    } else {
+        // before dx is written, which may be dy
+        if (A.partial) k_gain_shares<T><<<dim3((unsigned)ceil_div(d, kBlock), (unsigned)cut.teams), kBlock, 0, st>>>(A);
+        k_rms_norm_grad_wide<T><<<block_grid(A.m), 1024, 0, st>>>(A);
+    }
+    TRON_HIP(hipGetLastError());
+    return dgain ? column_sums(A.partial, cut.teams, d, dgain, st) : TRON_OK;
+}
+
+}  // namespace
+}  // namespace tron
+
+using namespace tron;
+
+extern "C" {
+
+int tron_rms_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr, const float *gain, double eps,
+                  void *total, int64_t ldt, int out_type, void *y, int64_t ldy, float *scale, float *rstd, void *hip_stream)
+{
+    const bool eight = out_type == TRON_TYPE_E4M3;
+    if (m < 0 || d < 1 || m > INT32_MAX || !type_is_float(type) || (out_type != type && !eight) || !(eps >= 0.0) || !(eps < HUGE_VAL)) {
+        set_error("tron_rms_norm: bad argument (need 0 <= m < 2^31, d >= 1, type f32, bf16 or f16, out_type that type or e4m3, finite eps >= 0)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && (!x || !y || (eight && !scale) || !rows_ok(m, d, ldx, false) || (residual && !rows_ok(m, d, ldr, false)) ||
+                  (total && !rows_ok(m, d, ldt, true)) || !rows_ok(m, d, ldy, true) || !extent_ok(m, ldx, d) || !extent_ok(m, residual ? ldr : 0, d) ||
+                  !extent_ok(m, total ? ldt : 0, d) || !extent_ok(m, ldy, d))) {
+        set_error("tron_rms_norm: bad argument (x, y and, for e4m3, scale are needed; rows that are written may not overlap)");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    if (m == 0) return TRON_OK;
+    const NormArgs A{x, residual, gain, total, y, scale, rstd, m, d, ldx, ldr, ldt, ldy, (float)eps, (float)(1.0 / (double)d)};
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    return type == TRON_TYPE_F32 ? norm_typed<float>(A, eight, st) : type == TRON_TYPE_BF16 ? norm_typed<__bf16>(A, eight, st) : norm_typed<_Float16>(A, eight, st);
+}
+
+int64_t tron_rms_norm_grad_work(int64_t m, int64_t d)
+{
+    if (m < 1 || d < 1 || m > INT32_MAX || !extent_ok(grad_cut(m, d).teams, d, d)) return 0;
+    return grad_cut(m, d).teams * d * (int64_t)sizeof(float);
+}
+
+int tron_rms_norm_grad(int64_t m, int64_t d, int type, const void *total, int64_t lds, const float *rstd, const float *gain, const void *dy, int64_t lddy,
+                       const void *dtotal, int64_t lddt, void *dx, int64_t lddx, float *dgain, void *work, int64_t work_bytes, void *hip_stream)
+{
+    if (m < 0 || d < 1 || m > INT32_MAX || !type_is_float(type)) {
+        set_error("tron_rms_norm_grad: bad argument (need 0 <= m < 2^31, d >= 1, type f32, bf16 or f16)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && (!total || !rstd || !dy || !dx || !rows_ok(m, d, lds, false) || !rows_ok(m, d, lddy, false) || (dtotal && !rows_ok(m, d, lddt, false)) ||
+                  !rows_ok(m, d, lddx, true) || !extent_ok(m, lds, d) || !extent_ok(m, lddy, d) || !extent_ok(m, dtotal ? lddt : 0, d) || !extent_ok(m, lddx, d))) {
+        set_error("tron_rms_norm_grad: bad argument (total, rstd, dy and dx are needed; the rows of dx may not overlap)");
+        return TRON_EINVAL;
+    }
+    if (dgain && !work_ok(work, work_bytes, tron_rms_norm_grad_work(m, d))) {
+        set_error("tron_rms_norm_grad: dgain needs a work space of tron_rms_norm_grad_work(m, d) bytes at a multiple of 16");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    if (m == 0) return dgain ? column_sums(nullptr, 0, d, dgain, st) : TRON_OK;
+    const NormGradArgs A{total, dy, dtotal, gain, rstd, dx, dgain ? static_cast<float *>(work) : nullptr, m, d, lds, lddy, lddt, lddx, (float)(1.0 / (double)d)};
+    return type == TRON_TYPE_F32 ? norm_grad_typed<float>(A, dgain, st)
+           : type == TRON_TYPE_BF16 ? norm_grad_typed<__bf16>(A, dgain, st) : norm_grad_typed<_Float16>(A, dgain, st);
+}
+
+}  // extern "C"

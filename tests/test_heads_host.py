@@ -1,0 +1,69 @@
+"""Operators of a multi-class head, without a GPU: argument checks at the C boundary and sizes of work spaces."""
+import ctypes
+
+import pytest
+
+import paper_2008_03433_amd as tron
+from paper_2008_03433_amd import binding
+
+P = ctypes.c_void_p(4096)   # some address: every call here is refused before it is used
+
+
+def _code(name, *args):
+    return getattr(tron.load_library(), name)(*args)
+
+
+def test_bad_arguments_are_refused_before_the_device_is_asked_for():
+    E = binding.EINVAL
+    assert _code("tron_rms_norm", -1, 8, 0, P, 8, None, 0, None, 1e-6, None, 0, 0, P, 8, None, None, None) == E
+    assert _code("tron_rms_norm", 4, 0, 0, P, 8, None, 0, None, 1e-6, None, 0, 0, P, 8, None, None, None) == E
+    assert _code("tron_rms_norm", 4, 8, 3, P, 8, None, 0, None, 1e-6, None, 0, 3, P, 8, P, None, None) == E
+    assert _code("tron_rms_norm", 4, 8, 0, P, 8, None, 0, None, 1e-6, None, 0, 1, P, 8, None, None, None) == E
+    assert _code("tron_rms_norm", 4, 8, 0, P, 8, None, 0, None, 1e-6, None, 0, 0, P, 7, None, None, None) == E
+    assert _code("tron_rms_norm", 4, 8, 0, P, -8, None, 0, None, 1e-6, None, 0, 0, P, 8, None, None, None) == E
+    assert _code("tron_rms_norm", 4, 8, 0, P, 2 ** 62, None, 0, None, 1e-6, None, 0, 0, P, 8, None, None, None) == E
+    assert _code("tron_rms_norm_grad", 4, 8, 0, P, 8, P, None, P, 8, None, 0, P, 8, P, None, 0, None) == E
+    assert _code("tron_rms_norm_grad", 4, 8, 0, P, 8, None, None, P, 8, None, 0, P, 8, None, None, 0, None) == E
+    assert _code("tron_linear", 4, 4, 8, 0, P, 8, None, P, 8, None, None, 0, None, 0, 0, P, 4, None, 0, None, 0, None) == E
+    assert _code("tron_linear", 4, 4, 8, 1, P, 8, P, P, 8, P, None, 0, None, 0, 0, P, 4, None, 0, None, 0, None) == E
+    assert _code("tron_linear", 4, 4, 8, 1, P, 8, None, P, 8, None, None, 9, None, 0, 0, P, 4, None, 0, None, 0, None) == E
+    assert _code("tron_linear", 4, 4, 8, 1, P, 8, None, P, 8, None, None, 0, None, 0, 0, P, 3, None, 0, None, 0, None) == E
+    assert _code("tron_linear", 4, 4, 0, 1, P, 8, None, P, 8, None, None, 0, None, 0, 0, P, 4, None, 0, None, 0, None) == E
+    m, n, k = 4, 64, 65536   # the inner length is cut
+    need = _code("tron_linear_work", m, n, k, 1)
+    assert need >= 2 * m * n * 4
+    for address, size in ((None, need), (P, need - 1), (ctypes.c_void_p(4100), need)):
+        assert _code("tron_linear", m, n, k, 1, P, k, None, P, k, None, None, 0, None, 0, 0, P, n, None, 0, address, size, None) == E
+        assert "work space" in tron.tron_last_error()
+    assert _code("tron_linear_grad", 4, 4, 8, 3, P, 8, P, 8, P, 4, 0, None, 0, P, 8, 0, None, 0, None, None, 0, None) == E
+    assert _code("tron_linear_grad", 4, 4, 8, 1, P, 8, P, 8, P, 4, 2, None, 0, P, 8, 0, None, 0, None, P, 1 << 30, None) == E
+    assert _code("tron_linear_grad", 4, 4, 8, 1, P, 8, P, 8, P, 4, 0, None, 0, P, 8, 0, None, 0, None, None, 0, None) == E
+    assert _code("tron_distill", 4, 8, 3, P, 8, 2, P, 8, 2, P, 2, 1.0, None, P, None, None, 0, None, 0, None) == E
+    assert _code("tron_distill", 4, 8, 0, P, 8, 2, P, 2, 2, P, 2, 1.0, None, P, None, None, 0, None, 0, None) == E
+    assert _code("tron_distill", 4, 8, 0, P, 8, 1025, P, 8, 2, P, 2, 1.0, None, P, None, None, 0, None, 0, None) == E
+    assert _code("tron_distill", 4, 8, 0, P, 8, 2, None, 8, 2, P, 2, 1.0, None, P, None, None, 0, None, 0, None) == E
+    assert _code("tron_distill", 4, 8, 0, P, 8, 2, P, 8, 2, P, 2, float("nan"), None, P, None, None, 0, None, 0, None) == E
+    assert "temperature" in tron.tron_last_error()
+    assert _code("tron_distill_grad", 4, 8, 0, P, 8, None, 2, P, 8, 2, P, 2, 1.0, None, P, 8, None) == E
+    assert _code("tron_distill", 4, 2 ** 31 - 1, 0, P, 2 ** 31, 2, P, 8, 2, P, 2, 1.0, None, P, None, None, 0, None, 0, None) == E
+
+
+def test_sizes_of_work_spaces():
+    lib = tron.load_library()
+    assert lib.tron_rms_norm_grad_work(0, 8) == 0 and lib.tron_rms_norm_grad_work(3, 8) >= 3 * 8 * 4
+    assert lib.tron_linear_work(0, 4, 4, 1) == 0 and lib.tron_linear_work(4, 4, 4, 7) == 0
+    assert lib.tron_linear_grad_work(5, 7, 9, 0, 0, 0, 0) == 0
+    alone = [lib.tron_linear_grad_work(100, 70, 90, 2, *w) for w in ((1, 0, 0), (0, 1, 0), (0, 0, 1))]
+    assert all(a > 0 for a in alone) and lib.tron_linear_grad_work(100, 70, 90, 2, 1, 1, 1) >= max(alone)
+    assert lib.tron_distill_work(4096, 100) == 0 and lib.tron_distill_work(1, 100000) > 0
+    for m in (1, 3, 100, 511, 512, 1024, 5000):
+        for V in (1, 4096, 4097, 200000):
+            assert lib.tron_distill_work(m, V) % 16 == 0
+
+
+def test_tensors_on_the_host_are_refused():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(2, 3)
+    with pytest.raises(tron.TronError) as e:
+        tron.tron_rms_norm(x, x.clone())
+    assert "no CPU fallback" in str(e.value)
