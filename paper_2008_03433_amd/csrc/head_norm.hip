@@ -204,7 +204,7 @@ struct NormGradArgs {
     const void *total, *dy, *dtotal;
     const float *gain, *rstd;
     void *dx;
-    float *partial;   // [teams][d]: each team's share of dgain, or NULL
+    float *partial;   // [workgroups][d]: their shares of dgain, or NULL
     int64_t m, d, lds, lddy, lddt, lddx;
     float inv_d;
 };
@@ -277,7 +277,26 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm_gr
             }
         }
     }
-    if (A.partial) {
+    if (!A.partial) return;
+    if (WAVE) {   // the wavefronts of a workgroup join their shares, a chunk of columns at a time
+        __shared__ float join[kWaveRows][kWave * kVec];
+        const int wave = threadIdx.x / kWave;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (c) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) join[wave][me * kVec + i] = dg[c][i];
+            __syncthreads();
+            for (int k = threadIdx.x; k < kWave * kVec; k += kWaveRows * kWave) {
+                const int64_t j = (int64_t)c * kWave * kVec + k;
+                if (j >= d) break;
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWaveRows; ++w) sum += join[w][k];
+                A.partial[(int64_t)blockIdx.x * d + j] = sum;
+            }
+        }
+    } else {
         float *p = A.partial + first * d;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -336,27 +355,36 @@ __global__ __launch_bounds__(kBlock) void k_gain_shares(NormGradArgs A)
 
 }  // namespace
 
-// out_j = sum over the rows of shares, in a fixed order: a wavefront a share modulo 16, 64 columns a workgroup
+// out_j = sum over the rows of shares, in a fixed order: 16 columns a workgroup, which 64 groups of 16 lanes walk down, four loads ahead
 __global__ __launch_bounds__(1024) void k_column_sums(const float *shares, int64_t count, int64_t d, float *out)
 {
-    __shared__ float room[kMostWaves][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t j = (int64_t)blockIdx.x * kWave + lane;
+    constexpr int kColumns = 16, kGroups = 1024 / kColumns;
+    __shared__ float room[kGroups][kColumns + 1];
+    const int c = threadIdx.x % kColumns, group = threadIdx.x / kColumns;
+    const int64_t j = (int64_t)blockIdx.x * kColumns + c;
     float sum = 0.f;
-    if (j < d)
-        for (int64_t i = wave; i < count; i += kMostWaves) sum += shares[i * d + j];
-    room[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && j < d) {
-        sum = 0.f;
-        for (int w = 0; w < kMostWaves; ++w) sum += room[w][lane];
-        out[j] = sum;
+    if (j < d) {
+        int64_t i = group;
+        for (; i + 3 * kGroups < count; i += 4 * kGroups) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = shares[(i + k * kGroups) * d + j];
+            sum += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; i < count; i += kGroups) sum += shares[i * d + j];
     }
+    room[group][c] = sum;
+    __syncthreads();
+    for (int half = kGroups / 2; half; half /= 2) {
+        if (group < half) room[group][c] += room[group + half][c];
+        __syncthreads();
+    }
+    if (group == 0 && j < d) out[j] = room[0][c];
 }
 
 int column_sums(const float *shares, int64_t count, int64_t d, float *out, hipStream_t st)
 {
-    k_column_sums<<<(unsigned)ceil_div(d, kWave), 1024, 0, st>>>(shares, count, d, out);
+    k_column_sums<<<(unsigned)ceil_div(d, 16), 1024, 0, st>>>(shares, count, d, out);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -392,42 +420,34 @@ int norm_typed(const NormArgs &A, bool eight, hipStream_t st)
     return eight ? norm_launch<T, e4m3>(A, st) : norm_launch<T, T>(A, st);
 }
 
-// how the gradient is cut: its teams, which are its shares of dgain too
+// Workgroups of the gradient, each with a share of dgain.
 constexpr int64_t kGradWide = 16384;
-struct GradCut {
-    int64_t teams;
-    unsigned grid;
-};
-GradCut grad_cut(int64_t m, int64_t d)
+int64_t grad_shares(int64_t m, int64_t d)
 {
-    if (d <= kNarrow) {
-        const int64_t grid = std::min<int64_t>(ceil_div(m, kWaveRows), 1024);
-        return {grid * kWaveRows, (unsigned)grid};
-    }
-    const int64_t teams = std::min<int64_t>(m, d <= 8192 ? 1024 : d <= kGradWide ? 512 : 64);
-    return {teams, (unsigned)teams};
+    if (d <= kNarrow) return std::min<int64_t>(ceil_div(m, kWaveRows), 1024);
+    return std::min<int64_t>(m, d <= 8192 ? 1024 : d <= kGradWide ? 512 : 64);
 }
 
 template <typename T>
 int norm_grad_typed(const NormGradArgs &A, float *dgain, hipStream_t st)
 {
     const int64_t d = A.d;
-    const GradCut cut = grad_cut(A.m, d);
+    const unsigned shares = (unsigned)grad_shares(A.m, d);
     if (d <= kNarrow) {
-        if (d <= 512) k_rms_norm_grad<T, 1, true><<<cut.grid, kWaveRows * kWave, 0, st>>>(A);
-        else if (d <= 1024) k_rms_norm_grad<T, 2, true><<<cut.grid, kWaveRows * kWave, 0, st>>>(A);
-        else k_rms_norm_grad<T, 4, true><<<cut.grid, kWaveRows * kWave, 0, st>>>(A);
+        if (d <= 512) k_rms_norm_grad<T, 1, true><<<shares, kWaveRows * kWave, 0, st>>>(A);
+        else if (d <= 1024) k_rms_norm_grad<T, 2, true><<<shares, kWaveRows * kWave, 0, st>>>(A);
+        else k_rms_norm_grad<T, 4, true><<<shares, kWaveRows * kWave, 0, st>>>(A);
     } else if (d <= 8192) {
-        k_rms_norm_grad<T, 1, false><<<cut.grid, row_threads(d, 1), 0, st>>>(A);
+        k_rms_norm_grad<T, 1, false><<<shares, row_threads(d, 1), 0, st>>>(A);
     } else if (d <= kGradWide) {
-        k_rms_norm_grad<T, 2, false><<<cut.grid, row_threads(d, 2), 0, st>>>(A);
+        k_rms_norm_grad<T, 2, false><<<shares, row_threads(d, 2), 0, st>>>(A);
     } else {
         // before dx is written, which may be dy
-        if (A.partial) k_gain_shares<T><<<dim3((unsigned)ceil_div(d, kBlock), (unsigned)cut.teams), kBlock, 0, st>>>(A);
+        if (A.partial) k_gain_shares<T><<<dim3((unsigned)ceil_div(d, kBlock), shares), kBlock, 0, st>>>(A);
         k_rms_norm_grad_wide<T><<<block_grid(A.m), 1024, 0, st>>>(A);
     }
     TRON_HIP(hipGetLastError());
-    return dgain ? column_sums(A.partial, cut.teams, d, dgain, st) : TRON_OK;
+    return dgain ? column_sums(A.partial, shares, d, dgain, st) : TRON_OK;
 }
 
 }  // namespace
@@ -460,8 +480,8 @@ int tron_rms_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, co
 
 int64_t tron_rms_norm_grad_work(int64_t m, int64_t d)
 {
-    if (m < 1 || d < 1 || m > INT32_MAX || !extent_ok(grad_cut(m, d).teams, d, d)) return 0;
-    return grad_cut(m, d).teams * d * (int64_t)sizeof(float);
+    if (m < 1 || d < 1 || m > INT32_MAX || !extent_ok(grad_shares(m, d), d, d)) return 0;
+    return grad_shares(m, d) * d * (int64_t)sizeof(float);
 }
 
 int tron_rms_norm_grad(int64_t m, int64_t d, int type, const void *total, int64_t lds, const float *rstd, const float *gain, const void *dy, int64_t lddy,
