@@ -8,12 +8,14 @@
 // registers are read once; the others are read again for the gradient, while they are still in the caches.  Few rows are split
 // over many workgroups, whose maxima and sums the second launch joins.  The teacher's part of a row, K entries, is one wavefront's
 // work, in 64 bits: its terms and the logarithm of the sum cancel to the loss.
+#include <type_traits>
+
 #include "head_util.h"
 
 namespace tron {
 namespace {
 
-constexpr int kThreads = 512;         // of a workgroup over a row or a part of one
+constexpr int kThreads = 512;         // of a workgroup over a part of a row
 constexpr int kMostTop = 1024;        // listed entries a row
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -36,6 +38,7 @@ struct DistillArgs {
     int splits, top;
     bool lists;          // whether there are lists (of no entry, where top = 0)
     bool ids64;
+    bool past;           // outputs go past the caches
     float temperature;
     double inv_t;
     float c;             // log2(e) / T
@@ -46,15 +49,28 @@ template <typename T>
 constexpr bool kFull = sizeof(T) == 4;   // results in 32 bits: 1 / T in two parts
 
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+// what exponents are differences to: no -inf minus -inf
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // ------------------------------------------------------------------ the teacher's part of a row
+// In LDS, as long as the launch says: three arrays of the listed entries
 struct Teacher {
-    float q[kMostTop];
-    int id[kMostTop];    // -1: an entry that is missing
+    float *q, *z;        // mass and logit
+    int *id;             // -1: an entry that is missing
+};
+// A bit for every column's hash: where no bit is met twice, no column is listed twice, and nobody has to compare all pairs (loss
+// and gradient of 2000 x 4000, 64 entries a row: 21.8 -> 16.2 us).  64 entries meet by chance in one row of sixteen.
+constexpr int kSeenWords = 1024;
+__device__ __forceinline__ unsigned column_hash(int id) { return (unsigned)id * 2654435761u >> 17; }
+struct TeacherSums {
     double terms;        // sum_j q_j (log q_j - (z_j - base) / T)
     float base;          // the largest z_j that has mass: terms of masks of the type's lowest value keep their other parts
     int any;             // whether an entry has mass
+    int twice;           // whether a column may be listed twice
 };
+extern __shared__ float g_lists[];
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs &A) { return {g_lists, g_lists + A.top, reinterpret_cast<int *>(g_lists + 2 * A.top)}; }
+unsigned teacher_bytes(const DistillArgs &A) { return 3u * sizeof(float) * A.top; }
 
 __device__ __forceinline__ int64_t listed_id(const DistillArgs &A, int64_t row, int j)
 {
@@ -62,65 +78,79 @@ __device__ __forceinline__ int64_t listed_id(const DistillArgs &A, int64_t row, 
 }
 
 // By one wavefront.  Ids outside [0, V) are missing entries, whatever their t.
-template <typename T, bool TERMS>
-__device__ __forceinline__ void teacher_part(const DistillArgs &A, int64_t row, Teacher &S, int lane)
+template <typename T>
+__device__ __forceinline__ TeacherSums teacher_part(const DistillArgs &A, int64_t row, const Teacher &S, int lane, unsigned *seen = nullptr)
 {
+    if (seen) {
+        typedef unsigned words __attribute__((ext_vector_type(4)));
+        for (int i = lane; i < kSeenWords / 4; i += kWave) reinterpret_cast<words *>(seen)[i] = words{0, 0, 0, 0};
+    }
+    bool met = false;
     const float *t = A.t + row * A.ldt;
     const T *z = static_cast<const T *>(A.z) + row * A.ldz;
-    float top = -INFINITY;
+    float top = -INFINITY, base = -INFINITY;
     bool bad = false;
     for (int j = lane; j < A.top; j += kWave) {
         const int64_t id = listed_id(A, row, j);
         const bool there = id >= 0 && id < A.V;
-        const float v = there ? t[j] : -INFINITY;
+        const float v = there ? t[j] : -INFINITY, x = there ? static_cast<float>(z[id]) : 0.f;
         S.id[j] = there ? (int)id : -1;
         S.q[j] = v;
+        S.z[j] = x;
         top = fmaxf(top, v);
         bad |= v != v;
+        if (v > -INFINITY) base = fmaxf(base, x);
+        if (seen && there) {
+            const unsigned h = column_hash((int)id), bit = 1u << (h & 31);
+            met |= (atomicOr(&seen[h >> 5], bit) & bit) != 0;
+        }
     }
     top = wave_maxf(top);
-    bad = __any(bad);
-    double sum = 0.0;
-    // a wavefront's own LDS operations complete in order
-    for (int j = lane; j < A.top; j += kWave)
-        if (S.id[j] >= 0) sum += exp(((double)S.q[j] - (double)top) * A.inv_t);
-    sum = wave_sum(sum);
-    const bool any = bad || top > -INFINITY;
-    const double log_sum = log(sum);
-    float base = -INFINITY;
-    if (TERMS) {
-        for (int j = lane; j < A.top; j += kWave)
-            if (S.id[j] >= 0 && S.q[j] > -INFINITY) base = fmaxf(base, static_cast<float>(z[S.id[j]]));
-        base = wave_maxf(base);
-        if (base == -INFINITY) base = 0.f;
+    base = base_of(wave_maxf(base));
+    TeacherSums R;
+    R.any = __any(bad) || top > -INFINITY;
+    // a wavefront's own LDS operations complete in order.  Exponents in 64 bits, of which the instruction takes 32 and a factor the rest: a
+    // small q keeps its digits, for the difference to a p that is as small.
+    const double per_t = A.inv_t * kLog2e, from_top = base_of(top);
+    auto mass = [&](double t_top) {
+        const double e = t_top * per_t;
+        const float hi = (float)e;
+        return exp2_(hi) * fmaf((float)(e - (double)hi), 0.69314718f, 1.f);
+    };
+    float sum = 0.f;
+    for (int j = lane; j < A.top; j += kWave) {
+        const float v = S.q[j];
+        if (S.id[j] >= 0 && v != -INFINITY) sum += mass((double)v - from_top);
     }
+    sum = wave_sumf(sum);
+    const float per = 1.f / sum;
+    const double log_sum = (double)logf(sum);
     double terms = 0.0;
     for (int j = lane; j < A.top; j += kWave) {
-        const int id = S.id[j];
-        if (id < 0) {
-            S.q[j] = 0.f;
-            continue;
-        }
-        const double log_q = any ? ((double)S.q[j] - (double)top) * A.inv_t - log_sum : 0.0, q = any ? exp(log_q) : 0.0;
-        S.q[j] = (float)q;
-        if (TERMS && q != 0.0) terms += q * (log_q - ((double)static_cast<float>(z[id]) - (double)base) * A.inv_t);
+        const float v = S.q[j];
+        const double t_top = (double)v - from_top;
+        const float q = S.id[j] < 0 || v == -INFINITY ? 0.f : mass(t_top) * per;
+        S.q[j] = q;
+        if (q != 0.f) terms += (double)q * ((t_top - ((double)S.z[j] - (double)base)) * A.inv_t - log_sum);
     }
-    if (TERMS) terms = wave_sum(terms);
-    if (lane == 0) {
-        S.any = any;
-        S.terms = terms;
-        S.base = base;
-    }
+    R.terms = wave_sum(terms);
+    R.base = base;
+    R.twice = __any(met);
+    return R;
 }
 
 // The listed columns in [from, to) of a row whose workgroup has stored w T p everywhere and passed a barrier: w T (p - q), where a
-// column that is listed several times has the sum of its q.  `keep` holds the listed z, scaled(z) = w T p.
+// column that is listed several times has the sum of its q.  scaled(z) = w T p.
 template <typename T, typename P>
-__device__ __forceinline__ void subtract_teacher(const DistillArgs &A, const Teacher &S, const float *keep, T *out, int64_t from, int64_t to, float wt, P scaled)
+__device__ __forceinline__ void subtract_teacher(const DistillArgs &A, const Teacher &S, T *out, int64_t from, int64_t to, float wt, bool twice, P scaled)
 {
     for (int j = threadIdx.x; j < A.top; j += blockDim.x) {
         const int id = S.id[j];
         if (id < from || id >= to) continue;
+        if (!twice) {
+            out[id] = static_cast<T>(scaled(S.z[j]) - wt * S.q[j]);
+            continue;
+        }
         float q = 0.f;
         bool first = true;
         for (int i = 0; i < A.top; ++i)
@@ -128,7 +158,7 @@ __device__ __forceinline__ void subtract_teacher(const DistillArgs &A, const Tea
                 first &= i >= j;
                 q += S.q[i];
             }
-        if (first) out[id] = static_cast<T>(scaled(keep[j]) - wt * q);
+        if (first) out[id] = static_cast<T>(scaled(S.z[j]) - wt * q);
     }
 }
 
@@ -137,7 +167,6 @@ struct Running {
     float m = -INFINITY, s = 0.f;   // s = sum exp2((z - m) c); m = -inf: nothing yet, or nothing but -inf
 };
 
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 template <typename T>
 __device__ __forceinline__ void take8(Running &r, const Raw8<T> &raw, float c)
@@ -169,13 +198,17 @@ __device__ __forceinline__ Running join(const Running &a, const Running &b, floa
     return r;
 }
 
-// over the workgroup; every thread has the result.  room: 2 * kMostWaves floats
+// over the wavefront; every lane has the result
+__device__ __forceinline__ Running join_wave(const Running &r, float c)
+{
+    const float top = wave_maxf(r.m);
+    return {top, wave_sumf(r.s * exp2_((r.m - base_of(top)) * c))};
+}
+
+// over the workgroup; every thread has the result, behind a barrier.  room: 2 * kMostWaves floats
 __device__ __forceinline__ Running join_block(Running r, float c, float *room)
 {
-    const float m = base_of(wave_maxf(r.m));
-    const float top = wave_maxf(r.m);
-    r.s = wave_sumf(r.s * exp2_((r.m - m) * c));
-    r.m = top;
+    r = join_wave(r, c);
     const int waves = blockDim.x / kWave;
     if (threadIdx.x % kWave == 0) {
         room[threadIdx.x / kWave] = r.m;
@@ -201,10 +234,11 @@ __device__ __forceinline__ float loss_of(const DistillArgs &A, double terms, dou
 }
 
 // ------------------------------------------------------------------ whole rows
+// eight elements from j on; from `to` on they are `fill`
 template <typename T>
-__device__ __forceinline__ Raw8<T> at8(const T *row, int64_t j, int64_t to)
+__device__ __forceinline__ Raw8<T> at8(const T *row, int64_t j, int64_t to, float fill = -INFINITY)
 {
-    return j + kVec <= to ? load8(row + j) : load_first(row + j, (int)(to - j), static_cast<T>(-INFINITY));
+    return j + kVec <= to ? load8(row + j) : load_first(row + j, (int)(to - j), static_cast<T>(fill));
 }
 
 // f p = f exp2((z - m) c) / s where the row's maximum m and sum s are known, with per = f / s
@@ -233,83 +267,101 @@ __device__ __forceinline__ ByLse<T> by_lse(const DistillArgs &A, int64_t row, fl
     return {A.it_hi, A.it_lo, lse == -INFINITY ? 0.f : lse, f};
 }
 
-template <typename T>
-__device__ __forceinline__ void fill8(T *out, int64_t j, int64_t to)
+// Columns that a workgroup takes at once, and how many of these a thread has under way
+constexpr int kAhead = 2;
+__device__ __forceinline__ int64_t block_step() { return (int64_t)blockDim.x * kVec; }
+
+// f(j, eight elements of z from j on) over [from, to), kAhead loads at a time
+template <typename T, typename F>
+__device__ __forceinline__ void over_row(const T *z, int64_t from, int64_t to, F f)
 {
-    const float zero[kVec] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    store8_of<T>(out + j, zero, to - j);
+    const int64_t step = block_step();
+    int64_t j = from + (int64_t)threadIdx.x * kVec;
+    for (; j + (kAhead - 1) * step + kVec <= to; j += kAhead * step) {
+        Raw8<T> raw[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) raw[k] = load8(z + j + k * step);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) f(j + k * step, raw[k]);
+    }
+    for (; j < to; j += step) f(j, at8(z, j, to));
 }
 
-// A workgroup a row.  CH > 0: the row stays in registers, CH chunks of eight a thread; 0: it is read again for the gradient.
-template <typename T, int CH, bool GRAD>
-__global__ __launch_bounds__(kThreads) void k_distill_row(DistillArgs A)
+// the same over two rows; beyond `to` the second has zeros
+template <typename T, typename F>
+__device__ __forceinline__ void over_rows(const T *z, const T *u, int64_t from, int64_t to, F f)
 {
-    __shared__ Teacher S;
-    __shared__ float keep[GRAD ? kMostTop : 1];
+    const int64_t step = block_step();
+    int64_t j = from + (int64_t)threadIdx.x * kVec;
+    for (; j + (kAhead - 1) * step + kVec <= to; j += kAhead * step) {
+        Raw8<T> x[kAhead], y[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            x[k] = load8(z + j + k * step);
+            y[k] = load8(u + j + k * step);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) f(j + k * step, x[k], y[k]);
+    }
+    for (; j < to; j += step) f(j, at8(z, j, to), at8(u, j, to, 0.f));
+}
+
+template <typename T, typename P>
+__device__ __forceinline__ void write_scaled(const DistillArgs &A, const T *z, T *out, int64_t from, int64_t to, P scaled)
+{
+    auto all = [&](auto past) {
+        over_row(z, from, to, [&](int64_t j, const Raw8<T> &x) {
+            float v[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = scaled(static_cast<float>(x.v[i]));
+            store8_of<T, past.value>(out + j, v, to - j);
+        });
+    };
+    if (A.past) all(std::true_type{});
+    else all(std::false_type{});
+}
+
+template <typename T>
+__device__ __forceinline__ void write_zeros(const DistillArgs &A, T *out, int64_t from, int64_t to)
+{
+    const float zero[kVec] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += block_step()) store8_of<T>(out + j, zero, to - j);
+}
+
+// A workgroup a row, which is read again for the gradient.
+template <typename T, bool GRAD>
+__global__ __launch_bounds__(1024) void k_distill_row(DistillArgs A)
+{
+    __shared__ TeacherSums sums;
     __shared__ float room[2 * kMostWaves];
+    __shared__ __align__(16) unsigned seen[GRAD ? kSeenWords : 4];
     const int64_t row = block_number();
     if (row >= A.m) return;
-    const int64_t V = A.V;
-    constexpr int64_t kStep = (int64_t)kThreads * kVec;
+    const Teacher S = teacher_of(A);
     const T *z = static_cast<const T *>(A.z) + row * A.ldz;
-    const float c = A.c;
-    Raw8<T> raw[CH ? CH : 1];
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-        const int64_t j = threadIdx.x * kVec + k * kStep;
-        if (j < V) raw[k] = at8(z, j, V);
+    if (threadIdx.x < kWave) {
+        const TeacherSums R = teacher_part<T>(A, row, S, threadIdx.x, GRAD ? seen : nullptr);
+        if (threadIdx.x == 0) sums = R;
     }
-    if (threadIdx.x < kWave) teacher_part<T, true>(A, row, S, threadIdx.x);
     Running r;
-    if (CH) {
-#pragma unroll
-        for (int k = 0; k < CH; ++k)
-            if ((int64_t)threadIdx.x * kVec + k * kStep < V) take8(r, raw[k], c);
-    } else {
-        int64_t j = (int64_t)threadIdx.x * kVec;
-        for (; j + 3 * kStep + kVec <= V; j += 4 * kStep) {
-            Raw8<T> four[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) four[k] = load8(z + j + k * kStep);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) take8(r, four[k], c);
-        }
-        for (; j < V; j += kStep) take8(r, at8(z, j, V), c);
-    }
-    r = join_block(r, c, room);   // its barrier shows the teacher's part too
-    const float w = S.any ? (A.weight ? A.weight[row] : 1.f) : 0.f;
+    over_row(z, 0, A.V, [&](int64_t, const Raw8<T> &x) { take8(r, x, A.c); });
+    r = join_block(r, A.c, room);   // its barrier shows the teacher's part too
+    const float w = sums.any ? (A.weight ? A.weight[row] : 1.f) : 0.f;
     if (threadIdx.x == 0) {
         if (A.lse) A.lse[row] = (float)log_sum(r, A.inv_t);
-        A.loss[row] = w == 0.f ? 0.f : loss_of(A, S.terms, S.base, r, w);
+        A.loss[row] = w == 0.f ? 0.f : loss_of(A, sums.terms, sums.base, r, w);
     }
     if (!GRAD) return;
     T *out = static_cast<T *>(A.out) + row * A.ldo;
     if (w == 0.f) {
-        for (int64_t j = (int64_t)threadIdx.x * kVec; j < V; j += kStep) fill8(out, j, V);
+        write_zeros(A, out, 0, A.V);
         return;
     }
-    // z of the listed columns, before `out`, which may be z, is written
-    for (int j = threadIdx.x; j < A.top; j += kThreads) keep[j] = S.id[j] >= 0 ? static_cast<float>(z[S.id[j]]) : 0.f;
-    __syncthreads();
     const float wt = w * A.temperature;
-    const ByMax scaled = by_max(r, c, wt);
-    auto write8 = [&](int64_t j, const Raw8<T> &x) {
-        float v[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = scaled(static_cast<float>(x.v[i]));
-        store8_of<T>(out + j, v, V - j);
-    };
-    if (CH) {
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int64_t j = threadIdx.x * kVec + k * kStep;
-            if (j < V) write8(j, raw[k]);
-        }
-    } else {
-        for (int64_t j = (int64_t)threadIdx.x * kVec; j < V; j += kStep) write8(j, at8(z, j, V));
-    }
+    const ByMax scaled = by_max(r, A.c, wt);
+    write_scaled(A, z, out, 0, A.V, scaled);
     __syncthreads();
-    subtract_teacher(A, S, keep, out, 0, V, wt, scaled);
+    subtract_teacher(A, S, out, 0, A.V, wt, sums.twice, scaled);
 }
 
 // ------------------------------------------------------------------ parts of rows
@@ -317,24 +369,22 @@ __global__ __launch_bounds__(kThreads) void k_distill_row(DistillArgs A)
 __device__ __forceinline__ int64_t part_row() { return (int64_t)blockIdx.z * gridDim.y + blockIdx.y; }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_distill_part(DistillArgs A)
+__global__ __launch_bounds__(1024) void k_distill_part(DistillArgs A)
 {
-    __shared__ Teacher S;
     __shared__ float room[2 * kMostWaves];
     const int64_t row = part_row();
     if (row >= A.m) return;
     const int64_t from = blockIdx.x * A.per, to = from + A.per < A.V ? from + A.per : A.V;
-    constexpr int64_t kStep = (int64_t)kThreads * kVec;
     const T *z = static_cast<const T *>(A.z) + row * A.ldz;
     if (blockIdx.x == 0 && threadIdx.x < kWave) {
-        teacher_part<T, true>(A, row, S, threadIdx.x);
+        const TeacherSums R = teacher_part<T>(A, row, teacher_of(A), threadIdx.x);
         if (threadIdx.x == 0) {
-            A.part_teacher[2 * row] = S.terms;
-            A.part_teacher[2 * row + 1] = S.base;
+            A.part_teacher[2 * row] = R.terms;
+            A.part_teacher[2 * row + 1] = R.base;
         }
     }
     Running r;
-    for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += kStep) take8(r, at8(z, j, to), A.c);
+    over_row(z, from, to, [&](int64_t, const Raw8<T> &x) { take8(r, x, A.c); });
     r = join_block(r, A.c, room);
     if (threadIdx.x == 0) {
         A.part_max[row * A.splits + blockIdx.x] = r.m;
@@ -342,54 +392,69 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(DistillArgs A)
     }
 }
 
-// The gradient of a part of a row.  JOIN: behind k_distill_part, whose maxima and sums it joins, and the first part writes loss and
-// lse (without GRAD that is all there is); otherwise lse is given.
-template <typename T, bool JOIN, bool GRAD>
-__global__ __launch_bounds__(kThreads) void k_distill_grad(DistillArgs A)
+__device__ __forceinline__ bool row_listed(const DistillArgs &A, int64_t row);
+
+// Behind k_distill_part where there is no gradient: a wavefront a row joins its parts
+template <typename T>
+__global__ __launch_bounds__(kWave) void k_distill_join(DistillArgs A)
 {
-    __shared__ Teacher S;
-    __shared__ float keep[GRAD ? kMostTop : 1];
+    const int64_t row = block_number();
+    if (row >= A.m) return;
+    const float w = row_listed(A, row) ? (A.weight ? A.weight[row] : 1.f) : 0.f;
+    Running r;
+    for (int k = threadIdx.x; k < A.splits; k += kWave) r = join(r, Running{A.part_max[row * A.splits + k], A.part_sum[row * A.splits + k]}, A.c);
+    r = join_wave(r, A.c);
+    if (threadIdx.x == 0) {
+        if (A.lse) A.lse[row] = (float)log_sum(r, A.inv_t);
+        A.loss[row] = w == 0.f ? 0.f : loss_of(A, A.part_teacher[2 * row], A.part_teacher[2 * row + 1], r, w);
+    }
+}
+
+// The gradient of a part of a row.  JOIN: behind k_distill_part, whose maxima and sums every wavefront joins, and the first part writes
+// loss and lse; otherwise lse is given.
+template <typename T, bool JOIN>
+__global__ __launch_bounds__(1024) void k_distill_grad(DistillArgs A)
+{
+    __shared__ int any, twice;
+    __shared__ __align__(16) unsigned seen[kSeenWords];
     const int64_t row = part_row();
     if (row >= A.m) return;
     const int64_t V = A.V, from = blockIdx.x * A.per, to = from + A.per < V ? from + A.per : V;
-    constexpr int64_t kStep = (int64_t)kThreads * kVec;
+    const Teacher S = teacher_of(A);
     const T *z = static_cast<const T *>(A.z) + row * A.ldz;
-    if (threadIdx.x < kWave) teacher_part<T, false>(A, row, S, threadIdx.x);
-    __syncthreads();
-    const float w = S.any ? (A.weight ? A.weight[row] : 1.f) : 0.f;
-    Running r;
-    if (JOIN) {
-        for (int k = 0; k < A.splits; ++k) r = join(r, Running{A.part_max[row * A.splits + k], A.part_sum[row * A.splits + k]}, A.c);
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            if (A.lse) A.lse[row] = (float)log_sum(r, A.inv_t);
-            A.loss[row] = w == 0.f ? 0.f : loss_of(A, A.part_teacher[2 * row], A.part_teacher[2 * row + 1], r, w);
+    // z of the listed columns too, before `out`, which may be z, is written
+    if (threadIdx.x < kWave) {
+        const TeacherSums R = teacher_part<T>(A, row, S, threadIdx.x, seen);
+        if (threadIdx.x == 0) {
+            any = R.any;
+            twice = R.twice;
         }
     }
-    if (!GRAD) return;
-    T *out = static_cast<T *>(A.out) + row * A.ldo;
-    if (w == 0.f) {
-        for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += kStep) fill8(out, j, to);
-        return;
-    }
-    for (int j = threadIdx.x; j < A.top; j += kThreads) {
-        const int id = S.id[j];
-        keep[j] = id >= from && id < to ? static_cast<float>(z[id]) : 0.f;
+    Running r;
+    if (JOIN) {
+        const int lane = threadIdx.x % kWave;
+        for (int k = lane; k < A.splits; k += kWave) r = join(r, Running{A.part_max[row * A.splits + k], A.part_sum[row * A.splits + k]}, A.c);
+        r = join_wave(r, A.c);
     }
     __syncthreads();
+    const float w = any ? (A.weight ? A.weight[row] : 1.f) : 0.f;
+    if (JOIN && blockIdx.x == 0 && threadIdx.x == 0) {
+        if (A.lse) A.lse[row] = (float)log_sum(r, A.inv_t);
+        A.loss[row] = w == 0.f ? 0.f : loss_of(A, A.part_teacher[2 * row], A.part_teacher[2 * row + 1], r, w);
+    }
+    T *out = static_cast<T *>(A.out) + row * A.ldo;
+    if (w == 0.f) {
+        write_zeros(A, out, from, to);
+        return;
+    }
     const float wt = w * A.temperature;
     const auto scaled = [&] {
         if constexpr (JOIN) return by_max(r, A.c, wt);
         else return by_lse<T>(A, row, wt);
     }();
-    for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += kStep) {
-        const Raw8<T> x = at8(z, j, to);
-        float v[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = scaled(static_cast<float>(x.v[i]));
-        store8_of<T>(out + j, v, to - j);
-    }
+    write_scaled(A, z, out, from, to, scaled);
     __syncthreads();
-    subtract_teacher(A, S, keep, out, from, to, wt, scaled);
+    subtract_teacher(A, S, out, from, to, wt, twice, scaled);
 }
 
 // ------------------------------------------------------------------ Hessian-vector product
@@ -405,78 +470,95 @@ __device__ __forceinline__ bool row_listed(const DistillArgs &A, int64_t row)
     return __syncthreads_or(any);
 }
 
-template <typename T, int CH>
-__global__ __launch_bounds__(kThreads) void k_distill_hv_row(DistillArgs A)
+// The same values, of which the compiler no longer knows what it has computed from them: exponentials are taken again where their
+// registers would cost a workgroup.
+template <typename T>
+__device__ __forceinline__ void forget(Raw8<T> &r)
 {
+    typedef int words __attribute__((ext_vector_type(4)));
+    words w[sizeof(r) / 16];
+    __builtin_memcpy(w, &r, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(r) / 16; ++i) asm volatile("" : "+v"(w[i]));
+    __builtin_memcpy(&r, w, sizeof(r));
+}
+
+// CH > 0: z and u of a row stay in registers, CH chunks of eight a thread; 0: they are read again.
+template <typename T, int CH, bool PAST>
+__global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_hv_row(DistillArgs A)
+{
+    constexpr bool kAnew = CH * sizeof(T) >= 8;   // 32 registers hold z and u (two workgroups of 1024 a compute unit), or 64
     __shared__ float room[kMostWaves];
     const int64_t row = block_number();
     if (row >= A.m) return;
     const int64_t V = A.V;
-    constexpr int64_t kStep = (int64_t)kThreads * kVec;
+    const int64_t step = CH > 1 ? 1024 * kVec : block_step();   // CH > 1: launched with 1024 threads
     T *out = static_cast<T *>(A.out) + row * A.ldo;
     const float w = row_listed(A, row) ? (A.weight ? A.weight[row] : 1.f) : 0.f;
     if (w == 0.f) {
-        for (int64_t j = (int64_t)threadIdx.x * kVec; j < V; j += kStep) fill8(out, j, V);
+        write_zeros(A, out, 0, V);
         return;
     }
     const T *z = static_cast<const T *>(A.z) + row * A.ldz, *u = static_cast<const T *>(A.u) + row * A.ldu;
     const ByLse<T> p = by_lse<T>(A, row, 1.f);
     Raw8<T> zr[CH ? CH : 1], ur[CH ? CH : 1];
     float dot = 0.f;
-    auto dot8 = [&](const Raw8<T> &x, const Raw8<T> &y, int64_t j) {
+    auto dot8 = [&](const Raw8<T> &x, const Raw8<T> &y) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
-            if (j + i < V) dot = fmaf(p(static_cast<float>(x.v[i])), static_cast<float>(y.v[i]), dot);
+            dot = fmaf(p(static_cast<float>(x.v[i])), static_cast<float>(y.v[i]), dot);
     };
     auto write8 = [&](const Raw8<T> &x, const Raw8<T> &y, int64_t j) {
         float v[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = w * (p(static_cast<float>(x.v[i])) * (static_cast<float>(y.v[i]) - dot));
-        store8_of<T>(out + j, v, V - j);
+        store8_of<T, PAST>(out + j, v, V - j);
     };
     if (CH) {
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t j = threadIdx.x * kVec + k * kStep;
+            const int64_t j = threadIdx.x * kVec + k * step;
             if (j < V) {
                 zr[k] = at8(z, j, V);
-                ur[k] = at8(u, j, V);
+                ur[k] = at8(u, j, V, 0.f);
             }
         }
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t j = threadIdx.x * kVec + k * kStep;
-            if (j < V) dot8(zr[k], ur[k], j);
+            const int64_t j = threadIdx.x * kVec + k * step;
+            if (j < V) dot8(zr[k], ur[k]);
         }
     } else {
-        for (int64_t j = (int64_t)threadIdx.x * kVec; j < V; j += kStep) dot8(at8(z, j, V), at8(u, j, V), j);
+        over_rows(z, u, 0, V, [&](int64_t, const Raw8<T> &x, const Raw8<T> &y) { dot8(x, y); });
     }
     dot = block_sumf(dot, room);
     if (CH) {
+        if (kAnew) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) forget(zr[k]);
+        }
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int64_t j = threadIdx.x * kVec + k * kStep;
+            const int64_t j = threadIdx.x * kVec + k * step;
             if (j < V) write8(zr[k], ur[k], j);
         }
     } else {
-        for (int64_t j = (int64_t)threadIdx.x * kVec; j < V; j += kStep) write8(at8(z, j, V), at8(u, j, V), j);
+        over_rows(z, u, 0, V, [&](int64_t j, const Raw8<T> &x, const Raw8<T> &y) { write8(x, y, j); });
     }
 }
 
 // FIRST: p.u of the parts; otherwise the product, behind that
 template <typename T, bool FIRST>
-__global__ __launch_bounds__(kThreads) void k_distill_hv_part(DistillArgs A)
+__global__ __launch_bounds__(1024) void k_distill_hv_part(DistillArgs A)
 {
     __shared__ float room[kMostWaves];
     const int64_t row = part_row();
     if (row >= A.m) return;
     const int64_t V = A.V, from = blockIdx.x * A.per, to = from + A.per < V ? from + A.per : V;
-    constexpr int64_t kStep = (int64_t)kThreads * kVec;
     T *out = static_cast<T *>(A.out) + row * A.ldo;
     const float w = row_listed(A, row) ? (A.weight ? A.weight[row] : 1.f) : 0.f;
     if (w == 0.f) {
-        if (!FIRST)
-            for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += kStep) fill8(out, j, to);
+        if (!FIRST) write_zeros(A, out, from, to);
         return;
     }
     const T *z = static_cast<const T *>(A.z) + row * A.ldz, *u = static_cast<const T *>(A.u) + row * A.ldu;
@@ -484,17 +566,16 @@ __global__ __launch_bounds__(kThreads) void k_distill_hv_part(DistillArgs A)
     float dot = 0.f;
     if (!FIRST)
         for (int k = 0; k < A.splits; ++k) dot += A.part_sum[row * A.splits + k];
-    for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += kStep) {
-        const Raw8<T> x = at8(z, j, to), y = at8(u, j, to);
+    over_rows(z, u, from, to, [&](int64_t j, const Raw8<T> &x, const Raw8<T> &y) {
         float v[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const float e = p(static_cast<float>(x.v[i])), f = static_cast<float>(y.v[i]);
-            if (FIRST) dot = j + i < to ? fmaf(e, f, dot) : dot;
+            if (FIRST) dot = fmaf(e, f, dot);
             else v[i] = w * (e * (f - dot));
         }
         if (!FIRST) store8_of<T>(out + j, v, to - j);
-    }
+    });
     if (FIRST) {
         dot = block_sumf(dot, room);
         if (threadIdx.x == 0) A.part_sum[row * A.splits + blockIdx.x] = dot;
@@ -502,6 +583,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_hv_part(DistillArgs A)
 }
 
 // ------------------------------------------------------------------ launches
+constexpr double kPast = 32e6;         // bytes of an output above which it goes past the caches: what the L2s hold together
 constexpr int64_t kLeastPart = 4096;   // columns of a part: one chunk of eight a thread
 constexpr int64_t kWanted = 1024;      // workgroups that fill the device: four of kThreads a compute unit
 
@@ -524,36 +606,28 @@ dim3 part_grid(const DistillArgs &A)
 
 int64_t work_of(int64_t m, int64_t V) { return parts_of(m, V) > 1 ? ceil_div(m * (16 + 2 * 4 * (int64_t)parts_of(m, V)), 16) * 16 : 0; }
 
-template <typename T, bool GRAD>
-int distill_rows(const DistillArgs &A, hipStream_t st)
-{
-    const dim3 grid = block_grid(A.m);
-    constexpr int64_t kStep = (int64_t)kThreads * kVec;
-    if (A.V <= kStep) k_distill_row<T, 1, GRAD><<<grid, kThreads, 0, st>>>(A);
-    else if (A.V <= 4 * kStep) k_distill_row<T, 4, GRAD><<<grid, kThreads, 0, st>>>(A);
-    else if (A.V <= 8 * kStep && sizeof(T) == 2) k_distill_row<T, sizeof(T) == 2 ? 8 : 4, GRAD><<<grid, kThreads, 0, st>>>(A);
-    else k_distill_row<T, 0, GRAD><<<grid, kThreads, 0, st>>>(A);
-    TRON_HIP(hipGetLastError());
-    return TRON_OK;
-}
+// Threads of a workgroup over a row, with so many chunks of eight each, up to 1024.  Eight: the barriers of rows of some thousand columns wait
+// for fewer, and long rows have few workgroups under way, whose rows are still in the caches when they are read again.
+unsigned row_threads(int64_t V, int chunks) { return (unsigned)std::min<int64_t>(1024, ceil_div(ceil_div(V, kVec * chunks), kWave) * kWave); }
 
 template <typename T>
 int distill_typed(DistillArgs A, void *work, hipStream_t st)
 {
     const int parts = parts_of(A.m, A.V);
-    if (parts == 1) return A.out ? distill_rows<T, true>(A, st) : distill_rows<T, false>(A, st);
+    if (parts == 1) {
+        const unsigned threads = row_threads(A.V, 8);
+        if (A.out) k_distill_row<T, true><<<block_grid(A.m), threads, teacher_bytes(A), st>>>(A);
+        else k_distill_row<T, false><<<block_grid(A.m), threads, teacher_bytes(A), st>>>(A);
+        TRON_HIP(hipGetLastError());
+        return TRON_OK;
+    }
     set_parts(A, parts);
     A.part_teacher = static_cast<double *>(work);
     A.part_max = reinterpret_cast<float *>(A.part_teacher + 2 * A.m);
     A.part_sum = A.part_max + A.m * A.splits;
-    k_distill_part<T><<<part_grid(A), kThreads, 0, st>>>(A);
-    if (A.out) {
-        k_distill_grad<T, true, true><<<part_grid(A), kThreads, 0, st>>>(A);
-    } else {
-        dim3 grid = part_grid(A);
-        grid.x = 1;
-        k_distill_grad<T, true, false><<<grid, kWave, 0, st>>>(A);
-    }
+    k_distill_part<T><<<part_grid(A), kThreads, teacher_bytes(A), st>>>(A);
+    if (A.out) k_distill_grad<T, true><<<part_grid(A), kThreads, teacher_bytes(A), st>>>(A);
+    else k_distill_join<T><<<block_grid(A.m), kWave, 0, st>>>(A);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -562,7 +636,7 @@ template <typename T>
 int distill_grad_typed(DistillArgs A, hipStream_t st)
 {
     set_parts(A, parts_of(A.m, A.V));
-    k_distill_grad<T, false, true><<<part_grid(A), kThreads, 0, st>>>(A);
+    k_distill_grad<T, false><<<part_grid(A), std::min<unsigned>(kThreads, row_threads(A.per, 8)), teacher_bytes(A), st>>>(A);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -573,11 +647,18 @@ int distill_hv_typed(DistillArgs A, void *work, hipStream_t st)
     const int parts = parts_of(A.m, A.V);
     if (parts == 1) {
         const dim3 grid = block_grid(A.m);
-        constexpr int64_t kStep = (int64_t)kThreads * kVec;
-        if (A.V <= kStep) k_distill_hv_row<T, 1><<<grid, kThreads, 0, st>>>(A);
-        else if (A.V <= 4 * kStep) k_distill_hv_row<T, 4><<<grid, kThreads, 0, st>>>(A);
-        else if (A.V <= 8 * kStep && sizeof(T) == 2) k_distill_hv_row<T, sizeof(T) == 2 ? 8 : 4><<<grid, kThreads, 0, st>>>(A);
-        else k_distill_hv_row<T, 0><<<grid, kThreads, 0, st>>>(A);
+        const unsigned threads = row_threads(A.V, 1);
+        const int64_t chunks = ceil_div(A.V, (int64_t)threads * kVec);
+        constexpr int kHeld = sizeof(T) == 2 ? 8 : 4;   // 64 registers
+        auto launch = [&](auto past) {
+            if (chunks == 1) k_distill_hv_row<T, 1, past.value><<<grid, threads, 0, st>>>(A);
+            else if (chunks <= kHeld / 4) k_distill_hv_row<T, kHeld / 4, past.value><<<grid, threads, 0, st>>>(A);
+            else if (chunks <= kHeld / 2) k_distill_hv_row<T, kHeld / 2, past.value><<<grid, threads, 0, st>>>(A);
+            else if (chunks <= kHeld) k_distill_hv_row<T, kHeld, past.value><<<grid, threads, 0, st>>>(A);
+            else k_distill_hv_row<T, 0, past.value><<<grid, threads, 0, st>>>(A);
+        };
+        if (A.past) launch(std::true_type{});
+        else launch(std::false_type{});
     } else {
         set_parts(A, parts);
         A.part_sum = static_cast<float *>(work);
@@ -622,6 +703,7 @@ int check(const char *name, int64_t m, int64_t V, int type, const void *z, int64
     A.lists = K >= 0;
     A.top = K > 0 ? (int)K : 0;
     A.ids64 = id_bytes == 8;
+    A.past = (double)m * (double)V * type_bytes(type) > kPast;
     A.temperature = (float)temperature;
     A.inv_t = 1.0 / temperature;
     A.c = (float)(kLog2e / temperature);

@@ -60,20 +60,19 @@ __device__ __forceinline__ void store_first(T *p, int n, const Raw8<T> &r)
         if (i < n) p[i] = r.v[i];
 }
 
-// rounded to nearest, ties to even; above the largest finite value of f16: infinity
+// past the caches: for matrices that no cache holds until they are read, so that what others still read stays there
 template <typename T>
-__device__ __forceinline__ void store8_of(T *p, const float *v, int64_t n)
+__device__ __forceinline__ void store8_past(T *p, const Raw8<T> &r)
 {
-    Raw8<T> r;
+    typedef int words __attribute__((ext_vector_type(4), aligned(2)));
+    const words *w = reinterpret_cast<const words *>(&r);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) r.v[i] = static_cast<T>(v[i]);
-    if (n >= kVec) store8(p, r);
-    else store_first(p, (int)n, r);
+    for (int i = 0; i < (int)sizeof(r) / 16; ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<words *>(p) + i);
 }
 
 // e4m3 (finite numbers up to 448, NaN), rounded to nearest, ties to even
-template <>
-__device__ __forceinline__ void store8_of<e4m3>(e4m3 *p, const float *v, int64_t n)
+template <bool PAST>
+__device__ __forceinline__ void store8_e4m3(e4m3 *p, const float *v, int64_t n)
 {
     int lo = 0, hi = 0;
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
@@ -81,13 +80,31 @@ __device__ __forceinline__ void store8_of<e4m3>(e4m3 *p, const float *v, int64_t
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
     if (n >= kVec) {
-        const int both[2] = {lo, hi};
-        __builtin_memcpy(p, both, 8);
+        typedef int words __attribute__((ext_vector_type(2), aligned(1)));
+        const words both = {lo, hi};
+        if (PAST) __builtin_nontemporal_store(both, reinterpret_cast<words *>(p));
+        else *reinterpret_cast<words *>(p) = both;
         return;
     }
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
         if (i < n) p[i].bits = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+}
+
+// rounded to nearest, ties to even; above the largest finite value of f16: infinity
+template <typename T, bool PAST = false>
+__device__ __forceinline__ void store8_of(T *p, const float *v, int64_t n)
+{
+    if constexpr (sizeof(T) == 1) {
+        store8_e4m3<PAST>(p, v, n);
+    } else {
+        Raw8<T> r;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) r.v[i] = static_cast<T>(v[i]);
+        if (n < kVec) store_first(p, (int)n, r);
+        else if (PAST) store8_past(p, r);
+        else store8(p, r);
+    }
 }
 
 // ---------------------------------------------------------------- sums and maxima in 32 bits
