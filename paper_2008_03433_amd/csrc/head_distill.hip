@@ -234,11 +234,10 @@ __device__ __forceinline__ float loss_of(const DistillArgs &A, double terms, dou
 }
 
 // ------------------------------------------------------------------ whole rows
-// eight elements from j on; from `to` on they are `fill`
 template <typename T>
 __device__ __forceinline__ Raw8<T> at8(const T *row, int64_t j, int64_t to, float fill = -INFINITY)
 {
-    return j + kVec <= to ? load8(row + j) : load_first(row + j, (int)(to - j), static_cast<T>(fill));
+    return load_row8(row, j, to, static_cast<T>(fill));
 }
 
 // f p = f exp2((z - m) c) / s where the row's maximum m and sum s are known, with per = f / s
@@ -583,7 +582,6 @@ __global__ __launch_bounds__(1024) void k_distill_hv_part(DistillArgs A)
 }
 
 // ------------------------------------------------------------------ launches
-constexpr double kPast = 32e6;         // bytes of an output above which it goes past the caches: what the L2s hold together
 constexpr int64_t kLeastPart = 4096;   // columns of a part: one chunk of eight a thread
 constexpr int64_t kWanted = 1024;      // workgroups that fill the device: four of kThreads a compute unit
 
@@ -703,7 +701,7 @@ int check(const char *name, int64_t m, int64_t V, int type, const void *z, int64
     A.lists = K >= 0;
     A.top = K > 0 ? (int)K : 0;
     A.ids64 = id_bytes == 8;
-    A.past = (double)m * (double)V * type_bytes(type) > kPast;
+    A.past = goes_past(m, V, type_bytes(type));
     A.temperature = (float)temperature;
     A.inv_t = 1.0 / temperature;
     A.c = (float)(kLog2e / temperature);

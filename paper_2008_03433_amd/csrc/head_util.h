@@ -52,6 +52,24 @@ __device__ __forceinline__ Raw8<T> load_first(const T *p, int n, T fill)
     return r;
 }
 
+// Eight elements of a row from j < to on; from `to` on they are `fill`.  A row's end is read with the wide load that ends there, whose
+// elements are moved down: single loads of up to seven elements one after the other hold up the whole workgroup.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_row8(const T *row, int64_t j, int64_t to, T fill)
+{
+    if (j + kVec <= to) return load8(row + j);
+    const int n = (int)(to - j);
+    if (to < kVec) return load_first(row + j, n, fill);
+    Raw8<T> r = load8(row + to - kVec);
+#pragma unroll
+    for (int by = 4; by; by /= 2)
+        if ((kVec - n) & by) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) r.v[i] = i + by < kVec ? r.v[i + by] : fill;
+        }
+    return r;
+}
+
 template <typename T>
 __device__ __forceinline__ void store_first(T *p, int n, const Raw8<T> &r)
 {
@@ -192,6 +210,10 @@ inline bool extent_ok(int64_t rows, int64_t ld, int64_t cols) { return rows < 1 
 
 // `bytes` of a caller's work space, at 16 bytes
 inline bool work_ok(const void *work, int64_t bytes, int64_t needed) { return needed == 0 || (work && bytes >= needed && ((uintptr_t)work & 15) == 0); }
+
+// Whether an output is stored past the caches: above 32 MB, what the eight L2s hold together.  Norm of 16384 x 8192 in bf16 with its sum,
+// output in 8 bits: 233 us through them, 195 us past them.
+inline bool goes_past(int64_t rows, int64_t cols, int64_t bytes) { return (double)rows * (double)cols * (double)bytes > 32e6; }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
