@@ -226,10 +226,137 @@ __device__ __forceinline__ void tile_of(const ProductArgs &A, int64_t block, int
     tn = in / high;
 }
 
+// LDS of a tile: two steps' chunks, or 128 rows of results
 template <int BM, int BN>
 constexpr int kTileLds = 2 * (BM + BN) * 128 > 128 * (BN + 4) * 4 ? 2 * (BM + BN) * 128 : 128 * (BN + 4) * 4;
 
-// A tile of BM x BN, WM x WN wavefronts.
+// a step's products of a wavefront's part of the tile
+template <typename T, int BM, int FM, int FN>
+__device__ __forceinline__ void tile_step(const char *lds, int wm, int wn, int lane, f32x4 (&acc)[FM][FN])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        Fragment<T> a[FM], b[FN];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) a[i] = fragment<T>(*reinterpret_cast<const i32x4 *>(lds + chunk_place(wm * FM * 16 + i * 16 + lane % 16, lane / 16 + 4 * h)));
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            b[j] = fragment<T>(*reinterpret_cast<const i32x4 *>(lds + chunk_place(BM + wn * FN * 16 + j * 16 + lane % 16, lane / 16 + 4 * h)));
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mma<T>(b[j], a[i], acc[i][j]);
+    }
+}
+
+// Lane l holds row l % 16 and columns l / 16 * 4 .. + 3 of a 16 x 16 piece.  Through LDS, 128 rows at a time, to stores of whole lines.
+template <int BM, int BN, int WM, int WN, int FM, int FN>
+__device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, int wn, int lane, const f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int part)
+{
+    constexpr int kThreads = WM * WN * kWave, kRows = BM < 128 ? BM : 128, kPitch = BN + 4;
+    float *out = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int half = 0; half < BM / kRows; ++half) {
+        if (half) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int r = wm * FM * 16 + i * 16 + lane % 16 - half * kRows;
+            if (r >= 0 && r < kRows) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + j * 16 + lane / 16 * 4) = acc[i][j];
+            }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int at = threadIdx.x; at < kRows * BN / kVec; at += kThreads) {
+            const int r = at / (BN / kVec), c = at % (BN / kVec) * kVec;
+            const int64_t i = m0 + half * kRows + r, j = n0 + c;
+            if (i >= E.m || j >= E.n) continue;
+            float v[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] = out[r * kPitch + c + e];
+            put8(E, v, i, j, part);
+        }
+    }
+}
+
+// Every wavefront's loads into LDS have arrived and its reads of LDS are done, for all of the workgroup.
+__device__ __forceinline__ void all_arrived()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// A tile whose operands' rows lie at multiples of 16 bytes and are whole chunks: chunks go from memory to LDS without registers, a step
+// ahead of the products.  A wavefront's load takes eight rows of 128 bytes; which chunk a lane fetches makes the exchange of places.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
+{
+    constexpr int kWaves = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int kX = BM / 8 / kWaves, kW = BN / 8 / kWaves, kStage = (BM + BN) * 128;
+    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "whole loads");
+    extern __shared__ __align__(16) char lds[];
+    const int64_t count = A.tiles_m * A.tiles_n;
+    if (block_number() >= count) return;
+    int64_t tm, tn;
+    tile_of(A, block_number(), tm, tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN;
+    const int part = blockIdx.z;
+    const int64_t k_from = part * A.k_part, k_to = k_from + A.k_part < A.k ? k_from + A.k_part : A.k;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, wm = wave / WN, wn = wave % WN;
+
+    // offsets from the tile's first row; rows past the end repeat the last one, and their results are not stored
+    constexpr unsigned kNowhere = 0x80000000u;   // past the buffer's end: zeros arrive
+    unsigned at[kX + kW];
+    int chunk[kX + kW];
+#pragma unroll
+    for (int i = 0; i < kX + kW; ++i) {
+        const int r = (i < kX ? wave + kWaves * i : wave + kWaves * (i - kX)) * 8 + lane / 8;
+        const int in_lds = i < kX ? r : BM + r;
+        chunk[i] = (lane % 8) ^ ((in_lds >> 1) & 7);
+        const int64_t left = i < kX ? A.x.rows - m0 : A.w.rows - n0;
+        at[i] = (unsigned)((r < left ? r : left - 1) * (i < kX ? A.x.ld : A.w.ld) * (int64_t)sizeof(T)) + chunk[i] * 16;
+    }
+    const __amdgpu_buffer_rsrc_t xs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<T *>(static_cast<const T *>(A.x.p) + m0 * A.x.ld + k_from), 0, 0x7ffffff0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ws = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<T *>(static_cast<const T *>(A.w.p) + n0 * A.w.ld + k_from), 0, 0x7ffffff0, 0x00020000);
+    const int bytes = (int)((k_to - k_from) * (int64_t)sizeof(T));   // of a row
+    auto fetch = [&](char *to, int from) {
+        const int left = bytes - from;   // below 128: the rest of a row
+#pragma unroll
+        for (int i = 0; i < kX + kW; ++i) {
+            const int group = i < kX ? wave + kWaves * i : BM / 8 + wave + kWaves * (i - kX);
+            const unsigned offset = chunk[i] * 16 < left ? at[i] : kNowhere;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kX ? xs : ws, (__attribute__((address_space(3))) void *)(to + group * 1024), 16, offset, from, 0, 0);
+        }
+    };
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // what is fetched and what is read lie apart
+    auto step = [&](const char *__restrict__ now, char *__restrict__ next, int from) {
+        if (from + 128 < bytes) fetch(next, from + 128);
+        tile_step<T, BM, FM, FN>(now, wm, wn, lane, acc);
+    };
+    fetch(lds, 0);
+    for (int from = 0;;) {
+        all_arrived();
+        step(lds, lds + kStage, from);
+        if ((from += 128) >= bytes) break;
+        all_arrived();
+        step(lds + kStage, lds, from);
+        if ((from += 128) >= bytes) break;
+    }
+    __syncthreads();
+    tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
+}
+
+// A tile whose operands lie anywhere: chunks go through registers, which know where a row ends.
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
 {
@@ -281,54 +408,14 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
     for (int64_t k = k_from; k < k_to; k += kStepElems<T>) {
         const bool more = k + kStepElems<T> < k_to;
         if (more) fetch(k + kStepElems<T>);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Fragment<T> a[FM], b[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-                a[i] = fragment<T>(*reinterpret_cast<const i32x4 *>(lds + chunk_place(wm * FM * 16 + i * 16 + lane % 16, lane / 16 + 4 * h)));
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-                b[j] = fragment<T>(*reinterpret_cast<const i32x4 *>(lds + chunk_place(BM + wn * FN * 16 + j * 16 + lane % 16, lane / 16 + 4 * h)));
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mma<T>(b[j], a[i], acc[i][j]);
-        }
+        tile_step<T, BM, FM, FN>(lds, wm, wn, lane, acc);
         __syncthreads();
         if (more) {
             put();
             __syncthreads();
         }
     }
-    // Lane l holds row l % 16 and columns l / 16 * 4 .. + 3 of a 16 x 16 piece.  Through LDS, 128 rows at a time, to stores of whole lines.
-    constexpr int kRows = BM < 128 ? BM : 128, kPitch = BN + 4;
-    float *out = reinterpret_cast<float *>(lds);
-#pragma unroll
-    for (int half = 0; half < BM / kRows; ++half) {
-        if (half) __syncthreads();
-        constexpr int kWaveTall = FM * 16;
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int r = wm * kWaveTall + i * 16 + lane % 16 - half * kRows;
-            if (r >= 0 && r < kRows) {
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + j * 16 + lane / 16 * 4) = acc[i][j];
-            }
-        }
-        __syncthreads();
-#pragma unroll 1
-        for (int at = threadIdx.x; at < kRows * BN / kVec; at += kThreads) {
-            const int r = at / (BN / kVec), c = at % (BN / kVec) * kVec;
-            const int64_t i = m0 + half * kRows + r, j = n0 + c;
-            if (i >= A.E.m || j >= A.E.n) continue;
-            float v[kVec];
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) v[e] = out[r * kPitch + c + e];
-            put8(A.E, v, i, j, part);
-        }
-    }
+    tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
 
 // ------------------------------------------------------------------ few rows
@@ -459,9 +546,21 @@ void launch_few(const ProductArgs &A, dim3 grid, hipStream_t st)
     k_linear_few<T, MT, 4><<<grid, kFewWaves * kWave, 0, st>>>(A);
 }
 
+// whether rows are whole chunks at multiples of 16 bytes, and a tile's offsets and a row's bytes fit 31 bits
+template <typename T>
+bool direct_ok(const Operand &a, int64_t k)
+{
+    return ((uintptr_t)a.p & 15) == 0 && a.ld % kChunkElems<T> == 0 && k % kChunkElems<T> == 0 && (a.ld * 256 + k) * (int64_t)sizeof(T) < 0x7fff0000;
+}
+
 template <typename T, int BM, int BN, int WM, int WN>
 int launch_tile(const ProductArgs &A, dim3 grid, hipStream_t st)
 {
+    if (direct_ok<T>(A.x, A.k) && direct_ok<T>(A.w, A.k)) {
+        TRON_TRY(allow_lds(k_linear_direct<T, BM, BN, WM, WN>, kTileLds<BM, BN>));
+        k_linear_direct<T, BM, BN, WM, WN><<<grid, WM * WN * kWave, kTileLds<BM, BN>, st>>>(A);
+        return TRON_OK;
+    }
     TRON_TRY(allow_lds(k_linear_tile<T, BM, BN, WM, WN>, kTileLds<BM, BN>));
     k_linear_tile<T, BM, BN, WM, WN><<<grid, WM * WN * kWave, kTileLds<BM, BN>, st>>>(A);
     return TRON_OK;
