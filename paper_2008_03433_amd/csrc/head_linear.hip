@@ -230,6 +230,35 @@ __device__ __forceinline__ void tile_of(const ProductArgs &A, int64_t block, int
 template <int BM, int BN>
 constexpr int kTileLds = 2 * (BM + BN) * 128 > 128 * (BN + 4) * 4 ? 2 * (BM + BN) * 128 : 128 * (BN + 4) * 4;
 
+// What a lane has of half a step: four of the eight chunks of a row
+template <int FM, int FN>
+struct Half {
+    i32x4 a[FM], b[FN];
+};
+
+template <int BM, int FM, int FN>
+__device__ __forceinline__ void load_half(Half<FM, FN> &f, const char *lds, int h, int wm, int wn, int lane)
+{
+#pragma unroll
+    for (int j = 0; j < FN; ++j) f.b[j] = *reinterpret_cast<const i32x4 *>(lds + chunk_place(BM + wn * FN * 16 + j * 16 + lane % 16, lane / 16 + 4 * h));
+#pragma unroll
+    for (int i = 0; i < FM; ++i) f.a[i] = *reinterpret_cast<const i32x4 *>(lds + chunk_place(wm * FM * 16 + i * 16 + lane % 16, lane / 16 + 4 * h));
+}
+
+template <typename T, int FM, int FN>
+__device__ __forceinline__ void mma_half(const Half<FM, FN> &f, f32x4 (&acc)[FM][FN])
+{
+    Fragment<T> b[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) b[j] = fragment<T>(f.b[j]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const Fragment<T> a = fragment<T>(f.a[i]);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mma<T>(b[j], a, acc[i][j]);
+    }
+}
+
 // a step's products of a wavefront's part of the tile
 template <typename T, int BM, int FM, int FN>
 __device__ __forceinline__ void tile_step(const char *lds, int wm, int wn, int lane, f32x4 (&acc)[FM][FN])
@@ -338,20 +367,48 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // what is fetched and what is read lie apart
-    auto step = [&](const char *__restrict__ now, char *__restrict__ next, int from) {
-        if (from + 128 < bytes) fetch(next, from + 128);
-        tile_step<T, BM, FM, FN>(now, wm, wn, lane, acc);
+    // Half a step is read from LDS while the other half's products run.  The wait for the next step lies in the middle: behind it
+    // nobody reads this step's chunks any more, and the step after the next is fetched to their place.
+    auto all = [&](char *__restrict__ even, char *__restrict__ odd) {
+        Half<FM, FN> first, second;
+        auto one = [&](char *now, char *next, int from) {
+            load_half<BM>(second, now, 1, wm, wn, lane);
+            __builtin_amdgcn_sched_barrier(0);
+            mma_half<T>(first, acc);
+            all_arrived();
+            if (from + 256 < bytes) fetch(now, from + 256);
+            if (from + 128 < bytes) load_half<BM>(first, next, 0, wm, wn, lane);
+            __builtin_amdgcn_sched_barrier(0);
+            mma_half<T>(second, acc);
+        };
+        fetch(even, 0);
+        all_arrived();
+        if (bytes > 128) fetch(odd, 128);
+        load_half<BM>(first, even, 0, wm, wn, lane);
+        for (int from = 0;;) {
+            one(even, odd, from);
+            if ((from += 128) >= bytes) break;
+            one(odd, even, from);
+            if ((from += 128) >= bytes) break;
+        }
     };
-    fetch(lds, 0);
-    for (int from = 0;;) {
-        all_arrived();
-        step(lds, lds + kStage, from);
-        if ((from += 128) >= bytes) break;
-        all_arrived();
-        step(lds + kStage, lds, from);
-        if ((from += 128) >= bytes) break;
-    }
+    // e4m3 in tiles of 256: its operands as bf16 leave no registers for a second half
+    auto plain = [&](char *__restrict__ even, char *__restrict__ odd) {
+        auto one = [&](char *now, char *next, int from) {
+            all_arrived();
+            if (from + 128 < bytes) fetch(next, from + 128);
+            tile_step<T, BM, FM, FN>(now, wm, wn, lane, acc);
+        };
+        fetch(even, 0);
+        for (int from = 0;;) {
+            one(even, odd, from);
+            if ((from += 128) >= bytes) break;
+            one(odd, even, from);
+            if ((from += 128) >= bytes) break;
+        }
+    };
+    if constexpr (sizeof(T) == 1 && BM == 256) plain(lds, lds + kStage);
+    else all(lds, lds + kStage);
     __syncthreads();
     tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
