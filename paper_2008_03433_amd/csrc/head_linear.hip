@@ -125,22 +125,35 @@ __device__ __forceinline__ void store_out(void *base, int out, int64_t at, const
     else store8_of<_Float16>(static_cast<_Float16 *>(base) + at, v, n);
 }
 
+// what eight columns have
+struct Columns {
+    float scale[kVec], bias[kVec];
+};
+__device__ __forceinline__ Columns columns_of(const Epilogue &E, int64_t j)
+{
+    Columns c;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+        c.scale[e] = 1.f;
+        c.bias[e] = 0.f;
+    }
+    if (j < E.n && E.w_scale) load_as<float>(c.scale, E.w_scale, j, E.n - j);
+    if (j < E.n && E.bias) load_as<float>(c.bias, E.bias, j, E.n - j);
+    return c;
+}
+
 // eight neighbouring sums of a row
-__device__ __forceinline__ void finish8(const Epilogue &E, float *v, int64_t i, int64_t j)
+__device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, float *v, int64_t i, int64_t j)
 {
     const int64_t n = E.n - j;
     float f[kVec];
     if (E.x_scale) {
         const float xs = E.x_scale[i];
-        load_as<float>(f, E.w_scale, j, n);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] *= xs * f[e];
+        for (int e = 0; e < kVec; ++e) v[e] *= xs * C.scale[e];
     }
-    if (E.bias) {
-        load_as<float>(f, E.bias, j, n);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] += f[e];
-    }
+    for (int e = 0; e < kVec; ++e) v[e] += C.bias[e];
     if (E.pre) store_out(E.pre, E.out, i * E.ldpre + j, v, n);
     if (E.act != TRON_ACT_NONE) {
 #pragma unroll
@@ -154,10 +167,10 @@ __device__ __forceinline__ void finish8(const Epilogue &E, float *v, int64_t i, 
     store_out(E.y, E.out, i * E.ldy + j, v, n);
 }
 
-__device__ __forceinline__ void put8(const Epilogue &E, float *v, int64_t i, int64_t j, int part)
+__device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float *v, int64_t i, int64_t j, int part)
 {
     if (E.part) store8_of<float>(E.part + ((int64_t)part * E.m + i) * E.n + j, v, E.n - j);
-    else finish8(E, v, i, j);
+    else finish8(E, C, v, i, j);
 }
 
 // behind a product whose inner index was cut, or is empty: eight sums a thread
@@ -174,7 +187,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_join(Epilogue E, int parts)
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[e] += f[e];
     }
-    finish8(E, v, i, j);
+    finish8(E, columns_of(E, j), v, i, j);
 }
 
 // ------------------------------------------------------------------ tiles
@@ -278,12 +291,17 @@ __device__ __forceinline__ void tile_step(const char *lds, int wm, int wn, int l
     }
 }
 
-// Lane l holds row l % 16 and columns l / 16 * 4 .. + 3 of a 16 x 16 piece.  Through LDS, 128 rows at a time, to stores of whole lines.
+// Lane l holds row l % 16 and columns l / 16 * 4 .. + 3 of a 16 x 16 piece.  Through LDS, 128 rows at a time, to stores of whole lines: a
+// thread keeps its eight columns and takes rows that lie apart, several at once.
 template <int BM, int BN, int WM, int WN, int FM, int FN>
 __device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, int wn, int lane, const f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int part)
 {
-    constexpr int kThreads = WM * WN * kWave, kRows = BM < 128 ? BM : 128, kPitch = BN + 4;
+    constexpr int kThreads = WM * WN * kWave, kRows = BM < 128 ? BM : 128, kPitch = BN + 4, kAcross = BN / kVec, kDown = kThreads / kAcross;
+    static_assert(kThreads % kAcross == 0 && kRows % (4 * kDown) == 0, "whole rows at once");
     float *out = reinterpret_cast<float *>(lds);
+    const int c = threadIdx.x % kAcross * kVec;
+    const int64_t j = n0 + c;
+    const Columns C = columns_of(E, j);
 #pragma unroll
     for (int half = 0; half < BM / kRows; ++half) {
         if (half) __syncthreads();
@@ -292,19 +310,26 @@ __device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, i
             const int r = wm * FM * 16 + i * 16 + lane % 16 - half * kRows;
             if (r >= 0 && r < kRows) {
 #pragma unroll
-                for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + j * 16 + lane / 16 * 4) = acc[i][j];
+                for (int k = 0; k < FN; ++k) *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + k * 16 + lane / 16 * 4) = acc[i][k];
             }
         }
         __syncthreads();
+        if (j >= E.n) continue;
 #pragma unroll 1
-        for (int at = threadIdx.x; at < kRows * BN / kVec; at += kThreads) {
-            const int r = at / (BN / kVec), c = at % (BN / kVec) * kVec;
-            const int64_t i = m0 + half * kRows + r, j = n0 + c;
-            if (i >= E.m || j >= E.n) continue;
-            float v[kVec];
+        for (int r = threadIdx.x / kAcross; r < kRows; r += 4 * kDown) {
+            float v[4][kVec];
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[e] = out[r * kPitch + c + e];
-            put8(E, v, i, j, part);
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < kVec; e += 4) {
+                    const f32x4 four = *reinterpret_cast<const f32x4 *>(out + (r + q * kDown) * kPitch + c + e);
+                    v[q][e] = four[0], v[q][e + 1] = four[1], v[q][e + 2] = four[2], v[q][e + 3] = four[3];
+                }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t i = m0 + half * kRows + r + q * kDown;
+                if (i < E.m) put8(E, C, v[q], i, j, part);
+            }
         }
     }
 }
@@ -548,7 +573,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
             v[e] = room[0][r][c + e];
             for (int u = 1; u < kFewWaves; ++u) v[e] += room[u][r][c + e];
         }
-        put8(A.E, v, r, n0 + c, part);
+        put8(A.E, columns_of(A.E, n0 + c), v, r, n0 + c, part);
     }
 }
 
@@ -580,7 +605,8 @@ Plan linear_plan(int64_t m, int64_t n, int64_t k, int type)
         const int64_t b = P.shape == SHAPE_256 ? 256 : 128;
         P.tiles_m = ceil_div(m, b);
         P.tiles_n = ceil_div(n, b);
-        most = std::min<int64_t>(steps / 8, 2 * kUnits / (P.tiles_m * P.tiles_n));
+        // a compute unit holds one workgroup of the large tiles, two of the small ones
+        most = std::min<int64_t>(steps / 8, (P.shape == SHAPE_256 ? 1 : 2) * kUnits / (P.tiles_m * P.tiles_n));
     }
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(most, 64));
     P.k_part = ceil_div(steps, parts) * step;
