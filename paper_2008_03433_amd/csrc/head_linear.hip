@@ -159,52 +159,91 @@ __device__ __forceinline__ Columns columns_of(const Epilogue &E, int64_t j)
     return c;
 }
 
-// eight neighbouring sums of a row
-__device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, float *v, int64_t i, int64_t j)
+// N times eight neighbouring sums, of rows that lie `step` apart: what is read before what is written
+template <int N>
+__device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, float (&v)[N][kVec], int64_t i, int64_t step, int64_t j)
 {
     const int64_t n = E.n - j;
-    float f[kVec];
-    if (E.x_scale) {
-        const float xs = E.x_scale[i];
+    float f[N][kVec], xs[N];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] *= xs * C.scale[e];
+    for (int q = 0; q < N; ++q) {
+        const int64_t row = i + q * step;
+        if (row >= E.m) break;
+        if (E.residual) load_out(f[q], E.residual, E.out, row * E.ldr + j, n);
+        if (E.x_scale) xs[q] = E.x_scale[row];
     }
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) v[e] += C.bias[e];
-    if (E.pre) store_out(E.pre, E.out, i * E.ldpre + j, v, n);
-    if (E.act != TRON_ACT_NONE) {
+    for (int q = 0; q < N; ++q) {
+        const int64_t row = i + q * step;
+        if (row >= E.m) break;
+        if (E.x_scale) {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] = act_of(v[e], E.act);
-    }
-    if (E.residual) {
-        load_out(f, E.residual, E.out, i * E.ldr + j, n);
+            for (int e = 0; e < kVec; ++e) v[q][e] *= xs[q] * C.scale[e];
+        }
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] += f[e];
+        for (int e = 0; e < kVec; ++e) v[q][e] += C.bias[e];
+        if (E.pre) store_out(E.pre, E.out, row * E.ldpre + j, v[q], n);
+        if (E.act != TRON_ACT_NONE) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[q][e] = act_of(v[q][e], E.act);
+        }
+        if (E.residual) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[q][e] += f[q][e];
+        }
+        store_out(E.y, E.out, row * E.ldy + j, v[q], n);
     }
-    store_out(E.y, E.out, i * E.ldy + j, v, n);
 }
 
-__device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float *v, int64_t i, int64_t j, int part)
+template <int N>
+__device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float (&v)[N][kVec], int64_t i, int64_t step, int64_t j, int part)
 {
-    if (E.part) store8_of<float>(E.part + ((int64_t)part * E.m + i) * E.n + j, v, E.n - j);
-    else finish8(E, C, v, i, j);
+    if (E.part) {
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+            if (i + q * step < E.m) store8_of<float>(E.part + ((int64_t)part * E.m + i + q * step) * E.n + j, v[q], E.n - j);
+    } else {
+        finish8(E, C, v, i, step, j);
+    }
 }
 
-// behind a product whose inner index was cut, or is empty: eight sums a thread
+// behind a product whose inner index was cut, or is empty: eight sums a thread, four parts at a time, blockIdx.y and z the row
 __global__ __launch_bounds__(kBlock) void k_linear_join(Epilogue E, int parts)
 {
-    const int64_t per_row = (E.n + kVec - 1) / kVec, at = block_number() * kBlock + threadIdx.x;
-    if (at >= per_row * E.m) return;
-    const int64_t i = at / per_row, j = at % per_row * kVec;
-    float v[kVec], f[kVec];
+    const int64_t i = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, j = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * kVec;
+    if (i >= E.m || j >= E.n) return;
+    const Columns C = columns_of(E, j);
+    const int64_t n = E.n - j, each = E.m * E.n;
+    const float *p = E.part + i * E.n + j;
+    float v[1][kVec];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) v[e] = 0.f;
-    for (int p = 0; p < parts; ++p) {
-        load_as<float>(f, E.part, ((int64_t)p * E.m + i) * E.n + j, E.n - j);
+    for (int e = 0; e < kVec; ++e) v[0][e] = 0.f;
+    int q = 0;
+    for (; q + 4 <= parts; q += 4) {
+        float f[4][kVec];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] += f[e];
+        for (int r = 0; r < 4; ++r) load_as<float>(f[r], p + (q + r) * each, 0, n);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[0][e] += f[r][e];
     }
-    finish8(E, columns_of(E, j), v, i, j);
+    for (; q < parts; ++q) {
+        float f[kVec];
+        load_as<float>(f, p + q * each, 0, n);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[0][e] += f[e];
+    }
+    finish8(E, C, v, i, 0, j);
+}
+
+int join_parts(const Epilogue &E, int parts, hipStream_t st)
+{
+    const int64_t chunks = ceil_div(E.n, kVec), y = std::min<int64_t>(E.m, 32768);
+    const unsigned threads = (unsigned)std::min<int64_t>(kBlock, ceil_div(chunks, kWave) * kWave);
+    k_linear_join<<<dim3((unsigned)ceil_div(chunks, threads), (unsigned)y, (unsigned)ceil_div(E.m, y)), threads, 0, st>>>(E, parts);
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
 }
 
 // ------------------------------------------------------------------ tiles
@@ -342,11 +381,7 @@ __device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, i
                     const f32x4 four = *reinterpret_cast<const f32x4 *>(out + (r + q * kDown) * kPitch + c + e);
                     v[q][e] = four[0], v[q][e + 1] = four[1], v[q][e + 2] = four[2], v[q][e + 3] = four[3];
                 }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t i = m0 + half * kRows + r + q * kDown;
-                if (i < E.m) put8(E, C, v[q], i, j, part);
-            }
+            put8(E, C, v, m0 + half * kRows + r, kDown, j, part);
         }
     }
 }
@@ -393,7 +428,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
         const_cast<T *>(static_cast<const T *>(A.x.p) + m0 * A.x.ld + k_from), 0, 0x7ffffff0, 0x00020000);
     const __amdgpu_buffer_rsrc_t ws = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<T *>(static_cast<const T *>(A.w.p) + n0 * A.w.ld + k_from), 0, 0x7ffffff0, 0x00020000);
-    const int bytes = (int)((k_to - k_from) * (int64_t)sizeof(T));   // of a row
+    const int bytes = (int)((k_to - k_from) * (int64_t)sizeof(T)), steps = (bytes + 127) / 128;   // of a row
     auto fetch = [&](char *to, int from) {
         const int left = bytes - from;   // below 128: the rest of a row
 #pragma unroll
@@ -412,15 +447,15 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
     // nobody reads this step's chunks any more, and the step after the next is fetched to their place.
     auto all = [&](char *__restrict__ even, char *__restrict__ odd) {
         Half<FM, FN> first, second;
-        auto one = [&](char *now, char *next, int from) {
+        auto one = [&](char *now, char *next, int i) {
             load_half<BM>(second, now, 1, wm, wn, lane);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);   // who multiplies goes before who loads
             mma_half<T>(first, acc);
             __builtin_amdgcn_s_setprio(0);
             all_arrived();
-            if (from + 256 < bytes) fetch(now, from + 256);
-            if (from + 128 < bytes) load_half<BM>(first, next, 0, wm, wn, lane);
+            if (i + 2 < steps) fetch(now, (i + 2) * 128);
+            if (i + 1 < steps) load_half<BM>(first, next, 0, wm, wn, lane);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
             mma_half<T>(second, acc);
@@ -428,31 +463,31 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
         };
         fetch(even, 0);
         all_arrived();
-        if (bytes > 128) fetch(odd, 128);
+        if (steps > 1) fetch(odd, 128);
         load_half<BM>(first, even, 0, wm, wn, lane);
-        for (int from = 0;;) {
-            one(even, odd, from);
-            if ((from += 128) >= bytes) break;
-            one(odd, even, from);
-            if ((from += 128) >= bytes) break;
+        for (int i = 0;;) {
+            one(even, odd, i);
+            if (++i == steps) break;
+            one(odd, even, i);
+            if (++i == steps) break;
         }
     };
-    // e4m3 in tiles of 256: its operands as bf16 leave no registers for a second half
+    // e4m3: its operands as bf16 leave no registers for a second half
     auto plain = [&](char *__restrict__ even, char *__restrict__ odd) {
-        auto one = [&](char *now, char *next, int from) {
+        auto one = [&](char *now, char *next, int i) {
             all_arrived();
-            if (from + 128 < bytes) fetch(next, from + 128);
+            if (i + 1 < steps) fetch(next, (i + 1) * 128);
             tile_step<T, BM, FM, FN>(now, wm, wn, lane, acc);
         };
         fetch(even, 0);
-        for (int from = 0;;) {
-            one(even, odd, from);
-            if ((from += 128) >= bytes) break;
-            one(odd, even, from);
-            if ((from += 128) >= bytes) break;
+        for (int i = 0;;) {
+            one(even, odd, i);
+            if (++i == steps) break;
+            one(odd, even, i);
+            if (++i == steps) break;
         }
     };
-    if constexpr (sizeof(T) == 1 && BM == 256) plain(lds, lds + kStage);
+    if constexpr (sizeof(T) == 1) plain(lds, lds + kStage);
     else all(lds, lds + kStage);
     __syncthreads();
     tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
@@ -517,6 +552,93 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
             __syncthreads();
         }
     }
+    tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
+}
+
+// Tiles of 128 x 128 of operands that lie anywhere, where there are few and the way to memory is what a step waits for: kDeep steps are under
+// way in registers.
+constexpr int kDeep = 2;
+
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave, 4) void k_linear_deep(ProductArgs A)
+{
+    constexpr int BM = 128, BN = 128, kThreads = WM * WN * kWave, FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int kChunks = (BM + BN) * 8 / kThreads, kRowsAtOnce = kThreads / 8, kStage = (BM + BN) * 128;
+    extern __shared__ __align__(16) char lds[];
+    const int64_t count = A.tiles_m * A.tiles_n;
+    if (block_number() >= count) return;
+    int64_t tm, tn;
+    tile_of(A, block_number(), tm, tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN;
+    const int part = blockIdx.z;
+    const int64_t k_from = part * A.k_part, k_to = k_from + A.k_part < A.k ? k_from + A.k_part : A.k;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, wm = wave / WN, wn = wave % WN;
+
+    // rows of x first, rows of w behind them; rows past the end repeat the last one, and their results are not stored
+    const T *rows[kChunks];
+    int place[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        const int r = c * kRowsAtOnce + threadIdx.x / 8;
+        const bool of_x = r < BM;
+        const int64_t i = of_x ? m0 + r : n0 + r - BM, end = of_x ? A.x.rows : A.w.rows;
+        rows[c] = static_cast<const T *>(of_x ? A.x.p : A.w.p) + (i < end ? i : end - 1) * (of_x ? A.x.ld : A.w.ld) + threadIdx.x % 8 * kChunkElems<T>;
+        place[c] = chunk_place(r, threadIdx.x % 8);
+    }
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    i32x4 under_way[kDeep][kChunks];
+    auto fetch_whole = [&](i32x4 (&to)[kChunks], int64_t k) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) __builtin_memcpy(&to[c], rows[c] + k, 16);
+    };
+    auto fetch = [&](i32x4 (&to)[kChunks], int64_t k) {
+        if (k + kStepElems<T> <= k_to) {
+            fetch_whole(to, k);
+        } else if (k < k_to) {
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) to[c] = load_chunk(rows[c], k, k_to - threadIdx.x % 8 * kChunkElems<T>);
+        }
+    };
+    auto put = [&](char *to, const i32x4 (&from)[kChunks]) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) *reinterpret_cast<i32x4 *>(to + place[c]) = from[c];
+    };
+    // two places in turn: who writes one again has passed the next step's barrier, behind which all have read it
+    auto multiply = [&](const char *now) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the loads from memory go on
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        tile_step<T, BM, FM, FN>(now, wm, wn, lane, acc);
+    };
+    const int whole = (int)((k_to - k_from) / kStepElems<T>), steps = (int)((k_to - k_from + kStepElems<T> - 1) / kStepElems<T>);
+    auto place_of = [&](int i) { return k_from + (int64_t)i * kStepElems<T>; };
+#pragma unroll
+    for (int q = 0; q < kDeep; ++q) fetch(under_way[q], place_of(q));
+    int i = 0;
+    // without a condition between the loads, so that only the oldest are waited for
+    for (; i + 2 * kDeep <= whole; i += kDeep) {
+#pragma unroll
+        for (int q = 0; q < kDeep; ++q) {
+            put(lds + q % 2 * kStage, under_way[q]);
+            fetch_whole(under_way[q], place_of(i + q + kDeep));
+            multiply(lds + q % 2 * kStage);
+        }
+    }
+    while (i < steps) {
+#pragma unroll
+        for (int q = 0; q < kDeep; ++q, ++i) {
+            if (i >= steps) break;
+            put(lds + q % 2 * kStage, under_way[q]);
+            fetch(under_way[q], place_of(i + kDeep));
+            multiply(lds + q % 2 * kStage);
+        }
+    }
+    __syncthreads();
     tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
 
@@ -587,13 +709,13 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
     for (int at = threadIdx.x; at < MT * 16 * NT * 2; at += kFewWaves * kWave) {
         const int r = at / (NT * 2), c = at % (NT * 2) * kVec;
         if (r >= A.E.m || n0 + c >= A.E.n) continue;
-        float v[kVec];
+        float v[1][kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-            v[e] = room[0][r][c + e];
-            for (int u = 1; u < kFewWaves; ++u) v[e] += room[u][r][c + e];
+            v[0][e] = room[0][r][c + e];
+            for (int u = 1; u < kFewWaves; ++u) v[0][e] += room[u][r][c + e];
         }
-        put8(A.E, columns_of(A.E, n0 + c), v, r, n0 + c, part);
+        put8(A.E, columns_of(A.E, n0 + c), v, r, 0, n0 + c, part);
     }
 }
 
@@ -606,29 +728,43 @@ struct Plan {
     int64_t k_part;
 };
 
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = 32;   // 33 rows of 32000 x 4096 bf16: 72 us by that kernel, 67 us in tiles of 128 rows
 constexpr int64_t kUnits = 256;   // compute units
+
+// In how many parts the inner index is cut, with `room` for so many at once: `turns` of `turn_us` one after the other, against the second
+// launch and the way of 32-bit sums of all parts to memory and back at some 4 TB/s.  (1024^3 in one part 14 us, in two 18 us;
+// 777 x 1001 x 2049 in two 26 us, in four 23 us; 128 x 4096 x 4096 in four 20 us, in eight 22 us.)
+int64_t parts_for(int64_t turns, double turn_us, int64_t room, double results)
+{
+    int64_t best = 1;
+    double best_us = turn_us * (double)turns;
+    for (int64_t p = 2; p <= std::min<int64_t>({room, turns, 64}); ++p) {
+        const double us = turn_us * (double)ceil_div(turns, p) + 4.0 + (double)p * results * 8.0 / 4e6;
+        if (us < best_us) {
+            best = p;
+            best_us = us;
+        }
+    }
+    return best;
+}
 
 Plan linear_plan(int64_t m, int64_t n, int64_t k, int type)
 {
     Plan P;
     const int64_t step = 128 / type_bytes(type), steps = std::max<int64_t>(1, ceil_div(k, step));
-    int64_t most;
+    int64_t parts;
     if (m <= kFewRows) {
         P.shape = SHAPE_FEW;
         P.tiles_m = 1;
         P.tiles_n = ceil_div(n, 64);
-        most = std::min<int64_t>(steps / (2 * kFewWaves), 2 * kUnits / P.tiles_n);
+        parts = parts_for(ceil_div(steps, 2 * kFewWaves), 1.0, 2 * kUnits / P.tiles_n, (double)m * (double)n);
     } else {
-        const int64_t large = ceil_div(m, 256) * ceil_div(n, 256);
-        P.shape = large >= kUnits ? SHAPE_256 : SHAPE_128;
+        P.shape = ceil_div(m, 256) * ceil_div(n, 256) >= kUnits ? SHAPE_256 : SHAPE_128;
         const int64_t b = P.shape == SHAPE_256 ? 256 : 128;
         P.tiles_m = ceil_div(m, b);
         P.tiles_n = ceil_div(n, b);
-        // a compute unit holds one workgroup of the large tiles, two of the small ones
-        most = std::min<int64_t>(steps / 8, (P.shape == SHAPE_256 ? 1 : 2) * kUnits / (P.tiles_m * P.tiles_n));
+        parts = parts_for(steps, 0.5, kUnits / (P.tiles_m * P.tiles_n), (double)m * (double)n);
     }
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(most, 64));
     P.k_part = ceil_div(steps, parts) * step;
     P.parts = (int)ceil_div(steps * step, P.k_part);
     return P;
@@ -656,16 +792,27 @@ bool direct_ok(const Operand &a, int64_t k)
     return ((uintptr_t)a.p & 15) == 0 && a.ld % kChunkElems<T> == 0 && k % kChunkElems<T> == 0 && (a.ld * 256 + k) * (int64_t)sizeof(T) < 0x7fff0000;
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
-int launch_tile(const ProductArgs &A, dim3 grid, hipStream_t st)
+// Kernels that take more LDS than a launch may without having said so
+template <typename T>
+int launch_256(const ProductArgs &A, dim3 grid, hipStream_t st)
 {
+    constexpr int kLds = kTileLds<256, 256>;
     if (direct_ok<T>(A.x, A.k) && direct_ok<T>(A.w, A.k)) {
-        TRON_TRY(allow_lds(k_linear_direct<T, BM, BN, WM, WN>, kTileLds<BM, BN>));
-        k_linear_direct<T, BM, BN, WM, WN><<<grid, WM * WN * kWave, kTileLds<BM, BN>, st>>>(A);
-        return TRON_OK;
+        TRON_TRY(allow_lds(k_linear_direct<T, 256, 256, 2, 4>, kLds));
+        k_linear_direct<T, 256, 256, 2, 4><<<grid, 512, kLds, st>>>(A);
+    } else {
+        TRON_TRY(allow_lds(k_linear_tile<T, 256, 256, 2, 4>, kLds));
+        k_linear_tile<T, 256, 256, 2, 4><<<grid, 512, kLds, st>>>(A);
     }
-    TRON_TRY(allow_lds(k_linear_tile<T, BM, BN, WM, WN>, kTileLds<BM, BN>));
-    k_linear_tile<T, BM, BN, WM, WN><<<grid, WM * WN * kWave, kTileLds<BM, BN>, st>>>(A);
+    return TRON_OK;
+}
+
+template <typename T>
+int launch_128(const ProductArgs &A, dim3 grid, hipStream_t st)
+{
+    constexpr int kLds = kTileLds<128, 128>;
+    TRON_TRY(allow_lds(k_linear_deep<T, 2, 4>, kLds));
+    k_linear_deep<T, 2, 4><<<grid, 512, kLds, st>>>(A);
     return TRON_OK;
 }
 
@@ -678,101 +825,116 @@ int product(Operand x, Operand w, int64_t k, const Plan &P, Epilogue E, float *p
     grid.z = (unsigned)P.parts;
     if (P.shape == SHAPE_FEW) {
         if (x.rows <= 16) launch_few<T, 1>(A, grid, st);
-        else if (x.rows <= 32) launch_few<T, 2>(A, grid, st);
-        else launch_few<T, 4>(A, grid, st);
+        else launch_few<T, 2>(A, grid, st);
     } else if (P.shape == SHAPE_128) {
-        TRON_TRY((launch_tile<T, 128, 128, 2, 2>(A, grid, st)));
+        TRON_TRY(launch_128<T>(A, grid, st));
     } else {
-        TRON_TRY((launch_tile<T, 256, 256, 2, 4>(A, grid, st)));
+        TRON_TRY(launch_256<T>(A, grid, st));
     }
     TRON_HIP(hipGetLastError());
-    if (P.parts > 1) {
-        k_linear_join<<<block_grid(ceil_div(ceil_div(E.n, kVec) * E.m, kBlock)), kBlock, 0, st>>>(A.E, P.parts);
-        TRON_HIP(hipGetLastError());
-    }
-    return TRON_OK;
+    return P.parts > 1 ? join_parts(A.E, P.parts, st) : TRON_OK;
 }
 
 // ------------------------------------------------------------------ gradients
-constexpr int kPatch = 64;   // columns and rows of a patch that one workgroup turns
+constexpr int kPatch = 64;   // rows and columns of a patch that one wavefront turns
 
 struct TurnArgs {
     const void *a, *pre;       // [rows][cols]; pre: a is multiplied by act'(pre)
     int64_t rows, cols, lda, ldpre;
     int act;
-    void *same, *turned;       // [rows][ldsame], [cols][ldturned], both zero up to their row's length; or NULL
+    void *same, *turned;       // [rows][ldsame], [cols][ldturned], zeros from the last element to the end of its chunk; or NULL
     int64_t ldsame, ldturned;
     float *shares;             // [patches of rows][cols]: column sums of the products before rounding, or NULL
 };
 
-// A patch of 64 x 64 through LDS, eight elements a thread at a time: read by rows, written by rows and by columns.
+// Eight rows of eight elements in a lane, turned: pairs of rows change elements, words and pairs of words.
+template <typename T>
+__device__ __forceinline__ void turn8(Raw8<T> (&r)[kVec])
+{
+    uint32_t w[kVec][4];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) __builtin_memcpy(w[i], &r[i], 16);
+    uint32_t t[kVec][4];   // t[c][p]: column c's elements of rows 2p and 2p + 1
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            t[2 * q][p] = __builtin_amdgcn_perm(w[2 * p + 1][q], w[2 * p][q], 0x05040100);
+            t[2 * q + 1][p] = __builtin_amdgcn_perm(w[2 * p + 1][q], w[2 * p][q], 0x07060302);
+        }
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) __builtin_memcpy(&r[i], t[i], 16);
+}
+
+// A wavefront a patch: lane 8 a + b holds rows 8 a .. + 7 and columns 8 b .. + 7, reads them as eight pieces of 16 bytes, and writes them so or
+// turned in its registers.  Bound by memory: 8192 x 4096 bf16 and its turned copy 30 us.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_turn(TurnArgs A)
 {
-    __shared__ T patch[kPatch][kPatch + 2];
-    __shared__ float sums[kBlock / kVec][kPatch];
-    const int64_t across = (A.cols + kPatch - 1) / kPatch, down = (A.rows + kPatch - 1) / kPatch, number = block_number();
+    static_assert(sizeof(T) == 2, "two elements a word");
+    const int64_t across = (A.cols + kPatch - 1) / kPatch, down = (A.rows + kPatch - 1) / kPatch;
+    const int64_t number = block_number() * kWavesPerBlock + threadIdx.x / kWave;
     if (number >= across * down) return;
-    const int64_t r0 = number / across * kPatch, c0 = number % across * kPatch;
-    const int lane8 = threadIdx.x % kVec, group = threadIdx.x / kVec;   // 32 rows at once
+    const int lane = threadIdx.x % kWave;
+    const int64_t i0 = number / across * kPatch + lane / 8 * kVec, j = number % across * kPatch + lane % 8 * kVec, n = A.cols - j;
+    Raw8<T> raw[kVec], p[kVec];
+#pragma unroll
+    for (int r = 0; r < kVec; ++r) {
+        const bool there = i0 + r < A.rows && n > 0;
+        if (there) raw[r] = load_row8(static_cast<const T *>(A.a) + (i0 + r) * A.lda, j, A.cols, static_cast<T>(0.f));
+        if (there && A.act != TRON_ACT_NONE) p[r] = load_row8(static_cast<const T *>(A.pre) + (i0 + r) * A.ldpre, j, A.cols, static_cast<T>(0.f));
+    }
     float sum[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
 #pragma unroll
-    for (int h = 0; h < kPatch / (kBlock / kVec); ++h) {
-        const int r = group + h * (kBlock / kVec);
-        const int64_t i = r0 + r, j = c0 + lane8 * kVec, n = A.cols - j;
-        float v[kVec];
+    for (int r = 0; r < kVec; ++r) {
+        if (i0 + r < A.rows && n > 0) {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] = 0.f;
-        if (i < A.rows && n > 0) {
-            load_as<T>(v, A.a, i * A.lda + j, n);
-            if (A.act != TRON_ACT_NONE) {
-                float p[kVec];
-                load_as<T>(p, A.pre, i * A.ldpre + j, n);
-#pragma unroll
-                for (int e = 0; e < kVec; ++e) v[e] = e < n ? v[e] * act_slope(p[e], A.act) : 0.f;
+            for (int e = 0; e < kVec; ++e) {
+                float v = static_cast<float>(raw[r].v[e]);
+                if (A.act != TRON_ACT_NONE) {
+                    v = e < n ? v * act_slope(static_cast<float>(p[r].v[e]), A.act) : 0.f;
+                    raw[r].v[e] = static_cast<T>(v);
+                }
+                sum[e] += v;
             }
+        } else {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) sum[e] += v[e];
+            for (int e = 0; e < kVec; ++e) raw[r].v[e] = static_cast<T>(0.f);
         }
-        if (A.same && i < A.rows && j < A.ldsame) store8_of<T>(static_cast<T *>(A.same) + i * A.ldsame + j, v, A.ldsame - j);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) patch[r][lane8 * kVec + e] = static_cast<T>(v[e]);
+        if (A.same && i0 + r < A.rows && j < A.ldsame) store8(static_cast<T *>(A.same) + (i0 + r) * A.ldsame + j, raw[r]);
     }
     if (A.shares) {
+        // over the eight lanes of a column
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sums[group][lane8 * kVec + e] = sum[e];
-    }
-    __syncthreads();
-    if (A.shares && threadIdx.x < kPatch && c0 + threadIdx.x < A.cols) {
-        float s = 0.f;
-        for (int g = 0; g < kBlock / kVec; ++g) s += sums[g][threadIdx.x];
-        A.shares[number / across * A.cols + c0 + threadIdx.x] = s;
+        for (int e = 0; e < kVec; ++e) {
+            sum[e] += __shfl_xor(sum[e], 8);
+            sum[e] += __shfl_xor(sum[e], 16);
+            sum[e] += __shfl_xor(sum[e], 32);
+        }
+        if (lane < 8 && n > 0) store8_of<float>(A.shares + number / across * A.cols + j, sum, n);
     }
     if (!A.turned) return;
+    turn8(raw);
+    if (i0 >= A.ldturned) return;
 #pragma unroll
-    for (int h = 0; h < kPatch / (kBlock / kVec); ++h) {
-        const int c = group + h * (kBlock / kVec);
-        const int64_t j = c0 + c, i = r0 + lane8 * kVec;
-        if (j >= A.cols || i >= A.ldturned) continue;
-        Raw8<T> v;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v.v[e] = patch[lane8 * kVec + e][c];
-        if (A.ldturned - i >= kVec) store8(static_cast<T *>(A.turned) + j * A.ldturned + i, v);
-        else store_first(static_cast<T *>(A.turned) + j * A.ldturned + i, (int)(A.ldturned - i), v);
-    }
+    for (int c = 0; c < kVec; ++c)
+        if (j + c < A.cols) store8(static_cast<T *>(A.turned) + (j + c) * A.ldturned + i0, raw[c]);
 }
 
 template <typename T>
 int turn(const TurnArgs &A, hipStream_t st)
 {
-    k_turn<T><<<block_grid(ceil_div(A.rows, kPatch) * ceil_div(A.cols, kPatch)), kBlock, 0, st>>>(A);
+    k_turn<T><<<block_grid(ceil_div(ceil_div(A.rows, kPatch) * ceil_div(A.cols, kPatch), kWavesPerBlock)), kBlock, 0, st>>>(A);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
 
-inline int64_t padded(int64_t n) { return ceil_div(n, kVec) * kVec; }
+// Row length of the copies: whole chunks, and no multiple of 1 KB, whose rows' equal columns lie in one channel of the L2 (8192 x 8192 x 4096:
+// 478 us with rows of 8 KB, 441 us with 128 bytes more).
+inline int64_t whole(int64_t n) { return ceil_div(n, kVec) * kVec; }
+inline int64_t padded(int64_t n) { return whole(n) % 512 == 0 ? whole(n) + 64 : whole(n); }
 
 // the work space of the gradients, in the order of its parts
 struct GradSpace {
@@ -792,8 +954,8 @@ GradSpace grad_space(int64_t m, int64_t n, int64_t k, bool act, bool dx, bool dw
     S.w_t = take(dx, k * padded(n) * 2);
     S.x_t = take(dw, k * padded(m) * 2);
     S.shares = take(db, ceil_div(m, kPatch) * n * 4);
-    const int64_t for_dx = dx ? plan_bytes(linear_plan(m, k, padded(n), TRON_TYPE_BF16), m, k) : 0;
-    const int64_t for_dw = dw ? plan_bytes(linear_plan(n, k, padded(m), TRON_TYPE_BF16), n, k) : 0;
+    const int64_t for_dx = dx ? plan_bytes(linear_plan(m, k, whole(n), TRON_TYPE_BF16), m, k) : 0;
+    const int64_t for_dw = dw ? plan_bytes(linear_plan(n, k, whole(m), TRON_TYPE_BF16), n, k) : 0;
     S.part = take(true, std::max(for_dx, for_dw));
     S.total = at;
     return S;
@@ -814,7 +976,7 @@ struct GradArgs {
 template <typename T>
 int linear_grad_typed(const GradArgs &G, hipStream_t st)
 {
-    const int64_t m = G.m, n = G.n, k = G.k, np = padded(n), mp = padded(m);
+    const int64_t m = G.m, n = G.n, k = G.k, np = padded(n), mp = padded(m), nw = whole(n), mw = whole(m);
     const bool act = G.act != TRON_ACT_NONE;
     const GradSpace S = grad_space(m, n, k, act, G.dx, G.dw, G.dbias);
     float *shares = reinterpret_cast<float *>(G.work + S.shares), *part = reinterpret_cast<float *>(G.work + S.part);
@@ -832,7 +994,7 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
         E.out = G.type;
         // without an activation dy itself, whose rows end at n
         const Operand a = act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy};
-        TRON_TRY(product<T>(a, Operand{w_t, k, np}, act ? np : n, linear_plan(m, k, np, G.type), E, part, st));
+        TRON_TRY(product<T>(a, Operand{w_t, k, np}, act ? nw : n, linear_plan(m, k, nw, G.type), E, part, st));
     }
     if (G.dw) {
         TRON_TRY(turn<T>(TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr}, st));
@@ -841,7 +1003,7 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
         E.n = k;
         E.ldy = G.lddw;
         E.out = G.dw_type;
-        TRON_TRY(product<T>(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mp, linear_plan(n, k, mp, G.type), E, part, st));
+        TRON_TRY(product<T>(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mw, linear_plan(n, k, mw, G.type), E, part, st));
     }
     return TRON_OK;
 }
@@ -941,9 +1103,7 @@ int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, i
         E.n = k;
         E.ldy = lddw;
         E.out = dw_type;
-        k_linear_join<<<block_grid(ceil_div(ceil_div(k, kVec) * n, kBlock)), kBlock, 0, st>>>(E, 0);
-        TRON_HIP(hipGetLastError());
-        return TRON_OK;
+        return join_parts(E, 0, st);
     }
     const GradArgs G{m, n, k, x, w, dy, pre, ldx, ldw, lddy, ldpre, act, type, dx, dw, lddx, lddw, dw_type, dbias, static_cast<char *>(work)};
     return type == TRON_TYPE_BF16 ? linear_grad_typed<__bf16>(G, st) : linear_grad_typed<_Float16>(G, st);
