@@ -10,6 +10,8 @@
 // Which kernel runs is a rule on the sizes (see linear_plan): tiles of 256 x 256 or 128 x 128 of the result for many rows, a kernel
 // that reads w once, straight into registers, for few rows; the inner index is cut where there are fewer tiles than
 // compute units, and the parts are added in a fixed order.
+#include <type_traits>
+
 #include "head_util.h"
 
 namespace tron {
@@ -77,6 +79,7 @@ struct Epilogue {
     int64_t m, n, ldr, ldy, ldpre;
     int act, out;
     float *part;   // [parts][m][n]: sums of a part of the inner index instead
+    bool past;     // y goes past the caches
 };
 
 // Phi(a) = (1 + erf(a / sqrt 2)) / 2 by Abramowitz and Stegun, 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x) for
@@ -135,11 +138,12 @@ __device__ __forceinline__ void load_out(float *v, const void *base, int out, in
     else load_as<_Float16>(v, base, at, n);
 }
 
+template <bool PAST = false>
 __device__ __forceinline__ void store_out(void *base, int out, int64_t at, const float *v, int64_t n)
 {
-    if (out == TRON_TYPE_F32) store8_of<float>(static_cast<float *>(base) + at, v, n);
-    else if (out == TRON_TYPE_BF16) store8_of<__bf16>(static_cast<__bf16 *>(base) + at, v, n);
-    else store8_of<_Float16>(static_cast<_Float16 *>(base) + at, v, n);
+    if (out == TRON_TYPE_F32) store8_of<float, PAST>(static_cast<float *>(base) + at, v, n);
+    else if (out == TRON_TYPE_BF16) store8_of<__bf16, PAST>(static_cast<__bf16 *>(base) + at, v, n);
+    else store8_of<_Float16, PAST>(static_cast<_Float16 *>(base) + at, v, n);
 }
 
 // what eight columns have
@@ -160,7 +164,7 @@ __device__ __forceinline__ Columns columns_of(const Epilogue &E, int64_t j)
 }
 
 // N times eight neighbouring sums, of rows that lie `step` apart: what is read before what is written
-template <int N>
+template <bool PAST, int N>
 __device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, float (&v)[N][kVec], int64_t i, int64_t step, int64_t j)
 {
     const int64_t n = E.n - j;
@@ -191,11 +195,11 @@ __device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, flo
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[q][e] += f[q][e];
         }
-        store_out(E.y, E.out, row * E.ldy + j, v[q], n);
+        store_out<PAST>(E.y, E.out, row * E.ldy + j, v[q], n);
     }
 }
 
-template <int N>
+template <bool PAST, int N>
 __device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float (&v)[N][kVec], int64_t i, int64_t step, int64_t j, int part)
 {
     if (E.part) {
@@ -203,45 +207,66 @@ __device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float 
         for (int q = 0; q < N; ++q)
             if (i + q * step < E.m) store8_of<float>(E.part + ((int64_t)part * E.m + i + q * step) * E.n + j, v[q], E.n - j);
     } else {
-        finish8(E, C, v, i, step, j);
+        finish8<PAST>(E, C, v, i, step, j);
     }
 }
 
-// behind a product whose inner index was cut, or is empty: eight sums a thread, four parts at a time, blockIdx.y and z the row
-__global__ __launch_bounds__(kBlock) void k_linear_join(Epilogue E, int parts)
+// Behind a product whose inner index was cut: eight sums a thread, four parts at a time, blockIdx.y and z the row.  More parts than
+// kJoinAlone are shared out over W wavefronts, whose sums meet in LDS in their order (64 parts of 16 x 4096: 13.8 us by one, 5 us by eight).
+constexpr int kJoinAlone = 8, kJoinWaves = 8;
+
+template <int W>
+__global__ __launch_bounds__(W == 1 ? kBlock : W * kWave) void k_linear_join(Epilogue E, int parts)
 {
-    const int64_t i = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, j = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * kVec;
-    if (i >= E.m || j >= E.n) return;
-    const Columns C = columns_of(E, j);
+    const int wave = W == 1 ? 0 : threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t i = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, j = (W == 1 ? (int64_t)blockIdx.x * blockDim.x + threadIdx.x : (int64_t)blockIdx.x * kWave + lane) * kVec;
+    if (i >= E.m) return;
     const int64_t n = E.n - j, each = E.m * E.n;
     const float *p = E.part + i * E.n + j;
     float v[1][kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) v[0][e] = 0.f;
-    int q = 0;
-    for (; q + 4 <= parts; q += 4) {
-        float f[4][kVec];
+    if (n > 0) {
+        int q = wave;
+        for (; q + 3 * W < parts; q += 4 * W) {
+            float f[4][kVec];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) load_as<float>(f[r], p + (q + r) * each, 0, n);
+            for (int r = 0; r < 4; ++r) load_as<float>(f[r], p + (q + r * W) * each, 0, n);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[0][e] += f[r][e];
+                for (int e = 0; e < kVec; ++e) v[0][e] += f[r][e];
+        }
+        for (; q < parts; q += W) {
+            float f[kVec];
+            load_as<float>(f, p + q * each, 0, n);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[0][e] += f[e];
+        }
     }
-    for (; q < parts; ++q) {
-        float f[kVec];
-        load_as<float>(f, p + q * each, 0, n);
+    if constexpr (W > 1) {
+        __shared__ float share[W - 1][kVec][kWave];
+        if (wave)
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[0][e] += f[e];
+            for (int e = 0; e < kVec; ++e) share[wave - 1][e][lane] = v[0][e];
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int u = 0; u < W - 1; ++u)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[0][e] += share[u][e][lane];
     }
-    finish8(E, C, v, i, 0, j);
+    if (n > 0) finish8<false>(E, columns_of(E, j), v, i, 0, j);
 }
 
 int join_parts(const Epilogue &E, int parts, hipStream_t st)
 {
     const int64_t chunks = ceil_div(E.n, kVec), y = std::min<int64_t>(E.m, 32768);
-    const unsigned threads = (unsigned)std::min<int64_t>(kBlock, ceil_div(chunks, kWave) * kWave);
-    k_linear_join<<<dim3((unsigned)ceil_div(chunks, threads), (unsigned)y, (unsigned)ceil_div(E.m, y)), threads, 0, st>>>(E, parts);
+    const bool alone = parts <= kJoinAlone;
+    const unsigned across = alone ? (unsigned)std::min<int64_t>(kBlock, ceil_div(chunks, kWave) * kWave) : kWave;
+    const dim3 grid((unsigned)ceil_div(chunks, across), (unsigned)y, (unsigned)ceil_div(E.m, y));
+    if (alone) k_linear_join<1><<<grid, across, 0, st>>>(E, parts);
+    else k_linear_join<kJoinWaves><<<grid, kJoinWaves * kWave, 0, st>>>(E, parts);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -371,18 +396,22 @@ __device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, i
         }
         __syncthreads();
         if (j >= E.n) continue;
+        auto rows = [&](auto past) {
 #pragma unroll 1
-        for (int r = threadIdx.x / kAcross; r < kRows; r += 4 * kDown) {
-            float v[4][kVec];
+            for (int r = threadIdx.x / kAcross; r < kRows; r += 4 * kDown) {
+                float v[4][kVec];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+                for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int e = 0; e < kVec; e += 4) {
-                    const f32x4 four = *reinterpret_cast<const f32x4 *>(out + (r + q * kDown) * kPitch + c + e);
-                    v[q][e] = four[0], v[q][e + 1] = four[1], v[q][e + 2] = four[2], v[q][e + 3] = four[3];
-                }
-            put8(E, C, v, m0 + half * kRows + r, kDown, j, part);
-        }
+                    for (int e = 0; e < kVec; e += 4) {
+                        const f32x4 four = *reinterpret_cast<const f32x4 *>(out + (r + q * kDown) * kPitch + c + e);
+                        v[q][e] = four[0], v[q][e + 1] = four[1], v[q][e + 2] = four[2], v[q][e + 3] = four[3];
+                    }
+                put8<past.value>(E, C, v, m0 + half * kRows + r, kDown, j, part);
+            }
+        };
+        if (E.past) rows(std::true_type{});
+        else rows(std::false_type{});
     }
 }
 
@@ -715,7 +744,93 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
             v[0][e] = room[0][r][c + e];
             for (int u = 1; u < kFewWaves; ++u) v[0][e] += room[u][r][c + e];
         }
-        put8(A.E, columns_of(A.E, n0 + c), v, r, 0, n0 + c, part);
+        put8<false>(A.E, columns_of(A.E, n0 + c), v, r, 0, n0 + c, part);
+    }
+}
+
+// ------------------------------------------------------------------ dx of few rows
+// dx = dpre w for up to M rows: w is read once, as it lies.  A lane has eight columns and sums over the rows that its wavefront takes; dpre's
+// factors of 256 rows of w lie in LDS, rounded to the operands' type as for the other products.  Bound by reading w: 262 MB of it in 52 us
+// (5.0 TB/s) for one row.  Against a turned copy of w and a product with it: all gradients of 3 x 29367 x 4841 f16 243 us (424 us), of
+// 8 x 4096 x 4096 72 us (73 us), of 16 x 32000 x 4096 273 us (326 us), but of 16 x 4096 x 4096 84 us (76 us) - hence the rule of few_grad_rows.
+inline bool few_grad_rows(int64_t m, int64_t n, int64_t k) { return m <= 8 || (m <= 16 && n * k >= (int64_t)1 << 25); }
+constexpr int kFewGradCols = kWave * kVec, kFewGradStage = kBlock;
+
+struct FewGradArgs {
+    const void *w, *dy, *pre;
+    int64_t m, n, k, ldw, lddy, ldpre, per;   // rows of w a part
+    int act;
+    Epilogue E;
+};
+
+template <typename T, int M>
+__global__ __launch_bounds__(kBlock) void k_few_grad(FewGradArgs A)
+{
+    __shared__ __align__(16) float factor[kFewGradStage][M];
+    __shared__ float sum[M][kVec][kWave];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t c0 = (int64_t)blockIdx.x * kFewGradCols, j = c0 + lane * kVec;
+    const int64_t from = blockIdx.z * A.per, to = from + A.per < A.n ? from + A.per : A.n;
+    const T *w = static_cast<const T *>(A.w);
+    float acc[M][kVec];
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) acc[i][e] = 0.f;
+    for (int64_t r0 = from; r0 < to; r0 += kFewGradStage) {
+        const int here = (int)(to - r0 < kFewGradStage ? to - r0 : kFewGradStage);
+        __syncthreads();
+        {
+            const int r = threadIdx.x;
+            const T *dy = static_cast<const T *>(A.dy) + r0 + r, *pre = static_cast<const T *>(A.pre) + r0 + r;
+            float v[M], at[M];
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                const bool there = i < A.m && r < here;
+                v[i] = there ? static_cast<float>(dy[i * A.lddy]) : 0.f;
+                at[i] = there && A.act != TRON_ACT_NONE ? static_cast<float>(pre[i * A.ldpre]) : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < M; ++i) factor[r][i] = A.act == TRON_ACT_NONE ? v[i] : static_cast<float>(static_cast<T>(v[i] * act_slope(at[i], A.act)));
+        }
+        __syncthreads();
+        if (j >= A.k) continue;
+        auto add = [&](const Raw8<T> &raw, int r) {
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) acc[i][e] = fmaf(factor[r][i], static_cast<float>(raw.v[e]), acc[i][e]);
+        };
+        constexpr int kAhead = M == 16 ? 2 : 4;
+        int r = wave;
+#pragma unroll 1
+        for (; r + (kAhead - 1) * kWavesPerBlock < here; r += kAhead * kWavesPerBlock) {
+            Raw8<T> raw[kAhead];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) raw[q] = load_row8(w + (r0 + r + q * kWavesPerBlock) * A.ldw, j, A.k, static_cast<T>(0.f));
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) add(raw[q], r + q * kWavesPerBlock);
+        }
+#pragma unroll 1
+        for (; r < here; r += kWavesPerBlock) add(load_row8(w + (r0 + r) * A.ldw, j, A.k, static_cast<T>(0.f)), r);
+    }
+    // the wavefronts' sums, one after the other
+    for (int u = 0; u < kWavesPerBlock; ++u) {
+        __syncthreads();
+        if (wave != u) continue;
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[i][e][lane] = u ? sum[i][e][lane] + acc[i][e] : acc[i][e];
+    }
+    __syncthreads();
+    if (j >= A.k) return;
+#pragma unroll 1
+    for (int i = wave; i < A.m; i += kWavesPerBlock) {
+        float v[1][kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[0][e] = sum[i][e][lane];
+        put8<false>(A.E, columns_of(A.E, j), v, i, 0, j, blockIdx.z);
     }
 }
 
@@ -729,45 +844,51 @@ struct Plan {
 };
 
 constexpr int64_t kFewRows = 32;   // 33 rows of 32000 x 4096 bf16: 72 us by that kernel, 67 us in tiles of 128 rows
-constexpr int64_t kUnits = 256;   // compute units
+constexpr int64_t kUnits = 256;    // compute units
+constexpr int64_t kMostParts = 64;
 
-// In how many parts the inner index is cut, with `room` for so many at once: `turns` of `turn_us` one after the other, against the second
-// launch and the way of 32-bit sums of all parts to memory and back at some 4 TB/s.  (1024^3 in one part 14 us, in two 18 us;
-// 777 x 1001 x 2049 in two 26 us, in four 23 us; 128 x 4096 x 4096 in four 20 us, in eight 22 us.)
-int64_t parts_for(int64_t turns, double turn_us, int64_t room, double results)
-{
-    int64_t best = 1;
-    double best_us = turn_us * (double)turns;
-    for (int64_t p = 2; p <= std::min<int64_t>({room, turns, 64}); ++p) {
-        const double us = turn_us * (double)ceil_div(turns, p) + 4.0 + (double)p * results * 8.0 / 4e6;
-        if (us < best_us) {
-            best = p;
-            best_us = us;
-        }
-    }
-    return best;
-}
+// What p parts of the inner index cost beside their products: the second launch, and the way of 32-bit sums to memory and back at some 4 TB/s
+double cut_us(int64_t p, double results) { return p > 1 ? 4.0 + (double)p * results * 8.0 / 4e6 : 0.0; }
 
+// Tiles and parts by the time that they take, measured in microseconds on bf16: a step of a tile of 256 x 256 1.5 (one workgroup a compute
+// unit) and its beginning and end 12; a step of a tile of 128 x 128 0.65 where a compute unit has one, 1.0 where it has two, and
+// 4.  Both sides: 4096^3 111 us in large tiles, 2048 x 2048 x 4096 47 us in small ones (70 us in large ones cut in four),
+// 1024^3 14 us in one part and 18 us in two, 777 x 1001 x 2049 26 us in two and 23 us in four.
 Plan linear_plan(int64_t m, int64_t n, int64_t k, int type)
 {
-    Plan P;
     const int64_t step = 128 / type_bytes(type), steps = std::max<int64_t>(1, ceil_div(k, step));
-    int64_t parts;
+    const double results = (double)m * (double)n, slow = type == TRON_TYPE_E4M3 ? 2.0 : 1.0;   // twice the inner index a step
+    Plan best{SHAPE_FEW, 1, ceil_div(n, 64), 1, 0};
+    double best_us = HUGE_VAL;
+    int64_t parts = 1;
     if (m <= kFewRows) {
-        P.shape = SHAPE_FEW;
-        P.tiles_m = 1;
-        P.tiles_n = ceil_div(n, 64);
-        parts = parts_for(ceil_div(steps, 2 * kFewWaves), 1.0, 2 * kUnits / P.tiles_n, (double)m * (double)n);
+        // eight steps a turn of its wavefronts, one microsecond
+        const int64_t turns = ceil_div(steps, 2 * kFewWaves);
+        for (int64_t p = 1; p == 1 || p <= std::min({2 * kUnits / best.tiles_n, turns, kMostParts}); ++p) {
+            const double us = (double)ceil_div(turns, p) + cut_us(p, results);
+            if (us < best_us) {
+                best_us = us;
+                parts = p;
+            }
+        }
     } else {
-        P.shape = ceil_div(m, 256) * ceil_div(n, 256) >= kUnits ? SHAPE_256 : SHAPE_128;
-        const int64_t b = P.shape == SHAPE_256 ? 256 : 128;
-        P.tiles_m = ceil_div(m, b);
-        P.tiles_n = ceil_div(n, b);
-        parts = parts_for(steps, 0.5, kUnits / (P.tiles_m * P.tiles_n), (double)m * (double)n);
+        for (const Shape shape : {SHAPE_256, SHAPE_128}) {
+            const int64_t b = shape == SHAPE_256 ? 256 : 128, tiles_m = ceil_div(m, b), tiles_n = ceil_div(n, b), tiles = tiles_m * tiles_n;
+            for (int64_t p = 1; p == 1 || p <= std::min({2 * kUnits / tiles, steps, kMostParts}); ++p) {
+                const int64_t each = ceil_div(steps, p);
+                const double rounds = shape == SHAPE_256 ? (double)ceil_div(tiles * p, kUnits) * 1.5 : tiles * p <= kUnits ? 0.65 : (double)ceil_div(tiles * p, 2 * kUnits);
+                const double us = rounds * slow * (double)each + (shape == SHAPE_256 ? 12.0 : 4.0) + cut_us(p, results);
+                if (us < best_us) {
+                    best_us = us;
+                    best = Plan{shape, tiles_m, tiles_n, 1, 0};
+                    parts = p;
+                }
+            }
+        }
     }
-    P.k_part = ceil_div(steps, parts) * step;
-    P.parts = (int)ceil_div(steps * step, P.k_part);
-    return P;
+    best.k_part = ceil_div(steps, parts) * step;
+    best.parts = (int)ceil_div(steps * step, best.k_part);
+    return best;
 }
 
 int64_t plan_bytes(const Plan &P, int64_t m, int64_t n) { return P.parts > 1 ? ceil_div(P.parts * m * n * 4, 16) * 16 : 0; }
@@ -820,6 +941,7 @@ template <typename T>
 int product(Operand x, Operand w, int64_t k, const Plan &P, Epilogue E, float *part, hipStream_t st)
 {
     E.part = P.parts > 1 ? part : nullptr;
+    E.past = goes_past(E.m, E.n, type_bytes(E.out));
     const ProductArgs A{x, w, k, P.k_part, P.tiles_m, P.tiles_n, E};
     dim3 grid = block_grid(P.tiles_m * P.tiles_n);
     grid.z = (unsigned)P.parts;
@@ -937,6 +1059,26 @@ int turn(const TurnArgs &A, hipStream_t st)
 inline int64_t whole(int64_t n) { return ceil_div(n, kVec) * kVec; }
 inline int64_t padded(int64_t n) { return whole(n) % 512 == 0 ? whole(n) + 64 : whole(n); }
 
+// Parts of the rows of w for dx of few rows: workgroups for four a compute unit, 64 rows of w each at least
+int64_t few_grad_parts(int64_t n, int64_t k)
+{
+    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, 64), 4 * kUnits / ceil_div(k, kFewGradCols)));
+}
+
+template <typename T>
+int few_grad(FewGradArgs A, float *part, hipStream_t st)
+{
+    A.per = ceil_div(A.n, few_grad_parts(A.n, A.k));
+    const int parts = (int)ceil_div(A.n, A.per);
+    A.E.part = parts > 1 ? part : nullptr;
+    const dim3 grid((unsigned)ceil_div(A.k, kFewGradCols), 1, (unsigned)parts);
+    if (A.m <= 4) k_few_grad<T, 4><<<grid, kBlock, 0, st>>>(A);
+    else if (A.m <= 8) k_few_grad<T, 8><<<grid, kBlock, 0, st>>>(A);
+    else k_few_grad<T, 16><<<grid, kBlock, 0, st>>>(A);
+    TRON_HIP(hipGetLastError());
+    return parts > 1 ? join_parts(A.E, parts, st) : TRON_OK;
+}
+
 // the work space of the gradients, in the order of its parts
 struct GradSpace {
     int64_t dpre, dpre_t, w_t, x_t, shares, part, total;
@@ -950,12 +1092,13 @@ GradSpace grad_space(int64_t m, int64_t n, int64_t k, bool act, bool dx, bool dw
         if (want) at += ceil_div(bytes, 256) * 256;
         return from;
     };
-    S.dpre = take(dx && act, m * padded(n) * 2);
+    const bool few = few_grad_rows(m, n, k);
+    S.dpre = take(dx && act && !few, m * padded(n) * 2);
     S.dpre_t = take(dw, n * padded(m) * 2);
-    S.w_t = take(dx, k * padded(n) * 2);
+    S.w_t = take(dx && !few, k * padded(n) * 2);
     S.x_t = take(dw, k * padded(m) * 2);
     S.shares = take(db, ceil_div(m, kPatch) * n * 4);
-    const int64_t for_dx = dx ? plan_bytes(linear_plan(m, k, whole(n), TRON_TYPE_BF16), m, k) : 0;
+    const int64_t for_dx = !dx ? 0 : few ? few_grad_parts(n, k) * m * k * 4 : plan_bytes(linear_plan(m, k, whole(n), TRON_TYPE_BF16), m, k);
     const int64_t for_dw = dw ? plan_bytes(linear_plan(n, k, whole(m), TRON_TYPE_BF16), n, k) : 0;
     S.part = take(true, std::max(for_dx, for_dw));
     S.total = at;
@@ -982,11 +1125,19 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     const GradSpace S = grad_space(m, n, k, act, G.dx, G.dw, G.dbias);
     float *shares = reinterpret_cast<float *>(G.work + S.shares), *part = reinterpret_cast<float *>(G.work + S.part);
     void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
-    if (G.dbias || G.dw || (G.dx && act))
-        TRON_TRY(turn<T>(TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, G.dx && act ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr}, st));
+    const bool few = few_grad_rows(m, n, k), same = G.dx && act && !few;
+    if (G.dbias || G.dw || same)
+        TRON_TRY(turn<T>(TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr}, st));
     if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
     Epilogue E{};
-    if (G.dx) {
+    if (G.dx && few) {
+        E.y = G.dx;
+        E.m = m;
+        E.n = k;
+        E.ldy = G.lddx;
+        E.out = G.type;
+        TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, E}, part, st));
+    } else if (G.dx) {
         TRON_TRY(turn<T>(TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr}, st));
         E.y = G.dx;
         E.m = m;
@@ -1052,7 +1203,7 @@ int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_
     }
     TRON_TRY(check_device());
     if (m == 0) return TRON_OK;
-    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr};
+    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr, false};
     const Operand a{x, m, ldx}, b{w, n, ldw};
     const Plan P = linear_plan(m, n, k, type);
     float *part = static_cast<float *>(work);

@@ -358,6 +358,31 @@ def test_linear_gradients(m, n, k, kind):
             assert got is None or torch.equal(got, all_at_once)
 
 
+# few rows, whose dx reads w as it lies: its ends inside a thread's columns, in one part and in many, either side of each bound on the rows
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(2, 700, 600), (4, 1000, 513), (5, 257, 1030), (8, 63, 64), (9, 2100, 520), (16, 4100, 1025), (16, 40, 7), (17, 1500, 96), (12, 34000, 1001)])
+def test_linear_gradients_of_few_rows(m, n, k, kind):
+    test_linear_gradients(m, n, k, kind)
+
+
+def test_linear_gradients_of_few_rows_keep_what_is_not_finite():
+    torch = torch_mod()
+    m, n, k = 6, 300, 530
+    dy, w = torch.randn(m, n, device="cuda").bfloat16(), torch.randn(n, k, device="cuda").bfloat16()
+    dy[2, 299], w[17, 529] = math.nan, math.inf
+    dx = torch.empty(m, k, device="cuda").bfloat16()
+    tron.tron_linear_grad(None, w, dy, dx=dx)
+    bad = torch.zeros(m, k, dtype=torch.bool, device="cuda")
+    bad[2], bad[:, 529] = True, True
+    assert torch.equal(~torch.isfinite(dx), bad)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("m,n,k", [(1, 60, 30000), (20, 9, 20001), (200, 100, 9000)])
+def test_linear_cut_in_many(m, n, k, kind):
+    _check_linear(m, n, k, kind, "f32", act=tron.ACT_SILU, bias=True, residual=True, pre=True)
+
+
 def test_linear_gradients_against_differences():
     torch = torch_mod()
     g = _gen(3)
