@@ -100,7 +100,7 @@ __device__ __forceinline__ float act_of(float a, int act)
     switch (act) {
     case TRON_ACT_RELU: return a > 0.f || a != a ? a : 0.f;
     case TRON_ACT_GELU: return a * normal_cdf(a, bell);
-    case TRON_ACT_SILU: return a / (1.f + __expf(-a));
+    case TRON_ACT_SILU: return a * __builtin_amdgcn_rcpf(1.f + __expf(-a));
     default: return a;
     }
 }
@@ -115,7 +115,7 @@ __device__ __forceinline__ float act_slope(float a, int act)
         return phi + a * 0.39894228f * bell;
     }
     case TRON_ACT_SILU: {
-        const float h = 1.f / (1.f + __expf(-a));
+        const float h = __builtin_amdgcn_rcpf(1.f + __expf(-a));
         return h * (1.f + a * (1.f - h));
     }
     default: return 1.f;
@@ -967,6 +967,12 @@ struct TurnArgs {
     void *same, *turned;       // [rows][ldsame], [cols][ldturned], zeros from the last element to the end of its chunk; or NULL
     int64_t ldsame, ldturned;
     float *shares;             // [patches of rows][cols]: column sums of the products before rounding, or NULL
+    int64_t blocks;
+};
+
+struct TurnList {
+    TurnArgs list[3];
+    int count;
 };
 
 // Eight rows of eight elements in a lane, turned: pairs of rows change elements, words and pairs of words.
@@ -991,12 +997,13 @@ __device__ __forceinline__ void turn8(Raw8<T> (&r)[kVec])
 // A wavefront a patch: lane 8 a + b holds rows 8 a .. + 7 and columns 8 b .. + 7, reads them as eight pieces of 16 bytes, and writes them so or
 // turned in its registers.  The four of a workgroup take patches one below the other: their pieces of a turned row are 512 bytes (side by
 // side 42 us, so 35 us for 8192 x 4096 bf16, 3.8 TB/s).
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_turn(TurnArgs A)
+// All copies of a call are one launch, and the activation is chosen once a patch: its code is long, and a small copy waits for it to be fetched.
+template <typename T, int ACT>
+__device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
 {
     static_assert(sizeof(T) == 2, "two elements a word");
     const int64_t across = (A.cols + kPatch - 1) / kPatch, down = (A.rows + kPatch - 1) / kPatch;
-    const int64_t patch_row = block_number() / across * kWavesPerBlock + threadIdx.x / kWave, patch_col = block_number() % across;
+    const int64_t patch_row = block / across * kWavesPerBlock + threadIdx.x / kWave, patch_col = block % across;
     if (patch_row >= down) return;
     const int lane = threadIdx.x % kWave;
     const int64_t i0 = patch_row * kPatch + lane / 8 * kVec, j = patch_col * kPatch + lane % 8 * kVec, n = A.cols - j;
@@ -1005,7 +1012,7 @@ __global__ __launch_bounds__(kBlock) void k_turn(TurnArgs A)
     for (int r = 0; r < kVec; ++r) {
         const bool there = i0 + r < A.rows && n > 0;
         if (there) raw[r] = load_row8(static_cast<const T *>(A.a) + (i0 + r) * A.lda, j, A.cols, static_cast<T>(0.f));
-        if (there && A.act != TRON_ACT_NONE) p[r] = load_row8(static_cast<const T *>(A.pre) + (i0 + r) * A.ldpre, j, A.cols, static_cast<T>(0.f));
+        if (there && ACT != TRON_ACT_NONE) p[r] = load_row8(static_cast<const T *>(A.pre) + (i0 + r) * A.ldpre, j, A.cols, static_cast<T>(0.f));
     }
     float sum[kVec];
 #pragma unroll
@@ -1016,8 +1023,8 @@ __global__ __launch_bounds__(kBlock) void k_turn(TurnArgs A)
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
                 float v = static_cast<float>(raw[r].v[e]);
-                if (A.act != TRON_ACT_NONE) {
-                    v = e < n ? v * act_slope(static_cast<float>(p[r].v[e]), A.act) : 0.f;
+                if (ACT != TRON_ACT_NONE) {
+                    v = e < n ? v * act_slope(static_cast<float>(p[r].v[e]), ACT) : 0.f;
                     raw[r].v[e] = static_cast<T>(v);
                 }
                 sum[e] += v;
@@ -1047,9 +1054,28 @@ __global__ __launch_bounds__(kBlock) void k_turn(TurnArgs A)
 }
 
 template <typename T>
-int turn(const TurnArgs &A, hipStream_t st)
+__global__ __launch_bounds__(kBlock) void k_turn(TurnList L)
 {
-    k_turn<T><<<block_grid(ceil_div(A.rows, kPatch * kWavesPerBlock) * ceil_div(A.cols, kPatch)), kBlock, 0, st>>>(A);
+    int64_t block = block_number();
+    int which = 0;
+    while (which < L.count && block >= L.list[which].blocks) block -= L.list[which++].blocks;
+    if (which == L.count) return;
+    const TurnArgs A = L.list[which];
+    switch (A.act) {
+    case TRON_ACT_RELU: return turn_patch<T, TRON_ACT_RELU>(A, block);
+    case TRON_ACT_GELU: return turn_patch<T, TRON_ACT_GELU>(A, block);
+    case TRON_ACT_SILU: return turn_patch<T, TRON_ACT_SILU>(A, block);
+    default: return turn_patch<T, TRON_ACT_NONE>(A, block);
+    }
+}
+
+template <typename T>
+int turn(TurnList &L, hipStream_t st)
+{
+    int64_t blocks = 0;
+    for (int i = 0; i < L.count; ++i) blocks += L.list[i].blocks = ceil_div(L.list[i].rows, kPatch * kWavesPerBlock) * ceil_div(L.list[i].cols, kPatch);
+    if (!blocks) return TRON_OK;
+    k_turn<T><<<block_grid(blocks), kBlock, 0, st>>>(L);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -1126,8 +1152,12 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     float *shares = reinterpret_cast<float *>(G.work + S.shares), *part = reinterpret_cast<float *>(G.work + S.part);
     void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
     const bool few = few_grad_rows(m, n, k), same = G.dx && act && !few;
+    TurnList L{};
     if (G.dbias || G.dw || same)
-        TRON_TRY(turn<T>(TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr}, st));
+        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, 0};
+    if (G.dx && !few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, 0};
+    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, 0};
+    TRON_TRY(turn<T>(L, st));
     if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
     Epilogue E{};
     if (G.dx && few) {
@@ -1138,7 +1168,6 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
         E.out = G.type;
         TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, E}, part, st));
     } else if (G.dx) {
-        TRON_TRY(turn<T>(TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr}, st));
         E.y = G.dx;
         E.m = m;
         E.n = k;
@@ -1149,7 +1178,6 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
         TRON_TRY(product<T>(a, Operand{w_t, k, np}, act ? nw : n, linear_plan(m, k, nw, G.type), E, part, st));
     }
     if (G.dw) {
-        TRON_TRY(turn<T>(TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr}, st));
         E.y = G.dw;
         E.m = n;
         E.n = k;

@@ -31,17 +31,26 @@ def _refuse(text: str):
     raise TronError(EINVAL, text)
 
 
+def _current_stream(index: int) -> int:
+    """Address of a device's current stream (without the Stream object: 2 of the 11 microseconds of a small call)."""
+    raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw else _torch.cuda.current_stream(index).cuda_stream
+
+
 class _Call:
     """One call's tensors: their device, stream and work space."""
+
+    __slots__ = ("name", "device", "index", "stream", "address")
 
     def __init__(self, name: str, first, stream):
         self.name = name
         if not getattr(first, "is_cuda", False):
             _refuse(f"{name}: CUDA tensors are needed; there is no CPU fallback")
         self.device = first.device
+        self.index = first.get_device()
         self.stream = stream
         if stream is None:
-            self.address = _torch.cuda.current_stream(self.device).cuda_stream
+            self.address = _current_stream(self.index)
         else:
             self.address = stream if isinstance(stream, int) else stream.cuda_stream
 
@@ -49,7 +58,7 @@ class _Call:
         """(address, rows, columns, row stride) of a tensor; (None, .., 0) for None."""
         if t is None:
             return None, rows, cols, 0
-        if t.device != self.device:
+        if t.get_device() != self.index:
             _refuse(f"{self.name}: {what} is on {t.device}, other arguments on {self.device}")
         shape = t.shape
         if len(shape) == 2:
@@ -71,9 +80,9 @@ class _Call:
         """Address of n contiguous floats, or None."""
         if t is None:
             return None
-        if t.device != self.device:
+        if t.get_device() != self.index:
             _refuse(f"{self.name}: {what} is on {t.device}, other arguments on {self.device}")
-        if t.dtype != _torch.float32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        if t.dtype is not _torch.float32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
             _refuse(f"{self.name}: {what} has to be {n} contiguous float32 values")
         return t.data_ptr()
 
@@ -100,7 +109,7 @@ class _Call:
         return t, t.data_ptr(), needed
 
     def run(self, function, *args):
-        if _torch.cuda.current_device() == self.device.index:
+        if _torch.cuda.current_device() == self.index:
             _check(function(*args))
         else:
             with _torch.cuda.device(self.device):
