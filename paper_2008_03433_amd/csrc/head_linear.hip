@@ -589,17 +589,13 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
 constexpr int kDeep = 2;
 
 template <typename T, int WM, int WN>
-__global__ __launch_bounds__(WM *WN *kWave, 4) void k_linear_deep(ProductArgs A)
+__device__ __forceinline__ void deep_tile(const ProductArgs &A, int64_t block, int part, char *lds)
 {
     constexpr int BM = 128, BN = 128, kThreads = WM * WN * kWave, FM = BM / WM / 16, FN = BN / WN / 16;
     constexpr int kChunks = (BM + BN) * 8 / kThreads, kRowsAtOnce = kThreads / 8, kStage = (BM + BN) * 128;
-    extern __shared__ __align__(16) char lds[];
-    const int64_t count = A.tiles_m * A.tiles_n;
-    if (block_number() >= count) return;
     int64_t tm, tn;
-    tile_of(A, block_number(), tm, tn);
+    tile_of(A, block, tm, tn);
     const int64_t m0 = tm * BM, n0 = tn * BN;
-    const int part = blockIdx.z;
     const int64_t k_from = part * A.k_part, k_to = k_from + A.k_part < A.k ? k_from + A.k_part : A.k;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, wm = wave / WN, wn = wave % WN;
 
@@ -669,6 +665,25 @@ __global__ __launch_bounds__(WM *WN *kWave, 4) void k_linear_deep(ProductArgs A)
     }
     __syncthreads();
     tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
+}
+
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave, 4) void k_linear_deep(ProductArgs A)
+{
+    extern __shared__ __align__(16) char lds[];
+    if (block_number() < A.tiles_m * A.tiles_n) deep_tile<T, WM, WN>(A, block_number(), blockIdx.z, lds);
+}
+
+// Two products in one launch, where the device has room for both: neither fills it.  Tiles of one after tiles of the other, parts in turn
+// (all gradients of 1024^3: 50 us with one after the other, 38 us together).
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(WM *WN *kWave, 4) void k_linear_deep_two(ProductArgs A, ProductArgs B, int first)
+{
+    extern __shared__ __align__(16) char lds[];
+    const int block = (int)blockIdx.x < first ? blockIdx.x : blockIdx.x - first;
+    const ProductArgs P = (int)blockIdx.x < first ? A : B;
+    const int tiles = (int)(P.tiles_m * P.tiles_n);
+    deep_tile<T, WM, WN>(P, block % tiles, block / tiles, lds);
 }
 
 // ------------------------------------------------------------------ few rows
@@ -937,16 +952,20 @@ int launch_128(const ProductArgs &A, dim3 grid, hipStream_t st)
     return TRON_OK;
 }
 
-template <typename T>
-int product(Operand x, Operand w, int64_t k, const Plan &P, Epilogue E, float *part, hipStream_t st)
+ProductArgs product_args(Operand x, Operand w, int64_t k, const Plan &P, Epilogue E, float *part)
 {
     E.part = P.parts > 1 ? part : nullptr;
     E.past = goes_past(E.m, E.n, type_bytes(E.out));
-    const ProductArgs A{x, w, k, P.k_part, P.tiles_m, P.tiles_n, E};
+    return ProductArgs{x, w, k, P.k_part, P.tiles_m, P.tiles_n, E};
+}
+
+template <typename T>
+int product(const ProductArgs &A, const Plan &P, hipStream_t st)
+{
     dim3 grid = block_grid(P.tiles_m * P.tiles_n);
     grid.z = (unsigned)P.parts;
     if (P.shape == SHAPE_FEW) {
-        if (x.rows <= 16) launch_few<T, 1>(A, grid, st);
+        if (A.x.rows <= 16) launch_few<T, 1>(A, grid, st);
         else launch_few<T, 2>(A, grid, st);
     } else if (P.shape == SHAPE_128) {
         TRON_TRY(launch_128<T>(A, grid, st));
@@ -955,6 +974,24 @@ int product(Operand x, Operand w, int64_t k, const Plan &P, Epilogue E, float *p
     }
     TRON_HIP(hipGetLastError());
     return P.parts > 1 ? join_parts(A.E, P.parts, st) : TRON_OK;
+}
+
+// whether two products go into one launch: both in tiles of 128 x 128, and all of these under way at once, two a compute unit
+bool together(const Plan &P, const Plan &Q)
+{
+    return P.shape == SHAPE_128 && Q.shape == SHAPE_128 && P.tiles_m * P.tiles_n * P.parts + Q.tiles_m * Q.tiles_n * Q.parts <= 2 * kUnits;
+}
+
+template <typename T>
+int two_products(const ProductArgs &A, const Plan &P, const ProductArgs &B, const Plan &Q, hipStream_t st)
+{
+    constexpr int kLds = kTileLds<128, 128>;
+    const int first = (int)(P.tiles_m * P.tiles_n * P.parts), second = (int)(Q.tiles_m * Q.tiles_n * Q.parts);
+    TRON_TRY(allow_lds(k_linear_deep_two<T, 2, 4>, kLds));
+    k_linear_deep_two<T, 2, 4><<<first + second, 512, kLds, st>>>(A, B, first);
+    TRON_HIP(hipGetLastError());
+    if (P.parts > 1) TRON_TRY(join_parts(A.E, P.parts, st));
+    return Q.parts > 1 ? join_parts(B.E, Q.parts, st) : TRON_OK;
 }
 
 // ------------------------------------------------------------------ gradients
@@ -1107,7 +1144,9 @@ int few_grad(FewGradArgs A, float *part, hipStream_t st)
 
 // the work space of the gradients, in the order of its parts
 struct GradSpace {
-    int64_t dpre, dpre_t, w_t, x_t, shares, part, total;
+    int64_t dpre, dpre_t, w_t, x_t, shares, part_dx, part_dw, total;
+    Plan for_dx, for_dw;
+    bool few, both;   // dx of few rows; dx and dw in one launch
 };
 GradSpace grad_space(int64_t m, int64_t n, int64_t k, bool act, bool dx, bool dw, bool db)
 {
@@ -1118,15 +1157,18 @@ GradSpace grad_space(int64_t m, int64_t n, int64_t k, bool act, bool dx, bool dw
         if (want) at += ceil_div(bytes, 256) * 256;
         return from;
     };
-    const bool few = few_grad_rows(m, n, k);
-    S.dpre = take(dx && act && !few, m * padded(n) * 2);
+    S.few = few_grad_rows(m, n, k);
+    S.for_dx = linear_plan(m, k, whole(n), TRON_TYPE_BF16);
+    S.for_dw = linear_plan(n, k, whole(m), TRON_TYPE_BF16);
+    S.both = dx && dw && !S.few && together(S.for_dx, S.for_dw);
+    S.dpre = take(dx && act && !S.few, m * padded(n) * 2);
     S.dpre_t = take(dw, n * padded(m) * 2);
-    S.w_t = take(dx && !few, k * padded(n) * 2);
+    S.w_t = take(dx && !S.few, k * padded(n) * 2);
     S.x_t = take(dw, k * padded(m) * 2);
     S.shares = take(db, ceil_div(m, kPatch) * n * 4);
-    const int64_t for_dx = !dx ? 0 : few ? few_grad_parts(n, k) * m * k * 4 : plan_bytes(linear_plan(m, k, whole(n), TRON_TYPE_BF16), m, k);
-    const int64_t for_dw = dw ? plan_bytes(linear_plan(n, k, whole(m), TRON_TYPE_BF16), n, k) : 0;
-    S.part = take(true, std::max(for_dx, for_dw));
+    const int64_t of_dx = !dx ? 0 : S.few ? few_grad_parts(n, k) * m * k * 4 : plan_bytes(S.for_dx, m, k), of_dw = dw ? plan_bytes(S.for_dw, n, k) : 0;
+    S.part_dx = take(true, S.both ? of_dx : std::max(of_dx, of_dw));
+    S.part_dw = S.both ? take(true, of_dw) : S.part_dx;
     S.total = at;
     return S;
 }
@@ -1149,43 +1191,34 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     const int64_t m = G.m, n = G.n, k = G.k, np = padded(n), mp = padded(m), nw = whole(n), mw = whole(m);
     const bool act = G.act != TRON_ACT_NONE;
     const GradSpace S = grad_space(m, n, k, act, G.dx, G.dw, G.dbias);
-    float *shares = reinterpret_cast<float *>(G.work + S.shares), *part = reinterpret_cast<float *>(G.work + S.part);
+    float *shares = reinterpret_cast<float *>(G.work + S.shares), *part_dx = reinterpret_cast<float *>(G.work + S.part_dx);
     void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
-    const bool few = few_grad_rows(m, n, k), same = G.dx && act && !few;
+    const bool same = G.dx && act && !S.few;
     TurnList L{};
     if (G.dbias || G.dw || same)
         L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, 0};
-    if (G.dx && !few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, 0};
+    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, 0};
     if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, 0};
     TRON_TRY(turn<T>(L, st));
     if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
-    Epilogue E{};
-    if (G.dx && few) {
-        E.y = G.dx;
-        E.m = m;
-        E.n = k;
-        E.ldy = G.lddx;
-        E.out = G.type;
-        TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, E}, part, st));
-    } else if (G.dx) {
-        E.y = G.dx;
-        E.m = m;
-        E.n = k;
-        E.ldy = G.lddx;
-        E.out = G.type;
-        // without an activation dy itself, whose rows end at n
-        const Operand a = act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy};
-        TRON_TRY(product<T>(a, Operand{w_t, k, np}, act ? nw : n, linear_plan(m, k, nw, G.type), E, part, st));
-    }
-    if (G.dw) {
-        E.y = G.dw;
-        E.m = n;
-        E.n = k;
-        E.ldy = G.lddw;
-        E.out = G.dw_type;
-        TRON_TRY(product<T>(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mw, linear_plan(n, k, mw, G.type), E, part, st));
-    }
-    return TRON_OK;
+    Epilogue E{}, F{};
+    E.y = G.dx;
+    E.m = m;
+    E.n = k;
+    E.ldy = G.lddx;
+    E.out = G.type;
+    F.y = G.dw;
+    F.m = n;
+    F.n = k;
+    F.ldy = G.lddw;
+    F.out = G.dw_type;
+    // without an activation dy itself, whose rows end at n
+    const ProductArgs A = product_args(act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy}, Operand{w_t, k, np}, act ? nw : n, S.for_dx, E, part_dx);
+    const ProductArgs B = product_args(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, F, reinterpret_cast<float *>(G.work + S.part_dw));
+    if (S.both) return two_products<T>(A, S.for_dx, B, S.for_dw, st);
+    if (G.dx && S.few) TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, E}, part_dx, st));
+    else if (G.dx) TRON_TRY(product<T>(A, S.for_dx, st));
+    return G.dw ? product<T>(B, S.for_dw, st) : TRON_OK;
 }
 
 bool sizes_ok(int64_t m, int64_t n, int64_t k)
@@ -1234,10 +1267,10 @@ int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_
     const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr, false};
     const Operand a{x, m, ldx}, b{w, n, ldw};
     const Plan P = linear_plan(m, n, k, type);
-    float *part = static_cast<float *>(work);
+    const ProductArgs A = product_args(a, b, k, P, E, static_cast<float *>(work));
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    return type == TRON_TYPE_BF16 ? product<__bf16>(a, b, k, P, E, part, st)
-           : type == TRON_TYPE_F16 ? product<_Float16>(a, b, k, P, E, part, st) : product<e4m3>(a, b, k, P, E, part, st);
+    return type == TRON_TYPE_BF16 ? product<__bf16>(A, P, st)
+           : type == TRON_TYPE_F16 ? product<_Float16>(A, P, st) : product<e4m3>(A, P, st);
 }
 
 int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias)
