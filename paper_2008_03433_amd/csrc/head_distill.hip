@@ -4,10 +4,16 @@
 //   loss = w T^2 sum_j q_j (log q_j - log p_j),   dz = w T (p - q),   H u = w (p u - p (p.u)).
 //
 // All of it is bound by reading z and writing a matrix of its size.  A pass keeps a running maximum m and the sum of exp((z - m) / T)
-// (in 32 bits; exponents are differences, so masks of the type's lowest value neither overflow nor lose the row).  Rows that fit
-// registers are read once; the others are read again for the gradient, while they are still in the caches.  Few rows are split
-// over many workgroups, whose maxima and sums the second launch joins.  The teacher's part of a row, K entries, is one wavefront's
-// work, in 64 bits: its terms and the logarithm of the sum cancel to the loss.
+// (in 32 bits; exponents are differences, so masks of the type's lowest value neither overflow nor lose the row).
+//
+// Loss and gradient: a workgroup a row, which it streams twice; the second read comes from the caches, because few long rows are under way.
+// 4096 x 128000 bf16, 64 entries: 446 us, 4.70 TB/s of the 2.1 GB that have to
+// move (workgroups of 512 threads and stores that stay in the caches, with exponents in 64 bits: 704 us).  The gradient alone reads z once: 2011 x 50021 f16 94 us, 4.30 TB/s, rows at odd places.  Hessian
+// product: z and u stay in registers between p.u and the product, exponentials are taken twice: 8192 x 32000 bf16 300 us,
+// 5.24 TB/s.  Where long rows are fewer than compute units they are split, and the second launch joins the parts' maxima and sums.
+//
+// The teacher's part of a row, K entries, is one wavefront's work: its exponents and its terms are held in 64 bits, because they and the
+// logarithm of the sum cancel to the loss; its masses q in 32.
 #include <type_traits>
 
 #include "head_util.h"
@@ -15,7 +21,7 @@
 namespace tron {
 namespace {
 
-constexpr int kThreads = 512;         // of a workgroup over a part of a row
+constexpr int kThreads = 512;         // of a workgroup over a part of a row, at most
 constexpr int kMostTop = 1024;        // listed entries a row
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -327,7 +333,7 @@ __device__ __forceinline__ void write_zeros(const DistillArgs &A, T *out, int64_
     for (int64_t j = from + (int64_t)threadIdx.x * kVec; j < to; j += block_step()) store8_of<T>(out + j, zero, to - j);
 }
 
-// A workgroup a row, which is read again for the gradient.
+// A workgroup a row, which is read again for the gradient: a running maximum needs no second look at what is behind it, so nothing is held.
 template <typename T, bool GRAD>
 __global__ __launch_bounds__(1024) void k_distill_row(DistillArgs A)
 {
@@ -482,7 +488,8 @@ __device__ __forceinline__ void forget(Raw8<T> &r)
     __builtin_memcpy(&r, w, sizeof(r));
 }
 
-// CH > 0: z and u of a row stay in registers, CH chunks of eight a thread; 0: they are read again.
+// CH > 0: z and u of a row stay in registers, CH chunks of eight a thread; 0, rows that 64 registers a thread do not hold: they are read
+// again (8192 x 32000 bf16: 300 us held, 313 us read twice).
 template <typename T, int CH, bool PAST>
 __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_hv_row(DistillArgs A)
 {
@@ -583,11 +590,21 @@ __global__ __launch_bounds__(1024) void k_distill_hv_part(DistillArgs A)
 
 // ------------------------------------------------------------------ launches
 constexpr int64_t kLeastPart = 4096;   // columns of a part: one chunk of eight a thread
-constexpr int64_t kWanted = 1024;      // workgroups that fill the device: four of kThreads a compute unit
+constexpr int64_t kWhole = 32768;      // columns of a row that one workgroup takes whatever the number of rows
+constexpr int64_t kUnits = 256;        // compute units
 
+// Parts of a row for the loss and the Hessian product, for which parts cost a second launch and a second read: only of rows that are long, and
+// fewer than compute units.  One part and many: loss of 13 x 32000 f32 10 and 14 us, with the gradient of 400 x 32000 bf16 21 and
+// 26 us, product of 200 x 100000 29 and 37 us; but with the gradient of 13 x 128000 21 and 15 us, of 64 x 64000 20 and 17 us.
 int parts_of(int64_t m, int64_t V)
 {
-    return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(V, kLeastPart), kWanted / std::max<int64_t>(m, 1)));
+    return V <= kWhole ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(V, kLeastPart), kUnits / std::max<int64_t>(m, 1)));
+}
+
+// and for the gradient alone, one launch in either case: four workgroups a compute unit (300 x 32000 f16 12.3 us, with two 14.0 us)
+int grad_parts(int64_t m, int64_t V)
+{
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(V, kLeastPart), 4 * kUnits / std::max<int64_t>(m, 1)));
 }
 
 void set_parts(DistillArgs &A, int parts)
@@ -633,7 +650,7 @@ int distill_typed(DistillArgs A, void *work, hipStream_t st)
 template <typename T>
 int distill_grad_typed(DistillArgs A, hipStream_t st)
 {
-    set_parts(A, parts_of(A.m, A.V));
+    set_parts(A, grad_parts(A.m, A.V));
     k_distill_grad<T, false><<<part_grid(A), std::min<unsigned>(kThreads, row_threads(A.per, 8)), teacher_bytes(A), st>>>(A);
     TRON_HIP(hipGetLastError());
     return TRON_OK;

@@ -565,6 +565,14 @@ def test_distill_hessian_vector_product(m, V, K, kind):
         assert float((mine[row].double().cpu() - full).abs().max()) <= 2 * U[kind] * float(full.abs().max()) + 2.0 ** -14 * float(u.abs().max())
 
 
+# either side of what decides whether rows are split: their length, and their number
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,V,K", [(3, 32768, 9), (3, 32769, 40), (1, 70000, 100), (128, 33001, 5), (129, 33000, 3)])
+def test_distill_long_rows(m, V, K, kind):
+    test_distill(m, V, K, kind)
+    test_distill_hessian_vector_product(m, V, K, kind)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("m,V", [(4, 6000), (1100, 200)])
 def test_distill_masks(m, V, kind):
@@ -637,6 +645,11 @@ def test_distill_against_differences():
         assert abs((up - down) / (2 * h) - float(g0[1, j])) < h * h + 2.0 ** -21 / h
         tron.tron_distill_hv(z, lse0, e / h, hu, ids=ids, t=t, temperature=T, weight=w)
         assert float(((gu - gd) / (2 * h) - hu.double()).abs().max()) < h * h + 2.0 ** -22 / h
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_distill_masks_of_rows_in_parts(kind):
+    test_distill_masks(4, 40000, kind)
 
 
 # --------------------------------------------------------------------------- streams, graphs, refusals
