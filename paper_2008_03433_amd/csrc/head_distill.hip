@@ -7,10 +7,11 @@
 // (in 32 bits; exponents are differences, so masks of the type's lowest value neither overflow nor lose the row).
 //
 // Loss and gradient: a workgroup a row, which it streams twice; the second read comes from the caches, because few long rows are under way.
-// 4096 x 128000 bf16, 64 entries: 446 us, 4.70 TB/s of the 2.1 GB that have to
-// move (workgroups of 512 threads and stores that stay in the caches, with exponents in 64 bits: 704 us).  The gradient alone reads z once: 2011 x 50021 f16 94 us, 4.30 TB/s, rows at odd places.  Hessian
-// product: z and u stay in registers between p.u and the product, exponentials are taken twice: 8192 x 32000 bf16 300 us,
-// 5.24 TB/s.  Where long rows are fewer than compute units they are split, and the second launch joins the parts' maxima and sums.
+// 4096 x 128000 bf16, 64 entries: 446 us, 4.70 TB/s of the 2.1 GB that have to move (with workgroups of 512 threads, stores that
+// stay in the caches and exponents in 64 bits 704 us).  The gradient alone reads z once: 2011 x 50021 f16 94 us, 4.30 TB/s, rows at
+// odd places.  Hessian product: z and u stay in registers between p.u and the product, exponentials are taken twice: 8192 x 32000
+// bf16 300 us, 5.24 TB/s.  Where long rows are fewer than compute units they are split, and the second launch joins the parts'
+// maxima and sums.
 //
 // The teacher's part of a row, K entries, is one wavefront's work: its exponents and its terms are held in 64 bits, because they and the
 // logarithm of the sum cancel to the loss; its masses q in 32.
