@@ -50,7 +50,7 @@ def test_bad_arguments_are_refused_before_the_device_is_asked_for():
 
 def test_sizes_of_work_spaces():
     lib = tron.load_library()
-    assert lib.tron_rms_norm_grad_work(0, 8) == 0 and lib.tron_rms_norm_grad_work(3, 8) >= 3 * 8 * 4
+    assert lib.tron_rms_norm_grad_work(0, 8) == 0 and lib.tron_rms_norm_grad_work(3, 8) >= 8 * 4   # one share of dgain at least
     assert lib.tron_linear_work(0, 4, 4, 1) == 0 and lib.tron_linear_work(4, 4, 4, 7) == 0
     assert lib.tron_linear_grad_work(5, 7, 9, 0, 0, 0, 0) == 0
     alone = [lib.tron_linear_grad_work(100, 70, 90, 2, *w) for w in ((1, 0, 0), (0, 1, 0), (0, 0, 1))]
