@@ -11,7 +11,7 @@
 // once, straight into registers, for up to 32 rows.  The inner index is cut where tiles leave compute units idle, and the parts are
 // added in a fixed order.
 //
-// Many rows are bound by the matrix units and what feeds them: 8192 x 32000 x 4096 bf16 1.70 ms, 1262 TFLOP/s; the units are busy 58% of the cycles of a
+// Many rows are bound by the matrix units and what feeds them: 8192 x 32000 x 4096 bf16 1.70 ms, 1262 TFLOP/s; the units are busy 57% of the cycles of a
 // clock that falls to 2.0 GHz under them.  Without the fetches the same loop runs at 1500 to 1600 TFLOP/s.  Few rows are bound by reading w: one
 // row of 32000 x 4096 bf16 55 us, 4.8 TB/s.  In between the way to memory and the launch count: 777 x 1001 x 2049 f16 23 us.
 #include <type_traits>
