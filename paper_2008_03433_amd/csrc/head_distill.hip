@@ -10,7 +10,7 @@
 // 4096 x 128000 bf16, 64 entries: 446 us, 4.70 TB/s of the 2.1 GB that have to move (with workgroups of 512 threads, stores that
 // stay in the caches and exponents in 64 bits 704 us).  The gradient alone reads z once: 2011 x 50021 f16 94 us, 4.30 TB/s, rows at
 // odd places.  Hessian product: z and u stay in registers between p.u and the product, exponentials are taken twice: 8192 x 32000
-// bf16 300 us, 5.24 TB/s.  Where long rows are fewer than compute units they are split, and the second launch joins the parts'
+// bf16 273 us, 5.76 TB/s.  Where long rows are fewer than compute units they are split, and the second launch joins the parts'
 // maxima and sums.
 //
 // The teacher's part of a row, K entries, is one wavefront's work: its exponents and its terms are held in 64 bits, because they and the
@@ -490,7 +490,7 @@ __device__ __forceinline__ void forget(Raw8<T> &r)
 }
 
 // CH > 0: z and u of a row stay in registers, CH chunks of eight a thread; 0, rows that 64 registers a thread do not hold: they are read
-// again (8192 x 32000 bf16: 300 us held, 313 us read twice).
+// again (8192 x 32000 bf16: 273 us held, 313 us read twice).
 template <typename T, int CH, bool PAST>
 __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_hv_row(DistillArgs A)
 {
@@ -542,7 +542,10 @@ __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_h
     if (CH) {
         if (kAnew) {
 #pragma unroll
-            for (int k = 0; k < CH; ++k) forget(zr[k]);
+            for (int k = 0; k < CH; ++k) {
+                forget(zr[k]);
+                forget(ur[k]);
+            }
         }
 #pragma unroll
         for (int k = 0; k < CH; ++k) {

@@ -674,8 +674,9 @@ __device__ __forceinline__ void deep_tile(const ProductArgs &A, int64_t block, i
     tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
 
+// e4m3: one workgroup a compute unit, because its operands as bf16 do not fit 128 registers (1024^3 17.3 us, with two and spilt ones 19.8 us)
 template <typename T, int WM, int WN>
-__global__ __launch_bounds__(WM *WN *kWave, 4) void k_linear_deep(ProductArgs A)
+__global__ __launch_bounds__(WM *WN *kWave, sizeof(T) == 1 ? 2 : 4) void k_linear_deep(ProductArgs A)
 {
     extern __shared__ __align__(16) char lds[];
     if (block_number() < A.tiles_m * A.tiles_n) deep_tile<T, WM, WN>(A, block_number(), blockIdx.z, lds);
