@@ -117,10 +117,11 @@ __device__ __forceinline__ TeacherSums teacher_part(const DistillArgs &A, int64_
     TeacherSums R;
     R.any = __any(bad) || top > -INFINITY;
     // a wavefront's own LDS operations complete in order.  Exponents in 64 bits, of which the instruction takes 32 and a factor the rest: a
-    // small q keeps its digits, for the difference to a p that is as small.
+    // small q keeps its digits, for the difference to a p that is as small.  Masks of the type's lowest value have exponents that no float
+    // holds: from -200 on, where the mass is 0, they are that.
     const double per_t = A.inv_t * kLog2e, from_top = base_of(top);
     auto mass = [&](double t_top) {
-        const double e = t_top * per_t;
+        const double exact = t_top * per_t, e = exact < -200.0 ? -200.0 : exact;   // NaN stays
         const float hi = (float)e;
         return exp2_(hi) * fmaf((float)(e - (double)hi), 0.69314718f, 1.f);
     };
