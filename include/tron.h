@@ -478,6 +478,8 @@ TRON_API int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const v
  * +inf where the teacher has mass; a row of nothing but -inf has p = 0), and NaN or +inf makes the row NaN; a NaN among the listed t makes the loss
  * and the listed columns NaN.  With K = 1 it is
  * the cross entropy of a label.  V < 2^31 - 64.
+ * lse is rounded to a float, +-inf beyond its range, and then says little about rows whose logits lie far from 0: where |lse| is 256 or more
+ * (z in 16 bits: 4096) the calls that take it read the row once more and form its sum anew, from the same z.
  */
 TRON_API int64_t tron_distill_work(int64_t m, int64_t V);
 TRON_API int tron_distill(int64_t m, int64_t V, int type, const void *z, int64_t ldz, int64_t K, const void *ids,

@@ -255,24 +255,19 @@ struct ByMax {
 };
 __device__ __forceinline__ ByMax by_max(const Running &r, float c, float f) { return {base_of(r.m), c, r.s == 0.f ? 0.f : f / r.s}; }
 
-// f p = f exp(z / T - lse), the exponent as that difference times log2(e): rows of the type's lowest value stay finite.  lse = -inf: a
-// row of nothing but -inf, p = 0.
+// f p = f exp((z - m) / T - less), the exponent as that difference times log2(e); m = 0 and less = lse where lse is known well enough.
+// A row of nothing but -inf has p = 0.
 template <typename T>
 struct ByLse {
-    float hi, lo, less, f;
+    float hi, lo, m, less, f;
     __device__ __forceinline__ float operator()(float z) const
     {
-        float e = fmaf(z, hi, -less);
-        if (kFull<T>) e += z == -INFINITY ? 0.f : z * lo;
+        const float d = z - m;
+        float e = fmaf(d, hi, -less);
+        if (kFull<T>) e += d == -INFINITY ? 0.f : d * lo;
         return f * exp2_(e * (float)kLog2e);
     }
 };
-template <typename T>
-__device__ __forceinline__ ByLse<T> by_lse(const DistillArgs &A, int64_t row, float f)
-{
-    const float lse = A.lse_in[row];
-    return {A.it_hi, A.it_lo, lse == -INFINITY ? 0.f : lse, f};
-}
 
 // Columns that a workgroup takes at once, and how many of these a thread has under way
 constexpr int kAhead = 2;
@@ -311,6 +306,27 @@ __device__ __forceinline__ void over_rows(const T *z, const T *u, int64_t from, 
         for (int k = 0; k < kAhead; ++k) f(j + k * step, x[k], y[k]);
     }
     for (; j < to; j += step) f(j, at8(z, j, to), at8(u, j, to, 0.f));
+}
+
+// A float holds lse to 2^-24 of its size, and p is off by that in proportion: rows of logits far from 0 (masks of the type's lowest value, whose
+// lse is that value or infinite; small temperatures) would have any p.  From here on, where it is 2^-17 of p (16 bits: 2^-13), the row's
+// maximum and sum are taken again from z.
+template <typename T>
+constexpr float kCoarseLse = kFull<T> ? 256.f : 4096.f;
+template <typename T>
+__device__ __forceinline__ bool coarse(float lse) { return fabsf(lse) >= kCoarseLse<T>; }
+
+// By the whole workgroup.  room: 2 * kMostWaves floats, free again on return
+template <typename T>
+__device__ __forceinline__ ByLse<T> by_lse(const DistillArgs &A, const T *z, float lse, float f, float *room)
+{
+    if (!coarse<T>(lse)) return {A.it_hi, A.it_lo, 0.f, lse, f};
+    Running r;
+    over_row(z, 0, A.V, [&](int64_t, const Raw8<T> &x) { take8(r, x, A.c); });
+    r = join_block(r, A.c, room);
+    __syncthreads();
+    const float m = base_of(r.m), less = r.s == 0.f ? 0.f : logf(r.s);
+    return {A.it_hi, A.it_lo, read_lanef(m, 0), read_lanef(less, 0), f};
 }
 
 template <typename T, typename P>
@@ -423,10 +439,18 @@ template <typename T, bool JOIN>
 __global__ __launch_bounds__(1024) void k_distill_grad(DistillArgs A)
 {
     __shared__ int any, twice;
+    __shared__ float room[2 * kMostWaves];
     __shared__ __align__(16) unsigned seen[kSeenWords];
     const int64_t row = part_row();
     if (row >= A.m) return;
-    const int64_t V = A.V, from = blockIdx.x * A.per, to = from + A.per < V ? from + A.per : V;
+    const int64_t V = A.V;
+    int64_t from = blockIdx.x * A.per, to = from + A.per < V ? from + A.per : V;
+    const float lse = JOIN ? 0.f : A.lse_in[row];
+    if (!JOIN && coarse<T>(lse)) {   // the whole row is read before any of `out`, which may be z, is written: by one workgroup
+        if (blockIdx.x) return;
+        from = 0;
+        to = V;
+    }
     const Teacher S = teacher_of(A);
     const T *z = static_cast<const T *>(A.z) + row * A.ldz;
     // z of the listed columns too, before `out`, which may be z, is written
@@ -457,7 +481,7 @@ __global__ __launch_bounds__(1024) void k_distill_grad(DistillArgs A)
     const float wt = w * A.temperature;
     const auto scaled = [&] {
         if constexpr (JOIN) return by_max(r, A.c, wt);
-        else return by_lse<T>(A, row, wt);
+        else return by_lse<T>(A, z, lse, wt, room);
     }();
     write_scaled(A, z, out, from, to, scaled);
     __syncthreads();
@@ -496,7 +520,7 @@ template <typename T, int CH, bool PAST>
 __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_hv_row(DistillArgs A)
 {
     constexpr bool kAnew = CH * sizeof(T) >= 8;   // 32 registers hold z and u (two workgroups of 1024 a compute unit), or 64
-    __shared__ float room[kMostWaves];
+    __shared__ float room[2 * kMostWaves];
     const int64_t row = block_number();
     if (row >= A.m) return;
     const int64_t V = A.V;
@@ -508,7 +532,7 @@ __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_h
         return;
     }
     const T *z = static_cast<const T *>(A.z) + row * A.ldz, *u = static_cast<const T *>(A.u) + row * A.ldu;
-    const ByLse<T> p = by_lse<T>(A, row, 1.f);
+    const ByLse<T> p = by_lse<T>(A, z, A.lse_in[row], 1.f, room);
     Raw8<T> zr[CH ? CH : 1], ur[CH ? CH : 1];
     float dot = 0.f;
     auto dot8 = [&](const Raw8<T> &x, const Raw8<T> &y) {
@@ -562,7 +586,7 @@ __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_h
 template <typename T, bool FIRST>
 __global__ __launch_bounds__(1024) void k_distill_hv_part(DistillArgs A)
 {
-    __shared__ float room[kMostWaves];
+    __shared__ float room[2 * kMostWaves];
     const int64_t row = part_row();
     if (row >= A.m) return;
     const int64_t V = A.V, from = blockIdx.x * A.per, to = from + A.per < V ? from + A.per : V;
@@ -573,7 +597,7 @@ __global__ __launch_bounds__(1024) void k_distill_hv_part(DistillArgs A)
         return;
     }
     const T *z = static_cast<const T *>(A.z) + row * A.ldz, *u = static_cast<const T *>(A.u) + row * A.ldu;
-    const ByLse<T> p = by_lse<T>(A, row, 1.f);
+    const ByLse<T> p = by_lse<T>(A, z, A.lse_in[row], 1.f, room);
     float dot = 0.f;
     if (!FIRST)
         for (int k = 0; k < A.splits; ++k) dot += A.part_sum[row * A.splits + k];

@@ -41,3 +41,78 @@ def test_distill_teacher_of_the_lowest_value(m, V, T, low):
     got.fill_(7.0)
     tron.tron_distill_grad(args[0], got_lse, *args[1:], got, temperature=T, weight=weight.cuda())
     _within(got, dz, bound, "dz from lse")
+
+
+# --------------------------------------------------------------------------- rows whose lse a float does not hold
+def _far_rows(kind, V, T, seed):
+    """Rows whose logits lie so far from 0 that a float's lse says little about them, and ordinary ones between them."""
+    torch = torch_mod()
+    g, dt = _gen(seed), _dt(kind)
+    top = torch.finfo(dt).max
+    z = (3 * T * _randn(g, 7, V)).to(dt)
+    z[0] = -top
+    z[2] = top
+    z[3] = (0.875 * top * torch.sign(_randn(g, V))).to(dt)   # half of them masked as deep as they can be
+    z[4] = (1e4 + 8 * _randn(g, V)).to(dt)
+    z[5] = -math.inf
+    return z
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [1.0, 0.5, 1.5])
+@pytest.mark.parametrize("V", [70, 6000, 40_000, 70_003])
+def test_distill_gradient_and_hessian_vector_product_of_rows_far_from_zero(V, T, kind):
+    """tron_distill_grad and tron_distill_hv agree with the definition where lse has no digits left, in place too."""
+    torch = torch_mod()
+    z, dt, K = _far_rows(kind, V, T, V), _dt(kind), 3
+    m = z.shape[0]
+    ids, t, weight = torch.arange(K).repeat(m, 1), torch.zeros(m, K), torch.linspace(0.5, 2.0, m)
+    # from differences to the row's maximum: 64 bits do not hold such an lse either
+    p = torch.softmax(z.double() / T, 1).nan_to_num(nan=0.0)
+    q, w = torch.zeros_like(p), weight.double()[:, None]
+    q[:, :K] = 1 / K
+    dz = w * T * (p - q)
+    got_loss, lse = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    fused, got = torch.empty(m, V, dtype=dt, device="cuda"), torch.empty(m, V, dtype=dt, device="cuda")
+    args = (ids.cuda(), t.cuda())
+    tron.tron_distill(z.cuda(), *args, got_loss, lse, temperature=T, weight=weight.cuda(), dz=fused)
+    # exponents are differences to the row's maximum, up to 64 where p counts; below 2^-120 p may be 0.  Ordinary rows: from lse, up to some 20
+    off = (V / 512 + 160) * E + 4 * 20 * E
+    p_off = p * (off + 8 * E)
+    bound = U[kind] * dz.abs() + (w * T * (p_off + q * 8 * E)) * (1 + U[kind]) + 4 * E * dz.abs() + TINY[kind] + 2.0 ** -120
+    _within(fused, dz, bound, "dz")
+    tron.tron_distill_grad(z.cuda(), lse, *args, got, temperature=T, weight=weight.cuda())
+    _within(got, dz, bound, "dz from lse")
+    mine = z.cuda()
+    tron.tron_distill_grad(mine, lse, *args, mine, temperature=T, weight=weight.cuda())
+    assert torch.equal(mine, got)
+
+    u = _randn(_gen(V + 1), m, V).to(dt)
+    u64 = u.double()
+    want = w * (p * u64 - p * (p * u64).sum(1, keepdim=True))
+    size = p * (u64.abs() + (p * u64.abs()).sum(1, keepdim=True))
+    tron.tron_distill_hv(z.cuda(), lse, u.cuda(), got, ids=args[0], t=args[1], temperature=T, weight=weight.cuda())
+    _within(got, want, U[kind] * want.abs() + w * size * (2 * off + (V / 512 + 40) * 2 * E) * (1 + U[kind]) + TINY[kind] + 2.0 ** -120, "hu")
+    mine = u.cuda()
+    tron.tron_distill_hv(z.cuda(), lse, mine, mine, ids=args[0], t=args[1], temperature=T, weight=weight.cuda())
+    assert torch.equal(mine, got)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [500, 40_000])
+def test_distill_gradient_of_rows_far_from_zero_that_are_not_finite(V, kind):
+    torch = torch_mod()
+    dt, T = _dt(kind), 0.5
+    z = torch.full((3, V), torch.finfo(dt).min).to(dt)
+    z[0, 7], z[1, 8] = math.nan, math.inf
+    ids, t = torch.zeros(3, 1, dtype=torch.int64, device="cuda"), torch.zeros(3, 1, device="cuda")
+    loss, lse = torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    dz = torch.empty(3, V, dtype=dt, device="cuda")
+    tron.tron_distill(z.cuda(), ids, t, loss, lse, temperature=T)
+    tron.tron_distill_grad(z.cuda(), lse, ids, t, dz, temperature=T)
+    assert torch.isnan(dz[:2].float()).all() and torch.isfinite(dz[2].float()).all()
+    # rows that do not count are 0 whatever they hold
+    weight = torch.tensor([0.0, 1.0, 0.0], device="cuda")
+    ids[1] = -1
+    tron.tron_distill_grad(z.cuda(), lse, ids, t, dz, temperature=T, weight=weight)
+    assert (dz == 0).all()
