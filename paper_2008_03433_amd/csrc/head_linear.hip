@@ -774,7 +774,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
 
 // ------------------------------------------------------------------ dx of few rows
 // dx = dpre w for up to M rows: w is read once, as it lies.  A lane has eight columns and sums over the rows that its wavefront takes; dpre's
-// factors of 256 rows of w lie in LDS, rounded to the operands' type as for the other products.  Bound by reading w: 262 MB of it in 52 us
+// factors of 256 rows of w lie in LDS, in 32 bits: no matrix unit takes them here, so they are not rounded.  Bound by reading w: 262 MB of it in 52 us
 // (5.0 TB/s) for one row.  Against a turned copy of w and a product with it: all gradients of 3 x 29367 x 4841 f16 243 us (424 us), of
 // 8 x 4096 x 4096 72 us (73 us), of 16 x 32000 x 4096 273 us (326 us), but of 16 x 4096 x 4096 84 us (76 us) - hence the rule of few_grad_rows.
 inline bool few_grad_rows(int64_t m, int64_t n, int64_t k) { return m <= 8 || (m <= 16 && n * k >= (int64_t)1 << 25); }
@@ -815,7 +815,7 @@ __global__ __launch_bounds__(kBlock) void k_few_grad(FewGradArgs A)
                 at[i] = there && A.act != TRON_ACT_NONE ? static_cast<float>(pre[i * A.ldpre]) : 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < M; ++i) factor[r][i] = A.act == TRON_ACT_NONE ? v[i] : static_cast<float>(static_cast<T>(v[i] * act_slope(at[i], A.act)));
+            for (int i = 0; i < M; ++i) factor[r][i] = A.act == TRON_ACT_NONE ? v[i] : v[i] * act_slope(at[i], A.act);
         }
         __syncthreads();
         if (j >= A.k) continue;

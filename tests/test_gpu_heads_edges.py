@@ -116,3 +116,32 @@ def test_distill_gradient_of_rows_far_from_zero_that_are_not_finite(V, kind):
     ids[1] = -1
     tron.tron_distill_grad(z.cuda(), lse, ids, t, dz, temperature=T, weight=weight)
     assert (dz == 0).all()
+
+
+# --------------------------------------------------------------------------- gradients of the matrix product
+def _grad_inputs(g, m, n, k, kind, act):
+    """x, w, dy, pre of a type; dpre = dy act'(pre), X and W in 64 bits."""
+    torch = torch_mod()
+    dt = _dt(kind)
+    x, w, dy, pre = (a.to(dt) for a in (_randn(g, m, k), _randn(g, n, k) * k ** -0.5, _randn(g, m, n), _randn(g, m, n)))
+    return x, w, dy, pre, _dpre(dy, pre, act)
+
+
+def _dpre(dy, pre, act):
+    torch = torch_mod()
+    a = pre.double().requires_grad_()
+    y = [lambda v: v * 1.0, torch.relu, torch.nn.functional.gelu, torch.nn.functional.silu][act](a)
+    return torch.autograd.grad(y, a, dy.double())[0]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU])
+@pytest.mark.parametrize("m,n,k", [(1, 700, 600), (8, 300, 530), (5, 63, 64)])
+def test_linear_gradient_of_few_rows_takes_dpre_unrounded(m, n, k, act, kind):
+    torch = torch_mod()
+    x, w, dy, pre, d = _grad_inputs(_gen(m + n + k), m, n, k, kind, act)
+    dx = torch.empty(m, k, dtype=_dt(kind), device="cuda")
+    tron.tron_linear_grad(None, w.cuda(), dy.cuda(), dx=dx, act=act, pre=pre.cuda())
+    want, W = d @ w.double(), w.double().abs()
+    # the factors' roundings of 32 bits, the sum, and the rounding of the result alone
+    _within(dx, want, U[kind] * want.abs() + ((32 * E * dy.double().abs() + (n + 8) * 2 * E * d.abs()) @ W) * (1 + U[kind]) + TINY[kind], "dx")
