@@ -145,3 +145,33 @@ def test_linear_gradient_of_few_rows_takes_dpre_unrounded(m, n, k, act, kind):
     want, W = d @ w.double(), w.double().abs()
     # the factors' roundings of 32 bits, the sum, and the rounding of the result alone
     _within(dx, want, U[kind] * want.abs() + ((32 * E * dy.double().abs() + (n + 8) * 2 * E * d.abs()) @ W) * (1 + U[kind]) + TINY[kind], "dx")
+
+
+@pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU, tron.ACT_RELU])
+@pytest.mark.parametrize("size", [65504.0, 2.0 ** -16])
+@pytest.mark.parametrize("m,n,k", [(70, 40, 130), (200, 264, 96), (12, 50, 64)])
+def test_linear_gradients_in_f16_whose_dpre_lies_beyond_its_range(m, n, k, size, act):
+    """Gradients next to f16's largest value times slopes above 1, and small ones times small slopes: the products have results that f16
+    holds.  (12 rows: dx by the kernel that reads w as it lies.)"""
+    torch = torch_mod()
+    g, u = _gen(m + n + k), U["f16"]
+    dy = (size * torch.sign(_randn(g, m, n)) * (1.0 - 0.25 * torch.rand(m, n, generator=g, dtype=torch.float64))).half()
+    dy[0, :2] = size
+    pre = (1.5 + 0.3 * _randn(g, m, n) if size > 1 else -3.0 + 0.5 * _randn(g, m, n)).half()
+    scale = 2.0 ** -14 if size > 1 else 2.0 ** 13
+    x, w = (_randn(g, m, k) * scale).half(), (_randn(g, n, k) * scale).half()
+    d = _dpre(dy, pre, act)
+    dx, dw, db = torch.empty(m, k, dtype=torch.float16, device="cuda"), torch.empty(n, k, dtype=torch.float16, device="cuda"), torch.empty(n, device="cuda")
+    tron.tron_linear_grad(x.cuda(), w.cuda(), dy.cuda(), dx=dx, dw=dw, dbias=db, act=act, pre=pre.cuda())
+    # dpre rounded to f16 times a power of two by which the largest |dy| is 2^14 at least: below f16's normal numbers half of 2^-24 over that power
+    off = u * d.abs() + 32 * E * dy.double().abs() + 2.0 ** -25 * float(dy.double().abs().max()) / 2.0 ** 14
+    X, W = x.double(), w.double()
+    for got, want, bound in ((dx, d @ W, (off + (n + 8) * 2 * E * d.abs()) @ W.abs()), (dw, d.T @ X, (off + (m + 8) * 2 * E * d.abs()).T @ X.abs())):
+        assert float(want.abs().max()) < 65504.0
+        _within(got, want, u * want.abs() * (1 + u) + bound * (1 + u) + TINY["f16"], "dx" if got is dx else "dw")
+    _within(db, d.sum(0), ((m + 8) * 2 * E * d.abs() + 32 * E * dy.double().abs()).sum(0), "dbias")
+    # all of it infinite or NaN where dy is, and nothing else
+    dy[3, 5], dy[m - 1, 7] = math.inf, math.nan
+    tron.tron_linear_grad(x.cuda(), w.cuda(), dy.cuda(), dx=dx, dw=dw, act=act, pre=pre.abs().cuda())
+    assert torch.equal(~torch.isfinite(dx).all(1).cpu(), torch.isin(torch.arange(m), torch.tensor([3, m - 1])))
+    assert torch.equal(~torch.isfinite(dw).all(1).cpu(), torch.isin(torch.arange(n), torch.tensor([5, 7])))
