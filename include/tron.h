@@ -459,7 +459,7 @@ TRON_API int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *
  *   dx = dpre w  (m x k, of `type`);   dw = dpre' x  (n x k, of dw_type);   dbias_j = sum_i dpre_ij  (n floats).
  * Each may be NULL; the residual's gradient is dy.  With an activation the products of the matrix units take dpre rounded to `type`, as
  * their operands are (f16: times a power of two that the largest |dy| gives, so that neither end of f16's range is met before the results'
- * own); dbias, and dx of few rows (up to 8, or 16 where n k >= 2^25), sum it unrounded.
+ * own); dw of 32 bits has a second product with what that rounding left.  dbias, and dx of few rows (up to 8, or 16 where n k >= 2^25), sum it unrounded.
  */
 TRON_API int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias);
 TRON_API int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const void *w,

@@ -1020,6 +1020,7 @@ struct TurnArgs {
     int64_t ldsame, ldturned;
     float *shares;             // [patches of rows][cols]: column sums of the products before rounding, or NULL
     const float *factor;       // one number that the products are multiplied by before they are rounded, or NULL
+    void *rest;                // as `turned`: what that rounding left, times kRestLift, or NULL
     int64_t blocks;
 };
 
@@ -1047,11 +1048,15 @@ __device__ __forceinline__ void turn8(Raw8<T> (&r)[kVec])
     for (int i = 0; i < kVec; ++i) __builtin_memcpy(&r[i], t[i], 16);
 }
 
+// What the rounding of dpre left is up to half a unit of its last place; f16 holds it times 2^11 with all its digits.
+template <typename T>
+constexpr float kRestLift = __is_same(T, __bf16) ? 1.f : 2048.f;
+
 // A wavefront a patch: lane 8 a + b holds rows 8 a .. + 7 and columns 8 b .. + 7, reads them as eight pieces of 16 bytes, and writes them so or
 // turned in its registers.  The four of a workgroup take patches one below the other: their pieces of a turned row are 512 bytes (side by
 // side 42 us, so 35 us for 8192 x 4096 bf16, 3.8 TB/s).
 // All copies of a call are one launch, and the activation is chosen once a patch: its code is long, and a small copy waits for it to be fetched.
-template <typename T, int ACT>
+template <typename T, int ACT, bool REST = false>
 __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
 {
     static_assert(sizeof(T) == 2, "two elements a word");
@@ -1080,12 +1085,16 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
                 if (ACT != TRON_ACT_NONE) {
                     v = e < n ? v * act_slope(static_cast<float>(p[r].v[e]), ACT) : 0.f;
                     raw[r].v[e] = static_cast<T>(v * factor);
+                    if (REST) {
+                        const float left = v * factor - static_cast<float>(raw[r].v[e]);
+                        p[r].v[e] = static_cast<T>(left == left ? left * kRestLift<T> : 0.f);   // none of what is not finite
+                    }
                 }
                 sum[e] += v;
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) raw[r].v[e] = static_cast<T>(0.f);
+            for (int e = 0; e < kVec; ++e) raw[r].v[e] = p[r].v[e] = static_cast<T>(0.f);
         }
         if (A.same && i0 + r < A.rows && j < A.ldsame) store8(static_cast<T *>(A.same) + (i0 + r) * A.ldsame + j, raw[r]);
     }
@@ -1100,11 +1109,15 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
         if (lane < 8 && n > 0) store8_of<float>(A.shares + patch_row * A.cols + j, sum, n);
     }
     if (!A.turned) return;
-    turn8(raw);
-    if (i0 >= A.ldturned) return;
+    auto put = [&](Raw8<T> (&r)[kVec], void *to) {
+        turn8(r);
+        if (i0 >= A.ldturned) return;
 #pragma unroll
-    for (int c = 0; c < kVec; ++c)
-        if (j + c < A.cols) store8(static_cast<T *>(A.turned) + (j + c) * A.ldturned + i0, raw[c]);
+        for (int c = 0; c < kVec; ++c)
+            if (j + c < A.cols) store8(static_cast<T *>(to) + (j + c) * A.ldturned + i0, r[c]);
+    };
+    put(raw, A.turned);
+    if (REST) put(p, A.rest);
 }
 
 template <typename T>
@@ -1117,8 +1130,8 @@ __global__ __launch_bounds__(kBlock) void k_turn(TurnList L)
     const TurnArgs A = L.list[which];
     switch (A.act) {
     case TRON_ACT_RELU: return turn_patch<T, TRON_ACT_RELU>(A, block);
-    case TRON_ACT_GELU: return turn_patch<T, TRON_ACT_GELU>(A, block);
-    case TRON_ACT_SILU: return turn_patch<T, TRON_ACT_SILU>(A, block);
+    case TRON_ACT_GELU: return A.rest ? turn_patch<T, TRON_ACT_GELU, true>(A, block) : turn_patch<T, TRON_ACT_GELU>(A, block);
+    case TRON_ACT_SILU: return A.rest ? turn_patch<T, TRON_ACT_SILU, true>(A, block) : turn_patch<T, TRON_ACT_SILU>(A, block);
     default: return turn_patch<T, TRON_ACT_NONE>(A, block);
     }
 }
@@ -1136,9 +1149,9 @@ int turn(TurnList &L, hipStream_t st)
 
 // f16: dpre is dy times a slope of up to 1.13, which may lie above the largest value or below the smallest where the products' results
 // do not.  It is held times a power of two, by which the largest |dy| comes to lie in [2^14, 2^15), and the results are multiplied by its
-// reciprocal.  factors: that power, its reciprocal.  8192 x 4096: 25 us for the maximum and 5 us for the factors, where all gradients
+// reciprocal.  factors: that power, its reciprocal, and that for what the rounding left.  8192 x 4096: 25 us for the maximum and 5 us for the factors, where all gradients
 // with 4096 inputs take 580 us without.
-constexpr int kRangeBlocks = 512;
+constexpr int kRangeBlocks = 512, kFactors = 3;
 
 __global__ __launch_bounds__(kBlock) void k_range_parts(const _Float16 *dy, int64_t m, int64_t n, int64_t ld, float *parts)
 {
@@ -1165,14 +1178,15 @@ __global__ __launch_bounds__(kWave) void k_range_factors(const float *parts, int
         const int e = top == 0.f ? 0 : top < INFINITY ? 14 - ilogbf(top) : -1;
         factors[0] = ldexpf(1.f, e);
         factors[1] = ldexpf(1.f, -e);
+        factors[2] = ldexpf(1.f / kRestLift<_Float16>, -e);
     }
 }
 
 int range_factors(const void *dy, int64_t m, int64_t n, int64_t ld, float *space, hipStream_t st)
 {
     const unsigned blocks = (unsigned)std::min<int64_t>(kRangeBlocks, ceil_div(m * ceil_div(n, kVec), kBlock));
-    k_range_parts<<<blocks, kBlock, 0, st>>>(static_cast<const _Float16 *>(dy), m, n, ld, space + 2);
-    k_range_factors<<<1, kWave, 0, st>>>(space + 2, (int)blocks, space);
+    k_range_parts<<<blocks, kBlock, 0, st>>>(static_cast<const _Float16 *>(dy), m, n, ld, space + kFactors);
+    k_range_factors<<<1, kWave, 0, st>>>(space + kFactors, (int)blocks, space);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -1204,7 +1218,7 @@ int few_grad(FewGradArgs A, float *part, hipStream_t st)
 
 // the work space of the gradients, in the order of its parts
 struct GradSpace {
-    int64_t dpre, dpre_t, w_t, x_t, shares, factors, part_dx, part_dw, total;
+    int64_t dpre, dpre_t, rest_t, w_t, x_t, shares, factors, part_dx, part_dw, total;
     Plan for_dx, for_dw;
     bool few, both;   // dx of few rows; dx and dw in one launch
 };
@@ -1226,10 +1240,11 @@ GradSpace grad_space(int64_t m, int64_t n, int64_t k, int act, bool dx, bool dw,
     S.both = dx && dw && !S.few && together(S.for_dx, S.for_dw);
     S.dpre = take(dx && act != TRON_ACT_NONE && !S.few, m * padded(n) * 2);
     S.dpre_t = take(dw, n * padded(m) * 2);
+    S.rest_t = take(dw && smooth(act), n * padded(m) * 2);   // whatever the type of dw, which is not asked for here
     S.w_t = take(dx && !S.few, k * padded(n) * 2);
     S.x_t = take(dw, k * padded(m) * 2);
     S.shares = take(db, ceil_div(m, kPatch) * n * 4);
-    S.factors = take(smooth(act) && (dw || (dx && !S.few)), (2 + kRangeBlocks) * 4);
+    S.factors = take(smooth(act) && (dw || (dx && !S.few)), (kFactors + kRangeBlocks) * 4);
     const int64_t of_dx = !dx ? 0 : S.few ? few_grad_parts(n, k) * m * k * 4 : plan_bytes(S.for_dx, m, k), of_dw = dw ? plan_bytes(S.for_dw, n, k) : 0;
     S.part_dx = take(true, S.both ? of_dx : std::max(of_dx, of_dw));
     S.part_dw = S.both ? take(true, of_dw) : S.part_dx;
@@ -1256,8 +1271,8 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     const bool act = G.act != TRON_ACT_NONE;
     const GradSpace S = grad_space(m, n, k, G.act, G.dx, G.dw, G.dbias);
     float *shares = reinterpret_cast<float *>(G.work + S.shares), *part_dx = reinterpret_cast<float *>(G.work + S.part_dx);
-    void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
-    const bool same = G.dx && act && !S.few;
+    void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *rest_t = G.work + S.rest_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
+    const bool same = G.dx && act && !S.few, rest = G.dw && G.dw_type == TRON_TYPE_F32 && smooth(G.act);
     float *factors = nullptr;
     if (sizeof(T) == 2 && !__is_same(T, __bf16) && smooth(G.act) && (same || G.dw)) {
         factors = reinterpret_cast<float *>(G.work + S.factors);
@@ -1265,9 +1280,9 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     }
     TurnList L{};
     if (G.dbias || G.dw || same)
-        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, factors, 0};
-    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, nullptr, 0};
-    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, nullptr, 0};
+        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, factors, rest ? rest_t : nullptr, 0};
+    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, nullptr, nullptr, 0};
+    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, nullptr, nullptr, 0};
     TRON_TRY(turn<T>(L, st));
     if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
     Epilogue E{}, F{};
@@ -1286,10 +1301,23 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     // without an activation dy itself, whose rows end at n
     const ProductArgs A = product_args(act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy}, Operand{w_t, k, np}, act ? nw : n, S.for_dx, E, part_dx);
     const ProductArgs B = product_args(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, F, reinterpret_cast<float *>(G.work + S.part_dw));
-    if (S.both) return two_products<T>(A, S.for_dx, B, S.for_dw, st);
-    if (G.dx && S.few) TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, few}, part_dx, st));
-    else if (G.dx) TRON_TRY(product<T>(A, S.for_dx, st));
-    return G.dw ? product<T>(B, S.for_dw, st) : TRON_OK;
+    if (S.both) {
+        TRON_TRY(two_products<T>(A, S.for_dx, B, S.for_dw, st));
+    } else {
+        if (G.dx && S.few) TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, few}, part_dx, st));
+        else if (G.dx) TRON_TRY(product<T>(A, S.for_dx, st));
+        if (G.dw) TRON_TRY(product<T>(B, S.for_dw, st));
+    }
+    if (!rest) return TRON_OK;
+    // A result in 32 bits would have the rounding of dpre as its whole error: what that left is multiplied too, and added.  Results of 16
+    // bits have a rounding of that size themselves.  8192 x 4096 x 4096 bf16 gelu, errors against 64 bits as a share of the result: dw in
+    // 32 bits 1.7e-3 without and 2.5e-6 with the second product, all gradients 567 and 818 us; dx and dw in bf16 2.35e-3 as they are,
+    // in 554 us, 1.66e-3 if their dpre had 32 bits.
+    Epilogue R = F;
+    R.residual = G.dw;
+    R.ldr = G.lddw;
+    if (factors) R.factor = factors + 2;
+    return product<T>(product_args(Operand{rest_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, R, reinterpret_cast<float *>(G.work + S.part_dw)), S.for_dw, st);
 }
 
 bool sizes_ok(int64_t m, int64_t n, int64_t k)

@@ -175,3 +175,21 @@ def test_linear_gradients_in_f16_whose_dpre_lies_beyond_its_range(m, n, k, size,
     tron.tron_linear_grad(x.cuda(), w.cuda(), dy.cuda(), dx=dx, dw=dw, act=act, pre=pre.abs().cuda())
     assert torch.equal(~torch.isfinite(dx).all(1).cpu(), torch.isin(torch.arange(m), torch.tensor([3, m - 1])))
     assert torch.equal(~torch.isfinite(dw).all(1).cpu(), torch.isin(torch.arange(n), torch.tensor([5, 7])))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU, tron.ACT_RELU])
+@pytest.mark.parametrize("m,n,k", [(3, 40, 70), (130, 70, 257), (700, 24, 16), (9000, 100, 130)])
+def test_linear_gradient_dw_in_32_bits_has_no_rounding_of_dpre(m, n, k, act, kind):
+    """Shapes with dx and dw in one launch, in one part and in several; rows that lie apart."""
+    torch = torch_mod()
+    u = U[kind]
+    x, w, dy, pre, d = _grad_inputs(_gen(m + n + k + act), m, n, k, kind, act)
+    dw, dx, only = torch.full((n, k + 3), math.nan, device="cuda")[:, :k], torch.empty(m, k, dtype=_dt(kind), device="cuda"), torch.empty(n, k, device="cuda")
+    tron.tron_linear_grad(x.cuda(), w.cuda(), dy.cuda(), dx=dx, dw=dw, act=act, pre=pre.cuda())
+    # dpre in two parts, each rounded: u of u; of f16's smallest steps 2^-25 where the largest |dy| is 2^14 at least, and 2^-11 of that behind the lift
+    off = u * u * d.abs() + 32 * E * dy.double().abs() + 2.0 ** -36 * float(dy.double().abs().max()) / 2.0 ** 14
+    want, X = d.T @ x.double(), x.double().abs()
+    _within(dw, want, 2 * E * want.abs() + (off + (m + 8) * 4 * E * d.abs()).T @ X, "dw")
+    tron.tron_linear_grad(x.cuda(), None, dy.cuda(), dw=only, act=act, pre=pre.cuda())
+    assert torch.equal(only, dw)
