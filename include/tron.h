@@ -407,8 +407,9 @@ TRON_API int tron_probe_copy_bandwidth(double *dst_dev, const double *src_dev, i
  * overlap.  m = 0 is allowed: nothing is written but sums over rows, which are 0.  Where a call needs a work space,
  * tron_..._work says its bytes; it lies at a multiple of 16, its contents are undefined before and after, and calls on
  * different streams need different ones.  Outputs may not overlap inputs except where it is said.
- * Sums, softmax statistics and activations are held in 32 bits or more; results are rounded once to the output's type, to nearest, ties to
- * even.  No atomics: the same call gives the same bits.
+ * Sums, softmax statistics and activations are held in 32 bits or more (gelu and silu are off by a dozen units of their
+ * last place at most, or by 2^-120); results are rounded once to the output's type, to nearest, ties to even.  No atomics:
+ * the same call gives the same bits.
  * ------------------------------------------------------------------------------------------ */
 enum {
     TRON_TYPE_F32 = 0,

@@ -87,41 +87,66 @@ struct Epilogue {
     const float *factor;   // one number that every sum is multiplied by, or NULL
 };
 
-// Phi(a) = (1 + erf(a / sqrt 2)) / 2 by Abramowitz and Stegun, 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x) for
-// x >= 0, off by 1.5e-7 at most.  The library's erff made the product of 8192 x 8192 x 4096 e4m3 operands with gelu a tenth
-// slower.  bell: exp(-a^2 / 2).
+// exp(-v) from the two parts hi + lo = -v log2(e), |lo| at most a unit of the last place of hi: one part alone is off by 2^-24 of the exponent
+__device__ __forceinline__ float exp_of_parts(float hi, float lo)
+{
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return fmaf(e, lo * 0.69314718f, e);
+}
+
+// Phi(a) = (1 + erf(a / sqrt 2)) / 2 = bell t P(t) for a <= 0, with t = 1 / (1 + p |a| / sqrt 2), bell = exp(-a^2 / 2), and 1 minus that
+// of -a above.  P is a polynomial fitted to exp(a^2 / 2) Phi(a) / t by the least largest relative error, 1.9e-7 over |a| <= 20; in 32 bits Phi of
+// either sign is off by 6e-7 of itself, so small values of gelu have their digits too.  Beyond 13 bell is 0.  8192 x 8192 x
+// 4096 e4m3 operands with gelu: 438 us, 428 us by a shorter formula that is off by 0.6% of Phi(-7), a tenth more by erff.
 __device__ __forceinline__ float normal_cdf(float a, float &bell)
 {
-    const float x = fabsf(a) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-    bell = __expf(-x * x);
-    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float beyond = 0.5f * p * bell;   // Phi(-|a|)
+    const float b = fminf(fabsf(a), 20.f), t = __builtin_amdgcn_rcpf(fmaf(0.44f * 0.70710678f, b, 1.f));
+    const float square = b * b, hi = square * -0.72134752f;
+    const float lo = fmaf(square, -0.72134752f, -hi) + fmaf(fmaf(b, b, -square), -0.72134752f, square * -9.629815e-9f);   // b^2 and log2(e) / 2 to 48 bits
+    bell = exp_of_parts(hi, lo);
+    float p = fmaf(t, 0.0357501879f, -0.139577508f);
+    p = fmaf(t, p, 0.149435416f);
+    p = fmaf(t, p, -0.0111487368f);
+    p = fmaf(t, p, 0.108497597f);
+    p = fmaf(t, p, 0.108467117f);
+    p = fmaf(t, p, 0.124467745f);
+    p = fmaf(t, p, 0.124108262f);
+    const float beyond = t * p * bell;   // Phi(-|a|)
     return a < 0.f ? beyond : 1.f - beyond;
+}
+
+// h = 1 / (1 + exp(-a)) and 1 - h, both with their digits
+__device__ __forceinline__ float logistic(float a, float &rest)
+{
+    const float b = fminf(fabsf(a), 120.f), hi = b * -1.44269502f;
+    const float e = exp_of_parts(hi, fmaf(b, -1.44269502f, -hi) + b * -1.925963e-8f), r = __builtin_amdgcn_rcpf(1.f + e);
+    rest = a < 0.f ? r : e * r;
+    return a < 0.f ? e * r : r;
 }
 
 __device__ __forceinline__ float act_of(float a, int act)
 {
-    float bell;
+    float other;
     switch (act) {
     case TRON_ACT_RELU: return a > 0.f || a != a ? a : 0.f;
-    case TRON_ACT_GELU: return a * normal_cdf(a, bell);
-    case TRON_ACT_SILU: return a * __builtin_amdgcn_rcpf(1.f + __expf(-a));
+    case TRON_ACT_GELU: return a * normal_cdf(a, other);
+    case TRON_ACT_SILU: return a * logistic(a, other);
     default: return a;
     }
 }
 
 __device__ __forceinline__ float act_slope(float a, int act)
 {
-    float bell;
+    float other;
     switch (act) {
     case TRON_ACT_RELU: return a > 0.f || a != a ? 1.f : 0.f;
     case TRON_ACT_GELU: {
-        const float phi = normal_cdf(a, bell);
-        return phi + a * 0.39894228f * bell;
+        const float phi = normal_cdf(a, other);
+        return phi + a * 0.39894228f * other;
     }
     case TRON_ACT_SILU: {
-        const float h = __builtin_amdgcn_rcpf(1.f + __expf(-a));
-        return h * (1.f + a * (1.f - h));
+        const float h = logistic(a, other);
+        return h * (1.f + a * other);
     }
     default: return 1.f;
     }

@@ -193,3 +193,48 @@ def test_linear_gradient_dw_in_32_bits_has_no_rounding_of_dpre(m, n, k, act, kin
     _within(dw, want, 2 * E * want.abs() + (off + (m + 8) * 4 * E * d.abs()).T @ X, "dw")
     tron.tron_linear_grad(x.cuda(), None, dy.cuda(), dw=only, act=act, pre=pre.cuda())
     assert torch.equal(only, dw)
+
+
+# --------------------------------------------------------------------------- activations
+def _phi(a):
+    """Phi(a) and its density in 64 bits; erfc keeps the digits of the lower tail."""
+    torch = torch_mod()
+    return 0.5 * torch.special.erfc(-a * math.sqrt(0.5)), torch.exp(-0.5 * a * a) / math.sqrt(2 * math.pi)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU])
+@pytest.mark.parametrize("m", [2, 40])
+def test_activations_have_the_digits_of_their_output(m, act, out):
+    """Values before the activation that are given exactly, by the bias: small results of the negative side too."""
+    torch = torch_mod()
+    n, k = 5003, 8
+    a = torch.linspace(-8.0, 8.0, n) if act == tron.ACT_GELU else torch.linspace(-60.0, 60.0, n)
+    a[:8] = torch.tensor([-11.0, -12.5, 0.0, 30.0, -30.0, -86.0, 86.0, 1e30])
+    x, w = torch.zeros(m, k, device="cuda", dtype=torch.float16), torch.zeros(n, k, device="cuda", dtype=torch.float16)
+    a64, dt = a.double(), _dt(out)
+    if out == "f16":
+        x, w, a64[7], a[7] = x, w, 3e4, 3e4
+    y = torch.empty(m, n, dtype=dt, device="cuda")
+    tron.tron_linear(x, w, y, bias=a.cuda(), act=act)
+    want = a64 * (_phi(a64)[0] if act == tron.ACT_GELU else torch.sigmoid(a64))
+    # a dozen roundings of 32 bits and the fit's 1.9e-7, 4 E; nothing below 2^-120
+    _within(y, want.expand(m, n), (U[out] + 20 * E) * want.abs().expand(m, n) + TINY[out] + 2.0 ** -120, "y")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU])
+def test_slopes_of_activations_have_32_bits(act, kind):
+    torch = torch_mod()
+    n = 4001
+    pre = torch.linspace(-12.0, 12.0, n).to(_dt(kind))
+    dy, db = torch.ones(1, n, dtype=_dt(kind), device="cuda"), torch.empty(n, device="cuda")
+    tron.tron_linear_grad(None, None, dy, dbias=db, act=act, pre=pre[None].cuda())
+    a = pre.double()
+    if act == tron.ACT_GELU:
+        phi, density = _phi(a)
+        want, size = phi + a * density, phi + a.abs() * density
+    else:
+        h, rest = torch.sigmoid(a), torch.sigmoid(-a)
+        want, size = h * (1 + a * rest), h * (1 + a.abs() * rest)
+    _within(db, want, 20 * E * size + 2.0 ** -120, "slope")
