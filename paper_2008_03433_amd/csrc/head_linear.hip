@@ -176,20 +176,31 @@ __device__ __forceinline__ void store_out(void *base, int out, int64_t at, const
     else store8_of<_Float16, PAST>(static_cast<_Float16 *>(base) + at, v, n);
 }
 
+// A scale as fraction and exponent: the product of a row's and a column's may lie outside the range of 32 bits where the result does not.
+struct Scale {
+    float fraction;
+    int exponent;
+};
+__device__ __forceinline__ Scale scale_of(float s) { return {__builtin_amdgcn_frexp_mantf(s), __builtin_amdgcn_frexp_expf(s)}; }
+__device__ __forceinline__ float scaled(float v, const Scale &a, const Scale &b) { return ldexpf(v * (a.fraction * b.fraction), a.exponent + b.exponent); }
+
 // what eight columns have
 struct Columns {
-    float scale[kVec], bias[kVec], factor;
+    Scale scale[kVec];
+    float bias[kVec], factor;
 };
 __device__ __forceinline__ Columns columns_of(const Epilogue &E, int64_t j)
 {
     Columns c;
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-        c.scale[e] = 1.f;
-        c.bias[e] = 0.f;
-    }
+    for (int e = 0; e < kVec; ++e) c.bias[e] = 0.f;
     c.factor = E.factor ? *E.factor : 1.f;
-    if (j < E.n && E.w_scale) load_as<float>(c.scale, E.w_scale, j, E.n - j);
+    if (j < E.n && E.w_scale) {
+        float s[kVec];
+        load_as<float>(s, E.w_scale, j, E.n - j);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) c.scale[e] = scale_of(s[e]);
+    }
     if (j < E.n && E.bias) load_as<float>(c.bias, E.bias, j, E.n - j);
     return c;
 }
@@ -199,13 +210,14 @@ template <bool PAST, int N>
 __device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, float (&v)[N][kVec], int64_t i, int64_t step, int64_t j)
 {
     const int64_t n = E.n - j;
-    float f[N][kVec], xs[N];
+    float f[N][kVec];
+    Scale xs[N];
 #pragma unroll
     for (int q = 0; q < N; ++q) {
         const int64_t row = i + q * step;
         if (row >= E.m) break;
         if (E.residual) load_out(f[q], E.residual, E.out, row * E.ldr + j, n);
-        if (E.x_scale) xs[q] = E.x_scale[row];
+        if (E.x_scale) xs[q] = scale_of(E.x_scale[row]);
     }
 #pragma unroll
     for (int q = 0; q < N; ++q) {
@@ -217,7 +229,7 @@ __device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, flo
         }
         if (E.x_scale) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[q][e] *= xs[q] * C.scale[e];
+            for (int e = 0; e < kVec; ++e) v[q][e] = scaled(v[q][e], xs[q], C.scale[e]);
         }
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[q][e] += C.bias[e];

@@ -238,3 +238,24 @@ def test_slopes_of_activations_have_32_bits(act, kind):
         h, rest = torch.sigmoid(a), torch.sigmoid(-a)
         want, size = h * (1 + a * rest), h * (1 + a.abs() * rest)
     _within(db, want, 20 * E * size + 2.0 ** -120, "slope")
+
+
+# --------------------------------------------------------------------------- scales of 8-bit operands
+@pytest.mark.parametrize("m,n,k", [(3, 40, 96), (150, 140, 512), (40, 60, 20_000)])
+def test_scales_whose_product_leaves_the_range_of_32_bits(m, n, k):
+    """Row and column scales that lie far apart: one large and one small, two small ones and a large sum, down to numbers that are not normal."""
+    torch = torch_mod()
+    g = _gen(m + n)
+    x, w = ((_randn(g, r, k) * 100).clamp(-440, 440).float().to(torch.float8_e4m3fn) for r in (m, n))
+    xs, ws = torch.full((m,), 1.0), torch.full((n,), 1.0)
+    xs[0], ws[0] = 2.0 ** -80 * 1.37, 2.0 ** -66 * 1.71       # 2^-146: three bits left of their product
+    xs[1], ws[1] = 2.0 ** 120 * 1.37, 2.0 ** -120 * 1.71      # sums of 2^20 times 2^120
+    xs[2], ws[2] = 2.0 ** -120 * 1.37, 2.0 ** 120 * 1.71
+    ws[3], ws[4], ws[5] = 2.0 ** -140, 2.0 ** 100, 0.0
+    y = torch.empty(m, n, device="cuda")
+    tron.tron_linear(x.cuda(), w.cuda(), y, x_scale=xs.cuda(), w_scale=ws.cuda())
+    X, W = x.float().double() * xs.double()[:, None], w.float().double() * ws.double()[:, None]
+    want, size = X @ W.T, X.abs() @ W.abs().T
+    inside = size < 2.0 ** 127
+    assert int(inside.sum()) > m * n // 2 and bool(inside[:3, :3].diagonal().all())
+    _within(torch.where(inside, y.cpu(), torch.zeros(())), torch.where(inside, want, 0.0), torch.where(inside, (k + 8) * 2 * E * size + 4 * E * want.abs(), 0.0) + TINY["f32"], "y")
