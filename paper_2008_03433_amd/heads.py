@@ -251,7 +251,12 @@ class SoftmaxHead:
         f(W) = 1/2 W.W + C sum_i loss_i(z_i),   z = X W',   X = rms_norm(hidden + residual) gain
 
     for hidden states (m x d, bfloat16 or float16) and a teacher's ids and t (m x K).  W is n x d float32; the products take it rounded to
-    the states' type.  fun_grad keeps the logits of its W for hv, as Dataset keeps D."""
+    the states' type.  fun_grad keeps the logits of its W for hv, as Dataset keeps D.
+
+    hv is linear in its direction, whose size is the caller's (a gradient's, in the first product of a solve).  In float16 the products take it
+    times a power of two, and the result by its reciprocal, so that neither the direction nor X V' leaves the type's range."""
+
+    _LARGEST = 12   # log2 of a bound on |X V'|: four bits below float16's largest value, for weights and roundings
 
     def __init__(self, hidden, ids, t, gain=None, residual=None, eps=1e-6, temperature=1.0, weight=None):
         _load()
@@ -262,10 +267,21 @@ class SoftmaxHead:
         self.loss = _torch.empty(self.m, dtype=_torch.float32, device=hidden.device)
         self.lse = _torch.empty_like(self.loss)
         self.z = None
+        self._reach = self._exponent(self.X.abs().sum(1, dtype=_torch.float32)) if self.X.dtype == _torch.float16 and self.m else None
+
+    @staticmethod
+    def _exponent(a):
+        """e with |a| <= 2^e in every element, on the device."""
+        return _torch.frexp(_torch.linalg.vector_norm(a, ord=float("inf"))).exponent
+
+    def _scale(self, V):
+        """The power of two by which |V| and |X V'| are at most 2^_LARGEST (|X V'| <= the largest sum of a row's |x| times the largest |v|)."""
+        return _torch.exp2((self._LARGEST - self._reach.clamp(min=0) - self._exponent(V)).float().clamp(-120.0, 120.0))
 
     def _logits(self, W):
+        """X W' of weights in the states' type."""
         z = _torch.empty((self.m, W.shape[0]), dtype=self.X.dtype, device=W.device)
-        tron_linear(self.X, W.to(self.X.dtype), z)
+        tron_linear(self.X, W, z)
         return z
 
     def _to_weights(self, dz, C, V, out):
@@ -274,7 +290,7 @@ class SoftmaxHead:
 
     def fun_grad(self, C, W, G: Optional[object] = None) -> float:
         """f(W); the gradient goes to G (n x d float32) when given."""
-        self.z = self._logits(W)
+        self.z = self._logits(W.to(self.X.dtype))
         dz = None if G is None else _torch.empty_like(self.z)
         tron_distill(self.z, self.ids, self.t, self.loss, self.lse, temperature=self.temperature, weight=self.weight, dz=dz)
         if G is not None:
@@ -285,6 +301,11 @@ class SoftmaxHead:
         """HV = V + C X' (H_z (X V')) for the W of the last fun_grad."""
         if self.z is None:
             raise TronError(-4, "SoftmaxHead.hv before fun_grad")
-        u = self._logits(V)
+        if self._reach is None:   # bfloat16 has the range of 32 bits
+            direction = V.to(self.X.dtype)
+        else:
+            scale = self._scale(V)
+            C, direction = C / scale, _torch.mul(V, scale, out=_torch.empty_like(V, dtype=self.X.dtype))
+        u = self._logits(direction)
         tron_distill_hv(self.z, self.lse, u, u, ids=self.ids, t=self.t, temperature=self.temperature, weight=self.weight)
         self._to_weights(u, C, V, HV)

@@ -259,3 +259,42 @@ def test_scales_whose_product_leaves_the_range_of_32_bits(m, n, k):
     inside = size < 2.0 ** 127
     assert int(inside.sum()) > m * n // 2 and bool(inside[:3, :3].diagonal().all())
     _within(torch.where(inside, y.cpu(), torch.zeros(())), torch.where(inside, want, 0.0), torch.where(inside, (k + 8) * 2 * E * size + 4 * E * want.abs(), 0.0) + TINY["f32"], "y")
+
+
+# --------------------------------------------------------------------------- the head's Hessian-vector product
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+def test_softmax_head_hv_of_directions_of_any_size(kind):
+    """The curvature term scales with its direction, from sizes that float16 does not hold to such that it rounds to 0."""
+    torch = torch_mod()
+    g = _gen(21)
+    m, d, V, K, C = 60, 200, 37, 3, 0.5
+    hidden, dt = _randn(g, m, d).to(_dt(kind)), _dt(kind)
+    ids, t = torch.randint(0, V, (m, K), generator=g), _randn(g, m, K).float()
+    W, D = (_randn(g, V, d) / 16).to(dt).float(), (_randn(g, V, d)).to(dt).float()
+    head = tron.SoftmaxHead(hidden.cuda(), ids.cuda(), t.cuda())
+    head.fun_grad(C, W.cuda())
+    X, z = head.X.double().cpu(), head.z.double().cpu()
+    p, u = torch.softmax(z, 1), X @ D.double().T
+    h = p * u - p * (p * u).sum(1, keepdim=True)
+    want = C * h.T @ X
+    # u and H u are rounded to the states' type, H u down to steps of 2^-25 (f16) where |u| is below 2^12 and above 2^12 / (d 2)
+    off = p * (u.abs() + (p * u.abs()).sum(1, keepdim=True)) * (U[kind] + 2.0 ** -10) + h.abs() * U[kind] + 2.0 ** -24
+    bound = C * off.T @ X.abs()
+    curvature = {}
+    for power in (0, 20, -30, 60, -100):
+        size = 2.0 ** power
+        HV = torch.empty(V, d, device="cuda")
+        V_ = (D * size).cuda()
+        head.hv(C, V_, HV)
+        assert torch.isfinite(HV).all(), power
+        # the sum with V is rounded to 32 bits
+        curvature[power] = (HV.double().cpu() - (D * size).double()) / size
+        _within(curvature[power], want, bound + 2 * E * (want.abs() + D.double().abs()), f"direction times 2^{power}")
+        again = torch.empty_like(HV)
+        head.hv(C, V_, again)
+        assert torch.equal(again, HV)
+    # a power of two changes no bit
+    assert all(torch.equal(c, curvature[0]) for c in curvature.values())
+    HV.fill_(7.0)
+    head.hv(C, torch.zeros(V, d, device="cuda"), HV)
+    assert (HV == 0).all()
