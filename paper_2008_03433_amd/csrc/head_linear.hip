@@ -683,8 +683,10 @@ __device__ __forceinline__ void deep_tile(const ProductArgs &A, int64_t block, i
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) *reinterpret_cast<i32x4 *>(to + place[c]) = from[c];
     };
-    // two places in turn: who writes one again has passed the next step's barrier, behind which all have read it
+    // two places in turn: who writes one again has passed the next step's barrier, behind which all have read it.  Neither the compiler's
+    // stores to LDS before nor its reads behind may pass the barrier.
     auto multiply = [&](const char *now) {
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the loads from memory go on
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
