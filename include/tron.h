@@ -381,6 +381,8 @@ TRON_API int tron_probe_read_bandwidth(const double *src_dev, int64_t count, int
  * "batch_mfma" (-1/0/1): batches created afterwards run the multi-problem pass on the fp64 matrix units (1), or on the
  *                vector units where those can hold the batch, i.e. up to eight problems (0); -1 (default): the matrix
  *                units from nine problems on, and for seven or eight logistic ones over 26 or 28 to 32 columns, eight above 288 MB.
+ * "linear_tile" (0/128/256): rows and columns of a tile of tron_linear and tron_linear_grad where there are more than 32 rows,
+ *                read at every call and by the calls that give the size of its work space; 0 (default): by what each would take.
  * Unknown names or values return TRON_EINVAL.
  */
 TRON_API int tron_tuning_set(const char *name, int64_t value);

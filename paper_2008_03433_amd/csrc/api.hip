@@ -893,6 +893,10 @@ int tron_tuning_set(const char *name, int64_t value)
         g_tuning.batch_mfma = value;
         return TRON_OK;
     }
+    if (name && strcmp(name, "linear_tile") == 0 && (value == 0 || value == 128 || value == 256)) {
+        g_tuning.linear_tile = value;
+        return TRON_OK;
+    }
     set_error("tron_tuning_set: unknown knob or value out of range");
     return TRON_EINVAL;
 }

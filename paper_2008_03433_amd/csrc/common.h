@@ -60,6 +60,7 @@ struct Tuning {
     int64_t batch_grid = 0;  // workgroups of the multi-problem pass: 0 = as many as are resident at once
     int64_t batch_mfma = -1; // multi-problem pass on the matrix units: 1 = yes, 0 = no, -1 = the library decides
     int64_t batch_lean = 1;         // matrix-unit pass: rounds without function / gradient requests run a kernel compiled without those steps
+    int64_t linear_tile = 0;        // rows and columns of a tile of matrix products over more than 32 rows: 128 or 256; 0 = by the rule
     int64_t batch_mfma_rows = 0;    // rows of X a wavefront of that pass keeps in LDS at a time: 32 or 64; 0 = by LDS footprint
 };
 extern Tuning g_tuning;

@@ -942,6 +942,7 @@ Plan linear_plan(int64_t m, int64_t n, int64_t k, int type)
         }
     } else {
         for (const Shape shape : {SHAPE_256, SHAPE_128}) {
+            if (g_tuning.linear_tile == (shape == SHAPE_256 ? 128 : 256)) continue;
             const int64_t b = shape == SHAPE_256 ? 256 : 128, tiles_m = ceil_div(m, b), tiles_n = ceil_div(n, b), tiles = tiles_m * tiles_n;
             for (int64_t p = 1; p == 1 || p <= std::min({2 * kUnits / tiles, steps, kMostParts}); ++p) {
                 const int64_t each = ceil_div(steps, p);

@@ -5,7 +5,8 @@ import math
 import pytest
 
 import paper_2008_03433_amd as tron
-from test_gpu_heads import E, TINY, U, _distill_bounds, _distill_plain, _dt, _gen, _randn, _within
+import test_gpu_heads as heads
+from test_gpu_heads import E, TINY, U, _check_linear, _distill_bounds, _distill_plain, _dt, _gen, _randn, _within
 from util import torch_mod
 
 pytestmark = pytest.mark.gpu
@@ -298,3 +299,93 @@ def test_softmax_head_hv_of_directions_of_any_size(kind):
     HV.fill_(7.0)
     head.hv(C, torch.zeros(V, d, device="cuda"), HV)
     assert (HV == 0).all()
+
+
+# --------------------------------------------------------------------------- every kernel of the matrix product, whatever the rule takes
+@pytest.fixture
+def tile():
+    """Sets the tiles of products over more than 32 rows."""
+    yield lambda side: tron.tron_tuning_set("linear_tile", side)
+    tron.tron_tuning_set("linear_tile", 0)
+
+
+# whole chunks at multiples of 16 bytes (from memory straight to LDS): one step, a step that ends inside a row of chunks, several; rows that end
+# inside a chunk, and rows that lie apart (through registers); an inner index cut in many
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f16", "f16"), ("e4m3", "bf16"), ("e4m3", "f32")])
+@pytest.mark.parametrize("m,n,k", [(33, 40, 16), (257, 255, 1008), (300, 520, 2048), (256, 512, 64), (129, 300, 1031), (70, 60, 20_000), (300, 258, 20_001)])
+def test_linear_in_tiles_of_256(tile, m, n, k, kind, out):
+    tile(256)
+    for act in (m % 4, 2):
+        _check_linear(m, n, k, kind, out, act=act, bias=True, residual=True, pre=True)
+    _check_linear(m, n, k, kind, out, act=0, bias=False, residual=False, pre=False, pads=(7, 3))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "e4m3"])
+@pytest.mark.parametrize("m,n,k", [(4100, 4099, 272), (2300, 4099, 1040), (4000, 4099, 77)])
+def test_linear_in_tiles_of_256_with_a_result_past_the_caches(tile, m, n, k, kind):
+    tile(256)
+    heads.test_linear_large(m, n, k, kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(300, 520, 264), (300, 520, 265), (515, 262, 129), (700, 258, 300), (2000, 40, 72)])
+def test_linear_gradients_in_tiles_of_256(tile, m, n, k, kind):
+    """All activations, dx and dw from the padded copies, parts where the inner index is long."""
+    tile(256)
+    heads.test_linear_gradients(m, n, k, kind)
+    tile(128)
+    heads.test_linear_gradients(m, n, k, kind)
+
+
+@pytest.mark.parametrize("side", [128, 256])
+def test_tiles_in_a_graph(tile, side):
+    """A captured product and its gradients, replayed on other inputs beside eager work."""
+    torch = torch_mod()
+    tile(side)
+    m, n, k = 300, 264, 520
+    x, w, dy = (torch.empty(*s, dtype=torch.float16, device="cuda") for s in ((m, k), (n, k), (m, n)))
+
+    def outputs():
+        return (torch.empty(m, n, device="cuda"), torch.empty(m, n, dtype=torch.float16, device="cuda"), torch.empty(m, k, dtype=torch.float16, device="cuda"),
+                torch.empty(n, k, device="cuda"), torch.empty(n, device="cuda"))
+
+    def go(y, pre, dx, dw, db):
+        tron.tron_linear(x, w, pre, act=tron.ACT_NONE)
+        tron.tron_linear(x, w, y, act=tron.ACT_GELU)
+        tron.tron_linear_grad(x, w, dy, dx=dx, dw=dw, dbias=db, act=tron.ACT_GELU, pre=pre)
+
+    def fill(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for t, std in ((x, 1.0), (w, k ** -0.5), (dy, 1.0)):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda") * std)
+
+    eager, captured = outputs(), outputs()
+    fill(0)
+    go(*captured)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go(*captured)
+    for seed in range(1, 4):
+        fill(seed)
+        for t in captured:
+            t.fill_(-1.0)
+        go(*eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, captured))
+
+
+# --------------------------------------------------------------------------- norms whose outputs go past the caches
+@pytest.mark.parametrize("out", ["same", "e4m3"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,d", [(12_500, 1001), (2_700, 4099), (340, 33_001)])
+def test_norm_with_outputs_past_the_caches(m, d, kind, out):
+    """Rows of a wavefront, of a workgroup, and such that are read twice; odd strides."""
+    heads.test_norm(m, d, kind, out)
+
+
+@pytest.mark.parametrize("kind,m,d", [("f32", 8_100, 1001), ("bf16", 16_100, 1001), ("f16", 4_100, 4099), ("f32", 2_000, 4099), ("bf16", 1_000, 16_501)])
+def test_norm_gradient_with_outputs_past_the_caches(kind, m, d):
+    heads.test_norm_gradient(m, d, kind)
