@@ -1059,7 +1059,8 @@ struct TurnArgs {
     void *same, *turned;       // [rows][ldsame], [cols][ldturned], zeros from the last element to the end of its chunk; or NULL
     int64_t ldsame, ldturned;
     float *shares;             // [patches of rows][cols]: column sums of the products before rounding, or NULL
-    const float *factor;       // one number that the products are multiplied by before they are rounded, or NULL
+    float *factors;            // f16: see k_range_parts; or NULL, and the products are rounded as they are
+    int range_parts;
     void *rest;                // as `turned`: what that rounding left, times kRestLift, or NULL
     int64_t blocks;
 };
@@ -1092,6 +1093,46 @@ __device__ __forceinline__ void turn8(Raw8<T> (&r)[kVec])
 template <typename T>
 constexpr float kRestLift = __is_same(T, __bf16) ? 1.f : 2048.f;
 
+// f16: dpre is dy times a slope of up to 1.13, which may lie above the largest value or below the smallest where the products' results
+// do not.  It is held times a power of two, by which the largest |dy| comes to lie in [2^14, 2^15), and the results are multiplied by its
+// reciprocal.  This launch takes the maximum, in parts behind the factors; the next one joins them, and its first wavefront writes the
+// factors of the products: the reciprocal, and that for what the rounding left.  8192 x 4096: 25 us; all gradients with 4096 inputs 628 us,
+// 586 us without.
+constexpr int kRangeBlocks = 512, kFactors = 2;
+
+__global__ __launch_bounds__(kBlock) void k_range_parts(const _Float16 *dy, int64_t m, int64_t n, int64_t ld, float *parts)
+{
+    __shared__ float room[2 * kMostWaves];
+    const int64_t across = (n + kVec - 1) / kVec, chunks = m * across;
+    float top = 0.f, none = 0.f;
+    for (int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * kBlock) {
+        const int64_t i = c / across;
+        const Raw8<_Float16> r = load_row8(dy + i * ld, (c - i * across) * kVec, n, static_cast<_Float16>(0.f));
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) top = fmaxf(top, fabsf(static_cast<float>(r.v[e])));
+    }
+    block_sum_max(none, top, room);
+    if (threadIdx.x == 0) parts[blockIdx.x] = top;
+}
+
+int range_blocks(int64_t m, int64_t n) { return (int)std::min<int64_t>(kRangeBlocks, ceil_div(m * ceil_div(n, kVec), kBlock)); }
+
+// by a wavefront; `writes`: whether it is the one that writes the factors
+template <typename T>
+__device__ __forceinline__ float range_factor(float *factors, int parts, int lane, bool writes)
+{
+    float top = 0.f;
+    for (int i = lane; i < parts; i += kWave) top = fmaxf(top, factors[kFactors + i]);
+    top = wave_maxf(top);
+    // infinities stay what they are; all others are safe as beside 65504
+    const int e = top == 0.f ? 0 : top < INFINITY ? 14 - ilogbf(top) : -1;
+    if (writes && lane == 0) {
+        factors[0] = ldexpf(1.f, -e);
+        factors[1] = ldexpf(1.f / kRestLift<T>, -e);
+    }
+    return ldexpf(1.f, e);
+}
+
 // A wavefront a patch: lane 8 a + b holds rows 8 a .. + 7 and columns 8 b .. + 7, reads them as eight pieces of 16 bytes, and writes them so or
 // turned in its registers.  The four of a workgroup take patches one below the other: their pieces of a turned row are 512 bytes (side by
 // side 42 us, so 35 us for 8192 x 4096 bf16, 3.8 TB/s).
@@ -1115,7 +1156,7 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
     float sum[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
-    const float factor = A.factor ? *A.factor : 1.f;
+    const float factor = ACT != TRON_ACT_NONE && !__is_same(T, __bf16) && A.factors ? range_factor<T>(A.factors, A.range_parts, lane, patch_row == 0 && patch_col == 0) : 1.f;
 #pragma unroll
     for (int r = 0; r < kVec; ++r) {
         if (i0 + r < A.rows && n > 0) {
@@ -1183,50 +1224,6 @@ int turn(TurnList &L, hipStream_t st)
     for (int i = 0; i < L.count; ++i) blocks += L.list[i].blocks = ceil_div(L.list[i].rows, kPatch * kWavesPerBlock) * ceil_div(L.list[i].cols, kPatch);
     if (!blocks) return TRON_OK;
     k_turn<T><<<block_grid(blocks), kBlock, 0, st>>>(L);
-    TRON_HIP(hipGetLastError());
-    return TRON_OK;
-}
-
-// f16: dpre is dy times a slope of up to 1.13, which may lie above the largest value or below the smallest where the products' results
-// do not.  It is held times a power of two, by which the largest |dy| comes to lie in [2^14, 2^15), and the results are multiplied by its
-// reciprocal.  factors: that power, its reciprocal, and that for what the rounding left.  8192 x 4096: 25 us for the maximum and 5 us for the factors, where all gradients
-// with 4096 inputs take 580 us without.
-constexpr int kRangeBlocks = 512, kFactors = 3;
-
-__global__ __launch_bounds__(kBlock) void k_range_parts(const _Float16 *dy, int64_t m, int64_t n, int64_t ld, float *parts)
-{
-    __shared__ float room[2 * kMostWaves];
-    const int64_t across = (n + kVec - 1) / kVec, chunks = m * across;
-    float top = 0.f, none = 0.f;
-    for (int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * kBlock) {
-        const int64_t i = c / across;
-        const Raw8<_Float16> r = load_row8(dy + i * ld, (c - i * across) * kVec, n, static_cast<_Float16>(0.f));
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) top = fmaxf(top, fabsf(static_cast<float>(r.v[e])));
-    }
-    block_sum_max(none, top, room);
-    if (threadIdx.x == 0) parts[blockIdx.x] = top;
-}
-
-__global__ __launch_bounds__(kWave) void k_range_factors(const float *parts, int count, float *factors)
-{
-    float top = 0.f;
-    for (int i = threadIdx.x; i < count; i += kWave) top = fmaxf(top, parts[i]);
-    top = wave_maxf(top);
-    if (threadIdx.x == 0) {
-        // infinities stay what they are; all others are safe as beside 65504
-        const int e = top == 0.f ? 0 : top < INFINITY ? 14 - ilogbf(top) : -1;
-        factors[0] = ldexpf(1.f, e);
-        factors[1] = ldexpf(1.f, -e);
-        factors[2] = ldexpf(1.f / kRestLift<_Float16>, -e);
-    }
-}
-
-int range_factors(const void *dy, int64_t m, int64_t n, int64_t ld, float *space, hipStream_t st)
-{
-    const unsigned blocks = (unsigned)std::min<int64_t>(kRangeBlocks, ceil_div(m * ceil_div(n, kVec), kBlock));
-    k_range_parts<<<blocks, kBlock, 0, st>>>(static_cast<const _Float16 *>(dy), m, n, ld, space + kFactors);
-    k_range_factors<<<1, kWave, 0, st>>>(space + kFactors, (int)blocks, space);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -1316,13 +1313,13 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     float *factors = nullptr;
     if (sizeof(T) == 2 && !__is_same(T, __bf16) && smooth(G.act) && (same || G.dw)) {
         factors = reinterpret_cast<float *>(G.work + S.factors);
-        TRON_TRY(range_factors(G.dy, m, n, G.lddy, factors, st));
+        k_range_parts<<<range_blocks(m, n), kBlock, 0, st>>>(static_cast<const _Float16 *>(G.dy), m, n, G.lddy, factors + kFactors);
     }
     TurnList L{};
     if (G.dbias || G.dw || same)
-        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, factors, rest ? rest_t : nullptr, 0};
-    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, nullptr, nullptr, 0};
-    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, nullptr, nullptr, 0};
+        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, factors, range_blocks(m, n), rest ? rest_t : nullptr, 0};
+    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, nullptr, 0, nullptr, 0};
+    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, nullptr, 0, nullptr, 0};
     TRON_TRY(turn<T>(L, st));
     if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
     Epilogue E{}, F{};
@@ -1337,7 +1334,7 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     F.ldy = G.lddw;
     F.out = G.dw_type;
     Epilogue few = E;   // which multiplies dy itself
-    if (factors) E.factor = F.factor = factors + 1;
+    if (factors) E.factor = F.factor = factors;
     // without an activation dy itself, whose rows end at n
     const ProductArgs A = product_args(act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy}, Operand{w_t, k, np}, act ? nw : n, S.for_dx, E, part_dx);
     const ProductArgs B = product_args(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, F, reinterpret_cast<float *>(G.work + S.part_dw));
@@ -1356,7 +1353,7 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     Epilogue R = F;
     R.residual = G.dw;
     R.ldr = G.lddw;
-    if (factors) R.factor = factors + 2;
+    if (factors) R.factor = factors + 1;
     return product<T>(product_args(Operand{rest_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, R, reinterpret_cast<float *>(G.work + S.part_dw)), S.for_dw, st);
 }
 
