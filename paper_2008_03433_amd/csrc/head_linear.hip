@@ -85,6 +85,7 @@ struct Epilogue {
     float *part;   // [parts][m][n]: sums of a part of the inner index instead
     bool past;     // y goes past the caches
     const float *factor;   // one number that every sum is multiplied by, or NULL
+    bool small_part;       // the sums are what the residual has been rounded by: one that is not finite stays
 };
 
 // exp(-v) from the two parts hi + lo = -v log2(e), |lo| at most a unit of the last place of hi: one part alone is off by 2^-24 of the exponent
@@ -240,7 +241,7 @@ __device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, flo
         }
         if (E.residual) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[q][e] += f[q][e];
+            for (int e = 0; e < kVec; ++e) v[q][e] = E.small_part && !__builtin_isfinite(f[q][e]) ? f[q][e] : v[q][e] + f[q][e];
         }
         store_out<PAST>(E.y, E.out, row * E.ldy + j, v[q], n);
     }
@@ -1353,6 +1354,7 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     Epilogue R = F;
     R.residual = G.dw;
     R.ldr = G.lddw;
+    R.small_part = true;
     if (factors) R.factor = factors + 1;
     return product<T>(product_args(Operand{rest_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, R, reinterpret_cast<float *>(G.work + S.part_dw)), S.for_dw, st);
 }
@@ -1400,7 +1402,7 @@ int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_
     }
     TRON_TRY(check_device());
     if (m == 0) return TRON_OK;
-    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr, false, nullptr};
+    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr, false, nullptr, false};
     const Operand a{x, m, ldx}, b{w, n, ldw};
     const Plan P = linear_plan(m, n, k, type);
     const ProductArgs A = product_args(a, b, k, P, E, static_cast<float *>(work));

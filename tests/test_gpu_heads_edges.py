@@ -194,6 +194,13 @@ def test_linear_gradient_dw_in_32_bits_has_no_rounding_of_dpre(m, n, k, act, kin
     _within(dw, want, 2 * E * want.abs() + (off + (m + 8) * 4 * E * d.abs()).T @ X, "dw")
     tron.tron_linear_grad(x.cuda(), None, dy.cuda(), dw=only, act=act, pre=pre.cuda())
     assert torch.equal(only, dw)
+    # one infinite term: the result is that infinity, of its sign
+    x[1, 5] = math.inf
+    tron.tron_linear_grad(x.cuda(), None, dy.cuda(), dw=only, act=act, pre=pre.cuda())
+    if act != tron.ACT_RELU:   # its zeros times infinity are NaN
+        assert torch.equal(only[:, 5].cpu(), torch.sign(d[1]).float() * math.inf)
+    only[:, 5] = dw[:, 5]
+    assert torch.equal(only, dw)
 
 
 # --------------------------------------------------------------------------- activations
