@@ -563,7 +563,7 @@ __global__ __launch_bounds__(1024, CH * sizeof(T) <= 8 ? 8 : 4) void k_distill_h
     } else {
         over_rows(z, u, 0, V, [&](int64_t, const Raw8<T> &x, const Raw8<T> &y) { dot8(x, y); });
     }
-    dot = block_sumf(dot, room);
+    dot = block_sum_all(dot, room);
     if (CH) {
         if (kAnew) {
 #pragma unroll
@@ -612,7 +612,7 @@ __global__ __launch_bounds__(1024) void k_distill_hv_part(DistillArgs A)
         if (!FIRST) store8_of<T>(out + j, v, to - j);
     });
     if (FIRST) {
-        dot = block_sumf(dot, room);
+        dot = block_sum_all(dot, room);
         if (threadIdx.x == 0) A.part_sum[row * A.splits + blockIdx.x] = dot;
     }
 }

@@ -5,8 +5,8 @@
 //
 // Both are bound by memory: every matrix is read or written once, and a row stays in registers between the sums over it and the
 // outputs that need them.  A row belongs to one wavefront (narrow rows: no barriers) or to one workgroup.  The sums are taken in
-// 32 bits over the unrounded s; `total` is s rounded to its type, and the gradient reads that.  The scale's maximum is taken with
-// the sum of squares, over s gain, so 8 bits cost no further pass.
+// 32 bits over the unrounded s (those of squares in 64 where 32 lose their range); `total` is s rounded to its type, and the gradient
+// reads that.  The scale's maximum is taken with the sum of squares, over s gain, so 8 bits cost no further pass.
 //
 // Measured: 16384 x 8192 bf16 with a residual to e4m3 158 us (939 MB, 5.95 TB/s: outputs larger than 32 MB go past the caches, which keep what
 // is read); one row of 4096 3.7 us of the device's time, 9 us a call; gradient of 20011 x 2047 f16 with all its inputs 100 us, of which 5 us
@@ -32,6 +32,7 @@ struct NormArgs {
 };
 
 constexpr float kE4m3Max = 448.f;
+constexpr float kLeastSquares = 0x1p-60f, kMostSquares = 0x1p100f;   // where a sum of squares has its digits in 32 bits, whatever parts are lost
 
 template <typename T>
 struct Elements {
@@ -56,10 +57,25 @@ __device__ __forceinline__ void gain8(float *g, const float *gain, int64_t j, in
 struct RowFactors {
     float rstd, scale, per_scale;
 };
-__device__ __forceinline__ RowFactors row_factors(float sum2, float top, float eps, float inv_d)
+// From a thread's sum of squares and its max |s gain|, by a wavefront or a workgroup.  The sum is joined in 32 bits, and in 64 once more where
+// these have lost its range, so that rows of any size have their rstd.
+template <bool WAVE, bool EIGHT>
+__device__ __forceinline__ RowFactors row_factors(double own, float top, float eps, float inv_d)
 {
+    __shared__ float room[2 * kMostWaves];
+    __shared__ double wide_room[kMostWaves];
+    float sum2 = (float)own;
+    if (WAVE) {
+        sum2 = wave_sumf(sum2);
+        if (EIGHT) top = wave_maxf(top);
+    } else if (EIGHT) {
+        block_sum_max(sum2, top, room);
+    } else {
+        sum2 = block_sum_all(sum2, room);
+    }
     RowFactors f;
-    f.rstd = 1.f / sqrtf(sum2 * inv_d + eps);
+    if (sum2 >= kLeastSquares && sum2 <= kMostSquares) f.rstd = 1.f / sqrtf(sum2 * inv_d + eps);
+    else f.rstd = (float)(1.0 / sqrt((WAVE ? wave_sum(own) : block_sum_all(own, wide_room)) * (double)inv_d + (double)eps));
     // max |y| = rstd max |s gain|; a row of zeros (and one with a NaN, which every y then is) has scale 1.  The smallest normal
     // number as the least scale has a finite reciprocal.
     const float largest = top * f.rstd;
@@ -68,19 +84,36 @@ __device__ __forceinline__ RowFactors row_factors(float sum2, float top, float e
     return f;
 }
 
+// A thread's sum of squares: in 64 bits anew where 32 have lost its range.  (All sums in 64 bits: 16384 x 8192 bf16 to e4m3 167 us instead of 162.)
+template <int CH>
+__device__ __forceinline__ double squares(const float (&s)[CH][kVec])
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum = fmaf(s[c][i], s[c][i], sum);
+    if (sum >= kLeastSquares && sum <= kMostSquares) return sum;
+    double wide = 0.0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) wide = fma((double)s[c][i], (double)s[c][i], wide);
+    return wide;
+}
+
 // CH chunks of eight elements a thread; WAVE: a wavefront a row, otherwise a workgroup
 template <typename T, typename O, int CH, bool WAVE, bool PAST>
 __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm(NormArgs A)
 {
     constexpr bool kEight = sizeof(O) == 1;
-    __shared__ float room[2 * kMostWaves];
     const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     const int64_t row = WAVE ? block_number() * kWaveRows + threadIdx.x / kWave : block_number();
     if (row >= A.m) return;
     const int64_t d = A.d;
     const Elements<T> x{static_cast<const T *>(A.x) + row * A.ldx, d};
     float s[CH][kVec];
-    float sum2 = 0.f, top = 0.f;
+    float top = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int64_t j = (int64_t)(me + c * team) * kVec;
@@ -105,10 +138,7 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm(No
             }
         }
     }
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) sum2 = fmaf(s[c][i], s[c][i], sum2);
+    const double sum2 = squares(s);
     if (A.total) {
         T *t = static_cast<T *>(A.total) + row * A.ldt;
 #pragma unroll
@@ -131,15 +161,7 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm(No
             }
         }
     }
-    if (WAVE) {
-        sum2 = wave_sumf(sum2);
-        if (kEight) top = wave_maxf(top);
-    } else if (kEight) {
-        block_sum_max(sum2, top, room);
-    } else {
-        sum2 = block_sumf(sum2, room);
-    }
-    const RowFactors f = row_factors(sum2, top, A.eps, A.inv_d);
+    const RowFactors f = row_factors<WAVE, kEight>(sum2, top, A.eps, A.inv_d);
     if (me == 0) {
         if (A.rstd) A.rstd[row] = f.rstd;
         if (kEight) A.scale[row] = f.scale;
@@ -162,7 +184,6 @@ template <typename T, typename O, bool PAST>
 __global__ __launch_bounds__(1024) void k_rms_norm_wide(NormArgs A)
 {
     constexpr bool kEight = sizeof(O) == 1;
-    __shared__ float room[2 * kMostWaves];
     const int64_t row = block_number(), d = A.d, step = (int64_t)blockDim.x * kVec;
     if (row >= A.m) return;
     const Elements<T> x{static_cast<const T *>(A.x) + row * A.ldx, d}, r{static_cast<const T *>(A.residual) + (A.residual ? row * A.ldr : 0), d};
@@ -176,19 +197,19 @@ __global__ __launch_bounds__(1024) void k_rms_norm_wide(NormArgs A)
             for (int i = 0; i < kVec; ++i) s[i] += static_cast<float>(u.v[i]);
         }
     };
-    float sum2 = 0.f, top = 0.f;
+    double sum2 = 0.0;
+    float top = 0.f;
     for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
         float s[kVec], g[kVec];
         sum8(s, j);
         if (kEight) gain8(g, A.gain, j, d);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            sum2 = fmaf(s[i], s[i], sum2);
+            sum2 = fma((double)s[i], (double)s[i], sum2);
             if (kEight) top = fmaxf(top, fabsf(s[i] * g[i]));
         }
     }
-    block_sum_max(sum2, top, room);
-    const RowFactors f = row_factors(sum2, top, A.eps, A.inv_d);
+    const RowFactors f = row_factors<false, kEight>(sum2, top, A.eps, A.inv_d);
     if (threadIdx.x == 0) {
         if (A.rstd) A.rstd[row] = f.rstd;
         if (kEight) A.scale[row] = f.scale;
@@ -291,7 +312,7 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm_gr
         for (int q = 0; q < kRows; ++q) {
             const int64_t row = row0 + q * teams;
             if (row >= A.m) break;
-            const float back = rstd[q] * rstd[q] * (dot[q] * A.inv_d);
+            const float back = rstd[q] * (rstd[q] * (dot[q] * A.inv_d));   // not rstd^2, which may be no number of 32 bits
             T *dx = static_cast<T *>(A.dx) + row * A.lddx;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -353,8 +374,8 @@ __global__ __launch_bounds__(1024) void k_rms_norm_grad_wide(NormGradArgs A)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) dot = fmaf(static_cast<float>(dy.v[i]) * g[i], static_cast<float>(s.v[i]), dot);
     }
-    dot = block_sumf(dot, room);
-    const float rstd = A.rstd[row], back = rstd * rstd * (dot * A.inv_d);
+    dot = block_sum_all(dot, room);
+    const float rstd = A.rstd[row], back = rstd * (rstd * (dot * A.inv_d));
     T *dx = static_cast<T *>(A.dx) + row * A.lddx;
     for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
         const Raw8<T> s = sv.at(j), dy = dyv.at(j);

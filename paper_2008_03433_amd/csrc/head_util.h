@@ -154,6 +154,10 @@ __device__ __forceinline__ float wave_maxf(float v)
     return wave_joinf(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
+// in 32 or 64 bits
+__device__ __forceinline__ float wave_sum_of(float v) { return wave_sumf(v); }
+__device__ __forceinline__ double wave_sum_of(double v) { return wave_sum(v); }
+
 // Largest workgroup of these kernels
 constexpr int kMostWaves = 16;
 
@@ -178,14 +182,15 @@ __device__ __forceinline__ void block_sum_max(float &a, float &b, float *room)
     }
 }
 
-__device__ __forceinline__ float block_sumf(float a, float *room)
+template <typename S>
+__device__ __forceinline__ S block_sum_all(S a, S *room)
 {
     const int waves = blockDim.x / kWave;
-    a = wave_sumf(a);
+    a = wave_sum_of(a);
     if (waves == 1) return a;
     if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = a;
     __syncthreads();
-    a = 0.f;
+    a = 0;
     for (int w = 0; w < waves; ++w) a += room[w];
     return a;
 }

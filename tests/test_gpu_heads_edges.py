@@ -396,3 +396,37 @@ def test_norm_with_outputs_past_the_caches(m, d, kind, out):
 @pytest.mark.parametrize("kind,m,d", [("f32", 8_100, 1001), ("bf16", 16_100, 1001), ("f16", 4_100, 4099), ("f32", 2_000, 4099), ("bf16", 1_000, 16_501)])
 def test_norm_gradient_with_outputs_past_the_caches(kind, m, d):
     heads.test_norm_gradient(m, d, kind)
+
+
+# --------------------------------------------------------------------------- norms of rows of any size
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [100, 3000, 20_000, 40_000])
+def test_norm_and_gradient_of_rows_whose_squares_leave_the_range_of_32_bits(d, kind):
+    """Rows of 1e-25 to 1e25: rstd, y (in 8 bits too) and the gradients as for rows of 1."""
+    torch = torch_mod()
+    g, dt, u = _gen(d), _dt(kind), U[kind]
+    sizes = torch.tensor([2.0 ** -83, 2.0 ** -70, 1.0, 2.0 ** 70, 2.0 ** 83], dtype=torch.float64)[:, None]
+    m = len(sizes)
+    s, dy, gain = (_randn(g, m, d) * sizes).to(dt), _randn(g, m, d).to(dt), (1.0 + 0.2 * _randn(g, d)).float()
+    S = s.double()
+    rstd = (S * S).mean(1, keepdim=True) ** -0.5
+    y = S * rstd * gain.double()
+    got, q, scale, got_rstd = torch.empty(m, d, dtype=dt, device="cuda"), torch.empty(m, d, dtype=_dt("e4m3"), device="cuda"), torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    lost = 64 * E
+    tron.tron_rms_norm(s.cuda(), got, gain=gain.cuda(), eps=0.0, rstd=got_rstd)
+    _within(got_rstd, rstd[:, 0], lost * rstd[:, 0], "rstd")
+    _within(got, y, (u + 2 * lost) * y.abs() + TINY[kind], "y")
+    tron.tron_rms_norm(s.cuda(), q, gain=gain.cuda(), eps=0.0, scale=scale)
+    want = y.abs().amax(1) / 448
+    _within(scale, want, 2 * lost * want, "scale")
+    _within(q.float().double().cpu() * scale.double().cpu()[:, None], y, (2.0 ** -4 + 4 * lost) * y.abs() + 2.0 ** -10 * (1 + lost) * want[:, None], "y in 8 bits")
+    # the gradient has the size of rstd
+    dx, dgain = torch.empty(m, d, dtype=dt, device="cuda"), torch.empty(d, device="cuda")
+    tron.tron_rms_norm_grad(s.cuda(), got_rstd, dy.cuda(), dx, gain=gain.cuda(), dgain=dgain)
+    R = got_rstd.double().cpu()[:, None]
+    A, H = dy.double() * gain.double(), S * R
+    want = R * (A - H * (A * H).mean(1, keepdim=True))
+    size = R * (A.abs() + H.abs() * (A * H).abs().mean(1, keepdim=True))
+    _within(dx, want, u * want.abs() + 80 * E * size + TINY[kind], "dx")
+    terms = dy.double() * H
+    _within(dgain, terms.sum(0), (m + 8) * 2 * E * terms.abs().sum(0), "dgain")
