@@ -419,7 +419,8 @@ enum {
     TRON_TYPE_F16 = 2,
     TRON_TYPE_E4M3 = 3 /* 8 bits: 4 of exponent, 3 of fraction, largest value 448, no infinities; held with a scale per row */
 };
-enum { TRON_ACT_NONE = 0, TRON_ACT_RELU = 1, TRON_ACT_GELU = 2 /* a/2 (1 + erf(a / sqrt 2)) */, TRON_ACT_SILU = 3 /* a / (1 + exp(-a)) */ };
+enum { TRON_ACT_NONE = 0, TRON_ACT_RELU = 1, TRON_ACT_GELU = 2 /* a/2 (1 + erf(a / sqrt 2)) */, TRON_ACT_SILU = 3 /* a / (1 + exp(-a)) */,
+       TRON_ACT_NARROW = 256 /* added to one of them: see tron_linear_grad */ };
 
 /*
  * Root-mean-square norm with the residual's addition, rows of d elements:
@@ -460,9 +461,12 @@ TRON_API int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *
 /*
  * Its gradients, for operands of 16 bits: with dpre = dy act'(pre) (the slope of relu at 0 is 0),
  *   dx = dpre w  (m x k, of `type`);   dw = dpre' x  (n x k, of dw_type);   dbias_j = sum_i dpre_ij  (n floats).
- * Each may be NULL; the residual's gradient is dy.  With an activation the products of the matrix units take dpre rounded to `type`, as
- * their operands are (f16: times a power of two that the largest |dy| gives, so that neither end of f16's range is met before the results'
- * own); dw of 32 bits has a second product with what that rounding left.  dbias, and dx of few rows (up to 8, or 16 where n k >= 2^25), sum it unrounded.
+ * Each may be NULL; the residual's gradient is dy.  Behind gelu and silu dpre has more bits than an operand of the matrix units: it
+ * is multiplied in two parts, rounded and what the rounding left, so that results have their own rounding alone.  With
+ * TRON_ACT_NARROW added to the activation, here and in the work space's call, it is rounded to `type` instead, for about half the time and
+ * the work space (results of 16 bits are off by half as much again).  In f16 it is held times a power of two that the largest |dy| gives, so
+ * that neither end of f16's range is met before the results' own.  dbias, and dx of few rows (up to 8, or 16 where n k >= 2^25), sum it
+ * unrounded in any case.
  */
 TRON_API int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias);
 TRON_API int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const void *w,

@@ -85,7 +85,6 @@ struct Epilogue {
     float *part;   // [parts][m][n]: sums of a part of the inner index instead
     bool past;     // y goes past the caches
     const float *factor;   // one number that every sum is multiplied by, or NULL
-    bool small_part;       // the sums are what the residual has been rounded by: one that is not finite stays
 };
 
 // exp(-v) from the two parts hi + lo = -v log2(e), |lo| at most a unit of the last place of hi: one part alone is off by 2^-24 of the exponent
@@ -241,7 +240,7 @@ __device__ __forceinline__ void finish8(const Epilogue &E, const Columns &C, flo
         }
         if (E.residual) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[q][e] = E.small_part && !__builtin_isfinite(f[q][e]) ? f[q][e] : v[q][e] + f[q][e];
+            for (int e = 0; e < kVec; ++e) v[q][e] += f[q][e];
         }
         store_out<PAST>(E.y, E.out, row * E.ldy + j, v[q], n);
     }
@@ -1060,9 +1059,9 @@ struct TurnArgs {
     void *same, *turned;       // [rows][ldsame], [cols][ldturned], zeros from the last element to the end of its chunk; or NULL
     int64_t ldsame, ldturned;
     float *shares;             // [patches of rows][cols]: column sums of the products before rounding, or NULL
-    float *factors;            // f16: see k_range_parts; or NULL, and the products are rounded as they are
+    float *factor;             // f16: see k_range_parts; or NULL, and the products are rounded as they are
     int range_parts;
-    void *rest;                // as `turned`: what that rounding left, times kRestLift, or NULL
+    int64_t again_same, again_turned;   // elements of a row of `same` and of `turned` behind which it is there again, for dpre in two parts; 0: it is not
     int64_t blocks;
 };
 
@@ -1090,16 +1089,11 @@ __device__ __forceinline__ void turn8(Raw8<T> (&r)[kVec])
     for (int i = 0; i < kVec; ++i) __builtin_memcpy(&r[i], t[i], 16);
 }
 
-// What the rounding of dpre left is up to half a unit of its last place; f16 holds it times 2^11 with all its digits.
-template <typename T>
-constexpr float kRestLift = __is_same(T, __bf16) ? 1.f : 2048.f;
-
 // f16: dpre is dy times a slope of up to 1.13, which may lie above the largest value or below the smallest where the products' results
 // do not.  It is held times a power of two, by which the largest |dy| comes to lie in [2^14, 2^15), and the results are multiplied by its
-// reciprocal.  This launch takes the maximum, in parts behind the factors; the next one joins them, and its first wavefront writes the
-// factors of the products: the reciprocal, and that for what the rounding left.  8192 x 4096: 25 us; all gradients with 4096 inputs 628 us,
-// 586 us without.
-constexpr int kRangeBlocks = 512, kFactors = 2;
+// reciprocal.  This launch takes the maximum, in parts behind that factor; the next one joins them, and its first wavefront writes the
+// factor.  8192 x 4096: 25 us.
+constexpr int kRangeBlocks = 512;
 
 __global__ __launch_bounds__(kBlock) void k_range_parts(const _Float16 *dy, int64_t m, int64_t n, int64_t ld, float *parts)
 {
@@ -1118,19 +1112,15 @@ __global__ __launch_bounds__(kBlock) void k_range_parts(const _Float16 *dy, int6
 
 int range_blocks(int64_t m, int64_t n) { return (int)std::min<int64_t>(kRangeBlocks, ceil_div(m * ceil_div(n, kVec), kBlock)); }
 
-// by a wavefront; `writes`: whether it is the one that writes the factors
-template <typename T>
-__device__ __forceinline__ float range_factor(float *factors, int parts, int lane, bool writes)
+// by a wavefront; `writes`: whether it is the one that writes the reciprocal
+__device__ __forceinline__ float range_factor(float *factor, int parts, int lane, bool writes)
 {
     float top = 0.f;
-    for (int i = lane; i < parts; i += kWave) top = fmaxf(top, factors[kFactors + i]);
+    for (int i = lane; i < parts; i += kWave) top = fmaxf(top, factor[1 + i]);
     top = wave_maxf(top);
     // infinities stay what they are; all others are safe as beside 65504
     const int e = top == 0.f ? 0 : top < INFINITY ? 14 - ilogbf(top) : -1;
-    if (writes && lane == 0) {
-        factors[0] = ldexpf(1.f, -e);
-        factors[1] = ldexpf(1.f / kRestLift<T>, -e);
-    }
+    if (writes && lane == 0) *factor = ldexpf(1.f, -e);
     return ldexpf(1.f, e);
 }
 
@@ -1138,7 +1128,9 @@ __device__ __forceinline__ float range_factor(float *factors, int parts, int lan
 // turned in its registers.  The four of a workgroup take patches one below the other: their pieces of a turned row are 512 bytes (side by
 // side 42 us, so 35 us for 8192 x 4096 bf16, 3.8 TB/s).
 // All copies of a call are one launch, and the activation is chosen once a patch: its code is long, and a small copy waits for it to be fetched.
-template <typename T, int ACT, bool REST = false>
+// TWO: dpre is followed by what its rounding left, none where it is not finite, and the other operands by themselves, with 0 for what is not
+// finite (its products are in the first part's sum).
+template <typename T, int ACT, bool TWO>
 __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
 {
     static_assert(sizeof(T) == 2, "two elements a word");
@@ -1157,7 +1149,7 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
     float sum[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
-    const float factor = ACT != TRON_ACT_NONE && !__is_same(T, __bf16) && A.factors ? range_factor<T>(A.factors, A.range_parts, lane, patch_row == 0 && patch_col == 0) : 1.f;
+    const float factor = ACT != TRON_ACT_NONE && !__is_same(T, __bf16) && A.factor ? range_factor(A.factor, A.range_parts, lane, patch_row == 0 && patch_col == 0) : 1.f;
 #pragma unroll
     for (int r = 0; r < kVec; ++r) {
         if (i0 + r < A.rows && n > 0) {
@@ -1167,10 +1159,12 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
                 if (ACT != TRON_ACT_NONE) {
                     v = e < n ? v * act_slope(static_cast<float>(p[r].v[e]), ACT) : 0.f;
                     raw[r].v[e] = static_cast<T>(v * factor);
-                    if (REST) {
+                    if (TWO) {
                         const float left = v * factor - static_cast<float>(raw[r].v[e]);
-                        p[r].v[e] = static_cast<T>(left == left ? left * kRestLift<T> : 0.f);   // none of what is not finite
+                        p[r].v[e] = static_cast<T>(__builtin_isfinite(left) ? left : 0.f);
                     }
+                } else if (TWO) {
+                    p[r].v[e] = static_cast<T>(__builtin_isfinite(v) ? v : 0.f);
                 }
                 sum[e] += v;
             }
@@ -1178,7 +1172,11 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
 #pragma unroll
             for (int e = 0; e < kVec; ++e) raw[r].v[e] = p[r].v[e] = static_cast<T>(0.f);
         }
-        if (A.same && i0 + r < A.rows && j < A.ldsame) store8(static_cast<T *>(A.same) + (i0 + r) * A.ldsame + j, raw[r]);
+        if (A.same && i0 + r < A.rows && j < A.ldsame) {
+            T *row = static_cast<T *>(A.same) + (i0 + r) * A.ldsame + j;
+            store8(row, raw[r]);
+            if (TWO) store8(row + A.again_same, p[r]);
+        }
     }
     if (A.shares) {
         // over the eight lanes of a column
@@ -1191,15 +1189,15 @@ __device__ __forceinline__ void turn_patch(const TurnArgs &A, int64_t block)
         if (lane < 8 && n > 0) store8_of<float>(A.shares + patch_row * A.cols + j, sum, n);
     }
     if (!A.turned) return;
-    auto put = [&](Raw8<T> (&r)[kVec], void *to) {
+    auto put = [&](Raw8<T> (&r)[kVec], int64_t at) {
         turn8(r);
-        if (i0 >= A.ldturned) return;
+        if (at >= A.ldturned) return;
 #pragma unroll
         for (int c = 0; c < kVec; ++c)
-            if (j + c < A.cols) store8(static_cast<T *>(to) + (j + c) * A.ldturned + i0, r[c]);
+            if (j + c < A.cols) store8(static_cast<T *>(A.turned) + (j + c) * A.ldturned + at, r[c]);
     };
-    put(raw, A.turned);
-    if (REST) put(p, A.rest);
+    put(raw, i0);
+    if (TWO) put(p, A.again_turned + i0);
 }
 
 template <typename T>
@@ -1210,11 +1208,12 @@ __global__ __launch_bounds__(kBlock) void k_turn(TurnList L)
     while (which < L.count && block >= L.list[which].blocks) block -= L.list[which++].blocks;
     if (which == L.count) return;
     const TurnArgs A = L.list[which];
+    const bool two = A.again_turned != 0;
     switch (A.act) {
-    case TRON_ACT_RELU: return turn_patch<T, TRON_ACT_RELU>(A, block);
-    case TRON_ACT_GELU: return A.rest ? turn_patch<T, TRON_ACT_GELU, true>(A, block) : turn_patch<T, TRON_ACT_GELU>(A, block);
-    case TRON_ACT_SILU: return A.rest ? turn_patch<T, TRON_ACT_SILU, true>(A, block) : turn_patch<T, TRON_ACT_SILU>(A, block);
-    default: return turn_patch<T, TRON_ACT_NONE>(A, block);
+    case TRON_ACT_RELU: return turn_patch<T, TRON_ACT_RELU, false>(A, block);
+    case TRON_ACT_GELU: return two ? turn_patch<T, TRON_ACT_GELU, true>(A, block) : turn_patch<T, TRON_ACT_GELU, false>(A, block);
+    case TRON_ACT_SILU: return two ? turn_patch<T, TRON_ACT_SILU, true>(A, block) : turn_patch<T, TRON_ACT_SILU, false>(A, block);
+    default: return two ? turn_patch<T, TRON_ACT_NONE, true>(A, block) : turn_patch<T, TRON_ACT_NONE, false>(A, block);
     }
 }
 
@@ -1256,14 +1255,20 @@ int few_grad(FewGradArgs A, float *part, hipStream_t st)
 
 // the work space of the gradients, in the order of its parts
 struct GradSpace {
-    int64_t dpre, dpre_t, rest_t, w_t, x_t, shares, factors, part_dx, part_dw, total;
+    int64_t dpre, dpre_t, w_t, x_t, shares, factor, part_dx, part_dw, total;
+    int64_t again_n, again_m;   // dpre in two parts: elements of each part of a row; 0: in one
+    int64_t inner_n, inner_m;   // inner lengths of dx and of dw in the copies
     Plan for_dx, for_dw;
     bool few, both;   // dx of few rows; dx and dw in one launch
 };
-// slopes other than 0 and 1, so that dpre has to be rounded
+// slopes other than 0 and 1, so that dpre has more bits than dy
 bool smooth(int act) { return act == TRON_ACT_GELU || act == TRON_ACT_SILU; }
 
-GradSpace grad_space(int64_t m, int64_t n, int64_t k, int act, bool dx, bool dw, bool db)
+// The products take dpre as two operands of 16 bits, rounded and what the rounding left, one behind the other along the inner index, against
+// the other operand twice: results have their own rounding alone.  narrow, the caller's choice: rounded alone.  8192 x 4096 x 4096
+// bf16 gelu, error against 64 bits as a share of the result: dx and dw in bf16 1.66e-3, dw in f32 2.6e-6, in 1046 us; narrow 2.35e-3, 1.7e-3,
+// in 566 us.  Parts of whole patches, whose ends are zeros.
+GradSpace grad_space(int64_t m, int64_t n, int64_t k, int act, bool narrow, bool dx, bool dw, bool db)
 {
     GradSpace S;
     int64_t at = 0;
@@ -1272,17 +1277,21 @@ GradSpace grad_space(int64_t m, int64_t n, int64_t k, int act, bool dx, bool dw,
         if (want) at += ceil_div(bytes, 256) * 256;
         return from;
     };
+    const bool two = smooth(act) && !narrow;
+    S.again_n = two ? ceil_div(n, kPatch) * kPatch : 0;
+    S.again_m = two ? ceil_div(m, kPatch) * kPatch : 0;
+    S.inner_n = two ? 2 * S.again_n : whole(n);
+    S.inner_m = two ? 2 * S.again_m : whole(m);
     S.few = few_grad_rows(m, n, k);
-    S.for_dx = linear_plan(m, k, whole(n), TRON_TYPE_BF16);
-    S.for_dw = linear_plan(n, k, whole(m), TRON_TYPE_BF16);
+    S.for_dx = linear_plan(m, k, S.inner_n, TRON_TYPE_BF16);
+    S.for_dw = linear_plan(n, k, S.inner_m, TRON_TYPE_BF16);
     S.both = dx && dw && !S.few && together(S.for_dx, S.for_dw);
-    S.dpre = take(dx && act != TRON_ACT_NONE && !S.few, m * padded(n) * 2);
-    S.dpre_t = take(dw, n * padded(m) * 2);
-    S.rest_t = take(dw && smooth(act), n * padded(m) * 2);   // whatever the type of dw, which is not asked for here
-    S.w_t = take(dx && !S.few, k * padded(n) * 2);
-    S.x_t = take(dw, k * padded(m) * 2);
+    S.dpre = take(dx && act != TRON_ACT_NONE && !S.few, m * padded(S.inner_n) * 2);
+    S.dpre_t = take(dw, n * padded(S.inner_m) * 2);
+    S.w_t = take(dx && !S.few, k * padded(S.inner_n) * 2);
+    S.x_t = take(dw, k * padded(S.inner_m) * 2);
     S.shares = take(db, ceil_div(m, kPatch) * n * 4);
-    S.factors = take(smooth(act) && (dw || (dx && !S.few)), (kFactors + kRangeBlocks) * 4);
+    S.factor = take(smooth(act) && (dw || (dx && !S.few)), (1 + kRangeBlocks) * 4);
     const int64_t of_dx = !dx ? 0 : S.few ? few_grad_parts(n, k) * m * k * 4 : plan_bytes(S.for_dx, m, k), of_dw = dw ? plan_bytes(S.for_dw, n, k) : 0;
     S.part_dx = take(true, S.both ? of_dx : std::max(of_dx, of_dw));
     S.part_dw = S.both ? take(true, of_dw) : S.part_dx;
@@ -1295,6 +1304,7 @@ struct GradArgs {
     const void *x, *w, *dy, *pre;
     int64_t ldx, ldw, lddy, ldpre;
     int act, type;
+    bool narrow;
     void *dx, *dw;
     int64_t lddx, lddw;
     int dw_type;
@@ -1305,22 +1315,24 @@ struct GradArgs {
 template <typename T>
 int linear_grad_typed(const GradArgs &G, hipStream_t st)
 {
-    const int64_t m = G.m, n = G.n, k = G.k, np = padded(n), mp = padded(m), nw = whole(n), mw = whole(m);
+    const int64_t m = G.m, n = G.n, k = G.k;
     const bool act = G.act != TRON_ACT_NONE;
-    const GradSpace S = grad_space(m, n, k, G.act, G.dx, G.dw, G.dbias);
+    const GradSpace S = grad_space(m, n, k, G.act, G.narrow, G.dx, G.dw, G.dbias);
+    const int64_t np = padded(S.inner_n), mp = padded(S.inner_m);
     float *shares = reinterpret_cast<float *>(G.work + S.shares), *part_dx = reinterpret_cast<float *>(G.work + S.part_dx);
-    void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *rest_t = G.work + S.rest_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
-    const bool same = G.dx && act && !S.few, rest = G.dw && G.dw_type == TRON_TYPE_F32 && smooth(G.act);
-    float *factors = nullptr;
-    if (sizeof(T) == 2 && !__is_same(T, __bf16) && smooth(G.act) && (same || G.dw)) {
-        factors = reinterpret_cast<float *>(G.work + S.factors);
-        k_range_parts<<<range_blocks(m, n), kBlock, 0, st>>>(static_cast<const _Float16 *>(G.dy), m, n, G.lddy, factors + kFactors);
+    void *dpre = G.work + S.dpre, *dpre_t = G.work + S.dpre_t, *w_t = G.work + S.w_t, *x_t = G.work + S.x_t;
+    const bool same = G.dx && act && !S.few, rounds = smooth(G.act) && (same || G.dw);
+    float *factor = nullptr;
+    if (!__is_same(T, __bf16) && rounds) {
+        factor = reinterpret_cast<float *>(G.work + S.factor);
+        k_range_parts<<<range_blocks(m, n), kBlock, 0, st>>>(static_cast<const _Float16 *>(G.dy), m, n, G.lddy, factor + 1);
     }
     TurnList L{};
     if (G.dbias || G.dw || same)
-        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, factors, range_blocks(m, n), rest ? rest_t : nullptr, 0};
-    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, nullptr, 0, nullptr, 0};
-    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, nullptr, 0, nullptr, 0};
+        L.list[L.count++] = TurnArgs{G.dy, G.pre, m, n, G.lddy, G.ldpre, G.act, same ? dpre : nullptr, G.dw ? dpre_t : nullptr, np, mp, G.dbias ? shares : nullptr, factor,
+                                     range_blocks(m, n), rounds ? S.again_n : 0, rounds ? S.again_m : 0, 0};
+    if (G.dx && !S.few) L.list[L.count++] = TurnArgs{G.w, nullptr, n, k, G.ldw, 0, TRON_ACT_NONE, nullptr, w_t, 0, np, nullptr, nullptr, 0, 0, S.again_n, 0};
+    if (G.dw) L.list[L.count++] = TurnArgs{G.x, nullptr, m, k, G.ldx, 0, TRON_ACT_NONE, nullptr, x_t, 0, mp, nullptr, nullptr, 0, 0, S.again_m, 0};
     TRON_TRY(turn<T>(L, st));
     if (G.dbias) TRON_TRY(column_sums(shares, ceil_div(m, kPatch), n, G.dbias, st));
     Epilogue E{}, F{};
@@ -1335,28 +1347,14 @@ int linear_grad_typed(const GradArgs &G, hipStream_t st)
     F.ldy = G.lddw;
     F.out = G.dw_type;
     Epilogue few = E;   // which multiplies dy itself
-    if (factors) E.factor = F.factor = factors;
+    E.factor = F.factor = factor;
     // without an activation dy itself, whose rows end at n
-    const ProductArgs A = product_args(act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy}, Operand{w_t, k, np}, act ? nw : n, S.for_dx, E, part_dx);
-    const ProductArgs B = product_args(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, F, reinterpret_cast<float *>(G.work + S.part_dw));
-    if (S.both) {
-        TRON_TRY(two_products<T>(A, S.for_dx, B, S.for_dw, st));
-    } else {
-        if (G.dx && S.few) TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, few}, part_dx, st));
-        else if (G.dx) TRON_TRY(product<T>(A, S.for_dx, st));
-        if (G.dw) TRON_TRY(product<T>(B, S.for_dw, st));
-    }
-    if (!rest) return TRON_OK;
-    // A result in 32 bits would have the rounding of dpre as its whole error: what that left is multiplied too, and added.  Results of 16
-    // bits have a rounding of that size themselves.  8192 x 4096 x 4096 bf16 gelu, errors against 64 bits as a share of the result: dw in
-    // 32 bits 1.7e-3 without and 2.5e-6 with the second product, all gradients 567 and 818 us; dx and dw in bf16 2.35e-3 as they are,
-    // in 554 us, 1.66e-3 if their dpre had 32 bits.
-    Epilogue R = F;
-    R.residual = G.dw;
-    R.ldr = G.lddw;
-    R.small_part = true;
-    if (factors) R.factor = factors + 1;
-    return product<T>(product_args(Operand{rest_t, n, mp}, Operand{x_t, k, mp}, mw, S.for_dw, R, reinterpret_cast<float *>(G.work + S.part_dw)), S.for_dw, st);
+    const ProductArgs A = product_args(act ? Operand{dpre, m, np} : Operand{G.dy, m, G.lddy}, Operand{w_t, k, np}, act ? S.inner_n : n, S.for_dx, E, part_dx);
+    const ProductArgs B = product_args(Operand{dpre_t, n, mp}, Operand{x_t, k, mp}, S.inner_m, S.for_dw, F, reinterpret_cast<float *>(G.work + S.part_dw));
+    if (S.both) return two_products<T>(A, S.for_dx, B, S.for_dw, st);
+    if (G.dx && S.few) TRON_TRY(few_grad<T>(FewGradArgs{G.w, G.dy, G.pre, m, n, k, G.ldw, G.lddy, G.ldpre, 0, G.act, few}, part_dx, st));
+    else if (G.dx) TRON_TRY(product<T>(A, S.for_dx, st));
+    return G.dw ? product<T>(B, S.for_dw, st) : TRON_OK;
 }
 
 bool sizes_ok(int64_t m, int64_t n, int64_t k)
@@ -1402,7 +1400,7 @@ int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_
     }
     TRON_TRY(check_device());
     if (m == 0) return TRON_OK;
-    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr, false, nullptr, false};
+    const Epilogue E{x_scale, w_scale, bias, residual, y, pre, m, n, ldr, ldy, ldpre, act, out_type, nullptr, false, nullptr};
     const Operand a{x, m, ldx}, b{w, n, ldw};
     const Plan P = linear_plan(m, n, k, type);
     const ProductArgs A = product_args(a, b, k, P, E, static_cast<float *>(work));
@@ -1413,13 +1411,17 @@ int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_
 
 int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias)
 {
-    return sizes_ok(m, n, k) && m > 0 && act_ok(act) ? grad_space(m, n, k, act, want_dx != 0, want_dw != 0, want_dbias != 0).total : 0;
+    const bool narrow = (act & TRON_ACT_NARROW) != 0;
+    act &= ~TRON_ACT_NARROW;
+    return sizes_ok(m, n, k) && m > 0 && act_ok(act) ? grad_space(m, n, k, act, narrow, want_dx != 0, want_dw != 0, want_dbias != 0).total : 0;
 }
 
 int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const void *w, int64_t ldw, const void *dy, int64_t lddy, int act,
                      const void *pre, int64_t ldpre, void *dx, int64_t lddx, int dw_type, void *dw, int64_t lddw, float *dbias, void *work, int64_t work_bytes,
                      void *hip_stream)
 {
+    const int act_and_narrow = act;
+    act &= ~TRON_ACT_NARROW;
     if (!sizes_ok(m, n, k) || (type != TRON_TYPE_BF16 && type != TRON_TYPE_F16) || !act_ok(act) || (dw && !type_is_float(dw_type))) {
         set_error("tron_linear_grad: bad argument (need 0 <= m < 2^31, 1 <= n, k < 2^31, type bf16 or f16, dw_type f32, bf16 or f16, a known activation)");
         return TRON_EINVAL;
@@ -1438,7 +1440,7 @@ int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, i
         set_error("tron_linear_grad: bad leading dimension of dw");
         return TRON_EINVAL;
     }
-    if (m > 0 && !work_ok(work, work_bytes, tron_linear_grad_work(m, n, k, act, dx != nullptr, dw != nullptr, dbias != nullptr))) {
+    if (m > 0 && !work_ok(work, work_bytes, tron_linear_grad_work(m, n, k, act_and_narrow, dx != nullptr, dw != nullptr, dbias != nullptr))) {
         set_error("tron_linear_grad: needs a work space of tron_linear_grad_work(...) bytes at a multiple of 16");
         return TRON_EINVAL;
     }
@@ -1456,7 +1458,7 @@ int tron_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void *x, i
         E.out = dw_type;
         return join_parts(E, 0, st);
     }
-    const GradArgs G{m, n, k, x, w, dy, pre, ldx, ldw, lddy, ldpre, act, type, dx, dw, lddx, lddw, dw_type, dbias, static_cast<char *>(work)};
+    const GradArgs G{m, n, k, x, w, dy, pre, ldx, ldw, lddy, ldpre, act, type, act != act_and_narrow, dx, dw, lddx, lddw, dw_type, dbias, static_cast<char *>(work)};
     return type == TRON_TYPE_BF16 ? linear_grad_typed<__bf16>(G, st) : linear_grad_typed<_Float16>(G, st);
 }
 

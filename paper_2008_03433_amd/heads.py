@@ -11,6 +11,7 @@ from typing import Optional
 from .binding import EINVAL, TronError, _check, load_library
 
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+_ACT_NARROW = 256
 
 _torch = None
 _types = {}
@@ -171,13 +172,16 @@ def tron_linear(x, w, y, bias=None, act=ACT_NONE, residual=None, pre=None, x_sca
              call.vector(bias, "bias", n), act, rp, ldr, call.type(y, "y"), yp, ldy, pp, ldp, sp, sb, call.address)
 
 
-def tron_linear_grad_work(m, n, k, act=ACT_NONE, want_dx=True, want_dw=True, want_dbias=True) -> int:
-    return load_library().tron_linear_grad_work(m, n, k, act, int(want_dx), int(want_dw), int(want_dbias))
+def tron_linear_grad_work(m, n, k, act=ACT_NONE, want_dx=True, want_dw=True, want_dbias=True, narrow=False) -> int:
+    return load_library().tron_linear_grad_work(m, n, k, act | _ACT_NARROW if narrow else act, int(want_dx), int(want_dw), int(want_dbias))
 
 
-def tron_linear_grad(x, w, dy, dx=None, dw=None, dbias=None, act=ACT_NONE, pre=None, work=None, stream=None) -> None:
-    """The gradients that are given: dx (m x k), dw (n x k, of any float type), dbias (n).  x may be None without dw, w without dx."""
+def tron_linear_grad(x, w, dy, dx=None, dw=None, dbias=None, act=ACT_NONE, pre=None, work=None, stream=None, narrow=False) -> None:
+    """The gradients that are given: dx (m x k), dw (n x k, of any float type), dbias (n).  x may be None without dw, w without dx.
+    narrow: the products take the gradient before the activation rounded to 16 bits, for about half the time."""
     lib = _load()
+    if narrow:
+        act |= _ACT_NARROW
     call = _Call("tron_linear_grad", dy, stream)
     dyp, m, n, lddy = call.matrix(dy, "dy")
     if (dw is not None and x is None) or (dx is not None and w is None):

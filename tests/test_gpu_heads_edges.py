@@ -180,27 +180,72 @@ def test_linear_gradients_in_f16_whose_dpre_lies_beyond_its_range(m, n, k, size,
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU, tron.ACT_RELU])
-@pytest.mark.parametrize("m,n,k", [(3, 40, 70), (130, 70, 257), (700, 24, 16), (9000, 100, 130)])
-def test_linear_gradient_dw_in_32_bits_has_no_rounding_of_dpre(m, n, k, act, kind):
-    """Shapes with dx and dw in one launch, in one part and in several; rows that lie apart."""
+@pytest.mark.parametrize("narrow", [False, True])
+@pytest.mark.parametrize("m,n,k", [(3, 40, 70), (20, 33, 64), (130, 70, 257), (700, 24, 16), (300, 520, 264), (9000, 100, 130)])
+def test_linear_gradients_have_the_rounding_of_their_type_alone(m, n, k, narrow, act, kind):
+    """dpre keeps its bits in the products, unless the caller asks for fewer.  Shapes with dx and dw in one launch, in one part and in several;
+    rows that lie apart."""
     torch = torch_mod()
     u = U[kind]
     x, w, dy, pre, d = _grad_inputs(_gen(m + n + k + act), m, n, k, kind, act)
-    dw, dx, only = torch.full((n, k + 3), math.nan, device="cuda")[:, :k], torch.empty(m, k, dtype=_dt(kind), device="cuda"), torch.empty(n, k, device="cuda")
-    tron.tron_linear_grad(x.cuda(), w.cuda(), dy.cuda(), dx=dx, dw=dw, act=act, pre=pre.cuda())
-    # dpre in two parts, each rounded: u of u; of f16's smallest steps 2^-25 where the largest |dy| is 2^14 at least, and 2^-11 of that behind the lift
-    off = u * u * d.abs() + 32 * E * dy.double().abs() + 2.0 ** -36 * float(dy.double().abs().max()) / 2.0 ** 14
-    want, X = d.T @ x.double(), x.double().abs()
-    _within(dw, want, 2 * E * want.abs() + (off + (m + 8) * 4 * E * d.abs()).T @ X, "dw")
-    tron.tron_linear_grad(x.cuda(), None, dy.cuda(), dw=only, act=act, pre=pre.cuda())
-    assert torch.equal(only, dw)
-    # one infinite term: the result is that infinity, of its sign
-    x[1, 5] = math.inf
-    tron.tron_linear_grad(x.cuda(), None, dy.cuda(), dw=only, act=act, pre=pre.cuda())
-    if act != tron.ACT_RELU:   # its zeros times infinity are NaN
-        assert torch.equal(only[:, 5].cpu(), torch.sign(d[1]).float() * math.inf)
-    only[:, 5] = dw[:, 5]
-    assert torch.equal(only, dw)
+    X, W, args = x.double(), w.double(), (x.cuda(), w.cuda(), dy.cuda())
+    # dpre in two parts, each rounded: u of u, or of one; f16's smallest step is 2^-24 where the largest |dy| is 2^14 at least.  Sums of 2 m or 2 n terms
+    rounded = 0.0 if act == tron.ACT_RELU else u if narrow else u * u
+    off = rounded * d.abs() + 32 * E * dy.double().abs() + 2.0 ** -25 * float(dy.double().abs().max()) / 2.0 ** 14
+    for wide in (True, False):
+        dw = torch.full((n, k + 3), math.nan, dtype=torch.float32 if wide else _dt(kind), device="cuda")[:, :k]
+        dx, db = torch.full((m, k + 5), math.nan, dtype=_dt(kind), device="cuda")[:, :k], torch.empty(n, device="cuda")
+        tron.tron_linear_grad(*args, dx=dx, dw=dw, dbias=db, act=act, pre=pre.cuda(), narrow=narrow)
+        want, bound = d @ W, (off + (2 * n + 8) * 2 * E * d.abs()) @ W.abs()
+        _within(dx, want, u * want.abs() + bound * (1 + u) + TINY[kind] * (1 + W.abs().sum(0)), "dx")
+        want, bound = d.T @ X, (off + (2 * m + 8) * 2 * E * d.abs()).T @ X.abs()
+        ud = E if wide else u
+        _within(dw, want, ud * want.abs() + bound * (1 + ud) + (0.0 if wide else TINY[kind]), "dw")
+        _within(db, d.sum(0), ((m + 8) * 2 * E * d.abs() + 32 * E * dy.double().abs()).sum(0), "dbias")
+        # one at a time: the same bits; with a work space of its own size
+        work = torch.empty(tron.tron_linear_grad_work(m, n, k, act, False, True, False, narrow=narrow), dtype=torch.uint8, device="cuda")
+        only = torch.empty(n, k, dtype=dw.dtype, device="cuda")
+        tron.tron_linear_grad(args[0], None, args[2], dw=only, act=act, pre=pre.cuda(), work=work, narrow=narrow)
+        assert torch.equal(only, dw)
+        only = torch.empty(m, k, dtype=dx.dtype, device="cuda")
+        tron.tron_linear_grad(None, *args[1:], dx=only, act=act, pre=pre.cuda(), narrow=narrow)
+        assert torch.equal(only, dx)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("act", [tron.ACT_GELU, tron.ACT_SILU])
+@pytest.mark.parametrize("m,n,k", [(40, 33, 64), (300, 130, 72)])
+def test_linear_gradients_keep_infinities(m, n, k, act, kind):
+    """One infinite term makes a result that infinity, of its sign: what the rounding of dpre left has no part in it."""
+    torch = torch_mod()
+    x, w, dy, pre, d = _grad_inputs(_gen(m + n + k), m, n, k, kind, act)
+    x[1, 5], w[2, 7] = math.inf, -math.inf
+    for narrow in (False, True):
+        dx, dw = torch.empty(m, k, dtype=_dt(kind), device="cuda"), torch.empty(n, k, device="cuda")
+        tron.tron_linear_grad(x.cuda(), w.cuda(), dy.cuda(), dx=dx, dw=dw, act=act, pre=pre.cuda(), narrow=narrow)
+        assert torch.equal(dw[:, 5].cpu(), torch.sign(d[1]).float() * math.inf)
+        assert torch.equal(dx[:, 7].float().cpu(), torch.sign(d[:, 2]).float() * -math.inf)
+        dx[:, 7], dw[:, 5] = 0.0, 0.0
+        assert torch.isfinite(dx).all() and torch.isfinite(dw).all()
+
+
+def test_linear_gradients_refuse_a_work_space_of_fewer_bits():
+    torch = torch_mod()
+    m, n, k = 100, 80, 64
+    x, w, dy, pre = (torch.zeros(*s, dtype=torch.bfloat16, device="cuda") for s in ((m, k), (n, k), (m, n), (m, n)))
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    sizes = [tron.tron_linear_grad_work(m, n, k, tron.ACT_SILU, True, True, False, narrow=narrow) for narrow in (False, True)]
+    assert sizes[1] < sizes[0]
+    work = torch.empty(sizes[1], dtype=torch.uint8, device="cuda")
+    with pytest.raises(tron.TronError):
+        tron.tron_linear_grad(x, w, dy, dx=dx, dw=dw, act=tron.ACT_SILU, pre=pre, work=work)
+    tron.tron_linear_grad(x, w, dy, dx=dx, dw=dw, act=tron.ACT_SILU, pre=pre, work=work, narrow=True)
+    for act in (tron.ACT_SILU + 256, 4, 260):   # of the gradients alone; no activation
+        with pytest.raises(tron.TronError):
+            tron.tron_linear(x, w, torch.empty(m, n, device="cuda"), act=act)
+        if act != tron.ACT_SILU + 256:
+            with pytest.raises(tron.TronError):
+                tron.tron_linear_grad(x, w, dy, dx=dx, act=act, pre=pre)
 
 
 # --------------------------------------------------------------------------- activations
