@@ -820,8 +820,8 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
 // ------------------------------------------------------------------ dx of few rows
 // dx = dpre w for up to M rows: w is read once, as it lies.  A lane has eight columns and sums over the rows that its wavefront takes; dpre's
 // factors of 256 rows of w lie in LDS, in 32 bits: no matrix unit takes them here, so they are not rounded.  Bound by reading w: 262 MB of it in 52 us
-// (5.0 TB/s) for one row.  Against a turned copy of w and a product with it: all gradients of 3 x 29367 x 4841 f16 243 us (424 us), of
-// 8 x 4096 x 4096 72 us (73 us), of 16 x 32000 x 4096 273 us (326 us), but of 16 x 4096 x 4096 84 us (76 us) - hence the rule of few_grad_rows.
+// (5.0 TB/s) for one row.  Against a turned copy of w and a product with it: all gradients of 3 x 29367 x 4841 f16 242 us (414 us), of
+// 8 x 4096 x 4096 51 us (54 us), of 16 x 32000 x 4096 245 us (323 us), but of 16 x 4096 x 4096 61 us (54 us) - hence the rule of few_grad_rows.
 inline bool few_grad_rows(int64_t m, int64_t n, int64_t k) { return m <= 8 || (m <= 16 && n * k >= (int64_t)1 << 25); }
 constexpr int kFewGradCols = kWave * kVec, kFewGradStage = kBlock;
 
