@@ -417,7 +417,8 @@ enum {
     TRON_TYPE_F32 = 0,
     TRON_TYPE_BF16 = 1,
     TRON_TYPE_F16 = 2,
-    TRON_TYPE_E4M3 = 3 /* 8 bits: 4 of exponent, 3 of fraction, largest value 448, no infinities; held with a scale per row */
+    TRON_TYPE_E4M3 = 3, /* 8 bits: 4 of exponent, 3 of fraction, largest value 448, no infinities; held with a scale per row */
+    TRON_TYPE_I8 = 4    /* whole numbers of 8 bits, held with a scale per row */
 };
 enum { TRON_ACT_NONE = 0, TRON_ACT_RELU = 1, TRON_ACT_GELU = 2 /* a/2 (1 + erf(a / sqrt 2)) */, TRON_ACT_SILU = 3 /* a / (1 + exp(-a)) */,
        TRON_ACT_NARROW = 256 /* added to one of them: see tron_linear_grad */ };
@@ -426,7 +427,8 @@ enum { TRON_ACT_NONE = 0, TRON_ACT_RELU = 1, TRON_ACT_GELU = 2 /* a/2 (1 + erf(a
  * Root-mean-square norm with the residual's addition, rows of d elements:
  *   s = x + residual;  rstd = (mean_j s_j^2 + eps)^-1/2;  y = s rstd gain.
  * x, residual (or NULL), total (or NULL: s, rounded) are of `type` (f32, bf16, f16); gain: d floats, or NULL for 1.
- * y is of `type`, or e4m3: then scale[i] = max_j |y_ij| / 448 (1 for a row of zeros) and what is stored is y / scale.
+ * y is of `type`, or in 8 bits: then scale[i] = max_j |y_ij| / 448 (e4m3) or / 127 (i8), 1 for a row of zeros, and what is stored is y / scale.
+ * Whole numbers cannot say what is not finite: a row of i8 where some y is NaN or infinite has the scale NaN.
  * rstd: m floats or NULL.  total may be x or residual (same leading dimension).
  */
 TRON_API int tron_rms_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
@@ -445,6 +447,27 @@ TRON_API int64_t tron_rms_norm_grad_work(int64_t m, int64_t d);
 TRON_API int tron_rms_norm_grad(int64_t m, int64_t d, int type, const void *total, int64_t lds, const float *rstd,
                                 const float *gain, const void *dy, int64_t lddy, const void *dtotal, int64_t lddt, void *dx,
                                 int64_t lddx, float *dgain, void *work, int64_t work_bytes, void *hip_stream);
+
+/*
+ * Layer norm with the residual's addition:
+ *   s = x + residual;  mean = mean_j s_j;  rstd = (mean_j (s_j - mean)^2 + eps)^-1/2;  y = (s - mean) rstd gain + shift.
+ * As tron_rms_norm; shift: d floats, or NULL for 0; mean: m floats or NULL.  Rows that lie far from 0 have the variance of their differences to the mean.
+ */
+TRON_API int tron_layer_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                             const float *gain, const float *shift, double eps, void *total, int64_t ldt, int out_type, void *y,
+                             int64_t ldy, float *scale, float *mean, float *rstd, void *hip_stream);
+
+/*
+ * Its gradient: with h = (total - mean) rstd and a = dy gain,
+ *   dx = rstd (a - mean_j a_j - h mean_j(a_j h_j)) + dtotal   (the gradient of x and of the residual alike);
+ *   dgain_j = sum_i dy_ij h_ij;   dshift_j = sum_i dy_ij.
+ * As tron_rms_norm_grad; dgain, dshift: d floats or NULL.  The work space is needed for these only.
+ */
+TRON_API int64_t tron_layer_norm_grad_work(int64_t m, int64_t d);
+TRON_API int tron_layer_norm_grad(int64_t m, int64_t d, int type, const void *total, int64_t lds, const float *mean,
+                                  const float *rstd, const float *gain, const void *dy, int64_t lddy, const void *dtotal,
+                                  int64_t lddt, void *dx, int64_t lddx, float *dgain, float *dshift, void *work,
+                                  int64_t work_bytes, void *hip_stream);
 
 /*
  * Matrix product with bias, activation and residual:

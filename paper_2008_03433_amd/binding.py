@@ -105,6 +105,9 @@ _SIGNATURES = {
     "tron_rms_norm": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _dbl, _vp, _i64, _int, _vp, _i64, _vp, _vp, _vp]),
     "tron_rms_norm_grad_work": (_i64, [_i64, _i64]),
     "tron_rms_norm_grad": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "tron_layer_norm": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _vp, _dbl, _vp, _i64, _int, _vp, _i64, _vp, _vp, _vp, _vp]),
+    "tron_layer_norm_grad_work": (_i64, [_i64, _i64]),
+    "tron_layer_norm_grad": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp]),
     "tron_linear_work": (_i64, [_i64, _i64, _i64, _int]),
     "tron_linear": (_int, [_i64, _i64, _i64, _int, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _int, _vp, _i64, _int, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
     "tron_linear_grad_work": (_i64, [_i64, _i64, _i64, _int, _int, _int, _int]),

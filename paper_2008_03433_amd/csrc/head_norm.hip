@@ -1,6 +1,6 @@
 // Root-mean-square norm of the sum of a row and its residual, with an output in the input's type or in 8 bits, and its gradient.
 //
-//   s = x + r,  rstd = (mean s^2 + eps)^-1/2,  y = s rstd gain          (e4m3: y / scale with scale = max |y| / 448)
+//   s = x + r,  rstd = (mean s^2 + eps)^-1/2,  y = s rstd gain          (8 bits: y / scale with scale = max |y| / 448 or 127)
 //   dx = rstd (a - s rstd^2 mean(a s)) + dtotal,  a = dy gain;          dgain_j = sum_i dy_ij s_ij rstd_i
 //
 // Both are bound by memory: every matrix is read or written once, and a row stays in registers between the sums over it and the
@@ -11,12 +11,11 @@
 // Measured: 16384 x 8192 bf16 with a residual to e4m3 158 us (939 MB, 5.95 TB/s: outputs larger than 32 MB go past the caches, which keep what
 // is read); one row of 4096 3.7 us of the device's time, 9 us a call; gradient of 20011 x 2047 f16 with all its inputs 100 us, of which 5 us
 // the columns' sums (328 MB, 3.3 TB/s, rows at odd places; 16384 x 1024: 4.4 TB/s).
-#include "head_util.h"
+#include "head_rows.h"
 
 namespace tron {
 namespace {
 
-constexpr int kWaveRows = 4;            // wavefronts, each with rows of its own, of a workgroup over narrow rows
 // Columns up to which a wavefront holds a row, and above which rows are read twice.  Both sides: 16384 x 2048 bf16 to e4m3 45 us by workgroups
 // and 50 us by wavefronts, x 1024 19.4 us by either; 2048 x 32768 99 us held and 118 us read twice.
 constexpr int64_t kNarrow = 1024;
@@ -31,75 +30,33 @@ struct NormArgs {
     float eps, inv_d;
 };
 
-constexpr float kE4m3Max = 448.f;
-constexpr float kLeastSquares = 0x1p-60f, kMostSquares = 0x1p100f;   // where a sum of squares has its digits in 32 bits, whatever parts are lost
-
-template <typename T>
-struct Elements {
-    const T *p;
-    int64_t d;
-    __device__ __forceinline__ Raw8<T> at(int64_t j) const { return load_row8(p, j, d, static_cast<T>(0.f)); }
-};
-
-__device__ __forceinline__ void gain8(float *g, const float *gain, int64_t j, int64_t d)
-{
-    if (!gain) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) g[i] = 1.f;
-        return;
-    }
-    const Raw8<float> r = Elements<float>{gain, d}.at(j);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) g[i] = r.v[i];
-}
-
 // What a row's sums give: its factors
 struct RowFactors {
     float rstd, scale, per_scale;
 };
 // From a thread's sum of squares and its max |s gain|, by a wavefront or a workgroup.  The sum is joined in 32 bits, and in 64 once more where
 // these have lost its range, so that rows of any size have their rstd.
-template <bool WAVE, bool EIGHT>
+template <bool WAVE, typename O>
 __device__ __forceinline__ RowFactors row_factors(double own, float top, float eps, float inv_d)
 {
     __shared__ float room[2 * kMostWaves];
     __shared__ double wide_room[kMostWaves];
+    constexpr bool kEight = sizeof(O) == 1, kWhole = __is_same(O, whole8);
     float sum2 = (float)own;
     if (WAVE) {
         sum2 = wave_sumf(sum2);
-        if (EIGHT) top = wave_maxf(top);
-    } else if (EIGHT) {
-        block_sum_max(sum2, top, room);
+        if (kEight) top = wave_top<kWhole>(top);
+    } else if (kEight) {
+        block_sum_max<kWhole>(sum2, top, room);
     } else {
         sum2 = block_sum_all(sum2, room);
     }
     RowFactors f;
     if (sum2 >= kLeastSquares && sum2 <= kMostSquares) f.rstd = 1.f / sqrtf(sum2 * inv_d + eps);
     else f.rstd = (float)(1.0 / sqrt((WAVE ? wave_sum(own) : block_sum_all(own, wide_room)) * (double)inv_d + (double)eps));
-    // max |y| = rstd max |s gain|; a row of zeros (and one with a NaN, which every y then is) has scale 1.  The smallest normal
-    // number as the least scale has a finite reciprocal.
-    const float largest = top * f.rstd;
-    f.scale = largest > 0.f ? fmaxf(largest / kE4m3Max, 0x1p-126f) : 1.f;
+    f.scale = kEight ? scale_for<O>(top * f.rstd) : 1.f;   // max |y| = rstd max |s gain|
     f.per_scale = 1.f / f.scale;
     return f;
-}
-
-// A thread's sum of squares: in 64 bits anew where 32 have lost its range.  (All sums in 64 bits: 16384 x 8192 bf16 to e4m3 167 us instead of 162.)
-template <int CH>
-__device__ __forceinline__ double squares(const float (&s)[CH][kVec])
-{
-    float sum = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) sum = fmaf(s[c][i], s[c][i], sum);
-    if (sum >= kLeastSquares && sum <= kMostSquares) return sum;
-    double wide = 0.0;
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) wide = fma((double)s[c][i], (double)s[c][i], wide);
-    return wide;
 }
 
 // CH chunks of eight elements a thread; WAVE: a wavefront a row, otherwise a workgroup
@@ -157,11 +114,11 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_rms_norm(No
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 s[c][i] *= g[i];
-                if (kEight) top = fmaxf(top, fabsf(s[c][i]));
+                if (kEight) top = larger<__is_same(O, whole8)>(top, fabsf(s[c][i]));
             }
         }
     }
-    const RowFactors f = row_factors<WAVE, kEight>(sum2, top, A.eps, A.inv_d);
+    const RowFactors f = row_factors<WAVE, O>(sum2, top, A.eps, A.inv_d);
     if (me == 0) {
         if (A.rstd) A.rstd[row] = f.rstd;
         if (kEight) A.scale[row] = f.scale;
@@ -206,10 +163,10 @@ __global__ __launch_bounds__(1024) void k_rms_norm_wide(NormArgs A)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             sum2 = fma((double)s[i], (double)s[i], sum2);
-            if (kEight) top = fmaxf(top, fabsf(s[i] * g[i]));
+            if (kEight) top = larger<__is_same(O, whole8)>(top, fabsf(s[i] * g[i]));
         }
     }
-    const RowFactors f = row_factors<false, kEight>(sum2, top, A.eps, A.inv_d);
+    const RowFactors f = row_factors<false, O>(sum2, top, A.eps, A.inv_d);
     if (threadIdx.x == 0) {
         if (A.rstd) A.rstd[row] = f.rstd;
         if (kEight) A.scale[row] = f.scale;
@@ -408,10 +365,15 @@ __global__ __launch_bounds__(kBlock) void k_gain_shares(NormGradArgs A)
 }  // namespace
 
 // out_j = sum over the rows of shares, in a fixed order: 16 columns a workgroup, which 64 groups of 16 lanes walk down, four loads ahead
-__global__ __launch_bounds__(1024) void k_column_sums(const float *shares, int64_t count, int64_t d, float *out)
+__global__ __launch_bounds__(1024) void k_column_sums(const float *shares, int64_t count, int64_t d, float *out, float *out2)
 {
     constexpr int kColumns = 16, kGroups = 1024 / kColumns;
     __shared__ float room[kGroups][kColumns + 1];
+    if (blockIdx.y) {
+        shares += count * d;
+        out = out2;
+    }
+    if (!out) return;
     const int c = threadIdx.x % kColumns, group = threadIdx.x / kColumns;
     const int64_t j = (int64_t)blockIdx.x * kColumns + c;
     float sum = 0.f;
@@ -434,17 +396,14 @@ __global__ __launch_bounds__(1024) void k_column_sums(const float *shares, int64
     if (group == 0 && j < d) out[j] = room[0][c];
 }
 
-int column_sums(const float *shares, int64_t count, int64_t d, float *out, hipStream_t st)
+int column_sums(const float *shares, int64_t count, int64_t d, float *out, hipStream_t st, float *out2)
 {
-    k_column_sums<<<(unsigned)ceil_div(d, 16), 1024, 0, st>>>(shares, count, d, out);
+    k_column_sums<<<dim3((unsigned)ceil_div(d, 16), out2 ? 2 : 1), 1024, 0, st>>>(shares, count, d, out, out2);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
 
 namespace {
-
-// threads of a workgroup that holds a row in CH chunks a thread
-inline unsigned row_threads(int64_t d, int ch) { return (unsigned)(ceil_div(ceil_div(d, kVec), (int64_t)ch * kWave) * kWave); }
 
 template <typename T, typename O, bool PAST>
 int norm_launch(const NormArgs &A, hipStream_t st)
@@ -466,10 +425,11 @@ int norm_launch(const NormArgs &A, hipStream_t st)
 }
 
 template <typename T>
-int norm_typed(const NormArgs &A, bool eight, hipStream_t st)
+int norm_typed(const NormArgs &A, int out_type, hipStream_t st)
 {
-    const bool past = goes_past(A.m, A.d, (A.total ? sizeof(T) : 0) + (eight ? 1 : sizeof(T)));
-    if (eight) return past ? norm_launch<T, e4m3, true>(A, st) : norm_launch<T, e4m3, false>(A, st);
+    const bool past = goes_past(A.m, A.d, (A.total ? sizeof(T) : 0) + type_bytes(out_type));
+    if (out_type == TRON_TYPE_E4M3) return past ? norm_launch<T, e4m3, true>(A, st) : norm_launch<T, e4m3, false>(A, st);
+    if (out_type == TRON_TYPE_I8) return past ? norm_launch<T, whole8, true>(A, st) : norm_launch<T, whole8, false>(A, st);
     return past ? norm_launch<T, T, true>(A, st) : norm_launch<T, T, false>(A, st);
 }
 
@@ -522,22 +482,22 @@ extern "C" {
 int tron_rms_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr, const float *gain, double eps,
                   void *total, int64_t ldt, int out_type, void *y, int64_t ldy, float *scale, float *rstd, void *hip_stream)
 {
-    const bool eight = out_type == TRON_TYPE_E4M3;
+    const bool eight = out_type == TRON_TYPE_E4M3 || out_type == TRON_TYPE_I8;
     if (m < 0 || d < 1 || m > INT32_MAX || !type_is_float(type) || (out_type != type && !eight) || !(eps >= 0.0) || !(eps < HUGE_VAL)) {
-        set_error("tron_rms_norm: bad argument (need 0 <= m < 2^31, d >= 1, type f32, bf16 or f16, out_type that type or e4m3, finite eps >= 0)");
+        set_error("tron_rms_norm: bad argument (need 0 <= m < 2^31, d >= 1, type f32, bf16 or f16, out_type that type, e4m3 or i8, finite eps >= 0)");
         return TRON_EINVAL;
     }
     if (m > 0 && (!x || !y || (eight && !scale) || !rows_ok(m, d, ldx, false) || (residual && !rows_ok(m, d, ldr, false)) ||
                   (total && !rows_ok(m, d, ldt, true)) || !rows_ok(m, d, ldy, true) || !extent_ok(m, ldx, d) || !extent_ok(m, residual ? ldr : 0, d) ||
                   !extent_ok(m, total ? ldt : 0, d) || !extent_ok(m, ldy, d))) {
-        set_error("tron_rms_norm: bad argument (x, y and, for e4m3, scale are needed; rows that are written may not overlap)");
+        set_error("tron_rms_norm: bad argument (x, y and, for 8 bits, scale are needed; rows that are written may not overlap)");
         return TRON_EINVAL;
     }
     TRON_TRY(check_device());
     if (m == 0) return TRON_OK;
     const NormArgs A{x, residual, gain, total, y, scale, rstd, m, d, ldx, ldr, ldt, ldy, (float)eps, (float)(1.0 / (double)d)};
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    return type == TRON_TYPE_F32 ? norm_typed<float>(A, eight, st) : type == TRON_TYPE_BF16 ? norm_typed<__bf16>(A, eight, st) : norm_typed<_Float16>(A, eight, st);
+    return type == TRON_TYPE_F32 ? norm_typed<float>(A, out_type, st) : type == TRON_TYPE_BF16 ? norm_typed<__bf16>(A, out_type, st) : norm_typed<_Float16>(A, out_type, st);
 }
 
 int64_t tron_rms_norm_grad_work(int64_t m, int64_t d)

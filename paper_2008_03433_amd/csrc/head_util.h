@@ -15,7 +15,12 @@ struct e4m3 {
     uint8_t bits;
 };
 
-inline int type_bytes(int type) { return type == TRON_TYPE_F32 ? 4 : type == TRON_TYPE_E4M3 ? 1 : 2; }
+// whole numbers of 8 bits, -127 .. 127 as outputs
+struct whole8 {
+    int8_t v;
+};
+
+inline int type_bytes(int type) { return type == TRON_TYPE_F32 ? 4 : type == TRON_TYPE_E4M3 || type == TRON_TYPE_I8 ? 1 : 2; }
 inline bool type_is_float(int type) { return type == TRON_TYPE_F32 || type == TRON_TYPE_BF16 || type == TRON_TYPE_F16; }
 
 // ---------------------------------------------------------------- eight elements at a time
@@ -109,11 +114,32 @@ __device__ __forceinline__ void store8_e4m3(e4m3 *p, const float *v, int64_t n)
         if (i < n) p[i].bits = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
 }
 
+// whole numbers, rounded to nearest, ties to even; NaN: 0.  What is given lies within +-127.
+template <bool PAST>
+__device__ __forceinline__ void store8_whole(whole8 *p, const float *v, int64_t n)
+{
+    int both[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) both[i / 4] |= ((v[i] == v[i] ? (int)rintf(v[i]) : 0) & 255) << (8 * (i & 3));
+    if (n >= kVec) {
+        typedef int words __attribute__((ext_vector_type(2), aligned(1)));
+        const words w = {both[0], both[1]};
+        if (PAST) __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));
+        else *reinterpret_cast<words *>(p) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+        if (i < n) p[i].v = (int8_t)(both[i / 4] >> (8 * (i & 3)));
+}
+
 // rounded to nearest, ties to even; above the largest finite value of f16: infinity
 template <typename T, bool PAST = false>
 __device__ __forceinline__ void store8_of(T *p, const float *v, int64_t n)
 {
-    if constexpr (sizeof(T) == 1) {
+    if constexpr (__is_same(T, whole8)) {
+        store8_whole<PAST>(p, v, n);
+    } else if constexpr (sizeof(T) == 1) {
         store8_e4m3<PAST>(p, v, n);
     } else {
         Raw8<T> r;
@@ -154,6 +180,20 @@ __device__ __forceinline__ float wave_maxf(float v)
     return wave_joinf(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
+// the larger one, or NaN where there is one
+__device__ __forceinline__ float max_or_nan(float a, float b) { return b > a || b != b ? b : a; }
+// NAN_TOO: NaN is kept, otherwise left out
+template <bool NAN_TOO>
+__device__ __forceinline__ float larger(float a, float b)
+{
+    return NAN_TOO ? max_or_nan(a, b) : fmaxf(a, b);
+}
+template <bool NAN_TOO>
+__device__ __forceinline__ float wave_top(float v)
+{
+    return wave_joinf(v, [](float a, float b) { return larger<NAN_TOO>(a, b); });
+}
+
 // in 32 or 64 bits
 __device__ __forceinline__ float wave_sum_of(float v) { return wave_sumf(v); }
 __device__ __forceinline__ double wave_sum_of(double v) { return wave_sum(v); }
@@ -163,11 +203,12 @@ constexpr int kMostWaves = 16;
 
 // Sums of a and maxima of b over the workgroup, in a fixed order.  `room`: 2 * kMostWaves floats of LDS that nobody reads or writes at
 // that time; after a call it may be used again behind one barrier.
+template <bool NAN_TOO = false>
 __device__ __forceinline__ void block_sum_max(float &a, float &b, float *room)
 {
     const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave;
     a = wave_sumf(a);
-    b = wave_maxf(b);
+    b = wave_top<NAN_TOO>(b);
     if (waves == 1) return;
     if (threadIdx.x % kWave == 0) {
         room[wave] = a;
@@ -178,8 +219,41 @@ __device__ __forceinline__ void block_sum_max(float &a, float &b, float *room)
     b = room[kMostWaves];
     for (int w = 0; w < waves; ++w) {
         a += room[w];
-        b = fmaxf(b, room[kMostWaves + w]);
+        b = larger<NAN_TOO>(b, room[kMostWaves + w]);
     }
+}
+
+// Sums of a and b over the workgroup, in the same way.
+__device__ __forceinline__ void block_sum_two(float &a, float &b, float *room)
+{
+    const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave;
+    a = wave_sumf(a);
+    b = wave_sumf(b);
+    if (waves == 1) return;
+    if (threadIdx.x % kWave == 0) {
+        room[wave] = a;
+        room[kMostWaves + wave] = b;
+    }
+    __syncthreads();
+    a = b = 0.f;
+    for (int w = 0; w < waves; ++w) {
+        a += room[w];
+        b += room[kMostWaves + w];
+    }
+}
+
+// The maximum over the workgroup.  `room`: kMostWaves floats.
+template <bool NAN_TOO>
+__device__ __forceinline__ float block_top(float a, float *room)
+{
+    const int waves = blockDim.x / kWave;
+    a = wave_top<NAN_TOO>(a);
+    if (waves == 1) return a;
+    if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = a;
+    __syncthreads();
+    a = room[0];
+    for (int w = 1; w < waves; ++w) a = larger<NAN_TOO>(a, room[w]);
+    return a;
 }
 
 template <typename S>
@@ -204,8 +278,9 @@ inline dim3 block_grid(int64_t blocks)
 }
 __device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
-// out_j = sum over `count` rows of shares [count][d], in a fixed order (head_norm.hip)
-int column_sums(const float *shares, int64_t count, int64_t d, float *out, hipStream_t st);
+// out_j = sum over `count` rows of shares [count][d], in a fixed order (head_norm.hip); a second matrix behind the first one goes to out2, where
+// that is not NULL, and either may be left out
+int column_sums(const float *shares, int64_t count, int64_t d, float *out, hipStream_t st, float *out2 = nullptr);
 
 // ---------------------------------------------------------------- checks of arguments
 // Rows that are read may lie anywhere, one on another too (ld 0: one row for all); rows that are written may not overlap.

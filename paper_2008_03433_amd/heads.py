@@ -23,7 +23,7 @@ def _load():
     lib = load_library()
     if _torch is None:
         import torch
-        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3})
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.int8: 4})
         _torch = torch
     return lib
 
@@ -90,7 +90,7 @@ class _Call:
     def type(self, t, what):
         code = _types.get(t.dtype)
         if code is None:
-            _refuse(f"{self.name}: {what} is of {t.dtype}; float32, bfloat16, float16 and float8_e4m3fn are known")
+            _refuse(f"{self.name}: {what} is of {t.dtype}; float32, bfloat16, float16, float8_e4m3fn and int8 are known")
         return code
 
     def work(self, given, needed):
@@ -118,7 +118,7 @@ class _Call:
 
 
 def tron_rms_norm(x, y, gain=None, eps=1e-6, residual=None, total=None, scale=None, rstd=None, stream=None) -> None:
-    """y = s rstd gain with s = x + residual, written to `total` when given; rows of x.  y of x's type, or float8_e4m3fn with `scale`."""
+    """y = s rstd gain with s = x + residual, written to `total` when given; rows of x.  y of x's type, or float8_e4m3fn or int8 with `scale`."""
     lib = _load()
     call = _Call("tron_rms_norm", x, stream)
     xp, m, d, ldx = call.matrix(x, "x")
@@ -146,6 +146,39 @@ def tron_rms_norm_grad(total, rstd, dy, dx, gain=None, dtotal=None, dgain=None, 
     space, wp, wb = call.work(work, lib.tron_rms_norm_grad_work(m, d) if dgain is not None else 0)
     call.run(lib.tron_rms_norm_grad, m, d, call.type(total, "total"), sp, lds, call.vector(rstd, "rstd", m), call.vector(gain, "gain", d), dyp, lddy, dtp, lddt,
              dxp, lddx, call.vector(dgain, "dgain", d), wp, wb, call.address)
+
+
+def tron_layer_norm(x, y, gain=None, shift=None, eps=1e-5, residual=None, total=None, scale=None, mean=None, rstd=None, stream=None) -> None:
+    """y = (s - mean) rstd gain + shift with s = x + residual, written to `total` when given; rows of x.  y of x's type, or float8_e4m3fn or int8
+    with `scale`."""
+    lib = _load()
+    call = _Call("tron_layer_norm", x, stream)
+    xp, m, d, ldx = call.matrix(x, "x")
+    rp, _, _, ldr = call.matrix(residual, "residual", m, d, x.dtype)
+    tp, _, _, ldt = call.matrix(total, "total", m, d, x.dtype)
+    yp, _, _, ldy = call.matrix(y, "y", m, d)
+    call.run(lib.tron_layer_norm, m, d, call.type(x, "x"), xp, ldx, rp, ldr, call.vector(gain, "gain", d), call.vector(shift, "shift", d), eps, tp, ldt,
+             call.type(y, "y"), yp, ldy, call.vector(scale, "scale", m), call.vector(mean, "mean", m), call.vector(rstd, "rstd", m), call.address)
+
+
+def tron_layer_norm_grad_work(m, d) -> int:
+    return load_library().tron_layer_norm_grad_work(m, d)
+
+
+def tron_layer_norm_grad(total, mean, rstd, dy, dx, gain=None, dtotal=None, dgain=None, dshift=None, work=None, stream=None) -> None:
+    """dx, the gradient of x and of the residual, and dgain and dshift when given, from the forward call's total (x itself without a residual), mean and
+    rstd."""
+    lib = _load()
+    call = _Call("tron_layer_norm_grad", total, stream)
+    sp, m, d, lds = call.matrix(total, "total")
+    dyp, _, _, lddy = call.matrix(dy, "dy", m, d, total.dtype)
+    dtp, _, _, lddt = call.matrix(dtotal, "dtotal", m, d, total.dtype)
+    dxp, _, _, lddx = call.matrix(dx, "dx", m, d, total.dtype)
+    if mean is None or rstd is None:
+        _refuse("tron_layer_norm_grad: mean and rstd are needed")
+    space, wp, wb = call.work(work, lib.tron_layer_norm_grad_work(m, d) if dgain is not None or dshift is not None else 0)
+    call.run(lib.tron_layer_norm_grad, m, d, call.type(total, "total"), sp, lds, call.vector(mean, "mean", m), call.vector(rstd, "rstd", m),
+             call.vector(gain, "gain", d), dyp, lddy, dtp, lddt, dxp, lddx, call.vector(dgain, "dgain", d), call.vector(dshift, "dshift", d), wp, wb, call.address)
 
 
 def tron_linear_work(m, n, k, dtype) -> int:
