@@ -472,8 +472,9 @@ TRON_API int tron_layer_norm_grad(int64_t m, int64_t d, int type, const void *to
 /*
  * Matrix product with bias, activation and residual:
  *   pre_ij = x_scale_i w_scale_j sum_l x_il w_jl + bias_j;   y = act(pre) + residual.
- * x: m x k and w: n x k of `type`: bf16, f16, or e4m3 with m and n scales (no scales otherwise).  bias: n floats or NULL.  y,
+ * x: m x k and w: n x k of `type`: bf16, f16, or e4m3 or i8 with m and n scales (no scales otherwise).  bias: n floats or NULL.  y,
  * residual (or NULL) and pre (or NULL) are m x n of `out_type` (f32, bf16, f16).  y may be residual (same leading dimension).
+ * i8: any whole numbers of 8 bits, k < 2^17: the sum is exact, in 32 bits, and rounded to a float before the scales.
  */
 TRON_API int64_t tron_linear_work(int64_t m, int64_t n, int64_t k, int type);
 TRON_API int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const float *x_scale,

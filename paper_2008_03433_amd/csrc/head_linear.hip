@@ -34,7 +34,8 @@ constexpr int kChunkElems = 16 / (int)sizeof(T);
 
 // What a lane has of a chunk, as operands of matrix instructions.  e4m3 is made bf16 on the way, which holds each of its values: the
 // matrix instructions for 8 bits keep 13 bits below the largest product of a step (a product 2^14 times smaller than another adds
-// nothing), those for 16 bits sum in 32.
+// nothing), those for 16 bits sum in 32.  Whole numbers have instructions of their own, which sum in whole numbers of 32 bits: exactly, for inner lengths
+// up to kMostWhole.
 template <typename T>
 struct Fragment {
     static constexpr int kCount = 1;
@@ -46,11 +47,28 @@ struct Fragment<e4m3> {
     i32x4 v[2];
 };
 
+constexpr int64_t kMostWhole = (1 << 17) - 1;   // (-128)^2 times that is below 2^31
+
+// Four sums of a lane.  Whole numbers stay such until the epilogue, and in the parts of a cut inner index, which hold their bits: whatever the tiles
+// and parts are, the sum is the same.
+template <typename T>
+struct SumOf {
+    typedef f32x4 four;
+    typedef float one;
+};
+template <>
+struct SumOf<whole8> {
+    typedef i32x4 four;
+    typedef int one;
+};
+template <typename T>
+using Sums = typename SumOf<T>::four;
+
 template <typename T>
 __device__ __forceinline__ Fragment<T> fragment(i32x4 chunk)
 {
     Fragment<T> f;
-    if constexpr (sizeof(T) == 1) {
+    if constexpr (__is_same(T, e4m3)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             f.v[i / 2][i % 2 * 2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(chunk[i], 1.f, false));
@@ -63,11 +81,13 @@ __device__ __forceinline__ Fragment<T> fragment(i32x4 chunk)
 }
 
 template <typename T>
-__device__ __forceinline__ f32x4 mma(const Fragment<T> &a, const Fragment<T> &b, f32x4 c)
+__device__ __forceinline__ Sums<T> mma(const Fragment<T> &a, const Fragment<T> &b, Sums<T> c)
 {
 #pragma unroll
     for (int i = 0; i < Fragment<T>::kCount; ++i) {
-        if constexpr (sizeof(T) == 2 && !__is_same(T, __bf16))
+        if constexpr (__is_same(T, whole8))
+            c = __builtin_amdgcn_mfma_i32_16x16x64_i8(a.v[i], b.v[i], c, 0, 0, 0);
+        else if constexpr (sizeof(T) == 2 && !__is_same(T, __bf16))
             c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.v[i]), __builtin_bit_cast(f16x8, b.v[i]), c, 0, 0, 0);
         else
             c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v[i]), __builtin_bit_cast(bf16x8, b.v[i]), c, 0, 0, 0);
@@ -82,7 +102,7 @@ struct Epilogue {
     void *y, *pre;
     int64_t m, n, ldr, ldy, ldpre;
     int act, out;
-    float *part;   // [parts][m][n]: sums of a part of the inner index instead
+    float *part;   // [parts][m][n]: sums of a part of the inner index instead (whole numbers: their bits)
     bool past;     // y goes past the caches
     const float *factor;   // one number that every sum is multiplied by, or NULL
 };
@@ -262,7 +282,14 @@ __device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float 
 // kJoinAlone are shared out over W wavefronts, whose sums meet in LDS in their order (64 parts of 16 x 4096: 13.8 us by one, 5 us by eight).
 constexpr int kJoinAlone = 8, kJoinWaves = 8;
 
-template <int W>
+// WHOLE: the parts hold whole numbers.
+template <bool WHOLE>
+__device__ __forceinline__ float join(float a, float b)
+{
+    return WHOLE ? __int_as_float(__float_as_int(a) + __float_as_int(b)) : a + b;
+}
+
+template <int W, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? kBlock : W * kWave) void k_linear_join(Epilogue E, int parts)
 {
     const int wave = W == 1 ? 0 : threadIdx.x / kWave, lane = threadIdx.x % kWave;
@@ -282,13 +309,13 @@ __global__ __launch_bounds__(W == 1 ? kBlock : W * kWave) void k_linear_join(Epi
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) v[0][e] += f[r][e];
+                for (int e = 0; e < kVec; ++e) v[0][e] = join<WHOLE>(v[0][e], f[r][e]);
         }
         for (; q < parts; q += W) {
             float f[kVec];
             load_as<float>(f, p + q * each, 0, n);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[0][e] += f[e];
+            for (int e = 0; e < kVec; ++e) v[0][e] = join<WHOLE>(v[0][e], f[e]);
         }
     }
     if constexpr (W > 1) {
@@ -301,19 +328,24 @@ __global__ __launch_bounds__(W == 1 ? kBlock : W * kWave) void k_linear_join(Epi
 #pragma unroll
         for (int u = 0; u < W - 1; ++u)
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[0][e] += share[u][e][lane];
+            for (int e = 0; e < kVec; ++e) v[0][e] = join<WHOLE>(v[0][e], share[u][e][lane]);
+    }
+    if (WHOLE) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[0][e] = (float)__float_as_int(v[0][e]);
     }
     if (n > 0) finish8<false>(E, columns_of(E, j), v, i, 0, j);
 }
 
+template <bool WHOLE = false>
 int join_parts(const Epilogue &E, int parts, hipStream_t st)
 {
     const int64_t chunks = ceil_div(E.n, kVec), y = std::min<int64_t>(E.m, 32768);
     const bool alone = parts <= kJoinAlone;
     const unsigned across = alone ? (unsigned)std::min<int64_t>(kBlock, ceil_div(chunks, kWave) * kWave) : kWave;
     const dim3 grid((unsigned)ceil_div(chunks, across), (unsigned)y, (unsigned)ceil_div(E.m, y));
-    if (alone) k_linear_join<1><<<grid, across, 0, st>>>(E, parts);
-    else k_linear_join<kJoinWaves><<<grid, kJoinWaves * kWave, 0, st>>>(E, parts);
+    if (alone) k_linear_join<1, WHOLE><<<grid, across, 0, st>>>(E, parts);
+    else k_linear_join<kJoinWaves, WHOLE><<<grid, kJoinWaves * kWave, 0, st>>>(E, parts);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
@@ -387,7 +419,7 @@ __device__ __forceinline__ void load_half(Half<FM, FN> &f, const char *lds, int 
 }
 
 template <typename T, int FM, int FN>
-__device__ __forceinline__ void mma_half(const Half<FM, FN> &f, f32x4 (&acc)[FM][FN])
+__device__ __forceinline__ void mma_half(const Half<FM, FN> &f, Sums<T> (&acc)[FM][FN])
 {
     Fragment<T> b[FN];
 #pragma unroll
@@ -402,7 +434,7 @@ __device__ __forceinline__ void mma_half(const Half<FM, FN> &f, f32x4 (&acc)[FM]
 
 // a step's products of a wavefront's part of the tile
 template <typename T, int BM, int FM, int FN>
-__device__ __forceinline__ void tile_step(const char *lds, int wm, int wn, int lane, f32x4 (&acc)[FM][FN])
+__device__ __forceinline__ void tile_step(const char *lds, int wm, int wn, int lane, Sums<T> (&acc)[FM][FN])
 {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -419,10 +451,14 @@ __device__ __forceinline__ void tile_step(const char *lds, int wm, int wn, int l
     }
 }
 
+// Sums on their way out: whole numbers as the nearest floats, or their bits where a part's sums go to memory.
+__device__ __forceinline__ f32x4 as_floats(f32x4 v, const float *) { return v; }
+__device__ __forceinline__ f32x4 as_floats(i32x4 v, const float *part) { return part ? __builtin_bit_cast(f32x4, v) : __builtin_convertvector(v, f32x4); }
+
 // Lane l holds row l % 16 and columns l / 16 * 4 .. + 3 of a 16 x 16 piece.  Through LDS, 128 rows at a time, to stores of whole lines: a
 // thread keeps its eight columns and takes rows that lie apart, several at once.
-template <int BM, int BN, int WM, int WN, int FM, int FN>
-__device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, int wn, int lane, const f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int part)
+template <typename T, int BM, int BN, int WM, int WN, int FM, int FN>
+__device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, int wn, int lane, const Sums<T> (&acc)[FM][FN], int64_t m0, int64_t n0, int part)
 {
     constexpr int kThreads = WM * WN * kWave, kRows = BM < 128 ? BM : 128, kPitch = BN + 4, kAcross = BN / kVec, kDown = kThreads / kAcross;
     static_assert(kThreads % kAcross == 0 && kRows % (4 * kDown) == 0, "whole rows at once");
@@ -438,7 +474,7 @@ __device__ __forceinline__ void tile_out(const Epilogue &E, char *lds, int wm, i
             const int r = wm * FM * 16 + i * 16 + lane % 16 - half * kRows;
             if (r >= 0 && r < kRows) {
 #pragma unroll
-                for (int k = 0; k < FN; ++k) *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + k * 16 + lane / 16 * 4) = acc[i][k];
+                for (int k = 0; k < FN; ++k) *reinterpret_cast<f32x4 *>(out + r * kPitch + wn * FN * 16 + k * 16 + lane / 16 * 4) = as_floats(acc[i][k], E.part);
             }
         }
         __syncthreads();
@@ -517,11 +553,11 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < kX ? xs : ws, (__attribute__((address_space(3))) void *)(to + group * 1024), 16, offset, from, 0, 0);
         }
     };
-    f32x4 acc[FM][FN];
+    Sums<T> acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < FN; ++j) acc[i][j] = Sums<T>{0, 0, 0, 0};
     // Half a step is read from LDS while the other half's products run.  The wait for the next step lies in the middle: behind it
     // nobody reads this step's chunks any more, and the step after the next is fetched to their place.
     auto all = [&](char *__restrict__ even, char *__restrict__ odd) {
@@ -566,10 +602,10 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_direct(ProductArgs A)
             if (++i == steps) break;
         }
     };
-    if constexpr (sizeof(T) == 1) plain(lds, lds + kStage);
+    if constexpr (__is_same(T, e4m3)) plain(lds, lds + kStage);
     else all(lds, lds + kStage);
     __syncthreads();
-    tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
+    tile_out<T, BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
 
 // A tile whose operands lie anywhere: chunks go through registers, which know where a row ends (8192 x 32000 x 4096 bf16: 2.1 ms).
@@ -602,11 +638,11 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
             rows[c] = static_cast<const T *>(A.w.p) + i * A.w.ld;
         }
     }
-    f32x4 acc[FM][FN];
+    Sums<T> acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < FN; ++j) acc[i][j] = Sums<T>{0, 0, 0, 0};
 
     i32x4 next[kChunks];
     auto fetch = [&](int64_t k) {
@@ -631,7 +667,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_linear_tile(ProductArgs A)
             __syncthreads();
         }
     }
-    tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
+    tile_out<T, BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
 
 // Tiles of 128 x 128 of operands that lie anywhere, where there are few and the way to memory is what a step waits for: kDeep steps are under
@@ -660,11 +696,11 @@ __device__ __forceinline__ void deep_tile(const ProductArgs &A, int64_t block, i
         rows[c] = static_cast<const T *>(of_x ? A.x.p : A.w.p) + (i < end ? i : end - 1) * (of_x ? A.x.ld : A.w.ld) + threadIdx.x % 8 * kChunkElems<T>;
         place[c] = chunk_place(r, threadIdx.x % 8);
     }
-    f32x4 acc[FM][FN];
+    Sums<T> acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < FN; ++j) acc[i][j] = Sums<T>{0, 0, 0, 0};
 
     i32x4 under_way[kDeep][kChunks];
     auto fetch_whole = [&](i32x4 (&to)[kChunks], int64_t k) {
@@ -716,12 +752,12 @@ __device__ __forceinline__ void deep_tile(const ProductArgs &A, int64_t block, i
         }
     }
     __syncthreads();
-    tile_out<BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
+    tile_out<T, BM, BN, WM, WN>(A.E, lds, wm, wn, lane, acc, m0, n0, part);
 }
 
 // e4m3: one workgroup a compute unit, because its operands as bf16 do not fit 128 registers (1024^3 17.3 us, with two and spilt ones 19.8 us)
 template <typename T, int WM, int WN>
-__global__ __launch_bounds__(WM *WN *kWave, sizeof(T) == 1 ? 2 : 4) void k_linear_deep(ProductArgs A)
+__global__ __launch_bounds__(WM *WN *kWave, __is_same(T, e4m3) ? 2 : 4) void k_linear_deep(ProductArgs A)
 {
     extern __shared__ __align__(16) char lds[];
     if (block_number() < A.tiles_m * A.tiles_n) deep_tile<T, WM, WN>(A, block_number(), blockIdx.z, lds);
@@ -748,7 +784,8 @@ constexpr int kFewWaves = 4;
 template <typename T, int MT, int NT>
 __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
 {
-    __shared__ float room[kFewWaves][MT * 16][NT * 16 + 4];
+    typedef typename SumOf<T>::one Sum;
+    __shared__ __align__(16) Sum room[kFewWaves][MT * 16][NT * 16 + 4];
     const int64_t tn = block_number();
     if (tn >= A.tiles_n) return;
     const int part = blockIdx.z;
@@ -762,11 +799,11 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
         const int64_t r = n0 + j * 16 + lane % 16;
         w[j] = static_cast<const T *>(A.w.p) + (r < A.w.rows ? r : A.w.rows - 1) * A.w.ld;
     }
-    f32x4 acc[MT][NT];
+    Sums<T> acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NT; ++j) acc[i][j] = Sums<T>{0, 0, 0, 0};
     constexpr int kSteps = 2;
     constexpr int64_t kTurn = kSteps * kStepElems<T>;
     for (int64_t k = k_from + wave * kTurn; k < k_to; k += kFewWaves * kTurn) {
@@ -802,7 +839,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&room[wave][i * 16 + lane % 16][j * 16 + lane / 16 * 4]) = acc[i][j];
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<Sums<T> *>(&room[wave][i * 16 + lane % 16][j * 16 + lane / 16 * 4]) = acc[i][j];
     __syncthreads();
     for (int at = threadIdx.x; at < MT * 16 * NT * 2; at += kFewWaves * kWave) {
         const int r = at / (NT * 2), c = at % (NT * 2) * kVec;
@@ -810,8 +847,9 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_linear_few(ProductArgs A)
         float v[1][kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-            v[0][e] = room[0][r][c + e];
-            for (int u = 1; u < kFewWaves; ++u) v[0][e] += room[u][r][c + e];
+            Sum sum = room[0][r][c + e];
+            for (int u = 1; u < kFewWaves; ++u) sum += room[u][r][c + e];
+            v[0][e] = __is_same(T, whole8) && A.E.part ? __builtin_bit_cast(float, sum) : (float)sum;
         }
         put8<false>(A.E, columns_of(A.E, n0 + c), v, r, 0, n0 + c, part);
     }
@@ -1028,7 +1066,7 @@ int product(const ProductArgs &A, const Plan &P, hipStream_t st)
         TRON_TRY(launch_256<T>(A, grid, st));
     }
     TRON_HIP(hipGetLastError());
-    return P.parts > 1 ? join_parts(A.E, P.parts, st) : TRON_OK;
+    return P.parts > 1 ? join_parts<__is_same(T, whole8)>(A.E, P.parts, st) : TRON_OK;
 }
 
 // whether two products go into one launch: both in tiles of 128 x 128, and all of these under way at once, two a compute unit
@@ -1361,6 +1399,7 @@ bool sizes_ok(int64_t m, int64_t n, int64_t k)
 {
     return m >= 0 && n >= 1 && k >= 1 && m <= INT32_MAX && n <= INT32_MAX && k <= INT32_MAX && extent_ok(m, n, n) && extent_ok(m, k, k) && extent_ok(n, k, k);
 }
+bool operand_ok(int type, int64_t k) { return type >= TRON_TYPE_BF16 && type <= TRON_TYPE_I8 && (type != TRON_TYPE_I8 || k <= kMostWhole); }
 bool act_ok(int act) { return act >= TRON_ACT_NONE && act <= TRON_ACT_SILU; }
 
 }  // namespace
@@ -1372,20 +1411,20 @@ extern "C" {
 
 int64_t tron_linear_work(int64_t m, int64_t n, int64_t k, int type)
 {
-    return sizes_ok(m, n, k) && m > 0 && type >= TRON_TYPE_BF16 && type <= TRON_TYPE_E4M3 ? plan_bytes(linear_plan(m, n, k, type), m, n) : 0;
+    return sizes_ok(m, n, k) && m > 0 && operand_ok(type, k) ? plan_bytes(linear_plan(m, n, k, type), m, n) : 0;
 }
 
 int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_t ldx, const float *x_scale, const void *w, int64_t ldw, const float *w_scale,
                 const float *bias, int act, const void *residual, int64_t ldr, int out_type, void *y, int64_t ldy, void *pre, int64_t ldpre, void *work,
                 int64_t work_bytes, void *hip_stream)
 {
-    const bool eight = type == TRON_TYPE_E4M3;
-    if (!sizes_ok(m, n, k) || type < TRON_TYPE_BF16 || type > TRON_TYPE_E4M3 || !type_is_float(out_type) || !act_ok(act)) {
-        set_error("tron_linear: bad argument (need 0 <= m < 2^31, 1 <= n, k < 2^31, operands bf16, f16 or e4m3, out_type f32, bf16 or f16, a known activation)");
+    const bool eight = type == TRON_TYPE_E4M3 || type == TRON_TYPE_I8;
+    if (!sizes_ok(m, n, k) || !operand_ok(type, k) || !type_is_float(out_type) || !act_ok(act)) {
+        set_error("tron_linear: bad argument (need 0 <= m < 2^31, 1 <= n, k < 2^31, operands bf16, f16, e4m3 or, up to k < 2^17, i8, out_type f32, bf16 or f16, a known activation)");
         return TRON_EINVAL;
     }
     if (m > 0 && (!x || !w || !y || (eight && (!x_scale || !w_scale)) || (!eight && (x_scale || w_scale)))) {
-        set_error("tron_linear: bad argument (x, w and y are needed; e4m3 operands, and they alone, have scales)");
+        set_error("tron_linear: bad argument (x, w and y are needed; operands of 8 bits, and they alone, have scales)");
         return TRON_EINVAL;
     }
     if (m > 0 && (!rows_ok(m, k, ldx, false) || !rows_ok(n, k, ldw, false) || (residual && !rows_ok(m, n, ldr, false)) || !rows_ok(m, n, ldy, true) ||
@@ -1406,7 +1445,7 @@ int tron_linear(int64_t m, int64_t n, int64_t k, int type, const void *x, int64_
     const ProductArgs A = product_args(a, b, k, P, E, static_cast<float *>(work));
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     return type == TRON_TYPE_BF16 ? product<__bf16>(A, P, st)
-           : type == TRON_TYPE_F16 ? product<_Float16>(A, P, st) : product<e4m3>(A, P, st);
+           : type == TRON_TYPE_F16 ? product<_Float16>(A, P, st) : type == TRON_TYPE_E4M3 ? product<e4m3>(A, P, st) : product<whole8>(A, P, st);
 }
 
 int64_t tron_linear_grad_work(int64_t m, int64_t n, int64_t k, int act, int want_dx, int want_dw, int want_dbias)

@@ -188,7 +188,7 @@ def tron_linear_work(m, n, k, dtype) -> int:
 
 def tron_linear(x, w, y, bias=None, act=ACT_NONE, residual=None, pre=None, x_scale=None, w_scale=None, work=None, stream=None) -> None:
     """y = act(x w' + bias) + residual; the values before the activation go to `pre` when given.  x (m x k) and w (n x k) of one type:
-    bfloat16, float16, or float8_e4m3fn with x_scale (m) and w_scale (n)."""
+    bfloat16, float16, or float8_e4m3fn or int8 with x_scale (m) and w_scale (n)."""
     lib = _load()
     call = _Call("tron_linear", x, stream)
     xp, m, k, ldx = call.matrix(x, "x")
