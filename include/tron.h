@@ -533,6 +533,50 @@ TRON_API int tron_distill_hv(int64_t m, int64_t V, int type, const void *z, int6
                              double temperature, const float *weight, void *hu, int64_t ldhu, void *work, int64_t work_bytes,
                              void *hip_stream);
 
+/*
+ * A step of a beam search over the head's logits.  Row r = item * beams + beam of z (batch * beams rows of V columns, of `type`: f32, bf16, f16)
+ * belongs to a beam whose log-probabilities so far sum to score[r] (batch * beams floats):
+ *   c_rv = score_r + (z_rv - log sum_u exp z_ru);
+ * of an item's beams * V candidates the `picks` largest are taken, in falling order, ties to the lowest beam, then the lowest column:
+ *   next_score: their c;  parent: their rows r;  token: their columns v   (batch x picks each, contiguous).
+ * Candidates are compared in 64 bits, before the rounding to next_score, and those of one beam by their z.
+ * ended (batch * beams bytes, or NULL): a beam whose byte is not 0 has one candidate, column `end` once more at its score, whatever its row of z
+ * holds.  next_ended (batch x picks bytes, or NULL): whether the beam that goes on has ended, its parent before or by the column `end` (-1: there is none).
+ * A probability of 0 (z = -inf) has c = -inf, and is taken behind all others, in the same order of beams and columns.  So are all candidates of a beam whose score
+ * is not finite (the beams that a first step has not), or whose row holds NaN, +inf or nothing but -inf.
+ * beams and picks up to 64, picks <= beams V, V < 2^31 - 64.
+ */
+TRON_API int64_t tron_beam_select_work(int64_t batch, int64_t beams, int64_t V, int64_t picks);
+TRON_API int tron_beam_select(int64_t batch, int64_t beams, int64_t V, int type, const void *z, int64_t ldz, const float *score,
+                              const uint8_t *ended, int64_t end, int64_t picks, float *next_score, int32_t *parent, int32_t *token,
+                              uint8_t *next_ended, void *work, int64_t work_bytes, void *hip_stream);
+
+/*
+ * The states of the beams that go on: in each of `layers` layers, row i * per + j of dst is a copy of row rows[i * ldrows + j] of src, i < batch, j < per.
+ * A row is `positions` pieces of `step` bytes, one behind the other; strides are in bytes.  lengths (rows_in counts, or NULL): how many positions a row of
+ * src has; what lies behind them in dst is left as it was.  So is a row whose entry in `rows` lies outside [0, rows_in).  dst may not overlap src.
+ */
+TRON_API int tron_beam_reorder(int64_t layers, int64_t batch, int64_t per, const int32_t *rows, int64_t ldrows, int64_t rows_in,
+                               const void *src, int64_t src_layer, int64_t src_row, void *dst, int64_t dst_layer, int64_t dst_row,
+                               int64_t positions, int64_t step, const int32_t *lengths, void *hip_stream);
+
+/*
+ * Embeddings: y_i = scale row_scale[id] table[id], id = ids[i], m rows of d elements; an id outside [0, V) has a row of zeros.
+ * ids: m as int32 or int64 (id_bytes 4 or 8).  table: V x d of `type`: f32, bf16, f16, or e4m3 or i8 with V scales (a head's own weights; no scales
+ * otherwise).  y of out_type: f32, bf16, f16.
+ */
+TRON_API int tron_embed(int64_t m, int64_t d, int64_t V, const void *ids, int id_bytes, int type, const void *table, int64_t ldtable,
+                        const float *row_scale, double scale, int out_type, void *y, int64_t ldy, void *hip_stream);
+
+/*
+ * Its gradient: dtable_v = scale sum over the i with ids[i] = v of dy_i, and added to the dtable that is there if `add` is not 0 (to that of a head with
+ * the same weights); rows without such an i are then left as they are, otherwise they are 0.  dy: m x d of `type`: f32, bf16, f16; dtable: V x d of out_type, the
+ * same types.  The rows of an id are summed in a fixed order.  m < 2^31, V < 2^31 - 64.
+ */
+TRON_API int64_t tron_embed_grad_work(int64_t m, int64_t d, int64_t V);
+TRON_API int tron_embed_grad(int64_t m, int64_t d, int64_t V, const void *ids, int id_bytes, int type, const void *dy, int64_t lddy, double scale,
+                             int add, int out_type, void *dtable, int64_t ldtable, void *work, int64_t work_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

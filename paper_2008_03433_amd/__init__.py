@@ -18,4 +18,5 @@ from .heads import (  # noqa: F401
     ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, SoftmaxHead, tron_rms_norm, tron_rms_norm_grad, tron_rms_norm_grad_work, tron_layer_norm,
     tron_layer_norm_grad, tron_layer_norm_grad_work, tron_linear,
     tron_linear_work, tron_linear_grad, tron_linear_grad_work, tron_distill, tron_distill_work, tron_distill_grad, tron_distill_hv,
+    tron_beam_select, tron_beam_select_work, tron_beam_reorder, tron_embed, tron_embed_grad, tron_embed_grad_work,
 )

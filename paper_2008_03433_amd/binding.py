@@ -102,6 +102,12 @@ _SIGNATURES = {
     "tron_tuning_set": (_int, [ctypes.c_char_p, _i64]),
     "tron_probe_copy_bandwidth": (_int, [_vp, _vp, _i64, _int, _vp, ctypes.POINTER(_dbl)]),
     # operators of a multi-class head (heads.py)
+    "tron_beam_select_work": (_i64, [_i64, _i64, _i64, _i64]),
+    "tron_beam_select": (_int, [_i64, _i64, _i64, _int, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "tron_beam_reorder": (_int, [_i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp]),
+    "tron_embed": (_int, [_i64, _i64, _i64, _vp, _int, _int, _vp, _i64, _vp, _dbl, _int, _vp, _i64, _vp]),
+    "tron_embed_grad_work": (_i64, [_i64, _i64, _i64]),
+    "tron_embed_grad": (_int, [_i64, _i64, _i64, _vp, _int, _int, _vp, _i64, _dbl, _int, _int, _vp, _i64, _vp, _i64, _vp]),
     "tron_rms_norm": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _dbl, _vp, _i64, _int, _vp, _i64, _vp, _vp, _vp]),
     "tron_rms_norm_grad_work": (_i64, [_i64, _i64]),
     "tron_rms_norm_grad": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),

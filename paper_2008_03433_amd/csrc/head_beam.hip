@@ -1,0 +1,574 @@
+// A step of a beam search over a softmax head's logits, and the states of the beams that go on.
+//
+// Row r = item * beams + beam holds z, score_r the beam's sum of log-probabilities so far:
+//   lse_r = log sum_v exp z_rv,   c_rv = score_r + (z_rv - lse_r),
+// and the K largest c of an item's beams * V are taken, ties to the lowest beam, then the lowest token.
+//
+// Bound by reading z, once.  Within a row c grows with z, so a row offers its K largest z whatever its lse will be.  A first launch
+// reads the rows (or parts of them): every wavefront keeps a running maximum and sum a lane, and a list in LDS of what may be among the K
+// largest.  A value enters the list only above the K-th largest seen so far, so that of n values some K log n are looked at more closely, and
+// the others cost a conversion, a maximum and an exponential.  A second launch, a workgroup an item, joins sums and lists.  Keys are unique (the value's
+// bits in order, then the column's complement), so lists may be filled in any order and the result is still the same.
+//
+// The sum is the more exact the more rows are compared by it: exponents are products with log2(e) in two parts, lanes' sums are joined in 64 bits,
+// scores are compared in 64 bits.
+#include "head_util.h"
+
+namespace tron {
+namespace {
+
+constexpr int kMostPicks = 64;       // one a lane
+constexpr int kMostBeams = 64;
+constexpr int kAhead = 4;            // chunks of eight columns of a lane under way
+constexpr int kTurn = kAhead * kWave * kVec;   // columns of a wavefront's turn
+constexpr int kSlack = 128;          // entries of a list beyond which it is cut to the K largest
+constexpr int kList = kSlack + kWave * kVec;
+constexpr int kMostParts = 64;       // of a row, one a lane
+constexpr int kMostOffers = kMostBeams * kMostPicks;   // of an item's rows' parts together
+
+typedef unsigned long long key_t64;
+
+struct BeamArgs {
+    const void *z;
+    int64_t ldz;
+    const float *score;
+    const uint8_t *ended;
+    int64_t batch, V, end, per;   // per: columns of a part
+    int beams, picks, parts;
+    double *part_sum;      // [rows][parts]
+    key_t64 *part_key;     // [rows][parts][picks]; 0: none
+    float *part_max;       // [rows][parts]
+    float *next_score;
+    int32_t *parent, *token;
+    uint8_t *next_ended;
+};
+
+// Bits whose order as whole numbers is that of the values; no number's are 0
+__device__ __forceinline__ uint32_t in_order(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.f);   // -0 is 0
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ key_t64 in_order(double v)
+{
+    const key_t64 b = (key_t64)__double_as_longlong(v + 0.0);
+    return b >> 63 ? ~b : b | (key_t64)1 << 63;
+}
+__device__ __forceinline__ double of_order(key_t64 o) { return __longlong_as_double((long long)(o >> 63 ? o & ~((key_t64)1 << 63) : ~o)); }
+constexpr uint32_t kOrderOfNothing = 0x007fffffu;   // of -inf
+
+__device__ __forceinline__ key_t64 key_of(float v, int64_t column) { return (key_t64)in_order(v) << 32 | (uint32_t)~(uint32_t)column; }
+
+__device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }   // what exponents are differences to: no -inf minus -inf
+// exp(d) for d <= 0
+__device__ __forceinline__ float exp_of(float d) { return exp2_(fmaf(d, 1.44269502f, d * 1.925963e-8f)); }
+
+// whether a row is read: a beam that has ended, or has no finite score, offers nothing of its logits
+__device__ __forceinline__ bool is_read(const BeamArgs &A, int64_t row) { return !(A.ended && A.ended[row]) && fabsf(A.score[row]) < INFINITY; }
+
+// The K largest of the first `count` keys of a wavefront's list, N a lane, go to its front, in no order; fewer are all kept.  Returns a bound
+// that they reach: 0 where there are fewer than K.  Keys are unique, so a bound that exactly K reach is found bit by bit.
+template <int N>
+__device__ __forceinline__ key_t64 cut_to(key_t64 *list, int &count, int K, int lane)
+{
+    key_t64 mine[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine[i] = i * kWave + lane < count ? list[i * kWave + lane] : 0;
+    if (count < K) return 0;
+    key_t64 bound = 0;
+    for (int b = 63; b >= 0; --b) {
+        const key_t64 trial = bound | (key_t64)1 << b;
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) reach += __popcll(__ballot(mine[i] >= trial));
+        if (reach >= K) bound = trial;
+        if (reach == K) break;
+    }
+    count = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool keep = mine[i] && mine[i] >= bound;
+        const uint64_t mask = __ballot(keep);
+        if (keep) list[count + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0))] = mine[i];
+        count += __popcll(mask);
+    }
+    return bound;
+}
+
+__device__ __forceinline__ key_t64 cut(key_t64 *list, int &count, int K, int lane)
+{
+    if (count <= 3 * kWave) return cut_to<3>(list, count, K, lane);
+    return cut_to<kList / kWave>(list, count, K, lane);
+}
+
+struct Running {
+    float m = -INFINITY, s = 0.f;   // s = sum exp(z - m); m = -inf: nothing yet, or nothing but -inf
+};
+
+// What a wavefront knows of the K largest values of its workgroup's columns: K of those that its list, or another's, holds are `least` or more.
+// `beyond`: K of its own, of earlier columns, are, so that a later value has to lie above.
+struct Bound {
+    float least = -INFINITY;
+    bool beyond = false;
+    __device__ __forceinline__ bool passes(float v) const { return beyond ? v > least : v >= least; }
+    __device__ __forceinline__ void raise(uint32_t order, bool own)
+    {
+        const float v = order > kOrderOfNothing ? of_order(order) : -INFINITY;
+        if (v > least) least = v, beyond = own;
+        else if (v == least && own) beyond = true;
+    }
+};
+
+__device__ __forceinline__ int lanes_before(uint64_t mask) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0)); }
+
+// A workgroup of WAVES wavefronts a part of a row: blockIdx.x the part, y and z the row
+template <typename T, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave) void k_beam_offers(BeamArgs A)
+{
+    __shared__ key_t64 lists[WAVES][kList];
+    __shared__ double sums[WAVES];
+    __shared__ float tops[WAVES];
+    __shared__ int counts[WAVES];
+    __shared__ uint32_t common;   // in order: what K of some wavefront's values reach
+    const int64_t row = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, part = blockIdx.x;
+    if (row >= A.batch * A.beams || !is_read(A, row)) return;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
+    const int64_t from = part * A.per, to = from + A.per < A.V ? from + A.per : A.V;
+    const T *z = static_cast<const T *>(A.z) + row * A.ldz;
+    if (WAVES > 1) {
+        if (threadIdx.x == 0) common = 0;
+        __syncthreads();
+    }
+    key_t64 *list = lists[wave];
+    Running run;
+    Bound bound;
+    int count = 0;
+    auto tell = [&](uint32_t order) {
+        if (WAVES > 1 && lane == 0) atomicMax(&common, order);
+    };
+    const int64_t begin = from + (int64_t)wave * kTurn;
+    for (int64_t j0 = begin; j0 < to; j0 += WAVES * kTurn) {
+        Raw8<T> raw[kAhead];
+        float top[kAhead], most = -INFINITY;
+        if (j0 + kTurn <= to) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) raw[u] = load8(z + j0 + (u * kWave + lane) * kVec);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t j = j0 + (u * kWave + lane) * kVec;
+                if (j < to) {
+                    raw[u] = load_row8(z, j, to, static_cast<T>(-INFINITY));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) raw[u].v[i] = static_cast<T>(-INFINITY);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float v[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = static_cast<float>(raw[u].v[i]);
+            top[u] = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+            most = fmaxf(most, top[u]);
+        }
+        if (most > run.m) {
+            run.s *= exp_of(run.m - most);   // 0 * exp(-inf) at first
+            run.m = most;
+        }
+        const float base = base_of(run.m);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < kVec; i += 2) {
+                s0 += exp_of(static_cast<float>(raw[u].v[i]) - base);
+                s1 += exp_of(static_cast<float>(raw[u].v[i + 1]) - base);
+            }
+            run.s += s0 + s1;   // NaN from here on, where there is a NaN or +inf
+        }
+        uint32_t first = 0;   // in order: what K values of this turn reach, if it is the first
+        if (j0 == begin) {
+            // the K-th largest of the lanes' largest
+            const uint32_t mine = j0 + (int64_t)lane * kVec < to ? in_order(most) : 0;
+            for (int b = 31; b >= 0; --b) {
+                const uint32_t trial = first | 1u << b;
+                const int reach = __popcll(__ballot(mine >= trial));
+                if (reach >= K) first = trial;
+                if (reach == K) break;
+            }
+            bound.raise(first, false);
+            tell(first);
+        } else if (WAVES > 1) {
+            bound.raise(__builtin_amdgcn_readfirstlane(*(volatile uint32_t *)&common), false);
+        }
+        if (__ballot(bound.passes(most))) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (count > kSlack) {
+                    const uint32_t order = (uint32_t)(cut(list, count, K, lane) >> 32);
+                    bound.raise(order, true);
+                    tell(order);
+                }
+                if (!__ballot(bound.passes(top[u]))) continue;
+                const int64_t j = j0 + (u * kWave + lane) * kVec;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    const float v = static_cast<float>(raw[u].v[i]);
+                    const bool in = j + i < to && bound.passes(v);
+                    const uint64_t mask = __ballot(in);
+                    if (in) list[count + lanes_before(mask)] = key_of(v, j + i);
+                    count += __popcll(mask);
+                }
+            }
+        }
+        if (first) bound.raise(first, true);   // all that reach it are in the list
+    }
+    if (count > K) cut(list, count, K, lane);
+    const float wave_most = wave_maxf(run.m);
+    const double wave_total = wave_sum((double)run.s * (double)exp_of(run.m - base_of(wave_most)));
+    float most = wave_most;
+    double total = wave_total;
+    if (WAVES > 1) {
+        if (lane == 0) {
+            tops[wave] = wave_most;
+            sums[wave] = wave_total;
+            counts[wave] = count;
+        }
+        __syncthreads();
+        if (wave) return;
+        for (int w = 1; w < WAVES; ++w) most = fmaxf(most, tops[w]);
+        total = 0.0;
+        for (int w = 0; w < WAVES; ++w) total += sums[w] * exp((double)tops[w] - (double)base_of(most));
+        // the others' lists behind this one's: K keys of each at most
+        const uint32_t least = common;
+        for (int w = 1; w < WAVES; ++w) {
+            const key_t64 key = lane < counts[w] ? lists[w][lane] : 0;
+            const bool in = key && (uint32_t)(key >> 32) >= least;
+            const uint64_t mask = __ballot(in);
+            if (in) list[count + lanes_before(mask)] = key;
+            count += __popcll(mask);
+        }
+        if (count > K) cut(list, count, K, lane);
+    }
+    const int64_t at = row * A.parts + part;
+    if (lane < K) A.part_key[at * K + lane] = lane < count ? list[lane] : 0;
+    if (lane == 0) {
+        A.part_max[at] = most;
+        A.part_sum[at] = total;
+    }
+}
+
+// ------------------------------------------------------------------ joining
+constexpr int kPickThreads = 256;
+constexpr int kRanked = kPickThreads;   // offers that are ranked, one a thread
+
+// Offers of an item: score in 64 bits, in order (0: none), beam and token.  The better one of two has the higher score, then the lower beam and token.
+struct Offers {
+    key_t64 *order;
+    uint32_t *token;
+    int of_beam;   // offers a beam
+    __device__ __forceinline__ uint64_t place(int e) const { return (uint64_t)(e / of_beam) << 32 | token[e]; }
+    // thirteen digits of eight bits, the first ones of the score, the others of the place, the higher the better
+    __device__ __forceinline__ unsigned digit(int e, int d) const
+    {
+        return d < 8 ? (unsigned)(order[e] >> (56 - 8 * d)) & 255u : (unsigned)(~place(e) >> (32 - 8 * (d - 8))) & 255u;
+    }
+};
+
+enum { LIVE = 0, OVER, DEAD };   // a beam whose logits make its offers, one that has ended, one of which nothing is possible
+
+// A workgroup an item
+__global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
+{
+    extern __shared__ __align__(16) key_t64 room[];
+    __shared__ double lse[kMostBeams];
+    __shared__ int kind[kMostBeams];
+    __shared__ unsigned digits[256];
+    __shared__ int found[2], survivors, chosen[kRanked];
+    const int64_t item = block_number();
+    if (item >= A.batch) return;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
+    const int of_beam = A.parts * K, count = A.beams * of_beam;
+    const Offers O{room, reinterpret_cast<uint32_t *>(room + count), of_beam};
+    for (int b = wave; b < A.beams; b += kPickThreads / kWave) {
+        const int64_t row = item * A.beams + b;
+        const float score = A.score[row];
+        int k = !(fabsf(score) < INFINITY) ? DEAD : A.ended && A.ended[row] ? OVER : LIVE;
+        if (k == LIVE) {
+            const bool there = lane < A.parts;
+            const float m = there ? A.part_max[row * A.parts + lane] : -INFINITY, most = wave_maxf(m);
+            const double s = there ? A.part_sum[row * A.parts + lane] : 0.0;
+            const double total = wave_sum(there ? s * exp((double)m - (double)base_of(most)) : 0.0);
+            if (!(total > 0.0 && total < INFINITY)) k = DEAD;   // nothing but -inf; a NaN or +inf
+            if (lane == 0) lse[b] = (double)most + log(total);
+        }
+        if (lane == 0) kind[b] = k;
+    }
+    if (threadIdx.x == 0) survivors = 0;
+    __syncthreads();
+    const int64_t listed = A.V < K ? A.V : K;
+    for (int e = threadIdx.x; e < count; e += kPickThreads) {
+        const int b = e / of_beam, i = e - b * of_beam;
+        const int64_t row = item * A.beams + b;
+        const bool live = kind[b] == LIVE, over = kind[b] == OVER;
+        // one condition after the other: of a choice of three in one, the compiler (ROCm 7.2) leaves the last one's token undefined
+        key_t64 key = 1;
+        if (live) key = A.part_key[row * of_beam + i];
+        const uint32_t other = over ? i == 0 ? (uint32_t)A.end : (uint32_t)(i - (i <= A.end)) : (uint32_t)i;   // columns in order, behind `end` where it is first
+        const uint32_t token = live ? ~(uint32_t)key : other;
+        const bool there = live ? key != 0 : i < listed;
+        const double score = A.score[row], logit = of_order((uint32_t)(key >> 32));
+        const double c = live ? score + (logit - lse[b]) : over && i == 0 ? score : -INFINITY;
+        O.order[e] = there ? in_order(c) : 0;
+        O.token[e] = token;
+    }
+    __syncthreads();
+    if (count > kRanked) {
+        // Digit by digit: who has a higher digit than the K-th best is chosen, who has the same is looked at further, until what is left fits
+        constexpr int kEach = kMostOffers / kPickThreads;
+        unsigned under = 0, taken = 0;   // one bit an offer of this thread
+#pragma unroll 1
+        for (int i = 0; i < kEach; ++i) {
+            const int e = i * kPickThreads + threadIdx.x;
+            if (e < count && O.order[e]) under |= 1u << i;
+        }
+        int need = K, have = 0;
+#pragma unroll 1
+        for (int d = 0; d < 13; ++d) {
+            digits[threadIdx.x] = 0;
+            __syncthreads();
+#pragma unroll 1
+            for (int i = 0; i < kEach; ++i)
+                if (under >> i & 1) atomicAdd(&digits[O.digit(i * kPickThreads + threadIdx.x, d)], 1u);
+            __syncthreads();
+            if (wave == 0) {
+                // the digit at which counts from the highest one on reach `need`: lane 0 has the four highest
+                int mine[4], own = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) own += mine[q] = (int)digits[255 - 4 * lane - q];
+                int before = wave_scan_add(own) - own;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (before < need && before + mine[q] >= need) {
+                        found[0] = 255 - 4 * lane - q;
+                        found[1] = before;
+                    }
+                    before += mine[q];
+                }
+            }
+            __syncthreads();
+            const unsigned at = (unsigned)found[0];
+            const int same = (int)digits[at];
+            need -= found[1];
+            have += found[1];
+#pragma unroll 1
+            for (int i = 0; i < kEach; ++i)
+                if (under >> i & 1) {
+                    const unsigned mine = O.digit(i * kPickThreads + threadIdx.x, d);
+                    if (mine > at) taken |= 1u << i;
+                    if (mine != at) under &= ~(1u << i);
+                }
+            if (have + same <= kRanked) break;
+            __syncthreads();
+        }
+        taken |= under;
+#pragma unroll 1
+        for (int i = 0; i < kEach; ++i)
+            if (taken >> i & 1) chosen[atomicAdd(&survivors, 1)] = i * kPickThreads + threadIdx.x;
+    } else if (threadIdx.x < count && O.order[threadIdx.x]) {
+        chosen[atomicAdd(&survivors, 1)] = threadIdx.x;
+    }
+    __syncthreads();
+    if (threadIdx.x >= survivors) return;
+    const int e = chosen[threadIdx.x], n = survivors;
+    const key_t64 order = O.order[e];
+    const uint64_t place = O.place(e);
+    int rank = 0;
+    for (int i = 0; i < n; ++i) {
+        const key_t64 other = O.order[chosen[i]];
+        rank += other > order || (other == order && O.place(chosen[i]) < place);
+    }
+    if (rank >= K) return;
+    const int b = e / of_beam;
+    const int64_t out = item * K + rank, row = item * A.beams + b;
+    const uint32_t token = O.token[e];
+    A.next_score[out] = (float)of_order(order);
+    A.parent[out] = (int32_t)row;
+    A.token[out] = (int32_t)token;
+    if (A.next_ended) A.next_ended[out] = (A.ended && A.ended[row]) || (int64_t)token == A.end;
+}
+
+// ------------------------------------------------------------------ states
+struct ReorderArgs {
+    const int32_t *rows, *lengths;
+    const char *src;
+    char *dst;
+    int64_t ld, per, count, rows_in, src_layer, src_row, dst_layer, dst_row, positions, step, pieces;   // strides in bytes
+};
+
+constexpr int kPiece = 16 * 1024;   // bytes that a workgroup copies, four loads a thread under way
+
+// Bound by memory: a workgroup copies a piece of a row; blockIdx.z the layer
+__global__ __launch_bounds__(kBlock) void k_beam_reorder(ReorderArgs A)
+{
+    const int64_t block = block_number(), i = block / A.pieces, piece = block - i * A.pieces;
+    if (i >= A.count) return;
+    const int64_t from = A.rows[i / A.per * A.ld + i % A.per];
+    if (from < 0 || from >= A.rows_in) return;
+    int64_t n = A.positions;
+    if (A.lengths) {
+        const int64_t l = A.lengths[from];
+        n = l < 0 ? 0 : l < n ? l : n;
+    }
+    const int64_t bytes = n * A.step, at = piece * kPiece;
+    if (at >= bytes) return;
+    const char *src = A.src + blockIdx.z * A.src_layer + from * A.src_row + at;
+    char *dst = A.dst + blockIdx.z * A.dst_layer + i * A.dst_row + at;
+    const int left = (int)(bytes - at < kPiece ? bytes - at : kPiece);
+    constexpr int kLoads = kPiece / (kBlock * 16);
+    typedef int words __attribute__((ext_vector_type(4), aligned(1)));
+    words v[kLoads];
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+        const int b = (q * kBlock + threadIdx.x) * 16;
+        if (b + 16 <= left) v[q] = *reinterpret_cast<const words *>(src + b);
+    }
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+        const int b = (q * kBlock + threadIdx.x) * 16;
+        if (b + 16 <= left) *reinterpret_cast<words *>(dst + b) = v[q];
+    }
+    // the rest of a row
+    const int rest = left % 16;
+    if ((int)threadIdx.x < rest) dst[left - rest + threadIdx.x] = src[left - rest + threadIdx.x];
+}
+
+// ------------------------------------------------------------------ host
+struct Split {
+    int waves, parts;
+    int64_t per;
+};
+
+// Wavefronts a workgroup by the row's length, so that each has two turns or more where it can; parts of a row where there are few rows
+Split split_of(int64_t rows, int64_t beams, int64_t V, int64_t picks)
+{
+    const int64_t turns = ceil_div(V, kTurn);
+    Split S{turns >= 16 ? 8 : turns >= 4 ? 4 : 1, 1, V};
+    const int64_t most = std::min<int64_t>({kMostParts, kMostOffers / (beams * picks), ceil_div(turns, S.waves)});
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(512, rows)));
+    S.per = ceil_div(turns, parts) * kTurn;
+    S.parts = (int)ceil_div(V, S.per);
+    return S;
+}
+
+bool beam_sizes_ok(int64_t batch, int64_t beams, int64_t V, int64_t picks)
+{
+    return batch >= 0 && beams >= 1 && beams <= kMostBeams && V >= 1 && V < INT32_MAX - 64 && picks >= 1 && picks <= kMostPicks && picks <= beams * V &&
+           batch <= INT32_MAX / kMostBeams;
+}
+
+template <typename T>
+void launch_offers(const BeamArgs &A, int waves, hipStream_t st)
+{
+    const int64_t rows = A.batch * A.beams, y = std::min<int64_t>(rows, 32768);
+    const dim3 grid((unsigned)A.parts, (unsigned)y, (unsigned)ceil_div(rows, y));
+    if (waves == 1) k_beam_offers<T, 1><<<grid, kWave, 0, st>>>(A);
+    else if (waves == 4) k_beam_offers<T, 4><<<grid, 4 * kWave, 0, st>>>(A);
+    else k_beam_offers<T, 8><<<grid, 8 * kWave, 0, st>>>(A);
+}
+
+// where two ranges of bytes, of layers and rows that lie `layer` and `row` apart, have their first and last byte
+bool apart(const char *a, int64_t a_bytes, const char *b, int64_t b_bytes) { return a + a_bytes <= b || b + b_bytes <= a; }
+
+}  // namespace
+}  // namespace tron
+
+using namespace tron;
+
+extern "C" {
+
+int64_t tron_beam_select_work(int64_t batch, int64_t beams, int64_t V, int64_t picks)
+{
+    if (!beam_sizes_ok(batch, beams, V, picks) || batch == 0) return 0;
+    const int64_t parts = batch * beams * split_of(batch * beams, beams, V, picks).parts;
+    return ceil_div(parts * (picks * 8 + 8 + 4), 16) * 16;
+}
+
+int tron_beam_select(int64_t batch, int64_t beams, int64_t V, int type, const void *z, int64_t ldz, const float *score, const uint8_t *ended, int64_t end,
+                     int64_t picks, float *next_score, int32_t *parent, int32_t *token, uint8_t *next_ended, void *work, int64_t work_bytes, void *hip_stream)
+{
+    if (!beam_sizes_ok(batch, beams, V, picks) || !type_is_float(type) || end < -1 || end >= V) {
+        set_error("tron_beam_select: bad argument (need batch >= 0, 1 <= beams <= 64, 1 <= V < 2^31 - 64, 1 <= picks <= 64, picks <= beams V, batch < 2^25, "
+                  "type f32, bf16 or f16, -1 <= end < V)");
+        return TRON_EINVAL;
+    }
+    if (batch > 0 && (!z || !score || !next_score || !parent || !token || (ended && end < 0) || !rows_ok(batch * beams, V, ldz, false) || !extent_ok(batch * beams, ldz, V))) {
+        set_error("tron_beam_select: bad argument (z, score, next_score, parent and token are needed, and an end where beams may have ended)");
+        return TRON_EINVAL;
+    }
+    if (batch > 0 && !work_ok(work, work_bytes, tron_beam_select_work(batch, beams, V, picks))) {
+        set_error("tron_beam_select: needs a work space of tron_beam_select_work(batch, beams, V, picks) bytes at a multiple of 16");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    if (batch == 0) return TRON_OK;
+    const int64_t rows = batch * beams;
+    const Split S = split_of(rows, beams, V, picks);
+    double *part_sum = static_cast<double *>(work);
+    key_t64 *part_key = reinterpret_cast<key_t64 *>(part_sum + rows * S.parts);
+    float *part_max = reinterpret_cast<float *>(part_key + rows * S.parts * picks);
+    const BeamArgs A{z, ldz, score, ended, batch, V, end, S.per, (int)beams, (int)picks, S.parts, part_sum, part_key, part_max, next_score, parent, token, next_ended};
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    if (type == TRON_TYPE_F32) launch_offers<float>(A, S.waves, st);
+    else if (type == TRON_TYPE_BF16) launch_offers<__bf16>(A, S.waves, st);
+    else launch_offers<_Float16>(A, S.waves, st);
+    TRON_HIP(hipGetLastError());
+    k_beam_pick<<<block_grid(batch), kPickThreads, beams * S.parts * picks * 12, st>>>(A);
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+int tron_beam_reorder(int64_t layers, int64_t batch, int64_t per, const int32_t *rows, int64_t ldrows, int64_t rows_in, const void *src, int64_t src_layer,
+                      int64_t src_row, void *dst, int64_t dst_layer, int64_t dst_row, int64_t positions, int64_t step, const int32_t *lengths, void *hip_stream)
+{
+    if (layers < 0 || batch < 0 || per < 0 || rows_in < 0 || positions < 0 || step < 0 || layers > 65535 || rows_in > INT32_MAX || batch > INT32_MAX || per > INT32_MAX ||
+        !extent_ok(positions, step, step)) {
+        set_error("tron_beam_reorder: bad argument (sizes are not negative; layers < 65536, batch, per and rows_in < 2^31)");
+        return TRON_EINVAL;
+    }
+    const int64_t count = batch * per, row_bytes = positions * step;
+    if (layers == 0 || count == 0 || row_bytes == 0) return check_device();
+    if (!rows || (rows_in && !src) || !dst || !rows_ok(batch, per, ldrows, false) || count > INT32_MAX || src_layer < 0 || src_row < 0 || !extent_ok(rows_in, src_row, row_bytes) ||
+        !extent_ok(layers, src_layer, row_bytes) || !extent_ok(count, dst_row, row_bytes) || !extent_ok(layers, dst_layer, row_bytes)) {
+        set_error("tron_beam_reorder: bad argument (rows, src and dst are needed; strides are not negative)");
+        return TRON_EINVAL;
+    }
+    const int64_t in_layer = rows_in ? (rows_in - 1) * src_row + row_bytes : 0, out_layer = (count - 1) * dst_row + row_bytes;
+    // rows in layers, or layers in rows
+    const bool whole = (count == 1 || dst_row >= row_bytes) &&
+                       (layers == 1 || dst_layer >= out_layer || (dst_layer >= row_bytes && (count == 1 || dst_row >= (layers - 1) * dst_layer + row_bytes)));
+    if (!whole || !apart(static_cast<const char *>(src), (layers - 1) * src_layer + in_layer, static_cast<const char *>(dst), (layers - 1) * dst_layer + out_layer)) {
+        set_error("tron_beam_reorder: rows that are written may overlap neither each other nor src");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    if (rows_in == 0) return TRON_OK;
+    const int64_t pieces = ceil_div(row_bytes, kPiece);
+    const ReorderArgs A{rows, lengths, static_cast<const char *>(src), static_cast<char *>(dst), ldrows, per, count, rows_in, src_layer, src_row, dst_layer, dst_row,
+                        positions, step, pieces};
+    dim3 grid = block_grid(count * pieces);
+    if (grid.y > 65535 || count > ((int64_t)1 << 36) / pieces) {
+        set_error("tron_beam_reorder: more than 2^36 pieces of 16 KB a layer");
+        return TRON_EINVAL;
+    }
+    grid.z = (unsigned)layers;
+    k_beam_reorder<<<grid, kBlock, 0, reinterpret_cast<hipStream_t>(hip_stream)>>>(A);
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,442 @@
+// Embeddings of tokens, and the gradient of their table.
+//
+//   y_i = scale row_scale[id_i] table[id_i];      dtable_v = scale sum_{i: id_i = v} dy_i  (+ dtable_v)
+//
+// The lookup is bound by reading the rows of the tokens and writing y.  The gradient is bound by reading dy once and writing the table; its
+// sums are those of the rows of equal tokens in the order of their places, whatever the tokens are, so that the same call gives the same bits.
+// Three launches: tokens are sorted (k_sort_tokens); the sorted places are cut into tiles of equal length, whatever tokens they hold, so that a frequent
+// token is many tiles' work, and a wavefront sums a tile's rows over 512 columns and stores those tokens that lie in its tile alone
+// (k_embed_sums, whose further wavefronts fill the rows of tokens that are not there); the others' shares are joined (k_embed_join).
+#include "head_util.h"
+
+namespace tron {
+namespace {
+
+constexpr int kColumns = kWave * kVec;   // of a wavefront
+
+template <typename T>
+__device__ __forceinline__ void floats_of(float *v, const Raw8<T> &r)
+{
+    if constexpr (__is_same(T, e4m3)) {
+        int w[2];
+        __builtin_memcpy(w, &r, 8);
+        v[0] = __builtin_amdgcn_cvt_f32_fp8(w[0], 0), v[1] = __builtin_amdgcn_cvt_f32_fp8(w[0], 1);
+        v[2] = __builtin_amdgcn_cvt_f32_fp8(w[0], 2), v[3] = __builtin_amdgcn_cvt_f32_fp8(w[0], 3);
+        v[4] = __builtin_amdgcn_cvt_f32_fp8(w[1], 0), v[5] = __builtin_amdgcn_cvt_f32_fp8(w[1], 1);
+        v[6] = __builtin_amdgcn_cvt_f32_fp8(w[1], 2), v[7] = __builtin_amdgcn_cvt_f32_fp8(w[1], 3);
+    } else if constexpr (__is_same(T, whole8)) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = (float)r.v[i].v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = static_cast<float>(r.v[i]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ T zero_of()
+{
+    T z;
+    __builtin_memset(&z, 0, sizeof(T));
+    return z;
+}
+
+struct Ids {
+    const void *p;
+    bool wide;
+    __device__ __forceinline__ int64_t at(int64_t i) const { return wide ? static_cast<const int64_t *>(p)[i] : (int64_t)static_cast<const int32_t *>(p)[i]; }
+};
+
+// ------------------------------------------------------------------ lookup
+struct EmbedArgs {
+    Ids ids;
+    const void *table;
+    const float *row_scale;
+    void *y;
+    int64_t m, d, V, ldtable, ldy, across;   // across: wavefronts a row
+    float scale;
+};
+
+// A wavefront 512 columns of a row
+template <typename T, typename O, bool PAST>
+__global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs A)
+{
+    const int64_t unit = block_number() * kWavesPerBlock + threadIdx.x / kWave, i = unit / A.across;
+    const int64_t j = (unit - i * A.across) * kColumns + threadIdx.x % kWave * kVec;
+    if (i >= A.m || j >= A.d) return;
+    const int64_t id = A.ids.at(i);
+    float v[kVec];
+    if (id >= 0 && id < A.V) {
+        floats_of(v, load_row8(static_cast<const T *>(A.table) + id * A.ldtable, j, A.d, zero_of<T>()));
+        const float by = A.row_scale ? A.scale * A.row_scale[id] : A.scale;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] *= by;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = 0.f;
+    }
+    store8_of<O, PAST>(static_cast<O *>(A.y) + i * A.ldy + j, v, A.d - j);
+}
+
+// ------------------------------------------------------------------ sorted tokens
+constexpr int kSortWaves = 16;
+constexpr int kMostIds = 1024;    // of a workgroup: counts of each for every wavefront lie in LDS
+
+struct Sorted {
+    int32_t *start;    // [V + 1]: first place of a token among the sorted ones
+    int32_t *key, *from;   // [m]: token and row of dy of a place
+};
+
+// A workgroup has `each` tokens of the table and reads all m ids: it counts those before its own, and its own by wavefront; each wavefront has a
+// contiguous range of the ids, and puts its places in their order behind those of the wavefronts before it.
+__global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int64_t m, int64_t V, int each, Sorted S)
+{
+    __shared__ int counts[kSortWaves][kMostIds];
+    __shared__ int totals[2][kSortWaves];
+    const int64_t low = block_number() * each;
+    if (low >= V) return;
+    const int here = (int)(V - low < each ? V - low : each);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    for (int k = threadIdx.x; k < kSortWaves * kMostIds; k += kSortWaves * kWave) (&counts[0][0])[k] = 0;
+    __syncthreads();
+    const int64_t share = (m + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave, begin = wave * share, end = begin + share < m ? begin + share : m;
+    constexpr int kAhead = 8;
+    int before = 0;
+    for (int64_t i0 = begin; i0 < end; i0 += kAhead * kWave) {
+        int64_t id[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t i = i0 + u * kWave + lane;
+            id[u] = i < end ? ids.at(i) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            before += id[u] >= 0 && id[u] < low;
+            const int64_t k = id[u] - low;
+            if (k >= 0 && k < here) atomicAdd(&counts[wave][(int)k], 1);
+        }
+    }
+    // places of the tokens: a thread a token
+    before = wave_scan_add(before);   // of all lanes, in the last one
+    __syncthreads();
+    int mine = 0;
+    const int k = threadIdx.x;
+    if (k < here)
+        for (int w = 0; w < kSortWaves; ++w) mine += counts[w][k];
+    const int scanned = wave_scan_add(mine);
+    if (lane == kWave - 1) {
+        totals[0][wave] = before;
+        totals[1][wave] = scanned;
+    }
+    __syncthreads();
+    int place = scanned - mine;
+    for (int w = 0; w < kSortWaves; ++w) {
+        place += totals[0][w];
+        if (w < wave) place += totals[1][w];
+    }
+    if (k < here) {
+        S.start[low + k] = place;
+        if (low + k == V - 1) S.start[V] = place + mine;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int c = counts[w][k];
+            counts[w][k] = place;
+            place += c;
+        }
+    }
+    __syncthreads();
+    for (int64_t i0 = begin; i0 < end; i0 += kAhead * kWave) {
+        int64_t id[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t i = i0 + u * kWave + lane;
+            id[u] = i < end ? ids.at(i) : -1;
+        }
+#pragma unroll 1
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t k = id[u] - low;
+            uint64_t left = __ballot(k >= 0 && k < here);
+            // one token of the 64 after the other, with all of its places
+            while (left) {
+                const int token = __builtin_amdgcn_readlane((int)k, __builtin_ctzll(left));
+                const uint64_t same = left & __ballot((int)k == token);
+                const int at = counts[wave][token];
+                if (same >> lane & 1) {
+                    const int to = at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0));
+                    S.key[to] = (int32_t)(low + token);
+                    S.from[to] = (int32_t)(i0 + u * kWave + lane);
+                }
+                if (lane == 0) counts[wave][token] = at + __popcll(same);
+                left &= ~same;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ sums
+struct EmbedGradArgs {
+    Sorted S;
+    const void *dy;
+    void *dtable;
+    float *shares;     // [tiles][2][d]: sums of a tile's first token, where its places begin before the tile, and of its last one, where they go on behind it
+    int64_t m, d, V, lddy, ldtable, across, tiles, tile_units;
+    int tile;          // places of a tile
+    float scale;
+    bool add;
+};
+
+template <typename O, bool PAST>
+__device__ __forceinline__ void put_row(const EmbedGradArgs &A, int64_t v, int64_t j, const float *sum)
+{
+    O *row = static_cast<O *>(A.dtable) + v * A.ldtable;
+    float out[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) out[e] = sum[e] * A.scale;
+    if (A.add) {
+        const Raw8<O> was = load_row8(row, j, A.d, static_cast<O>(0.f));
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) out[e] += static_cast<float>(was.v[e]);
+    }
+    store8_of<O, PAST>(row + j, out, A.d - j);
+}
+
+// The first wavefronts have a tile's 512 columns each, the others a row of the table each
+template <typename T, typename O, bool PAST>
+__global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
+{
+    const int64_t unit = block_number() * kWavesPerBlock + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x % kWave;
+    if (unit >= A.tile_units) {
+        const int64_t v = unit - A.tile_units;
+        if (v >= A.V || A.add || A.S.start[v] != A.S.start[v + 1]) return;
+        float zeros[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) zeros[e] = 0.f;
+        O *row = static_cast<O *>(A.dtable) + v * A.ldtable;
+        for (int64_t j = lane * kVec; j < A.d; j += kColumns) store8_of<O, PAST>(row + j, zeros, A.d - j);
+        return;
+    }
+    const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
+    const int64_t count = A.S.start[A.V], begin = t * A.tile, end = begin + A.tile < count ? begin + A.tile : count;
+    if (begin >= count) return;
+    const bool enters = begin > 0 && A.S.key[begin - 1] == A.S.key[begin], leaves = end < count && A.S.key[end] == A.S.key[end - 1];
+    const bool there = j < A.d;
+    const T *dy = static_cast<const T *>(A.dy);
+    float sum[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+    bool first = enters;
+    constexpr int kAhead = 8;
+    for (int64_t i0 = begin; i0 < end; i0 += kAhead) {
+        Raw8<T> raw[kAhead];
+        int key[kAhead + 1];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t i = i0 + u < end ? i0 + u : end - 1;
+            key[u] = __builtin_amdgcn_readfirstlane(A.S.key[i]);
+            const int64_t from = __builtin_amdgcn_readfirstlane(A.S.from[i]);
+            if (there) raw[u] = load_row8(dy + from * A.lddy, j, A.d, static_cast<T>(0.f));
+        }
+        key[kAhead] = i0 + kAhead < end ? __builtin_amdgcn_readfirstlane(A.S.key[i0 + kAhead]) : -1;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i0 + u >= end) break;
+            if (there) {
+                float v[kVec];
+                floats_of(v, raw[u]);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) sum[e] += v[e];
+            }
+            const bool last = i0 + u + 1 == end;
+            if (!last && key[u + 1] == key[u]) continue;
+            if (there) {
+                if (first) store8_of<float>(A.shares + 2 * t * A.d + j, sum, A.d - j);
+                else if (last && leaves) store8_of<float>(A.shares + (2 * t + 1) * A.d + j, sum, A.d - j);
+                else put_row<O, PAST>(A, key[u], j, sum);
+            }
+            first = false;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+        }
+    }
+}
+
+// Tokens of several tiles: the tile in which one begins adds the shares of those that follow, in their order
+template <typename O, bool PAST>
+__global__ __launch_bounds__(kBlock) void k_embed_join(EmbedGradArgs A)
+{
+    const int64_t unit = block_number() * kWavesPerBlock + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (unit >= A.tile_units) return;
+    const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + threadIdx.x % kWave * kVec;
+    const int64_t count = A.S.start[A.V], begin = t * A.tile, end = begin + A.tile;
+    if (end >= count || j >= A.d) return;
+    const int v = A.S.key[end - 1];
+    if (A.S.key[end] != v || A.S.start[v] < begin) return;
+    float sum[kVec];
+    auto take = [&](const float *p, float *to) {
+        const Raw8<float> r = load_row8(p, j, A.d, 0.f);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) to[e] = r.v[e];
+    };
+    take(A.shares + (2 * t + 1) * A.d, sum);
+    const int64_t last = (A.S.start[v + 1] - 1) / A.tile;
+    int64_t u = t + 1;
+    for (; u + 3 <= last; u += 4) {
+        float four[4][kVec];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) take(A.shares + 2 * (u + q) * A.d, four[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[e] += four[q][e];
+    }
+    for (; u <= last; ++u) {
+        float one[kVec];
+        take(A.shares + 2 * u * A.d, one);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] += one[e];
+    }
+    put_row<O, PAST>(A, v, j, sum);
+}
+
+// ------------------------------------------------------------------ host
+template <typename T, typename O>
+void embed_launch(const EmbedArgs &A, hipStream_t st)
+{
+    const dim3 grid = block_grid(ceil_div(A.m * A.across, kWavesPerBlock));
+    if (goes_past(A.m, A.d, sizeof(O))) k_embed<T, O, true><<<grid, kBlock, 0, st>>>(A);
+    else k_embed<T, O, false><<<grid, kBlock, 0, st>>>(A);
+}
+
+template <typename T>
+void embed_typed(const EmbedArgs &A, int out, hipStream_t st)
+{
+    if (out == TRON_TYPE_F32) embed_launch<T, float>(A, st);
+    else if (out == TRON_TYPE_BF16) embed_launch<T, __bf16>(A, st);
+    else embed_launch<T, _Float16>(A, st);
+}
+
+// Places of a tile: tiles of 512 columns for some eight wavefronts a compute unit, of 16 places at least and of 512 at most
+int tile_of_places(int64_t m, int64_t d)
+{
+    int tile = 16;
+    while (tile < 512 && ceil_div(m, tile) * ceil_div(d, kColumns) > 2048) tile *= 2;
+    return tile;
+}
+
+struct EmbedSpace {
+    int64_t start, key, from, shares, total;
+};
+EmbedSpace embed_space(int64_t m, int64_t d, int64_t V)
+{
+    EmbedSpace S;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t from = at;
+        at += ceil_div(bytes, 256) * 256;
+        return from;
+    };
+    S.start = take((V + 1) * 4);
+    S.key = take(m * 4);
+    S.from = take(m * 4);
+    S.shares = take(ceil_div(m, tile_of_places(m, d)) * 2 * d * 4);
+    S.total = at;
+    return S;
+}
+
+template <typename T, typename O, bool PAST>
+int embed_grad_launch(const EmbedGradArgs &A, hipStream_t st)
+{
+    const int64_t units = A.tile_units + (A.add ? 0 : A.V);
+    if (units) k_embed_sums<T, O, PAST><<<block_grid(ceil_div(units, kWavesPerBlock)), kBlock, 0, st>>>(A);
+    TRON_HIP(hipGetLastError());
+    if (A.tiles > 1) k_embed_join<O, PAST><<<block_grid(ceil_div(A.tile_units, kWavesPerBlock)), kBlock, 0, st>>>(A);
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+template <typename T, typename O>
+int embed_grad_to(const EmbedGradArgs &A, hipStream_t st)
+{
+    return !A.add && goes_past(A.V, A.d, sizeof(O)) ? embed_grad_launch<T, O, true>(A, st) : embed_grad_launch<T, O, false>(A, st);
+}
+
+template <typename T>
+int embed_grad_typed(const EmbedGradArgs &A, int out, hipStream_t st)
+{
+    return out == TRON_TYPE_F32 ? embed_grad_to<T, float>(A, st) : out == TRON_TYPE_BF16 ? embed_grad_to<T, __bf16>(A, st) : embed_grad_to<T, _Float16>(A, st);
+}
+
+bool embed_sizes_ok(int64_t m, int64_t d, int64_t V)
+{
+    return m >= 0 && m <= INT32_MAX && d >= 1 && V >= 1 && V < INT32_MAX - 64 && extent_ok(m, d, d) && extent_ok(V, d, d);
+}
+
+}  // namespace
+}  // namespace tron
+
+using namespace tron;
+
+extern "C" {
+
+int tron_embed(int64_t m, int64_t d, int64_t V, const void *ids, int id_bytes, int type, const void *table, int64_t ldtable, const float *row_scale, double scale,
+               int out_type, void *y, int64_t ldy, void *hip_stream)
+{
+    const bool eight = type == TRON_TYPE_E4M3 || type == TRON_TYPE_I8;
+    if (!embed_sizes_ok(m, d, V) || (id_bytes != 4 && id_bytes != 8) || (!eight && !type_is_float(type)) || !type_is_float(out_type)) {
+        set_error("tron_embed: bad argument (need 0 <= m < 2^31, d >= 1, 1 <= V < 2^31 - 64, ids of 4 or 8 bytes, type f32, bf16, f16, e4m3 or i8, out_type f32, bf16 or f16)");
+        return TRON_EINVAL;
+    }
+    if (m > 0 && (!ids || !table || !y || eight != (row_scale != nullptr) || !rows_ok(V, d, ldtable, false) || !rows_ok(m, d, ldy, true) || !extent_ok(V, ldtable, d) ||
+                  !extent_ok(m, ldy, d))) {
+        set_error("tron_embed: bad argument (ids, table and y are needed, tables of 8 bits, and they alone, have scales; rows that are written may not overlap)");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    if (m == 0) return TRON_OK;
+    const EmbedArgs A{Ids{ids, id_bytes == 8}, table, row_scale, y, m, d, V, ldtable, ldy, ceil_div(d, kColumns), (float)scale};
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    switch (type) {
+    case TRON_TYPE_F32: embed_typed<float>(A, out_type, st); break;
+    case TRON_TYPE_BF16: embed_typed<__bf16>(A, out_type, st); break;
+    case TRON_TYPE_F16: embed_typed<_Float16>(A, out_type, st); break;
+    case TRON_TYPE_E4M3: embed_typed<e4m3>(A, out_type, st); break;
+    default: embed_typed<whole8>(A, out_type, st);
+    }
+    TRON_HIP(hipGetLastError());
+    return TRON_OK;
+}
+
+int64_t tron_embed_grad_work(int64_t m, int64_t d, int64_t V) { return embed_sizes_ok(m, d, V) ? embed_space(m, d, V).total : 0; }
+
+int tron_embed_grad(int64_t m, int64_t d, int64_t V, const void *ids, int id_bytes, int type, const void *dy, int64_t lddy, double scale, int add, int out_type,
+                    void *dtable, int64_t ldtable, void *work, int64_t work_bytes, void *hip_stream)
+{
+    if (!embed_sizes_ok(m, d, V) || (id_bytes != 4 && id_bytes != 8) || !type_is_float(type) || !type_is_float(out_type)) {
+        set_error("tron_embed_grad: bad argument (need 0 <= m < 2^31, d >= 1, 1 <= V < 2^31 - 64, ids of 4 or 8 bytes, types f32, bf16 or f16)");
+        return TRON_EINVAL;
+    }
+    if ((m > 0 && (!ids || !dy || !rows_ok(m, d, lddy, false) || !extent_ok(m, lddy, d))) || !dtable || !rows_ok(V, d, ldtable, true) || !extent_ok(V, ldtable, d)) {
+        set_error("tron_embed_grad: bad argument (ids, dy and dtable are needed; rows that are written may not overlap)");
+        return TRON_EINVAL;
+    }
+    if (!work_ok(work, work_bytes, tron_embed_grad_work(m, d, V))) {
+        set_error("tron_embed_grad: needs a work space of tron_embed_grad_work(m, d, V) bytes at a multiple of 16");
+        return TRON_EINVAL;
+    }
+    TRON_TRY(check_device());
+    const EmbedSpace S = embed_space(m, d, V);
+    char *w = static_cast<char *>(work);
+    const Sorted sorted{reinterpret_cast<int32_t *>(w + S.start), reinterpret_cast<int32_t *>(w + S.key), reinterpret_cast<int32_t *>(w + S.from)};
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    // a workgroup a compute unit, of whom each reads all ids
+    const int each = (int)std::min<int64_t>(kMostIds, ceil_div(V, 256));
+    k_sort_tokens<<<block_grid(ceil_div(V, each)), kSortWaves * kWave, 0, st>>>(Ids{ids, id_bytes == 8}, m, V, each, sorted);
+    TRON_HIP(hipGetLastError());
+    const int tile = tile_of_places(m, d);
+    const int64_t across = ceil_div(d, kColumns), tiles = ceil_div(m, tile);
+    const EmbedGradArgs A{sorted, dy, dtable, reinterpret_cast<float *>(w + S.shares), m, d, V, lddy, ldtable, across, tiles, tiles * across, tile, (float)scale, add != 0};
+    return type == TRON_TYPE_F32 ? embed_grad_typed<float>(A, out_type, st)
+           : type == TRON_TYPE_BF16 ? embed_grad_typed<__bf16>(A, out_type, st) : embed_grad_typed<_Float16>(A, out_type, st);
+}
+
+}  // extern "C"

@@ -281,6 +281,109 @@ def tron_distill_hv(z, lse, u, hu, ids=None, t=None, temperature=1.0, weight=Non
              call.vector(weight, "weight", m), hp, ldh, sp, sb, call.address)
 
 
+def _entries(call, t, what, shape, dtypes):
+    """Address of a contiguous tensor of that shape and one of those types, or None."""
+    if t is None:
+        return None
+    if t.get_device() != call.index:
+        _refuse(f"{call.name}: {what} is on {t.device}, other arguments on {call.device}")
+    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _refuse(f"{call.name}: {what} has to be {' x '.join(map(str, shape))} contiguous values of {' or '.join(map(str, dtypes))}")
+    return t.data_ptr()
+
+
+def tron_beam_select_work(batch, beams, V, picks) -> int:
+    return load_library().tron_beam_select_work(batch, beams, V, picks)
+
+
+def tron_beam_select(z, score, next_score, parent, token, ended=None, end=-1, next_ended=None, work=None, stream=None) -> None:
+    """The step of a beam search: z (batch * beams x V) are the logits of beams with score (batch x beams); next_score, parent (rows of z) and token,
+    batch x picks each, are the picks of largest log-probability.  ended and next_ended: bool or uint8."""
+    lib = _load()
+    call = _Call("tron_beam_select", z, stream)
+    zp, rows, V, ldz = call.matrix(z, "z")
+    if score.dim() != 2 or next_score.dim() != 2 or score.shape[0] != next_score.shape[0]:
+        _refuse("tron_beam_select: score (batch x beams) and next_score (batch x picks) have 2 dimensions")
+    (batch, beams), picks = score.shape, next_score.shape[1]
+    if rows != batch * beams:
+        _refuse(f"tron_beam_select: z has {rows} rows, score {batch} x {beams}")
+    flags = (_torch.bool, _torch.uint8)
+    space, wp, wb = call.work(work, lib.tron_beam_select_work(batch, beams, V, picks))
+    call.run(lib.tron_beam_select, batch, beams, V, call.type(z, "z"), zp, ldz, _entries(call, score, "score", (batch, beams), (_torch.float32,)),
+             _entries(call, ended, "ended", (batch, beams), flags), end, picks, _entries(call, next_score, "next_score", (batch, picks), (_torch.float32,)),
+             _entries(call, parent, "parent", (batch, picks), (_torch.int32,)), _entries(call, token, "token", (batch, picks), (_torch.int32,)),
+             _entries(call, next_ended, "next_ended", (batch, picks), flags), wp, wb, call.address)
+
+
+def tron_beam_reorder(rows, states, out, lengths=None, stream=None) -> None:
+    """out[:, i] = states[:, rows[i]] for states and out of layers x rows x positions x ..., whose positions lie one behind the other; rows: int32 of 1 or 2 dimensions
+    (the parent of tron_beam_select, or its first columns).  lengths (int32, one a row of states): positions behind it are left as they were in out."""
+    lib = _load()
+    call = _Call("tron_beam_reorder", states, stream)
+    if rows.dtype != _torch.int32:
+        _refuse(f"tron_beam_reorder: rows are of {rows.dtype}, expected int32")
+    ip, batch, per, ldrows = call.matrix(rows, "rows")
+    if states.dim() < 3 or out.dim() != states.dim() or out.dtype != states.dtype or out.shape[0] != states.shape[0] or out.shape[2:] != states.shape[2:]:
+        _refuse("tron_beam_reorder: states and out have to be layers x rows x positions x ... of one type, alike but for the rows")
+    if out.get_device() != call.index:
+        _refuse(f"tron_beam_reorder: out is on {out.device}, other arguments on {call.device}")
+    if out.shape[1] != batch * per:
+        _refuse(f"tron_beam_reorder: out has {out.shape[1]} rows, expected {batch * per}")
+    layers, rows_in, positions = states.shape[:3]
+    size = states.element_size()
+    step = size
+    for n in states.shape[3:]:
+        step *= n
+    place = 1
+    for i in range(states.dim() - 1, 1, -1):
+        for t, what in ((states, "states"), (out, "out")):
+            if t.shape[i] > 1 and t.stride(i) != place:
+                _refuse(f"tron_beam_reorder: the positions of a row of {what} are not contiguous")
+        place *= max(1, states.shape[i])
+    call.run(lib.tron_beam_reorder, layers, batch, per, ip, ldrows, rows_in, states.data_ptr(), states.stride(0) * size, states.stride(1) * size, out.data_ptr(),
+             out.stride(0) * size, out.stride(1) * size, positions, step, _entries(call, lengths, "lengths", (rows_in,), (_torch.int32,)), call.address)
+
+
+def _ids(call, ids):
+    """(address, count, bytes) of contiguous ids."""
+    if ids.get_device() != call.index:
+        _refuse(f"{call.name}: ids are on {ids.device}, other arguments on {call.device}")
+    if ids.dtype not in (_torch.int32, _torch.int64) or ids.dim() != 1 or (ids.shape[0] > 1 and ids.stride(0) != 1):
+        _refuse(f"{call.name}: ids have to be contiguous int32 or int64 values of one dimension")
+    return ids.data_ptr(), ids.shape[0], 4 if ids.dtype == _torch.int32 else 8
+
+
+def tron_embed(ids, table, y, scale=1.0, row_scale=None, stream=None) -> None:
+    """y[i] = scale row_scale[ids[i]] table[ids[i]]; zeros where an id is not one of the table's rows.  table (V x d) of float32, bfloat16, float16, or float8_e4m3fn
+    or int8 with row_scale (V); y of float32, bfloat16, float16."""
+    lib = _load()
+    call = _Call("tron_embed", table, stream)
+    ip, m, ib = _ids(call, ids)
+    if table.dim() != 2:
+        _refuse("tron_embed: table has to have 2 dimensions")
+    tp, V, d, ldt = call.matrix(table, "table")
+    yp, _, _, ldy = call.matrix(y, "y", m, d)
+    call.run(lib.tron_embed, m, d, V, ip, ib, call.type(table, "table"), tp, ldt, call.vector(row_scale, "row_scale", V), scale, call.type(y, "y"), yp, ldy, call.address)
+
+
+def tron_embed_grad_work(m, d, V) -> int:
+    return load_library().tron_embed_grad_work(m, d, V)
+
+
+def tron_embed_grad(ids, dy, dtable, scale=1.0, add=False, work=None, stream=None) -> None:
+    """dtable[v] = scale times the sum of the dy[i] with ids[i] = v, added to what is there with `add`.  dy (m x d) and dtable (V x d) of float32, bfloat16 or
+    float16."""
+    lib = _load()
+    call = _Call("tron_embed_grad", dtable, stream)
+    ip, m, ib = _ids(call, ids)
+    if dtable.dim() != 2:
+        _refuse("tron_embed_grad: dtable has to have 2 dimensions")
+    tp, V, d, ldt = call.matrix(dtable, "dtable")
+    dp, _, _, ldd = call.matrix(dy, "dy", m, d)
+    space, wp, wb = call.work(work, lib.tron_embed_grad_work(m, d, V))
+    call.run(lib.tron_embed_grad, m, d, V, ip, ib, call.type(dy, "dy"), dp, ldd, scale, int(add), call.type(dtable, "dtable"), tp, ldt, wp, wb, call.address)
+
+
 # --------------------------------------------------------------------------- convenience wrapper
 class SoftmaxHead:
     """The problem that a softmax head is trained on, with the calls of Dataset:
