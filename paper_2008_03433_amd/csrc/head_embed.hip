@@ -93,11 +93,14 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int6
 {
     __shared__ int counts[kSortWaves][kMostIds];
     __shared__ int totals[2][kSortWaves];
+    __shared__ uint8_t marks[kSortWaves][kMostIds];
     const int64_t low = block_number() * each;
     if (low >= V) return;
     const int here = (int)(V - low < each ? V - low : each);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    for (int k = threadIdx.x; k < kSortWaves * kMostIds; k += kSortWaves * kWave) (&counts[0][0])[k] = 0;
+    if ((int)threadIdx.x < here) {
+        for (int w = 0; w < kSortWaves; ++w) counts[w][threadIdx.x] = 0;
+    }
     __syncthreads();
     const int64_t share = (m + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave, begin = wave * share, end = begin + share < m ? begin + share : m;
     constexpr int kAhead = 8;
@@ -154,19 +157,32 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int6
 #pragma unroll 1
         for (int u = 0; u < kAhead; ++u) {
             const int64_t k = id[u] - low;
-            uint64_t left = __ballot(k >= 0 && k < here);
-            // one token of the 64 after the other, with all of its places
-            while (left) {
-                const int token = __builtin_amdgcn_readlane((int)k, __builtin_ctzll(left));
+            const bool own = k >= 0 && k < here;
+            uint64_t left = __ballot(own);
+            if (!left) continue;
+            const int64_t from = i0 + u * kWave + lane;
+            auto put = [&](int to) {
+                S.key[to] = (int32_t)(low + k);
+                S.from[to] = (int32_t)from;
+            };
+            // Every lane writes its number to its token's mark.  Whose number is not there has a token that is there twice: these go one token after the other,
+            // in the order of their lanes; the others all at once
+            volatile uint8_t *mark = marks[wave];
+            if (own) mark[k] = (uint8_t)lane;
+            uint64_t twice = __ballot(own && mark[k] != lane);
+            while (twice) {
+                const int token = __builtin_amdgcn_readlane((int)k, __builtin_ctzll(twice));
                 const uint64_t same = left & __ballot((int)k == token);
                 const int at = counts[wave][token];
-                if (same >> lane & 1) {
-                    const int to = at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0));
-                    S.key[to] = (int32_t)(low + token);
-                    S.from[to] = (int32_t)(i0 + u * kWave + lane);
-                }
+                if (same >> lane & 1) put(at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0)));
                 if (lane == 0) counts[wave][token] = at + __popcll(same);
                 left &= ~same;
+                twice &= ~same;
+            }
+            if (left >> lane & 1) {
+                const int at = counts[wave][k];
+                put(at);
+                counts[wave][k] = at + 1;
             }
         }
     }
@@ -208,11 +224,18 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
     if (unit >= A.tile_units) {
         const int64_t v = unit - A.tile_units;
         if (v >= A.V || A.add || A.S.start[v] != A.S.start[v + 1]) return;
-        float zeros[kVec];
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) zeros[e] = 0.f;
+        // sixteen bytes a lane, side by side: whole lines from one instruction
+        typedef int words __attribute__((ext_vector_type(4), aligned(2)));
+        constexpr int kEach = 16 / (int)sizeof(O);
         O *row = static_cast<O *>(A.dtable) + v * A.ldtable;
-        for (int64_t j = lane * kVec; j < A.d; j += kColumns) store8_of<O, PAST>(row + j, zeros, A.d - j);
+        for (int64_t j = lane * kEach; j < A.d; j += kWave * kEach) {
+            if (j + kEach <= A.d) {
+                if (PAST) __builtin_nontemporal_store(words{0, 0, 0, 0}, reinterpret_cast<words *>(row + j));
+                else *reinterpret_cast<words *>(row + j) = words{0, 0, 0, 0};
+            } else {
+                for (int64_t k = j; k < A.d; ++k) row[k] = static_cast<O>(0.f);
+            }
+        }
         return;
     }
     const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
@@ -226,36 +249,38 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
     for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
     bool first = enters;
     constexpr int kAhead = 8;
-    for (int64_t i0 = begin; i0 < end; i0 += kAhead) {
-        Raw8<T> raw[kAhead];
-        int key[kAhead + 1];
+    for (int64_t c0 = begin; c0 < end; c0 += kWave) {
+        // tokens and rows of 64 places, one a lane; behind the tile's last place -1, and that place's row once more
+        const int here = (int)(end - c0 < kWave ? end - c0 : kWave);
+        const int at = lane < here ? lane : here - 1;
+        const int from = A.S.from[c0 + at], after = c0 + kWave < end ? A.S.key[c0 + kWave] : -1;
+        int key = A.S.key[c0 + at];
+        if (lane >= here) key = -1;
+        for (int i0 = 0; i0 < here; i0 += kAhead) {
+            Raw8<T> raw[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t i = i0 + u < end ? i0 + u : end - 1;
-            key[u] = __builtin_amdgcn_readfirstlane(A.S.key[i]);
-            const int64_t from = __builtin_amdgcn_readfirstlane(A.S.from[i]);
-            if (there) raw[u] = load_row8(dy + from * A.lddy, j, A.d, static_cast<T>(0.f));
-        }
-        key[kAhead] = i0 + kAhead < end ? __builtin_amdgcn_readfirstlane(A.S.key[i0 + kAhead]) : -1;
+            for (int u = 0; u < kAhead; ++u)
+                if (there) raw[u] = load_row8(dy + (int64_t)__builtin_amdgcn_readlane(from, i0 + u) * A.lddy, j, A.d, static_cast<T>(0.f));
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (i0 + u >= end) break;
-            if (there) {
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = i0 + u;
+                if (i >= here) break;
                 float v[kVec];
                 floats_of(v, raw[u]);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) sum[e] += v[e];
-            }
-            const bool last = i0 + u + 1 == end;
-            if (!last && key[u + 1] == key[u]) continue;
-            if (there) {
-                if (first) store8_of<float>(A.shares + 2 * t * A.d + j, sum, A.d - j);
-                else if (last && leaves) store8_of<float>(A.shares + (2 * t + 1) * A.d + j, sum, A.d - j);
-                else put_row<O, PAST>(A, key[u], j, sum);
-            }
-            first = false;
+                const int token = __builtin_amdgcn_readlane(key, i), next = i + 1 < kWave ? __builtin_amdgcn_readlane(key, (i + 1) % kWave) : after;
+                if (next == token) continue;
+                const bool last = next < 0;
+                if (there) {
+                    if (first) store8_of<float>(A.shares + 2 * t * A.d + j, sum, A.d - j);
+                    else if (last && leaves) store8_of<float>(A.shares + (2 * t + 1) * A.d + j, sum, A.d - j);
+                    else put_row<O, PAST>(A, token, j, sum);
+                }
+                first = false;
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+                for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+            }
         }
     }
 }
@@ -315,11 +340,11 @@ void embed_typed(const EmbedArgs &A, int out, hipStream_t st)
     else embed_launch<T, _Float16>(A, st);
 }
 
-// Places of a tile: tiles of 512 columns for some eight wavefronts a compute unit, of 16 places at least and of 512 at most
+// Places of a tile: tiles of 512 columns for some 32 wavefronts a compute unit, of 16 places at least and of 512 at most
 int tile_of_places(int64_t m, int64_t d)
 {
     int tile = 16;
-    while (tile < 512 && ceil_div(m, tile) * ceil_div(d, kColumns) > 2048) tile *= 2;
+    while (tile < 512 && ceil_div(m, tile) * ceil_div(d, kColumns) > 8192) tile *= 2;
     return tile;
 }
 
