@@ -22,7 +22,8 @@ constexpr int kMostBeams = 64;
 constexpr int kAhead = 4;            // chunks of eight columns of a lane under way
 constexpr int kTurn = kAhead * kWave * kVec;   // columns of a wavefront's turn
 constexpr int kSlack = 128;          // entries of a list beyond which it is cut to the K largest
-constexpr int kList = kSlack + kWave * kVec;
+constexpr int kList = 2 * kSlack;
+constexpr int kLooked = 4;           // lanes whose columns of a turn are looked at more closely at once: two columns a lane of the wavefront
 constexpr int kMostParts = 64;       // of a row, one a lane
 constexpr int kMostOffers = kMostBeams * kMostPicks;   // of an item's rows' parts together
 
@@ -78,6 +79,7 @@ __device__ __forceinline__ key_t64 cut_to(key_t64 *list, int &count, int K, int 
     for (int i = 0; i < N; ++i) mine[i] = i * kWave + lane < count ? list[i * kWave + lane] : 0;
     if (count < K) return 0;
     key_t64 bound = 0;
+#pragma unroll 1
     for (int b = 63; b >= 0; --b) {
         const key_t64 trial = bound | (key_t64)1 << b;
         int reach = 0;
@@ -97,10 +99,12 @@ __device__ __forceinline__ key_t64 cut_to(key_t64 *list, int &count, int K, int 
     return bound;
 }
 
+// `count` is one of the wavefront's; the compiler keeps what it may not know to be such in a register of each lane, and branches by masks
 __device__ __forceinline__ key_t64 cut(key_t64 *list, int &count, int K, int lane)
 {
-    if (count <= 3 * kWave) return cut_to<3>(list, count, K, lane);
-    return cut_to<kList / kWave>(list, count, K, lane);
+    const key_t64 bound = count <= kWave ? cut_to<1>(list, count, K, lane) : cut_to<kList / kWave>(list, count, K, lane);
+    count = __builtin_amdgcn_readfirstlane(count);
+    return bound;
 }
 
 struct Running {
@@ -123,57 +127,94 @@ struct Bound {
 
 __device__ __forceinline__ int lanes_before(uint64_t mask) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0)); }
 
+// A value, in order, that K of the wavefront's N a lane reach (0: fewer than K are not 0): the largest one of 16 bits, and zeros behind them
+template <int N>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&mine)[N], int K)
+{
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t trial = bound | 1u << b;
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) reach += __popcll(__ballot(mine[i] >= trial));
+        if (reach >= K) bound = trial;
+        if (reach == K) break;
+    }
+    return bound;
+}
+
+// Eight neighbouring columns in whole registers: elements of 16 bits that are copied one by one take a register each
+template <typename T>
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void set(const Raw8<T> &r) { __builtin_memcpy(w, &r, sizeof(w)); }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (__is_same(T, __bf16)) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else return static_cast<float>(__builtin_bit_cast(_Float16, (uint16_t)(i % 2 ? w[i / 2] >> 16 : w[i / 2])));
+    }
+};
+
+// A turn's columns of a wavefront: eight neighbouring ones a lane, kAhead times
+template <typename T>
+struct Turn {
+    Eight<T> e[kAhead];
+    __device__ __forceinline__ void load(const T *z, int64_t j0, int64_t to, int lane)
+    {
+        if (j0 + kTurn <= to) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) e[u].set(load8(z + j0 + (u * kWave + lane) * kVec));
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t j = j0 + (u * kWave + lane) * kVec;
+            Raw8<T> r;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) r.v[i] = static_cast<T>(-INFINITY);
+            if (j < to) r = load_row8(z, j, to, static_cast<T>(-INFINITY));
+            e[u].set(r);
+        }
+    }
+};
+
 // A workgroup of WAVES wavefronts a part of a row: blockIdx.x the part, y and z the row
 template <typename T, int WAVES>
-__global__ __launch_bounds__(WAVES *kWave) void k_beam_offers(BeamArgs A)
+__global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
 {
     __shared__ key_t64 lists[WAVES][kList];
+    __shared__ __align__(16) uint32_t looked[WAVES][kLooked][kAhead * 2 * sizeof(T)];
+    __shared__ uint32_t firsts[WAVES][kWave];   // the lanes' largest values of the first turns, in order
     __shared__ double sums[WAVES];
     __shared__ float tops[WAVES];
-    __shared__ int counts[WAVES];
+    __shared__ key_t64 join[WAVES > 1 ? WAVES * kWave : 1];
+    __shared__ int joined;
     __shared__ uint32_t common;   // in order: what K of some wavefront's values reach
     const int64_t row = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, part = blockIdx.x;
     if (row >= A.batch * A.beams || !is_read(A, row)) return;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, K = A.picks;
     const int64_t from = part * A.per, to = from + A.per < A.V ? from + A.per : A.V;
     const T *z = static_cast<const T *>(A.z) + row * A.ldz;
-    if (WAVES > 1) {
-        if (threadIdx.x == 0) common = 0;
-        __syncthreads();
-    }
     key_t64 *list = lists[wave];
     Running run;
     Bound bound;
     int count = 0;
-    auto tell = [&](uint32_t order) {
-        if (WAVES > 1 && lane == 0) atomicMax(&common, order);
-    };
     const int64_t begin = from + (int64_t)wave * kTurn;
-    for (int64_t j0 = begin; j0 < to; j0 += WAVES * kTurn) {
-        Raw8<T> raw[kAhead];
-        float top[kAhead], most = -INFINITY;
-        if (j0 + kTurn <= to) {
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) raw[u] = load8(z + j0 + (u * kWave + lane) * kVec);
-        } else {
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int64_t j = j0 + (u * kWave + lane) * kVec;
-                if (j < to) {
-                    raw[u] = load_row8(z, j, to, static_cast<T>(-INFINITY));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) raw[u].v[i] = static_cast<T>(-INFINITY);
-                }
-            }
-        }
+    Turn<T> now;
+    now.load(z, begin, to, lane);
+    for (int64_t j0 = begin;;) {
+        const int64_t next = j0 + WAVES * kTurn;
+        Turn<T> ahead;
+        if (next < to) ahead.load(z, next, to, lane);
+        float most = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             float v[kVec];
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) v[i] = static_cast<float>(raw[u].v[i]);
-            top[u] = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-            most = fmaxf(most, top[u]);
+            for (int i = 0; i < kVec; ++i) v[i] = now.e[u].at(i);
+            most = fmaxf(most, fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]))));
         }
         if (most > run.m) {
             run.s *= exp_of(run.m - most);   // 0 * exp(-inf) at first
@@ -185,79 +226,115 @@ __global__ __launch_bounds__(WAVES *kWave) void k_beam_offers(BeamArgs A)
             float s0 = 0.f, s1 = 0.f;
 #pragma unroll
             for (int i = 0; i < kVec; i += 2) {
-                s0 += exp_of(static_cast<float>(raw[u].v[i]) - base);
-                s1 += exp_of(static_cast<float>(raw[u].v[i + 1]) - base);
+                s0 += exp_of(now.e[u].at(i) - base);
+                s1 += exp_of(now.e[u].at(i + 1) - base);
             }
             run.s += s0 + s1;   // NaN from here on, where there is a NaN or +inf
         }
-        uint32_t first = 0;   // in order: what K values of this turn reach, if it is the first
+        uint32_t reached = 0;   // in order: what K values of this turn, or of earlier ones, reach
         if (j0 == begin) {
-            // the K-th largest of the lanes' largest
+            // The workgroup's first turns: of the lanes' largest values the K-th largest is a bound that K values reach
             const uint32_t mine = j0 + (int64_t)lane * kVec < to ? in_order(most) : 0;
-            for (int b = 31; b >= 0; --b) {
-                const uint32_t trial = first | 1u << b;
-                const int reach = __popcll(__ballot(mine >= trial));
-                if (reach >= K) first = trial;
-                if (reach == K) break;
+            uint32_t all[WAVES] = {mine};
+            if (WAVES > 1) {
+                firsts[wave][lane] = mine;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) all[w] = firsts[w][lane];
             }
-            bound.raise(first, false);
-            tell(first);
+            reached = reached_by(all, K);
+            if (WAVES > 1) {
+                if (threadIdx.x == 0) {
+                    common = reached;
+                    joined = 0;
+                }
+                __syncthreads();   // behind which `common` only rises
+            }
+            bound.raise(reached, false);
         } else if (WAVES > 1) {
             bound.raise(__builtin_amdgcn_readfirstlane(*(volatile uint32_t *)&common), false);
         }
-        if (__ballot(bound.passes(most))) {
+        // Few lanes have a value that passes.  Four of them at a time put theirs into LDS, and every lane takes two neighbouring ones of those.
+        uint64_t some = __ballot(bound.passes(most));
+        while (some) {
+            if (count > kSlack) {
+                const uint32_t order = (uint32_t)(cut(list, count, K, lane) >> 32);
+                bound.raise(order, false);   // lower columns of this turn may still come
+                if (WAVES > 1 && lane == 0) atomicMax(&common, order);
+                reached = reached > order ? reached : order;
+            }
+            constexpr int kWords = kAhead * 2 * sizeof(T), kTwo = sizeof(T) / 2;   // 32-bit words of a lane, of two columns
+            uint64_t rest = some;
+            int from_lane = 0;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                if (count > kSlack) {
-                    const uint32_t order = (uint32_t)(cut(list, count, K, lane) >> 32);
-                    bound.raise(order, true);
-                    tell(order);
-                }
-                if (!__ballot(bound.passes(top[u]))) continue;
-                const int64_t j = j0 + (u * kWave + lane) * kVec;
+            for (int q = 0; q < kLooked; ++q) {
+                const int l = rest ? __builtin_ctzll(rest) : 0;
+                if (lane / (kWave / kLooked) == q) from_lane = rest ? l : -1;
+                if (rest && lane == l) {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const float v = static_cast<float>(raw[u].v[i]);
-                    const bool in = j + i < to && bound.passes(v);
-                    const uint64_t mask = __ballot(in);
-                    if (in) list[count + lanes_before(mask)] = key_of(v, j + i);
-                    count += __popcll(mask);
+                    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                        for (int i = 0; i < kWords / kAhead; ++i) looked[wave][q][u * (kWords / kAhead) + i] = now.e[u].w[i];
                 }
+                rest &= rest - 1;
+            }
+            some = rest;
+            const int two = lane % (kWave / kLooked);   // of sixteen pairs, four a chunk
+            Eight<T> w;
+#pragma unroll
+            for (int i = 0; i < kTwo; ++i) w.w[i] = looked[wave][lane / (kWave / kLooked)][two * kTwo + i];
+            const int64_t j = j0 + ((two / (kVec / 2)) * kWave + from_lane) * kVec + two % (kVec / 2) * 2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float v = w.at(i);
+                const bool in = from_lane >= 0 && bound.passes(v) && j + i < to;
+                const uint64_t mask = __ballot(in);
+                if (in) list[count + lanes_before(mask)] = key_of(v, j + i);
+                count = __builtin_amdgcn_readfirstlane(count + __popcll(mask));
             }
         }
-        if (first) bound.raise(first, true);   // all that reach it are in the list
+        // later turns' columns are higher ones, and higher than those of all first turns, so their values have to lie above
+        if (reached) bound.raise(reached, true);
+        if (next >= to) break;
+        now = ahead;
+        j0 = next;
     }
-    if (count > K) cut(list, count, K, lane);
-    const float wave_most = wave_maxf(run.m);
-    const double wave_total = wave_sum((double)run.s * (double)exp_of(run.m - base_of(wave_most)));
-    float most = wave_most;
-    double total = wave_total;
+    float all_most = wave_maxf(run.m);
+    double total = wave_sum((double)run.s * (double)exp_of(run.m - base_of(all_most)));
     if (WAVES > 1) {
+        // one list of the wavefronts' keys that may be among the K, 64 of each at most
+        if (count > kWave) cut(list, count, K, lane);
         if (lane == 0) {
-            tops[wave] = wave_most;
-            sums[wave] = wave_total;
-            counts[wave] = count;
+            tops[wave] = all_most;
+            sums[wave] = total;
         }
+        const key_t64 key = lane < count ? list[lane] : 0;
+        const bool in = key && (uint32_t)(key >> 32) >= *(volatile uint32_t *)&common;
+        const uint64_t mask = __ballot(in);
+        int place = 0;
+        if (lane == 0) place = atomicAdd(&joined, __popcll(mask));
+        if (in) join[__builtin_amdgcn_readfirstlane(place) + lanes_before(mask)] = key;
         __syncthreads();
         if (wave) return;
-        for (int w = 1; w < WAVES; ++w) most = fmaxf(most, tops[w]);
-        total = 0.0;
-        for (int w = 0; w < WAVES; ++w) total += sums[w] * exp((double)tops[w] - (double)base_of(most));
-        // the others' lists behind this one's: K keys of each at most
-        const uint32_t least = common;
-        for (int w = 1; w < WAVES; ++w) {
-            const key_t64 key = lane < counts[w] ? lists[w][lane] : 0;
-            const bool in = key && (uint32_t)(key >> 32) >= least;
-            const uint64_t mask = __ballot(in);
-            if (in) list[count + lanes_before(mask)] = key;
-            count += __popcll(mask);
+        const float m = lane < WAVES ? tops[lane % WAVES] : -INFINITY;
+        all_most = wave_maxf(m);
+        total = wave_sum(lane < WAVES ? sums[lane % WAVES] * exp((double)m - (double)base_of(all_most)) : 0.0);
+        list = join;
+        const int keys = __builtin_amdgcn_readfirstlane(joined);
+        count = keys < kList ? keys : kList;
+        for (int read = count; read < keys;) {   // kList of them at a time
+            cut(list, count, K, lane);
+            const int more = keys - read < kList - count ? keys - read : kList - count;
+            for (int i = lane; i < more; i += kWave) list[count + i] = join[read + i];
+            count += more;
+            read += more;
         }
-        if (count > K) cut(list, count, K, lane);
     }
+    if (count > K) cut(list, count, K, lane);
     const int64_t at = row * A.parts + part;
     if (lane < K) A.part_key[at * K + lane] = lane < count ? list[lane] : 0;
     if (lane == 0) {
-        A.part_max[at] = most;
+        A.part_max[at] = all_most;
         A.part_sum[at] = total;
     }
 }
@@ -289,24 +366,34 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     __shared__ int kind[kMostBeams];
     __shared__ unsigned digits[256];
     __shared__ int found[2], survivors, chosen[kRanked];
+    __shared__ key_t64 orders[kRanked];
+    __shared__ uint64_t places[kRanked];
     const int64_t item = block_number();
     if (item >= A.batch) return;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
     const int of_beam = A.parts * K, count = A.beams * of_beam;
     const Offers O{room, reinterpret_cast<uint32_t *>(room + count), of_beam};
-    for (int b = wave; b < A.beams; b += kPickThreads / kWave) {
-        const int64_t row = item * A.beams + b;
+    const int64_t row0 = item * A.beams;
+    const key_t64 early = threadIdx.x < count ? A.part_key[row0 * of_beam + threadIdx.x] : 0;   // under way while the sums are joined
+    // a beam's parts lie in neighbouring lanes, a power of two of them
+    int lanes = 1;
+    while (lanes < A.parts) lanes *= 2;
+    for (int first = 0; first < A.beams; first += kPickThreads / lanes) {
+        const int b = first + (int)threadIdx.x / lanes, part = threadIdx.x % lanes;
+        const bool beam = b < A.beams, there = beam && part < A.parts;
+        const int64_t row = row0 + (beam ? b : 0);
         const float score = A.score[row];
-        int k = !(fabsf(score) < INFINITY) ? DEAD : A.ended && A.ended[row] ? OVER : LIVE;
-        if (k == LIVE) {
-            const bool there = lane < A.parts;
-            const float m = there ? A.part_max[row * A.parts + lane] : -INFINITY, most = wave_maxf(m);
-            const double s = there ? A.part_sum[row * A.parts + lane] : 0.0;
-            const double total = wave_sum(there ? s * exp((double)m - (double)base_of(most)) : 0.0);
-            if (!(total > 0.0 && total < INFINITY)) k = DEAD;   // nothing but -inf; a NaN or +inf
-            if (lane == 0) lse[b] = (double)most + log(total);
+        const float m = there ? A.part_max[row * A.parts + part] : -INFINITY;
+        const double s = there ? A.part_sum[row * A.parts + part] : 0.0;
+        float most = m;
+        for (int by = 1; by < lanes; by *= 2) most = fmaxf(most, __shfl_xor(most, by));
+        double total = there ? s * exp((double)m - (double)base_of(most)) : 0.0;
+        for (int by = 1; by < lanes; by *= 2) total += __shfl_xor(total, by);
+        if (beam && part == 0) {
+            const bool possible = total > 0.0 && total < INFINITY;   // not: nothing but -inf; a NaN or +inf
+            kind[b] = !(fabsf(score) < INFINITY) ? DEAD : A.ended && A.ended[row] ? OVER : possible ? LIVE : DEAD;
+            lse[b] = (double)most + log(total);
         }
-        if (lane == 0) kind[b] = k;
     }
     if (threadIdx.x == 0) survivors = 0;
     __syncthreads();
@@ -317,7 +404,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
         const bool live = kind[b] == LIVE, over = kind[b] == OVER;
         // one condition after the other: of a choice of three in one, the compiler (ROCm 7.2) leaves the last one's token undefined
         key_t64 key = 1;
-        if (live) key = A.part_key[row * of_beam + i];
+        if (live) key = e == (int)threadIdx.x ? early : A.part_key[row * of_beam + i];
         const uint32_t other = over ? i == 0 ? (uint32_t)A.end : (uint32_t)(i - (i <= A.end)) : (uint32_t)i;   // columns in order, behind `end` where it is first
         const uint32_t token = live ? ~(uint32_t)key : other;
         const bool there = live ? key != 0 : i < listed;
@@ -383,15 +470,29 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
         chosen[atomicAdd(&survivors, 1)] = threadIdx.x;
     }
     __syncthreads();
-    if (threadIdx.x >= survivors) return;
-    const int e = chosen[threadIdx.x], n = survivors;
-    const key_t64 order = O.order[e];
-    const uint64_t place = O.place(e);
-    int rank = 0;
-    for (int i = 0; i < n; ++i) {
-        const key_t64 other = O.order[chosen[i]];
-        rank += other > order || (other == order && O.place(chosen[i]) < place);
+    const int n = survivors;
+    if ((int)threadIdx.x < n) {
+        orders[threadIdx.x] = O.order[chosen[threadIdx.x]];
+        places[threadIdx.x] = O.place(chosen[threadIdx.x]);
     }
+    __syncthreads();
+    // one, two or four threads an offer
+    const int share = n <= kRanked / 4 ? 4 : n <= kRanked / 2 ? 2 : 1, mine = threadIdx.x / share;
+    int rank = 0;
+    if (mine < n) {
+        const key_t64 order = orders[mine];
+        const uint64_t place = places[mine];
+#pragma unroll 8
+        for (int i = threadIdx.x % share; i < n; i += share) {
+            const key_t64 other = orders[i];
+            rank += other > order || (other == order && places[i] < place);
+        }
+    }
+    if (share > 1) rank += __shfl_xor(rank, 1);
+    if (share > 2) rank += __shfl_xor(rank, 2);
+    if (mine >= n || threadIdx.x % share) return;
+    const int e = chosen[mine];
+    const key_t64 order = orders[mine];
     if (rank >= K) return;
     const int b = e / of_beam;
     const int64_t out = item * K + rank, row = item * A.beams + b;
