@@ -15,27 +15,26 @@ _ACT_NARROW = 256
 
 _torch = None
 _types = {}
+_FLOAT, _INT, _FLAG = [], [], []   # what lists of floats, of whole numbers and of flags are made of
+_raw_stream = _raw_device = None   # torch's own functions behind current_stream and current_device, which cost 2 of the 11 microseconds of a small call
 
 
 def _load():
     """The library, and torch (which the package does not import by itself)."""
-    global _torch
+    global _torch, _raw_stream, _raw_device
     lib = load_library()
     if _torch is None:
         import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.int8: 4})
+        _FLOAT[:], _INT[:], _FLAG[:] = [torch.float32], [torch.int32], [torch.bool, torch.uint8]
         _torch = torch
     return lib
 
 
 def _refuse(text: str):
     raise TronError(EINVAL, text)
-
-
-def _current_stream(index: int) -> int:
-    """Address of a device's current stream (without the Stream object: 2 of the 11 microseconds of a small call)."""
-    raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(index) if raw else _torch.cuda.current_stream(index).cuda_stream
 
 
 class _Call:
@@ -51,7 +50,7 @@ class _Call:
         self.index = first.get_device()
         self.stream = stream
         if stream is None:
-            self.address = _current_stream(self.index)
+            self.address = _raw_stream(self.index)
         else:
             self.address = stream if isinstance(stream, int) else stream.cuda_stream
 
@@ -110,7 +109,7 @@ class _Call:
         return t, t.data_ptr(), needed
 
     def run(self, function, *args):
-        if _torch.cuda.current_device() == self.index:
+        if _raw_device() == self.index:
             _check(function(*args))
         else:
             with _torch.cuda.device(self.device):
@@ -287,7 +286,7 @@ def _entries(call, t, what, shape, dtypes):
         return None
     if t.get_device() != call.index:
         _refuse(f"{call.name}: {what} is on {t.device}, other arguments on {call.device}")
-    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or t.dtype not in dtypes or not t.is_contiguous():
         _refuse(f"{call.name}: {what} has to be {' x '.join(map(str, shape))} contiguous values of {' or '.join(map(str, dtypes))}")
     return t.data_ptr()
 
@@ -307,12 +306,11 @@ def tron_beam_select(z, score, next_score, parent, token, ended=None, end=-1, ne
     (batch, beams), picks = score.shape, next_score.shape[1]
     if rows != batch * beams:
         _refuse(f"tron_beam_select: z has {rows} rows, score {batch} x {beams}")
-    flags = (_torch.bool, _torch.uint8)
     space, wp, wb = call.work(work, lib.tron_beam_select_work(batch, beams, V, picks))
-    call.run(lib.tron_beam_select, batch, beams, V, call.type(z, "z"), zp, ldz, _entries(call, score, "score", (batch, beams), (_torch.float32,)),
-             _entries(call, ended, "ended", (batch, beams), flags), end, picks, _entries(call, next_score, "next_score", (batch, picks), (_torch.float32,)),
-             _entries(call, parent, "parent", (batch, picks), (_torch.int32,)), _entries(call, token, "token", (batch, picks), (_torch.int32,)),
-             _entries(call, next_ended, "next_ended", (batch, picks), flags), wp, wb, call.address)
+    call.run(lib.tron_beam_select, batch, beams, V, call.type(z, "z"), zp, ldz, _entries(call, score, "score", (batch, beams), _FLOAT),
+             _entries(call, ended, "ended", (batch, beams), _FLAG), end, picks, _entries(call, next_score, "next_score", (batch, picks), _FLOAT),
+             _entries(call, parent, "parent", (batch, picks), _INT), _entries(call, token, "token", (batch, picks), _INT),
+             _entries(call, next_ended, "next_ended", (batch, picks), _FLAG), wp, wb, call.address)
 
 
 def tron_beam_reorder(rows, states, out, lengths=None, stream=None) -> None:
@@ -330,18 +328,18 @@ def tron_beam_reorder(rows, states, out, lengths=None, stream=None) -> None:
     if out.shape[1] != batch * per:
         _refuse(f"tron_beam_reorder: out has {out.shape[1]} rows, expected {batch * per}")
     layers, rows_in, positions = states.shape[:3]
-    size = states.element_size()
-    step = size
+    size = step = states.element_size()
     for n in states.shape[3:]:
         step *= n
-    place = 1
-    for i in range(states.dim() - 1, 1, -1):
-        for t, what in ((states, "states"), (out, "out")):
-            if t.shape[i] > 1 and t.stride(i) != place:
-                _refuse(f"tron_beam_reorder: the positions of a row of {what} are not contiguous")
-        place *= max(1, states.shape[i])
-    call.run(lib.tron_beam_reorder, layers, batch, per, ip, ldrows, rows_in, states.data_ptr(), states.stride(0) * size, states.stride(1) * size, out.data_ptr(),
-             out.stride(0) * size, out.stride(1) * size, positions, step, _entries(call, lengths, "lengths", (rows_in,), (_torch.int32,)), call.address)
+    if not (states.is_contiguous() and out.is_contiguous()):
+        place = 1
+        for i in range(states.dim() - 1, 1, -1):
+            if states.shape[i] > 1 and not states.stride(i) == out.stride(i) == place:
+                _refuse("tron_beam_reorder: the positions of a row of states or out are not contiguous")
+            place *= max(1, states.shape[i])
+    (src_layer, src_row), (dst_layer, dst_row) = states.stride()[:2], out.stride()[:2]
+    call.run(lib.tron_beam_reorder, layers, batch, per, ip, ldrows, rows_in, states.data_ptr(), src_layer * size, src_row * size, out.data_ptr(),
+             dst_layer * size, dst_row * size, positions, step, _entries(call, lengths, "lengths", (rows_in,), _INT), call.address)
 
 
 def _ids(call, ids):
