@@ -29,6 +29,65 @@ struct Moments {
     float mean, rest, rstd;   // c = (s - mean) - rest
 };
 
+// A thread's chunk of eight columns of a row of d.  The last one ends with the row: it begins in the chunk before, and its first `skip` elements are
+// that one's.  Both compute and store them, with the same bits; sums leave them out.  (A last chunk that is shorter takes loads and stores of its
+// own, by which the whole wavefront waits twice: 30011 x 1023 f16 31.8 us, x 1024 22.2 us.)  Rows of fewer than eight columns are one short chunk.
+struct Chunk {
+    int at, skip, end;
+    bool there;
+    __device__ __forceinline__ Chunk(int number, int d)
+    {
+        const int j = number * kVec;
+        there = j < d;
+        at = j + kVec <= d || d < kVec ? j : d - kVec;
+        skip = there ? j - at : kVec;
+        end = d < kVec ? d : kVec;
+    }
+    __device__ __forceinline__ bool counts(int i) const { return i >= skip && i < end; }
+    template <typename T>
+    __device__ __forceinline__ Eight<T> of(const T *row) const
+    {
+        Eight<T> e;
+        e.set(end == kVec ? load8(row + at) : load_first(row + at, end, static_cast<T>(0.f)));
+        return e;
+    }
+    __device__ __forceinline__ void factors(float *f, const float *p, float none) const
+    {
+        if (!p) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) f[i] = none;
+            return;
+        }
+        const Eight<float> e = of(p);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) f[i] = e.at(i);
+    }
+    template <typename O, bool PAST>
+    __device__ __forceinline__ void put(O *row, const float *v) const
+    {
+        store8_of<O, PAST>(row + at, v, end);
+    }
+};
+
+// f(value, whether it counts) for a thread's values of a row; all of them count where a row is whole chunks
+template <int CH, typename V, typename F>
+__device__ __forceinline__ void for_each(const V (&s)[CH][kVec], int me, int team, int d, F f)
+{
+    if (d % kVec == 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) f(s[c][i]);   // 0 where there is no chunk
+    } else {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const Chunk k(me + c * team, d);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) f(k.counts(i) ? s[c][i] : 0.f);
+        }
+    }
+}
+
 // CH chunks of eight elements a thread; WAVE: a wavefront a row, otherwise a workgroup
 template <typename T, typename O, int CH, bool WAVE, bool PAST>
 __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(LayerArgs A)
@@ -39,44 +98,36 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
     const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     const int64_t row = WAVE ? block_number() * kWaveRows + threadIdx.x / kWave : block_number();
     if (row >= A.m) return;
-    const int64_t d = A.d;
-    const Elements<T> x{static_cast<const T *>(A.x) + row * A.ldx, d};
+    const int d = (int)A.d;
+    const T *x = static_cast<const T *>(A.x) + row * A.ldx, *r = static_cast<const T *>(A.residual) + (A.residual ? row * A.ldr : 0);
     float s[CH][kVec];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int64_t j = (int64_t)(me + c * team) * kVec;
-        if (j < d) {
-            const Raw8<T> v = x.at(j);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) s[c][i] = static_cast<float>(v.v[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) s[c][i] = 0.f;
-        }
-    }
-    if (A.residual) {
-        const Elements<T> r{static_cast<const T *>(A.residual) + row * A.ldr, d};
+    float sum = 0.f;
+    {
+        Eight<T> raw[CH], more[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int64_t j = (int64_t)(me + c * team) * kVec;
-            if (j < d) {
-                const Raw8<T> v = r.at(j);
+            const Chunk k(me + c * team, d);
+            if (!k.there) continue;
+            raw[c] = k.of(x);
+            if (A.residual) more[c] = k.of(r);
+        }
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) s[c][i] += static_cast<float>(v.v[i]);
+        for (int c = 0; c < CH; ++c) {
+            const Chunk k(me + c * team, d);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                s[c][i] = k.there ? raw[c].at(i) : 0.f;
+                if (A.residual && k.there) s[c][i] += more[c].at(i);
             }
         }
     }
-    float sum = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) sum += s[c][i];
+    for_each<CH>(s, me, team, d, [&](float v) { sum += v; });
     if (A.total) {
         T *t = static_cast<T *>(A.total) + row * A.ldt;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int64_t j = (int64_t)(me + c * team) * kVec;
-            if (j < d) store8_of<T, PAST>(t + j, s[c], d - j);
+            const Chunk k(me + c * team, d);
+            if (k.there) k.put<T, PAST>(t, s[c]);
         }
     }
     Moments M;
@@ -84,25 +135,20 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
     M.mean = sum * (float)A.inv_d;
     if (!(fabsf(sum) <= kMostSquares)) {   // more than 32 bits hold, or no number
         double wide = 0.0;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) wide += (double)s[c][i];
+        for_each<CH>(s, me, team, d, [&](float v) { wide += (double)v; });
         M.mean = (float)((WAVE ? wave_sum(wide) : block_sum_all(wide, wide_room)) * A.inv_d);
     }
-    float own = 0.f;
+    float left = 0.f, sum2 = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        // columns behind the row's end stay 0
-        const int64_t n = d - (int64_t)(me + c * team) * kVec;
+        const bool there = (me + c * team) * kVec < d;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            s[c][i] = i < n ? s[c][i] - M.mean : 0.f;
-            own += s[c][i];
-        }
+        for (int i = 0; i < kVec; ++i) s[c][i] = there ? s[c][i] - M.mean : 0.f;
     }
-    const double own2 = squares(s);
-    float left = own, sum2 = (float)own2;
+    for_each<CH>(s, me, team, d, [&](float v) {
+        left += v;
+        sum2 = fmaf(v, v, sum2);
+    });
     if (WAVE) {
         left = wave_sumf(left);
         sum2 = wave_sumf(sum2);
@@ -113,14 +159,14 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
         const float inv_d = (float)A.inv_d;
         M.rest = left * inv_d;
         M.rstd = 1.f / sqrtf(fmaxf((sum2 - left * M.rest) * inv_d, 0.f) + (float)A.eps);
-    } else {
-        double wide = 0.0;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) wide += (double)s[c][i];
-        const double l = WAVE ? wave_sum(wide) : block_sum_all(wide, wide_room + kMostWaves);
-        const double l2 = WAVE ? wave_sum(own2) : block_sum_all(own2, wide_room + 2 * kMostWaves);
+    } else {   // in 64 bits where 32 have lost the range
+        double l = 0.0, l2 = 0.0;
+        for_each<CH>(s, me, team, d, [&](float v) {
+            l += (double)v;
+            l2 = fma((double)v, (double)v, l2);
+        });
+        l = WAVE ? wave_sum(l) : block_sum_all(l, wide_room + kMostWaves);
+        l2 = WAVE ? wave_sum(l2) : block_sum_all(l2, wide_room + 2 * kMostWaves);
         M.rest = (float)(l * A.inv_d);
         const double variance = (l2 - l * (l * A.inv_d)) * A.inv_d;
         M.rstd = (float)(1.0 / sqrt((variance < 0.0 ? 0.0 : variance) + A.eps));   // NaN stays NaN
@@ -129,22 +175,20 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
     float top = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int64_t j = (int64_t)(me + c * team) * kVec;
-        if (j < d) {
-            float g[kVec], b[kVec];
-            gain8(g, A.gain, j, d);
-            gain8(b, A.shift, j, d, 0.f);
+        const Chunk k(me + c * team, d);
+        if (!k.there) continue;
+        float g[kVec], b[kVec];
+        k.factors(g, A.gain, 1.f);
+        k.factors(b, A.shift, 0.f);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                s[c][i] = fmaf((s[c][i] - M.rest) * M.rstd, g[i], b[i]);
-                if (kEight && i < d - j) top = larger<kWhole>(top, fabsf(s[c][i]));
-            }
+        for (int i = 0; i < kVec; ++i) {
+            s[c][i] = fmaf((s[c][i] - M.rest) * M.rstd, g[i], b[i]);
+            if (kEight && i < k.end) top = larger<kWhole>(top, fabsf(s[c][i]));
         }
     }
     float scale = 1.f, per_scale = 1.f;
     if (kEight) {
-        if (kWhole) top = WAVE ? wave_top<true>(top) : block_top<true>(top, room + 3 * kMostWaves);
-        else top = WAVE ? wave_top<false>(top) : block_top<false>(top, room + 3 * kMostWaves);
+        top = WAVE ? wave_top<kWhole>(top) : block_top<kWhole>(top, room + 3 * kMostWaves);
         scale = scale_for<O>(top);
         per_scale = 1.f / scale;
     }
@@ -156,14 +200,13 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
     O *y = static_cast<O *>(A.y) + row * A.ldy;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int64_t j = (int64_t)(me + c * team) * kVec;
-        if (j < d) {
-            if (kEight) {
+        const Chunk k(me + c * team, d);
+        if (!k.there) continue;
+        if (kEight) {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) s[c][i] *= per_scale;
-            }
-            store8_of<O, PAST>(y + j, s[c], d - j);
+            for (int i = 0; i < kVec; ++i) s[c][i] *= per_scale;
         }
+        k.put<O, PAST>(y, s[c]);
     }
 }
 
@@ -256,107 +299,94 @@ struct LayerGradArgs {
     float inv_d;
 };
 
-// Teams (wavefronts or workgroups) keep their columns' shares of dgain and dshift in registers, and take two rows at a time where a thread holds one
-// chunk of a row: one barrier and one wait for memory serve both.
+// What a thread holds of a row
+template <typename T, int CH>
+struct HeldRow {
+    Eight<T> s[CH], dy[CH], dt[CH];
+    float mean, rstd;
+    __device__ __forceinline__ void load(const LayerGradArgs &A, int64_t row, int me, int team)
+    {
+        const T *sp = static_cast<const T *>(A.total) + row * A.lds, *dyp = static_cast<const T *>(A.dy) + row * A.lddy;
+        const T *dtp = static_cast<const T *>(A.dtotal) + (A.dtotal ? row * A.lddt : 0);
+        mean = A.mean[row];
+        rstd = A.rstd[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const Chunk k(me + c * team, (int)A.d);
+            s[c] = dy[c] = Eight<T>{};
+            if (!k.there) continue;
+            s[c] = k.of(sp);
+            dy[c] = k.of(dyp);
+            if (A.dtotal) dt[c] = k.of(dtp);
+        }
+    }
+};
+
+// Teams (wavefronts or workgroups) keep their columns' shares of dgain and dshift in registers.  Two rows at a time, or the next row under way while one is
+// summed, take registers that other teams' loads need more (40011 x 512 f16 43.5 and 32.1 us instead of 32.6, 16384 x 4096 102 and 98 us instead of 97).
 template <typename T, int CH, bool WAVE, bool PAST>
 __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm_grad(LayerGradArgs A)
 {
-    constexpr int kRows = CH == 1 ? 2 : 1;
-    __shared__ float room[2][2 * kRows][kMostWaves];
+    constexpr int kWords = sizeof(Eight<T>) / 4;
+    __shared__ float room[2][2 * kMostWaves];
     const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     const int64_t teams = WAVE ? (int64_t)gridDim.x * kWaveRows : gridDim.x;
     const int64_t first = WAVE ? (int64_t)blockIdx.x * kWaveRows + threadIdx.x / kWave : blockIdx.x;
-    const int64_t d = A.d;
+    const int d = (int)A.d;
     float g[CH][kVec], dg[CH][kVec], db[CH][kVec];
+    uint32_t counted[CH][kWords];   // ones where a chunk's elements count: sums take dy with zeros elsewhere
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int64_t j = (int64_t)(me + c * team) * kVec;
+        const Chunk k(me + c * team, d);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) g[c][i] = dg[c][i] = db[c][i] = 0.f;
-        if (j < d) gain8(g[c], A.gain, j, d);
+        if (k.there) k.factors(g[c], A.gain, 1.f);
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            if (sizeof(T) == 4) counted[c][w] = k.counts(w) ? ~0u : 0;
+            else counted[c][w] = (k.counts(2 * w) ? 0xffffu : 0) | (k.counts(2 * w + 1) ? 0xffff0000u : 0);
+        }
     }
     int turn = 0;
-    for (int64_t row0 = first; row0 < A.m; row0 += kRows * teams, turn ^= 1) {
-        Raw8<T> s[kRows][CH], dy[kRows][CH], dt[kRows][CH];
-        float mean[kRows], rstd[kRows], along[kRows], level[kRows];
+    for (int64_t row = first; row < A.m; row += teams, turn ^= 1) {
+        HeldRow<T, CH> now;
+        now.load(A, row, me, team);
+        float along = 0.f, level = 0.f;
 #pragma unroll
-        for (int q = 0; q < kRows; ++q) {
-            const int64_t row = row0 + q * teams;
-            const bool there = row < A.m;
-            const Elements<T> sv{static_cast<const T *>(A.total) + row * A.lds, d}, dyv{static_cast<const T *>(A.dy) + row * A.lddy, d};
-            const Elements<T> dtv{static_cast<const T *>(A.dtotal) + (A.dtotal ? row * A.lddt : 0), d};
-            mean[q] = there ? A.mean[row] : 0.f;
-            rstd[q] = there ? A.rstd[row] : 0.f;
+        for (int c = 0; c < CH; ++c) {
+            Eight<T> own;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int64_t j = (int64_t)(me + c * team) * kVec;
-                if (there && j < d) {
-                    s[q][c] = sv.at(j);
-                    dy[q][c] = dyv.at(j);
-                    if (A.dtotal) dt[q][c] = dtv.at(j);
-                } else {
+            for (int w = 0; w < kWords; ++w) own.w[w] = now.dy[c].w[w] & counted[c][w];
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) s[q][c].v[i] = dy[q][c].v[i] = static_cast<T>(0.f);
-                }
+            for (int i = 0; i < kVec; ++i) {
+                const float u = own.at(i), h = (now.s[c].at(i) - now.mean) * now.rstd, uh = u * h;
+                along = fmaf(uh, g[c][i], along);
+                level = fmaf(u, g[c][i], level);
+                dg[c][i] += uh;
+                db[c][i] += u;
             }
         }
-#pragma unroll
-        for (int q = 0; q < kRows; ++q) {
-            along[q] = level[q] = 0.f;
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    // behind the row's end dy is 0
-                    const float u = static_cast<float>(dy[q][c].v[i]), a = u * g[c][i], h = (static_cast<float>(s[q][c].v[i]) - mean[q]) * rstd[q];
-                    along[q] = fmaf(a, h, along[q]);
-                    level[q] += a;
-                    dg[c][i] = fmaf(u, h, dg[c][i]);
-                    db[c][i] += u;
-                }
-            along[q] = wave_sumf(along[q]);
-            level[q] = wave_sumf(level[q]);
+        // two rooms in turn: who writes the next row's sums has passed the barrier behind which the last ones of this room were read
+        if (WAVE) {
+            along = wave_sumf(along);
+            level = wave_sumf(level);
+        } else {
+            block_sum_two(along, level, room[turn]);
         }
-        if (!WAVE) {
-            // two rooms in turn: who writes the next rows' sums has passed the barrier behind which the last ones of this room were read
-            const int waves = blockDim.x / kWave;
-            if (threadIdx.x % kWave == 0) {
+        const float a_mean = level * A.inv_d, back = along * A.inv_d;
+        T *dx = static_cast<T *>(A.dx) + row * A.lddx;
 #pragma unroll
-                for (int q = 0; q < kRows; ++q) {
-                    room[turn][q][threadIdx.x / kWave] = along[q];
-                    room[turn][kRows + q][threadIdx.x / kWave] = level[q];
-                }
+        for (int c = 0; c < CH; ++c) {
+            const Chunk k(me + c * team, d);
+            if (!k.there) continue;
+            float v[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const float h = (now.s[c].at(i) - now.mean) * now.rstd;
+                v[i] = now.rstd * fmaf(-h, back, fmaf(now.dy[c].at(i), g[c][i], -a_mean));
+                if (A.dtotal) v[i] += now.dt[c].at(i);
             }
-            __syncthreads();
-#pragma unroll
-            for (int q = 0; q < kRows; ++q) {
-                along[q] = level[q] = 0.f;
-                for (int w = 0; w < waves; ++w) {
-                    along[q] += room[turn][q][w];
-                    level[q] += room[turn][kRows + q][w];
-                }
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < kRows; ++q) {
-            const int64_t row = row0 + q * teams;
-            if (row >= A.m) break;
-            const float a_mean = level[q] * A.inv_d, back = along[q] * A.inv_d;
-            T *dx = static_cast<T *>(A.dx) + row * A.lddx;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int64_t j = (int64_t)(me + c * team) * kVec;
-                if (j < d) {
-                    float v[kVec];
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) {
-                        const float h = (static_cast<float>(s[q][c].v[i]) - mean[q]) * rstd[q];
-                        v[i] = rstd[q] * (fmaf(static_cast<float>(dy[q][c].v[i]), g[c][i], -a_mean) - h * back);
-                        if (A.dtotal) v[i] += static_cast<float>(dt[q][c].v[i]);
-                    }
-                    store8_of<T, PAST>(dx + j, v, d - j);
-                }
-            }
+            k.put<T, PAST>(dx, v);
         }
     }
     auto shares = [&](float *to, float (&mine)[CH][kVec]) {
@@ -367,8 +397,12 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm_
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 __syncthreads();
+                const Chunk k0(me + c * team, d);
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) join[wave][me * kVec + i] = mine[c][i];
+                for (int i = 0; i < kVec; ++i) {   // what a chunk skips is the chunk's before, and stays there
+                    const int column = k0.at + i - c * kWave * kVec;
+                    if (k0.counts(i)) join[wave][column] = mine[c][i];
+                }
                 __syncthreads();
                 for (int k = threadIdx.x; k < kWave * kVec; k += kWaveRows * kWave) {
                     const int64_t j = (int64_t)c * kWave * kVec + k;
@@ -383,8 +417,15 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm_
             float *p = to + first * d;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int64_t j = (int64_t)(me + c * team) * kVec;
-                if (j < d) store8_of<float>(p + j, mine[c], d - j);
+                const Chunk k(me + c * team, d);
+                if (!k.there) continue;
+                if (k.skip == 0) {
+                    k.put<float, false>(p, mine[c]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i)
+                        if (k.counts(i)) p[k.at + i] = mine[c][i];
+                }
             }
         }
     };
@@ -477,14 +518,14 @@ int layer_typed(const LayerArgs &A, int out_type, hipStream_t st)
 }
 
 // Columns up to which a wavefront of the gradient holds its rows, and above which rows are read twice
-constexpr int64_t kGradNarrow = 1024;
+constexpr int64_t kGradNarrow = 512;
 constexpr int64_t kGradWide = 16384;
 
 // workgroups of the gradient, each with a share of dgain and of dshift
 int64_t layer_shares(int64_t m, int64_t d)
 {
     if (d <= kGradNarrow) return std::min<int64_t>(ceil_div(m, kWaveRows), 1024);
-    return std::min<int64_t>(m, d <= 2048 ? 1024 : d <= kGradWide ? 512 : 64);
+    return std::min<int64_t>(m, d <= 1024 ? 2048 : d <= 2048 ? 1024 : d <= kGradWide ? 512 : 64);
 }
 
 template <typename T, bool PAST>
@@ -493,8 +534,7 @@ int layer_grad_typed(const LayerGradArgs &A, float *dgain, float *dshift, const 
     const int64_t d = A.d;
     const unsigned shares = (unsigned)layer_shares(A.m, d);
     if (d <= kGradNarrow) {
-        if (d <= 512) k_layer_norm_grad<T, 1, true, PAST><<<shares, kWaveRows * kWave, 0, st>>>(A);
-        else k_layer_norm_grad<T, 2, true, PAST><<<shares, kWaveRows * kWave, 0, st>>>(A);
+        k_layer_norm_grad<T, 1, true, PAST><<<shares, kWaveRows * kWave, 0, st>>>(A);
     } else if (d <= 8192) {
         k_layer_norm_grad<T, 1, false, PAST><<<shares, row_threads(d, 1), 0, st>>>(A);
     } else if (d <= kGradWide) {

@@ -33,6 +33,19 @@ struct Raw8 {
     T v[kVec];
 };
 
+// The same in whole registers: elements of 16 bits that are copied from one place to another take a register each
+template <typename T>
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void set(const Raw8<T> &r) { __builtin_memcpy(w, &r, sizeof(w)); }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (__is_same(T, __bf16)) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else return static_cast<float>(__builtin_bit_cast(_Float16, (uint16_t)(i % 2 ? w[i / 2] >> 16 : w[i / 2])));
+    }
+};
+
 template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T *p)
 {
