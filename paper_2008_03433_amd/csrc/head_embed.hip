@@ -285,41 +285,61 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
     }
 }
 
-// Tokens of several tiles: the tile in which one begins adds the shares of those that follow, in their order
+// Tokens of several tiles: the workgroup of the tile in which one begins adds the shares of those that follow.  Its wavefronts have a range of them each, four
+// loads ahead, and their sums are added in their order; a token that is everywhere is thousands of tiles' (65536 x 1024 f32, half of them one token: 524 us by
+// one wavefront).
+constexpr int kJoinWaves = 8;
+
 template <typename O, bool PAST>
-__global__ __launch_bounds__(kBlock) void k_embed_join(EmbedGradArgs A)
+__global__ __launch_bounds__(kJoinWaves *kWave) void k_embed_join(EmbedGradArgs A)
 {
-    const int64_t unit = block_number() * kWavesPerBlock + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    __shared__ float room[kJoinWaves - 1][kVec][kWave];
+    const int64_t unit = block_number();
     if (unit >= A.tile_units) return;
-    const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + threadIdx.x % kWave * kVec;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
     const int64_t count = A.S.start[A.V], begin = t * A.tile, end = begin + A.tile;
-    if (end >= count || j >= A.d) return;
+    if (end >= count) return;
     const int v = A.S.key[end - 1];
     if (A.S.key[end] != v || A.S.start[v] < begin) return;
+    const int64_t last = (A.S.start[v + 1] - 1) / A.tile, each = (last - t + kJoinWaves - 1) / kJoinWaves;
+    const int64_t from = t + 1 + wave * each, to = from + each < last + 1 ? from + each : last + 1;
     float sum[kVec];
-    auto take = [&](const float *p, float *to) {
-        const Raw8<float> r = load_row8(p, j, A.d, 0.f);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) to[e] = r.v[e];
-    };
-    take(A.shares + (2 * t + 1) * A.d, sum);
-    const int64_t last = (A.S.start[v + 1] - 1) / A.tile;
-    int64_t u = t + 1;
-    for (; u + 3 <= last; u += 4) {
-        float four[4][kVec];
+    for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+    if (j < A.d) {
+        auto take = [&](const float *p, float *into) {
+            const Raw8<float> r = load_row8(p, j, A.d, 0.f);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) take(A.shares + 2 * (u + q) * A.d, four[q]);
+            for (int e = 0; e < kVec; ++e) into[e] = r.v[e];
+        };
+        if (wave == 0) take(A.shares + (2 * t + 1) * A.d, sum);
+        int64_t u = from;
+        for (; u + 3 < to; u += 4) {
+            float four[4][kVec];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q) take(A.shares + 2 * (u + q) * A.d, four[q]);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) sum[e] += four[q][e];
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) sum[e] += four[q][e];
+        }
+        for (; u < to; ++u) {
+            float one[kVec];
+            take(A.shares + 2 * u * A.d, one);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[e] += one[e];
+        }
     }
-    for (; u <= last; ++u) {
-        float one[kVec];
-        take(A.shares + 2 * u * A.d, one);
+    if (wave) {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sum[e] += one[e];
+        for (int e = 0; e < kVec; ++e) room[wave - 1][e][lane] = sum[e];
     }
+    __syncthreads();
+    if (wave || j >= A.d) return;
+    for (int w = 0; w < kJoinWaves - 1; ++w)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] += room[w][e][lane];
     put_row<O, PAST>(A, v, j, sum);
 }
 
@@ -340,11 +360,11 @@ void embed_typed(const EmbedArgs &A, int out, hipStream_t st)
     else embed_launch<T, _Float16>(A, st);
 }
 
-// Places of a tile: tiles of 512 columns for some 32 wavefronts a compute unit, of 16 places at least and of 512 at most
+// Places of a tile: tiles of 512 columns for some 16 wavefronts a compute unit, of 16 places at least and of 512 at most
 int tile_of_places(int64_t m, int64_t d)
 {
     int tile = 16;
-    while (tile < 512 && ceil_div(m, tile) * ceil_div(d, kColumns) > 8192) tile *= 2;
+    while (tile < 512 && ceil_div(m, tile) * ceil_div(d, kColumns) > 4096) tile *= 2;
     return tile;
 }
 
@@ -374,7 +394,7 @@ int embed_grad_launch(const EmbedGradArgs &A, hipStream_t st)
     const int64_t units = A.tile_units + (A.add ? 0 : A.V);
     if (units) k_embed_sums<T, O, PAST><<<block_grid(ceil_div(units, kWavesPerBlock)), kBlock, 0, st>>>(A);
     TRON_HIP(hipGetLastError());
-    if (A.tiles > 1) k_embed_join<O, PAST><<<block_grid(ceil_div(A.tile_units, kWavesPerBlock)), kBlock, 0, st>>>(A);
+    if (A.tiles > 1) k_embed_join<O, PAST><<<block_grid(A.tile_units), kJoinWaves * kWave, 0, st>>>(A);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }
