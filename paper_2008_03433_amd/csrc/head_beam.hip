@@ -353,8 +353,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     __shared__ int kind[kMostBeams];
     __shared__ unsigned digits[256];
     __shared__ int found[2], survivors, chosen[kRanked];
-    __shared__ key_t64 orders[kRanked];
-    __shared__ uint64_t places[kRanked];
+    __shared__ key_t64 orders[kRanked + 32];   // 0 behind the last one
+    __shared__ uint64_t places[kRanked + 32];
     const int64_t item = block_number();
     if (item >= A.batch) return;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
@@ -458,9 +458,9 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     }
     __syncthreads();
     const int n = survivors;
-    if ((int)threadIdx.x < n) {
-        orders[threadIdx.x] = O.order[chosen[threadIdx.x]];
-        places[threadIdx.x] = O.place(chosen[threadIdx.x]);
+    for (int i = threadIdx.x; i < kRanked + 32; i += kPickThreads) {
+        orders[i] = i < n ? O.order[chosen[i]] : 0;
+        places[i] = i < n ? O.place(chosen[i]) : 0;
     }
     __syncthreads();
     // one, two or four threads an offer
@@ -469,10 +469,16 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     if (mine < n) {
         const key_t64 order = orders[mine];
         const uint64_t place = places[mine];
-#pragma unroll 8
-        for (int i = threadIdx.x % share; i < n; i += share) {
-            const key_t64 other = orders[i];
-            rank += other > order || (other == order && places[i] < place);
+        for (int i = threadIdx.x % share; i < n; i += 8 * share) {   // eight at a time are under way from LDS
+            key_t64 other[8];
+            uint64_t at[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                other[k] = orders[i + k * share];
+                at[k] = places[i + k * share];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) rank += other[k] > order || (other[k] == order && at[k] < place);
         }
     }
     if (share > 1) rank += __shfl_xor(rank, 1);
