@@ -83,44 +83,56 @@ constexpr int kSortWaves = 16;
 constexpr int kMostIds = 1024;    // of a workgroup: counts of each for every wavefront lie in LDS
 
 struct Sorted {
-    int32_t *start;    // [V + 1]: first place of a token among the sorted ones
+    int32_t *start, *stop; // [V]: first place of a token among the sorted ones, and the first behind it
+    int32_t *count;        // places
     int32_t *key, *from;   // [m]: token and row of dy of a place
 };
 
-// A workgroup has `each` tokens of the table and reads all m ids: it counts those before its own, and its own by wavefront; each wavefront has a
-// contiguous range of the ids, and puts its places in their order behind those of the wavefronts before it.
-__global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int64_t m, int64_t V, int each, Sorted S)
+// Of 2^shift workgroups, number g has the tokens g, g + 2^shift, ... of the table, so that neighbouring ones, which vocabularies sort by frequency, are many
+// workgroups' (32768 tokens of 128000 by a cubic law 28 us in ranges).  It reads all m ids, counts those of the workgroups before it and its own by
+// wavefront; each wavefront has a contiguous range of the ids, and puts its places in their order behind those of the wavefronts before it.
+template <typename Id>
+__global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids, int64_t m, int64_t V, int shift, Sorted S)
 {
     __shared__ int counts[kSortWaves][kMostIds];
     __shared__ int totals[2][kSortWaves];
     __shared__ uint8_t marks[kSortWaves][kMostIds];
-    const int64_t low = block_number() * each;
-    if (low >= V) return;
-    const int here = (int)(V - low < each ? V - low : each);
+    const int64_t group = block_number(), below = (int64_t)1 << shift;
+    if (group >= below) return;
+    const int here = (int)((V - group + below - 1) >> shift);   // tokens; at most kMostIds
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     if ((int)threadIdx.x < here) {
         for (int w = 0; w < kSortWaves; ++w) counts[w][threadIdx.x] = 0;
     }
     __syncthreads();
+    // ids in 32 bits, the highest one for what is no token: V is less than 2^31
+    constexpr uint32_t kNone = ~0u;
+    auto token_at = [&](int64_t i, int64_t end) {   // without a branch, so that several are under way
+        const Id id = ids[i < end ? i : end - 1];
+        return i >= end || (sizeof(Id) == 8 && (uint64_t)id >> 32) ? kNone : (uint32_t)id;
+    };
+    const uint32_t tokens = (uint32_t)V, mask = (uint32_t)below - 1, mine_of = (uint32_t)group;
     const int64_t share = (m + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave, begin = wave * share, end = begin + share < m ? begin + share : m;
     constexpr int kAhead = 8;
     int before = 0;
     for (int64_t i0 = begin; i0 < end; i0 += kAhead * kWave) {
-        int64_t id[kAhead];
+        uint32_t id[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) id[u] = token_at(i0 + u * kWave + lane, end);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int64_t i = i0 + u * kWave + lane;
-            id[u] = i < end ? ids.at(i) : -1;
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            before += id[u] >= 0 && id[u] < low;
-            const int64_t k = id[u] - low;
-            if (k >= 0 && k < here) atomicAdd(&counts[wave][(int)k], 1);
+            const uint32_t of = id[u] & mask;
+            const uint64_t there = __ballot(id[u] < tokens), some = there & __ballot(of == mine_of);
+            before += __popcll(there & __ballot(of < mine_of));   // of the wavefront
+            if (!some) continue;
+            // the first one's token at once, as it may be most of them
+            const int k = (int)(id[u] >> shift), lead = __builtin_ctzll(some), token = __builtin_amdgcn_readlane(k, lead);
+            const uint64_t same = some & __ballot(k == token);
+            if (lane == lead) atomicAdd(&counts[wave][token], __popcll(same));
+            if ((some & ~same) >> lane & 1) atomicAdd(&counts[wave][k], 1);
         }
     }
     // places of the tokens: a thread a token
-    before = wave_scan_add(before);   // of all lanes, in the last one
     __syncthreads();
     int mine = 0;
     const int k = threadIdx.x;
@@ -138,8 +150,10 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int6
         if (w < wave) place += totals[1][w];
     }
     if (k < here) {
-        S.start[low + k] = place;
-        if (low + k == V - 1) S.start[V] = place + mine;
+        const int64_t v = ((int64_t)k << shift) + group;
+        S.start[v] = place;
+        S.stop[v] = place + mine;
+        if (group == below - 1 && k == here - 1) *S.count = place + mine;
         for (int w = 0; w < kSortWaves; ++w) {
             const int c = counts[w][k];
             counts[w][k] = place;
@@ -148,21 +162,18 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int6
     }
     __syncthreads();
     for (int64_t i0 = begin; i0 < end; i0 += kAhead * kWave) {
-        int64_t id[kAhead];
+        uint32_t id[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) id[u] = token_at(i0 + u * kWave + lane, end);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int64_t i = i0 + u * kWave + lane;
-            id[u] = i < end ? ids.at(i) : -1;
-        }
-#pragma unroll 1
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t k = id[u] - low;
-            const bool own = k >= 0 && k < here;
+            const bool own = id[u] < tokens && (id[u] & mask) == mine_of;
+            const int k = (int)(id[u] >> shift);
             uint64_t left = __ballot(own);
             if (!left) continue;
             const int64_t from = i0 + u * kWave + lane;
             auto put = [&](int to) {
-                S.key[to] = (int32_t)(low + k);
+                S.key[to] = (int32_t)id[u];
                 S.from[to] = (int32_t)from;
             };
             // Every lane writes its number to its token's mark.  Whose number is not there has a token that is there twice: these go one token after the other,
@@ -171,8 +182,8 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(Ids ids, int6
             if (own) mark[k] = (uint8_t)lane;
             uint64_t twice = __ballot(own && mark[k] != lane);
             while (twice) {
-                const int token = __builtin_amdgcn_readlane((int)k, __builtin_ctzll(twice));
-                const uint64_t same = left & __ballot((int)k == token);
+                const int token = __builtin_amdgcn_readlane(k, __builtin_ctzll(twice));
+                const uint64_t same = left & __ballot(k == token);
                 const int at = counts[wave][token];
                 if (same >> lane & 1) put(at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0)));
                 if (lane == 0) counts[wave][token] = at + __popcll(same);
@@ -223,7 +234,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
     const int lane = threadIdx.x % kWave;
     if (unit >= A.tile_units) {
         const int64_t v = unit - A.tile_units;
-        if (v >= A.V || A.add || A.S.start[v] != A.S.start[v + 1]) return;
+        if (v >= A.V || A.add || A.S.start[v] != A.S.stop[v]) return;
         // sixteen bytes a lane, side by side: whole lines from one instruction
         typedef int words __attribute__((ext_vector_type(4), aligned(2)));
         constexpr int kEach = 16 / (int)sizeof(O);
@@ -239,7 +250,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
         return;
     }
     const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
-    const int64_t count = A.S.start[A.V], begin = t * A.tile, end = begin + A.tile < count ? begin + A.tile : count;
+    const int64_t count = *A.S.count, begin = t * A.tile, end = begin + A.tile < count ? begin + A.tile : count;
     if (begin >= count) return;
     const bool enters = begin > 0 && A.S.key[begin - 1] == A.S.key[begin], leaves = end < count && A.S.key[end] == A.S.key[end - 1];
     const bool there = j < A.d;
@@ -298,11 +309,11 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void k_embed_join(EmbedGradArgs 
     if (unit >= A.tile_units) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
-    const int64_t count = A.S.start[A.V], begin = t * A.tile, end = begin + A.tile;
+    const int64_t count = *A.S.count, begin = t * A.tile, end = begin + A.tile;
     if (end >= count) return;
     const int v = A.S.key[end - 1];
     if (A.S.key[end] != v || A.S.start[v] < begin) return;
-    const int64_t last = (A.S.start[v + 1] - 1) / A.tile, each = (last - t + kJoinWaves - 1) / kJoinWaves;
+    const int64_t last = (A.S.stop[v] - 1) / A.tile, each = (last - t + kJoinWaves - 1) / kJoinWaves;
     const int64_t from = t + 1 + wave * each, to = from + each < last + 1 ? from + each : last + 1;
     float sum[kVec];
 #pragma unroll
@@ -369,7 +380,7 @@ int tile_of_places(int64_t m, int64_t d)
 }
 
 struct EmbedSpace {
-    int64_t start, key, from, shares, total;
+    int64_t start, stop, count, key, from, shares, total;
 };
 EmbedSpace embed_space(int64_t m, int64_t d, int64_t V)
 {
@@ -380,7 +391,9 @@ EmbedSpace embed_space(int64_t m, int64_t d, int64_t V)
         at += ceil_div(bytes, 256) * 256;
         return from;
     };
-    S.start = take((V + 1) * 4);
+    S.start = take(V * 4);
+    S.stop = take(V * 4);
+    S.count = take(4);
     S.key = take(m * 4);
     S.from = take(m * 4);
     S.shares = take(ceil_div(m, tile_of_places(m, d)) * 2 * d * 4);
@@ -471,11 +484,15 @@ int tron_embed_grad(int64_t m, int64_t d, int64_t V, const void *ids, int id_byt
     TRON_TRY(check_device());
     const EmbedSpace S = embed_space(m, d, V);
     char *w = static_cast<char *>(work);
-    const Sorted sorted{reinterpret_cast<int32_t *>(w + S.start), reinterpret_cast<int32_t *>(w + S.key), reinterpret_cast<int32_t *>(w + S.from)};
+    auto at = [&](int64_t offset) { return reinterpret_cast<int32_t *>(w + offset); };
+    const Sorted sorted{at(S.start), at(S.stop), at(S.count), at(S.key), at(S.from)};
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    // a workgroup a compute unit, of whom each reads all ids
-    const int each = (int)std::min<int64_t>(kMostIds, ceil_div(V, 256));
-    k_sort_tokens<<<block_grid(ceil_div(V, each)), kSortWaves * kWave, 0, st>>>(Ids{ids, id_bytes == 8}, m, V, each, sorted);
+    // a workgroup a compute unit, of whom each reads all ids, or as many as the tokens' counts need
+    int shift = 0;
+    while ((shift < 8 && (V >> shift) > 1) || (V >> shift) >= kMostIds) ++shift;
+    const dim3 groups = block_grid((int64_t)1 << shift);
+    if (id_bytes == 8) k_sort_tokens<<<groups, kSortWaves * kWave, 0, st>>>(static_cast<const int64_t *>(ids), m, V, shift, sorted);
+    else k_sort_tokens<<<groups, kSortWaves * kWave, 0, st>>>(static_cast<const int32_t *>(ids), m, V, shift, sorted);
     TRON_HIP(hipGetLastError());
     const int tile = tile_of_places(m, d);
     const int64_t across = ceil_div(d, kColumns), tiles = ceil_div(m, tile);
