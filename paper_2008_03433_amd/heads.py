@@ -388,7 +388,7 @@ class SoftmaxHead:
 
         f(W) = 1/2 W.W + C sum_i loss_i(z_i),   z = X W',   X = rms_norm(hidden + residual) gain
 
-    for hidden states (m x d, bfloat16 or float16) and a teacher's ids and t (m x K).  W is n x d float32; the products take it rounded to
+    or, with norm="layer", X = layer_norm(hidden + residual) gain + shift, for hidden states (m x d, bfloat16 or float16) and a teacher's ids and t (m x K).  W is n x d float32; the products take it rounded to
     the states' type.  fun_grad keeps the logits of its W for hv, as Dataset keeps D.
 
     hv is linear in its direction, whose size is the caller's (a gradient's, in the first product of a solve).  In float16 the products take it
@@ -396,12 +396,17 @@ class SoftmaxHead:
 
     _LARGEST = 12   # log2 of a bound on |X V'|: four bits below float16's largest value, for weights and roundings
 
-    def __init__(self, hidden, ids, t, gain=None, residual=None, eps=1e-6, temperature=1.0, weight=None):
+    def __init__(self, hidden, ids, t, gain=None, residual=None, eps=1e-6, temperature=1.0, weight=None, norm="rms", shift=None):
         _load()
+        if norm not in ("rms", "layer") or (shift is not None and norm != "layer"):
+            _refuse("SoftmaxHead: norm is 'rms' or 'layer', and the latter alone has a shift")
         self.m, self.d = hidden.shape
         self.ids, self.t, self.temperature, self.weight = ids, t, temperature, weight
         self.X = _torch.empty_like(hidden, memory_format=_torch.contiguous_format)
-        tron_rms_norm(hidden, self.X, gain=gain, eps=eps, residual=residual)
+        if norm == "layer":
+            tron_layer_norm(hidden, self.X, gain=gain, shift=shift, eps=eps, residual=residual)
+        else:
+            tron_rms_norm(hidden, self.X, gain=gain, eps=eps, residual=residual)
         self.loss = _torch.empty(self.m, dtype=_torch.float32, device=hidden.device)
         self.lse = _torch.empty_like(self.loss)
         self.z = None

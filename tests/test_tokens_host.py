@@ -1,0 +1,86 @@
+"""The operators of tokens without a GPU: argument checks at the C boundary and sizes of work spaces."""
+import ctypes
+
+import pytest
+
+import paper_2008_03433_amd as tron
+from paper_2008_03433_amd import binding
+
+P = ctypes.c_void_p(4096)   # some address: every call here is refused before it is used
+
+
+def _refused(name, *args, text=None):
+    assert getattr(tron.load_library(), name)(*args) == binding.EINVAL, (name, args)
+    assert name in tron.tron_last_error() and (text is None or text in tron.tron_last_error())
+
+
+def test_norms():
+    def call(m=4, d=8, type=0, x=P, ldx=8, out=0, y=P, ldy=8, scale=None, eps=1e-5):
+        return "tron_layer_norm", m, d, type, x, ldx, None, 0, None, None, eps, None, 0, out, y, ldy, scale, None, None, None
+    for wrong in (dict(m=-1), dict(d=0), dict(m=2 ** 31), dict(type=3), dict(type=4), dict(out=1), dict(out=3), dict(out=4), dict(out=5), dict(x=None), dict(y=None),
+                  dict(ldx=-1), dict(ldy=7), dict(ldy=2 ** 62), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf"))):
+        _refused(*call(**wrong))
+    _refused("tron_rms_norm", 4, 8, 0, P, 8, None, 0, None, 1e-6, None, 0, 4, P, 8, None, None, None, text="scale")
+
+    def grad(m=4, d=8, type=0, mean=P, rstd=P, dx=P, lddx=8, dgain=None, dshift=None, work=None, size=0):
+        return "tron_layer_norm_grad", m, d, type, P, 8, mean, rstd, None, P, 8, None, 0, dx, lddx, dgain, dshift, work, size, None
+    need = tron.tron_layer_norm_grad_work(4, 8)
+    for wrong in (dict(type=4), dict(mean=None), dict(rstd=None), dict(dx=None), dict(lddx=4), dict(m=2 ** 31)):
+        _refused(*grad(**wrong))
+    for wrong in (dict(dgain=P), dict(dshift=P), dict(dgain=P, work=P, size=need - 1), dict(dshift=P, work=ctypes.c_void_p(4104), size=need)):
+        _refused(*grad(**wrong), text="work space")
+
+
+def test_products_of_whole_numbers():
+    def call(k=8, type=4, xs=P, ws=P, out=0):
+        return "tron_linear", 4, 4, k, type, P, k, xs, P, k, ws, None, 0, None, 0, out, P, 4, None, 0, P, 1 << 30, None
+    for wrong in (dict(xs=None), dict(ws=None), dict(k=2 ** 17), dict(type=5), dict(out=4)):
+        _refused(*call(**wrong))
+    assert tron.load_library().tron_linear_work(4, 64, 2 ** 17, 4) == 0
+    assert tron.load_library().tron_linear_work(4, 64, 2 ** 17 - 1, 4) > 0
+
+
+def test_beams():
+    def call(batch=2, beams=2, V=8, type=0, z=P, ldz=8, score=P, ended=None, end=-1, picks=3, out=P, work=P, size=1 << 20):
+        return "tron_beam_select", batch, beams, V, type, z, ldz, score, ended, end, picks, out, P, P, None, work, size, None
+    for wrong in (dict(batch=-1), dict(batch=2 ** 26), dict(beams=0), dict(beams=65), dict(V=0), dict(V=2 ** 31 - 64), dict(picks=0), dict(picks=65), dict(V=1), dict(type=3),
+                  dict(type=4), dict(end=-2), dict(end=8), dict(z=None), dict(score=None), dict(out=None), dict(ended=P), dict(ldz=-1), dict(ldz=2 ** 62)):
+        _refused(*call(**wrong))
+    need = tron.tron_beam_select_work(2, 2, 8, 3)
+    for wrong in (dict(work=None), dict(size=need - 1), dict(work=ctypes.c_void_p(4100))):
+        _refused(*call(**wrong), text="work space")
+    assert need > 0 and need % 16 == 0 and tron.tron_beam_select_work(0, 2, 8, 3) == 0 and tron.tron_beam_select_work(2, 65, 8, 3) == 0
+
+    def reorder(layers=2, batch=2, per=2, rows=P, ld=2, rows_in=4, src=P, src_layer=400, src_row=100, dst=ctypes.c_void_p(8192), dst_layer=400, dst_row=100, positions=10, step=10):
+        return "tron_beam_reorder", layers, batch, per, rows, ld, rows_in, src, src_layer, src_row, dst, dst_layer, dst_row, positions, step, None, None
+    for wrong in (dict(layers=-1), dict(layers=65536), dict(batch=-1), dict(per=-1), dict(rows_in=-1), dict(positions=-1), dict(step=-1), dict(rows=None), dict(src=None),
+                  dict(dst=None), dict(ld=-1), dict(src_row=-1), dict(dst_row=99), dict(dst_layer=399), dict(dst_layer=50), dict(dst=ctypes.c_void_p(4096 + 799)),
+                  dict(dst=ctypes.c_void_p(4096 - 799)), dict(dst_row=2 ** 62), dict(positions=2 ** 40, step=2 ** 40)):
+        _refused(*reorder(**wrong))
+
+
+def test_embeddings():
+    def call(m=4, d=8, V=9, ids=P, size=8, type=0, table=P, ldt=8, scale=None, out=0, y=P, ldy=8):
+        return "tron_embed", m, d, V, ids, size, type, table, ldt, scale, 1.0, out, y, ldy, None
+    for wrong in (dict(m=-1), dict(m=2 ** 31), dict(d=0), dict(V=0), dict(V=2 ** 31 - 64), dict(size=2), dict(type=5), dict(type=3), dict(type=4), dict(scale=P), dict(out=3),
+                  dict(out=4), dict(ids=None), dict(table=None), dict(y=None), dict(ldt=-1), dict(ldy=7)):
+        _refused(*call(**wrong))
+
+    def grad(m=4, d=8, V=9, ids=P, size=8, type=0, dy=P, ld=8, out=0, table=P, ldt=8, work=P, bytes=1 << 24):
+        return "tron_embed_grad", m, d, V, ids, size, type, dy, ld, 1.0, 0, out, table, ldt, work, bytes, None
+    for wrong in (dict(m=-1), dict(d=0), dict(V=0), dict(size=1), dict(type=3), dict(type=4), dict(out=4), dict(ids=None), dict(dy=None), dict(table=None), dict(ld=-1), dict(ldt=7)):
+        _refused(*grad(**wrong))
+    need = tron.tron_embed_grad_work(4, 8, 9)
+    for wrong in (dict(work=None), dict(bytes=need - 1), dict(work=ctypes.c_void_p(4100))):
+        _refused(*grad(**wrong), text="work space")
+    assert tron.tron_embed_grad_work(-1, 8, 9) == 0 and tron.tron_embed_grad_work(0, 8, 9) > 0
+
+
+def test_tensors_on_the_host_are_refused():
+    torch = pytest.importorskip("torch")
+    x, i = torch.zeros(2, 3), torch.zeros(2, dtype=torch.int32)
+    for call, args in ((tron.tron_layer_norm, (x, x.clone())), (tron.tron_beam_select, (x, x, x, i, i)), (tron.tron_beam_reorder, (i, x[None], x[None])),
+                       (tron.tron_embed, (i, x, x.clone())), (tron.tron_embed_grad, (i, x, x.clone()))):
+        with pytest.raises(tron.TronError) as e:
+            call(*args)
+        assert "no CPU fallback" in str(e.value)
