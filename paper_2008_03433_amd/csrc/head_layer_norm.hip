@@ -12,9 +12,32 @@
 namespace tron {
 namespace {
 
-// Columns up to which a wavefront holds a row, and above which rows are read twice
+// Columns up to which sixteen lanes and a wavefront hold a row, and above which rows are read twice
+constexpr int64_t kSlim = 128;
 constexpr int64_t kNarrow = 1024;
 constexpr int64_t kWide = 32768;
+
+// Sums and maxima over a team of 16 or 64 lanes, in a fixed order; every lane has the result
+template <int TEAM, typename F>
+__device__ __forceinline__ float team_join(float v, F f)
+{
+    if (TEAM == kWave) return wave_joinf(v, f);
+    v = f(v, dpp_movef<0xB1>(v));
+    v = f(v, dpp_movef<0x4E>(v));
+    v = f(v, dpp_movef<0x141>(v));
+    return f(v, dpp_movef<0x140>(v));
+}
+template <int TEAM>
+__device__ __forceinline__ float team_sum(float v)
+{
+    return team_join<TEAM>(v, [](float a, float b) { return a + b; });
+}
+template <int TEAM>
+__device__ __forceinline__ double team_sum(double v)
+{
+    return TEAM == kWave ? wave_sum(v) : sum16(v);
+}
+constexpr int kTeamBlock = kWaveRows * kWave;   // threads of a workgroup of teams
 
 struct LayerArgs {
     const void *x, *residual;
@@ -88,15 +111,17 @@ __device__ __forceinline__ void for_each(const V (&s)[CH][kVec], int me, int tea
     }
 }
 
-// CH chunks of eight elements a thread; WAVE: a wavefront a row, otherwise a workgroup
-template <typename T, typename O, int CH, bool WAVE, bool PAST>
-__global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(LayerArgs A)
+// CH chunks of eight elements a thread; TEAM lanes a row (16: heads of a few dozen columns, 47454 x 69 bf16 by wavefronts 31 us for its gradient), 0: a
+// workgroup
+template <typename T, typename O, int CH, int TEAM, bool PAST>
+__global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm(LayerArgs A)
 {
     constexpr bool kEight = sizeof(O) == 1, kWhole = __is_same(O, whole8);
     __shared__ float room[5 * kMostWaves];
     __shared__ double wide_room[3 * kMostWaves];
-    const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
-    const int64_t row = WAVE ? block_number() * kWaveRows + threadIdx.x / kWave : block_number();
+    constexpr int kTeam = TEAM ? TEAM : kWave;
+    const int team = TEAM ? TEAM : (int)blockDim.x, me = TEAM ? (int)threadIdx.x % kTeam : (int)threadIdx.x;
+    const int64_t row = TEAM ? block_number() * (kTeamBlock / kTeam) + threadIdx.x / kTeam : block_number();
     if (row >= A.m) return;
     const int d = (int)A.d;
     const T *x = static_cast<const T *>(A.x) + row * A.ldx, *r = static_cast<const T *>(A.residual) + (A.residual ? row * A.ldr : 0);
@@ -131,12 +156,12 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
         }
     }
     Moments M;
-    sum = WAVE ? wave_sumf(sum) : block_sum_all(sum, room);
+    sum = TEAM ? team_sum<kTeam>(sum) : block_sum_all(sum, room);
     M.mean = sum * (float)A.inv_d;
     if (!(fabsf(sum) <= kMostSquares)) {   // more than 32 bits hold, or no number
         double wide = 0.0;
         for_each<CH>(s, me, team, d, [&](float v) { wide += (double)v; });
-        M.mean = (float)((WAVE ? wave_sum(wide) : block_sum_all(wide, wide_room)) * A.inv_d);
+        M.mean = (float)((TEAM ? team_sum<kTeam>(wide) : block_sum_all(wide, wide_room)) * A.inv_d);
     }
     float left = 0.f, sum2 = 0.f;
 #pragma unroll
@@ -149,9 +174,9 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
         left += v;
         sum2 = fmaf(v, v, sum2);
     });
-    if (WAVE) {
-        left = wave_sumf(left);
-        sum2 = wave_sumf(sum2);
+    if (TEAM) {
+        left = team_sum<kTeam>(left);
+        sum2 = team_sum<kTeam>(sum2);
     } else {
         block_sum_two(left, sum2, room + kMostWaves);
     }
@@ -165,8 +190,8 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
             l += (double)v;
             l2 = fma((double)v, (double)v, l2);
         });
-        l = WAVE ? wave_sum(l) : block_sum_all(l, wide_room + kMostWaves);
-        l2 = WAVE ? wave_sum(l2) : block_sum_all(l2, wide_room + 2 * kMostWaves);
+        l = TEAM ? team_sum<kTeam>(l) : block_sum_all(l, wide_room + kMostWaves);
+        l2 = TEAM ? team_sum<kTeam>(l2) : block_sum_all(l2, wide_room + 2 * kMostWaves);
         M.rest = (float)(l * A.inv_d);
         const double variance = (l2 - l * (l * A.inv_d)) * A.inv_d;
         M.rstd = (float)(1.0 / sqrt((variance < 0.0 ? 0.0 : variance) + A.eps));   // NaN stays NaN
@@ -188,7 +213,7 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm(
     }
     float scale = 1.f, per_scale = 1.f;
     if (kEight) {
-        top = WAVE ? wave_top<kWhole>(top) : block_top<kWhole>(top, room + 3 * kMostWaves);
+        top = TEAM ? team_join<kTeam>(top, [](float a, float b) { return larger<kWhole>(a, b); }) : block_top<kWhole>(top, room + 3 * kMostWaves);
         scale = scale_for<O>(top);
         per_scale = 1.f / scale;
     }
@@ -324,14 +349,15 @@ struct HeldRow {
 
 // Teams (wavefronts or workgroups) keep their columns' shares of dgain and dshift in registers.  Two rows at a time, or the next row under way while one is
 // summed, take registers that other teams' loads need more (40011 x 512 f16 43.5 and 32.1 us instead of 32.6, 16384 x 4096 102 and 98 us instead of 97).
-template <typename T, int CH, bool WAVE, bool PAST>
-__global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm_grad(LayerGradArgs A)
+template <typename T, int CH, int TEAM, bool PAST>
+__global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm_grad(LayerGradArgs A)
 {
+    constexpr int kTeam = TEAM ? TEAM : kWave, kTeams = kTeamBlock / kTeam;
     constexpr int kWords = sizeof(Eight<T>) / 4;
     __shared__ float room[2][2 * kMostWaves];
-    const int team = WAVE ? kWave : (int)blockDim.x, me = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x;
-    const int64_t teams = WAVE ? (int64_t)gridDim.x * kWaveRows : gridDim.x;
-    const int64_t first = WAVE ? (int64_t)blockIdx.x * kWaveRows + threadIdx.x / kWave : blockIdx.x;
+    const int team = TEAM ? TEAM : (int)blockDim.x, me = TEAM ? (int)threadIdx.x % kTeam : (int)threadIdx.x;
+    const int64_t teams = TEAM ? (int64_t)gridDim.x * kTeams : gridDim.x;
+    const int64_t first = TEAM ? (int64_t)blockIdx.x * kTeams + threadIdx.x / kTeam : blockIdx.x;
     const int d = (int)A.d;
     float g[CH][kVec], dg[CH][kVec], db[CH][kVec];
     uint32_t counted[CH][kWords];   // ones where a chunk's elements count: sums take dy with zeros elsewhere
@@ -367,9 +393,9 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm_
             }
         }
         // two rooms in turn: who writes the next row's sums has passed the barrier behind which the last ones of this room were read
-        if (WAVE) {
-            along = wave_sumf(along);
-            level = wave_sumf(level);
+        if (TEAM) {
+            along = team_sum<kTeam>(along);
+            level = team_sum<kTeam>(level);
         } else {
             block_sum_two(along, level, room[turn]);
         }
@@ -391,25 +417,25 @@ __global__ __launch_bounds__(WAVE ? kWaveRows * kWave : 1024) void k_layer_norm_
     }
     auto shares = [&](float *to, float (&mine)[CH][kVec]) {
         if (!to) return;
-        if (WAVE) {   // the wavefronts of a workgroup join their shares, a chunk of columns at a time
-            __shared__ float join[kWaveRows][kWave * kVec];
-            const int wave = threadIdx.x / kWave;
+        if (TEAM) {   // the teams of a workgroup join their shares, a chunk of columns at a time
+            __shared__ float join[kTeams][kTeam * kVec];
+            const int mine_of = threadIdx.x / kTeam;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 __syncthreads();
                 const Chunk k0(me + c * team, d);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {   // what a chunk skips is the chunk's before, and stays there
-                    const int column = k0.at + i - c * kWave * kVec;
-                    if (k0.counts(i)) join[wave][column] = mine[c][i];
+                    const int column = k0.at + i - c * kTeam * kVec;
+                    if (k0.counts(i)) join[mine_of][column] = mine[c][i];
                 }
                 __syncthreads();
-                for (int k = threadIdx.x; k < kWave * kVec; k += kWaveRows * kWave) {
-                    const int64_t j = (int64_t)c * kWave * kVec + k;
+                for (int k = threadIdx.x; k < kTeam * kVec; k += kTeamBlock) {
+                    const int j = c * kTeam * kVec + k;
                     if (j >= d) break;
                     float sum = 0.f;
 #pragma unroll
-                    for (int w = 0; w < kWaveRows; ++w) sum += join[w][k];
+                    for (int w = 0; w < kTeams; ++w) sum += join[w][k];
                     to[(int64_t)blockIdx.x * d + j] = sum;
                 }
             }
@@ -494,13 +520,14 @@ int layer_launch(const LayerArgs &A, hipStream_t st)
 {
     const int64_t d = A.d;
     if (d <= kNarrow) {
-        const dim3 grid = block_grid(ceil_div(A.m, kWaveRows));
-        if (d <= 512) k_layer_norm<T, O, 1, true, PAST><<<grid, kWaveRows * kWave, 0, st>>>(A);
-        else k_layer_norm<T, O, 2, true, PAST><<<grid, kWaveRows * kWave, 0, st>>>(A);
+        const dim3 grid = block_grid(ceil_div(A.m, kTeamBlock / (d <= kSlim ? 16 : kWave)));
+        if (d <= kSlim) k_layer_norm<T, O, 1, 16, PAST><<<grid, kTeamBlock, 0, st>>>(A);
+        else if (d <= 512) k_layer_norm<T, O, 1, kWave, PAST><<<grid, kTeamBlock, 0, st>>>(A);
+        else k_layer_norm<T, O, 2, kWave, PAST><<<grid, kTeamBlock, 0, st>>>(A);
     } else if (d <= 8192) {
-        k_layer_norm<T, O, 2, false, PAST><<<block_grid(A.m), row_threads(d, 2), 0, st>>>(A);
+        k_layer_norm<T, O, 2, 0, PAST><<<block_grid(A.m), row_threads(d, 2), 0, st>>>(A);
     } else if (d <= kWide) {
-        k_layer_norm<T, O, 4, false, PAST><<<block_grid(A.m), row_threads(d, 4), 0, st>>>(A);
+        k_layer_norm<T, O, 4, 0, PAST><<<block_grid(A.m), row_threads(d, 4), 0, st>>>(A);
     } else {
         k_layer_norm_wide<T, O, PAST><<<block_grid(A.m), 1024, 0, st>>>(A);
     }
@@ -524,7 +551,7 @@ constexpr int64_t kGradWide = 16384;
 // workgroups of the gradient, each with a share of dgain and of dshift
 int64_t layer_shares(int64_t m, int64_t d)
 {
-    if (d <= kGradNarrow) return std::min<int64_t>(ceil_div(m, kWaveRows), 1024);
+    if (d <= kGradNarrow) return std::min<int64_t>(ceil_div(m, kTeamBlock / (d <= kSlim ? 16 : kWave)), 1024);
     return std::min<int64_t>(m, d <= 1024 ? 2048 : d <= 2048 ? 1024 : d <= kGradWide ? 512 : 64);
 }
 
@@ -534,11 +561,12 @@ int layer_grad_typed(const LayerGradArgs &A, float *dgain, float *dshift, const 
     const int64_t d = A.d;
     const unsigned shares = (unsigned)layer_shares(A.m, d);
     if (d <= kGradNarrow) {
-        k_layer_norm_grad<T, 1, true, PAST><<<shares, kWaveRows * kWave, 0, st>>>(A);
+        if (d <= kSlim) k_layer_norm_grad<T, 1, 16, PAST><<<shares, kTeamBlock, 0, st>>>(A);
+        else k_layer_norm_grad<T, 1, kWave, PAST><<<shares, kTeamBlock, 0, st>>>(A);
     } else if (d <= 8192) {
-        k_layer_norm_grad<T, 1, false, PAST><<<shares, row_threads(d, 1), 0, st>>>(A);
+        k_layer_norm_grad<T, 1, 0, PAST><<<shares, row_threads(d, 1), 0, st>>>(A);
     } else if (d <= kGradWide) {
-        k_layer_norm_grad<T, 2, false, PAST><<<shares, row_threads(d, 2), 0, st>>>(A);
+        k_layer_norm_grad<T, 2, 0, PAST><<<shares, row_threads(d, 2), 0, st>>>(A);
     } else {
         // before dx is written, which may be dy
         if (dgain || dshift) k_layer_shares<T><<<dim3((unsigned)ceil_div(d, kBlock), shares), kBlock, 0, st>>>(A);

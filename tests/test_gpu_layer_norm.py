@@ -41,7 +41,7 @@ def _cuda(t):
 
 @pytest.mark.parametrize("out", ["same", "e4m3", "i8"])
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("m,d", NORM_SIZES)
+@pytest.mark.parametrize("m,d", NORM_SIZES + [(70, 128), (33, 127), (19, 8), (21, 6), (9, 129)])
 def test_layer_norm(m, d, kind, out):
     torch = torch_mod()
     g = _gen(7000 * m + d)
@@ -184,7 +184,7 @@ def _plain_grad(total, mean, rstd, gain, dy, dtotal):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("m,d", NORM_SIZES + [(1500, 40), (700, 1030), (41, 700), (300, 9000), (70, 17000)])
+@pytest.mark.parametrize("m,d", NORM_SIZES + [(1500, 40), (700, 128), (333, 121), (50, 8), (37, 129), (700, 1030), (41, 700), (300, 9000), (70, 17000)])
 def test_layer_norm_grad(m, d, kind):
     torch = torch_mod()
     g = _gen(11 * m + d)
