@@ -351,6 +351,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     extern __shared__ __align__(16) key_t64 room[];
     __shared__ double lse[kMostBeams];
     __shared__ int kind[kMostBeams];
+    __shared__ bool had_ended[kMostBeams];   // as next_ended may be ended
     __shared__ unsigned digits[256];
     __shared__ int found[2], survivors, chosen[kRanked];
     __shared__ key_t64 orders[kRanked + 32];   // 0 behind the last one
@@ -380,6 +381,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
             const bool possible = total > 0.0 && total < INFINITY;   // not: nothing but -inf; a NaN or +inf
             kind[b] = !(fabsf(score) < INFINITY) ? DEAD : A.ended && A.ended[row] ? OVER : possible ? LIVE : DEAD;
             lse[b] = (double)most + log(total);
+            had_ended[b] = A.ended && A.ended[row];
         }
     }
     if (threadIdx.x == 0) survivors = 0;
@@ -493,7 +495,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     A.next_score[out] = (float)of_order(order);
     A.parent[out] = (int32_t)row;
     A.token[out] = (int32_t)token;
-    if (A.next_ended) A.next_ended[out] = (A.ended && A.ended[row]) || (int64_t)token == A.end;
+    if (A.next_ended) A.next_ended[out] = had_ended[b] || (int64_t)token == A.end;
 }
 
 // ------------------------------------------------------------------ states
@@ -568,15 +570,21 @@ bool beam_sizes_ok(int64_t batch, int64_t beams, int64_t V, int64_t picks)
 template <typename T>
 void launch_offers(const BeamArgs &A, int waves, hipStream_t st)
 {
-    const int64_t rows = A.batch * A.beams, y = std::min<int64_t>(rows, 32768);
+    const int64_t rows = A.batch * A.beams, y = std::min<int64_t>(rows, 65535);
     const dim3 grid((unsigned)A.parts, (unsigned)y, (unsigned)ceil_div(rows, y));
     if (waves == 1) k_beam_offers<T, 1><<<grid, kWave, 0, st>>>(A);
     else if (waves == 4) k_beam_offers<T, 4><<<grid, 4 * kWave, 0, st>>>(A);
     else k_beam_offers<T, 8><<<grid, 8 * kWave, 0, st>>>(A);
 }
 
-// where two ranges of bytes, of layers and rows that lie `layer` and `row` apart, have their first and last byte
-bool apart(const char *a, int64_t a_bytes, const char *b, int64_t b_bytes) { return a + a_bytes <= b || b + b_bytes <= a; }
+// whether `layers` ranges of a_bytes that lie a_layer apart, and the same of b, have no byte in common: one behind the other, or side by side in each layer
+bool apart(int64_t layers, const char *a, int64_t a_layer, int64_t a_bytes, const char *b, int64_t b_layer, int64_t b_bytes)
+{
+    if (a + (layers - 1) * a_layer + a_bytes <= b || b + (layers - 1) * b_layer + b_bytes <= a) return true;
+    if (a_layer != b_layer || a_layer == 0) return false;
+    const int64_t behind = ((b - a) % a_layer + a_layer) % a_layer;
+    return behind >= a_bytes && behind + b_bytes <= a_layer;
+}
 
 }  // namespace
 }  // namespace tron
@@ -645,7 +653,7 @@ int tron_beam_reorder(int64_t layers, int64_t batch, int64_t per, const int32_t 
     // rows in layers, or layers in rows
     const bool whole = (count == 1 || dst_row >= row_bytes) &&
                        (layers == 1 || dst_layer >= out_layer || (dst_layer >= row_bytes && (count == 1 || dst_row >= (layers - 1) * dst_layer + row_bytes)));
-    if (!whole || !apart(static_cast<const char *>(src), (layers - 1) * src_layer + in_layer, static_cast<const char *>(dst), (layers - 1) * dst_layer + out_layer)) {
+    if (!whole || !apart(layers, static_cast<const char *>(src), src_layer, in_layer, static_cast<const char *>(dst), dst_layer, out_layer)) {
         set_error("tron_beam_reorder: rows that are written may overlap neither each other nor src");
         return TRON_EINVAL;
     }

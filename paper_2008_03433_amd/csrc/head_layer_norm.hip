@@ -147,14 +147,6 @@ __global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm(LayerAr
         }
     }
     for_each<CH>(s, me, team, d, [&](float v) { sum += v; });
-    if (A.total) {
-        T *t = static_cast<T *>(A.total) + row * A.ldt;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const Chunk k(me + c * team, d);
-            if (k.there) k.put<T, PAST>(t, s[c]);
-        }
-    }
     Moments M;
     sum = TEAM ? team_sum<kTeam>(sum) : block_sum_all(sum, room);
     M.mean = sum * (float)A.inv_d;
@@ -162,6 +154,15 @@ __global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm(LayerAr
         double wide = 0.0;
         for_each<CH>(s, me, team, d, [&](float v) { wide += (double)v; });
         M.mean = (float)((TEAM ? team_sum<kTeam>(wide) : block_sum_all(wide, wide_room)) * A.inv_d);
+    }
+    // behind the sum's barrier, as `total` may be x or r, of which a last chunk reads what another wavefront's thread writes
+    if (A.total) {
+        T *t = static_cast<T *>(A.total) + row * A.ldt;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const Chunk k(me + c * team, d);
+            if (k.there) k.put<T, PAST>(t, s[c]);
+        }
     }
     float left = 0.f, sum2 = 0.f;
 #pragma unroll

@@ -301,7 +301,7 @@ def tron_beam_select(z, score, next_score, parent, token, ended=None, end=-1, ne
     lib = _load()
     call = _Call("tron_beam_select", z, stream)
     zp, rows, V, ldz = call.matrix(z, "z")
-    if score.dim() != 2 or next_score.dim() != 2 or score.shape[0] != next_score.shape[0]:
+    if score is None or next_score is None or score.dim() != 2 or next_score.dim() != 2 or score.shape[0] != next_score.shape[0]:
         _refuse("tron_beam_select: score (batch x beams) and next_score (batch x picks) have 2 dimensions")
     (batch, beams), picks = score.shape, next_score.shape[1]
     if rows != batch * beams:
@@ -318,10 +318,10 @@ def tron_beam_reorder(rows, states, out, lengths=None, stream=None) -> None:
     (the parent of tron_beam_select, or its first columns).  lengths (int32, one a row of states): positions behind it are left as they were in out."""
     lib = _load()
     call = _Call("tron_beam_reorder", states, stream)
-    if rows.dtype != _torch.int32:
-        _refuse(f"tron_beam_reorder: rows are of {rows.dtype}, expected int32")
+    if rows is None or rows.dtype != _torch.int32:
+        _refuse("tron_beam_reorder: rows of int32 are needed")
     ip, batch, per, ldrows = call.matrix(rows, "rows")
-    if states.dim() < 3 or out.dim() != states.dim() or out.dtype != states.dtype or out.shape[0] != states.shape[0] or out.shape[2:] != states.shape[2:]:
+    if out is None or states.dim() < 3 or out.dim() != states.dim() or out.dtype != states.dtype or out.shape[0] != states.shape[0] or out.shape[2:] != states.shape[2:]:
         _refuse("tron_beam_reorder: states and out have to be layers x rows x positions x ... of one type, alike but for the rows")
     if out.get_device() != call.index:
         _refuse(f"tron_beam_reorder: out is on {out.device}, other arguments on {call.device}")
@@ -344,8 +344,8 @@ def tron_beam_reorder(rows, states, out, lengths=None, stream=None) -> None:
 
 def _ids(call, ids):
     """(address, count, bytes) of contiguous ids."""
-    if ids.get_device() != call.index:
-        _refuse(f"{call.name}: ids are on {ids.device}, other arguments on {call.device}")
+    if ids is None or ids.get_device() != call.index:
+        _refuse(f"{call.name}: ids are needed, on {call.device} as the other arguments")
     if ids.dtype not in (_torch.int32, _torch.int64) or ids.dim() != 1 or (ids.shape[0] > 1 and ids.stride(0) != 1):
         _refuse(f"{call.name}: ids have to be contiguous int32 or int64 values of one dimension")
     return ids.data_ptr(), ids.shape[0], 4 if ids.dtype == _torch.int32 else 8

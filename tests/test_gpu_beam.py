@@ -158,6 +158,17 @@ def test_scores_far_apart_and_rows_of_work_spaces_and_none():
     tron.tron_beam_select(z[:0].cuda(), torch.empty((0, 2), device="cuda"), *out)
 
 
+def test_the_next_beams_in_the_place_of_the_last_ones():
+    torch = torch_mod()
+    g = _gen(21)
+    z, score, ended = torch.randn(90 * 6, 3000, generator=g), -torch.rand(90, 6, generator=g), torch.rand(90, 6, generator=g) < 0.4
+    want = _check(z, score, 6, ended, 5)
+    s, e = score.cuda(), ended.cuda()
+    parent, token = torch.empty((90, 6), dtype=torch.int32, device="cuda"), torch.empty((90, 6), dtype=torch.int32, device="cuda")
+    tron.tron_beam_select(z.cuda(), s, s, parent, token, ended=e, end=5, next_ended=e)
+    assert all(torch.equal(a, b) for a, b in zip(want, (s, parent, token, e)))
+
+
 # --------------------------------------------------------------------------- states
 def _states(g, shape, dtype):
     torch = torch_mod()
@@ -211,3 +222,16 @@ def test_reorder_of_nothing():
     with pytest.raises(tron.TronError):
         tron.tron_beam_reorder(at, s, s[:, 1:])    # over itself
     assert (s == 1).all()
+
+
+def test_reorder_between_the_halves_of_each_layer():
+    torch = torch_mod()
+    both = torch.randn(3, 2, 4, 5, 6, device="cuda")
+    was = both.clone()
+    at = torch.tensor([[3, 0], [2, 2]], dtype=torch.int32, device="cuda")
+    tron.tron_beam_reorder(at, both[:, 0], both[:, 1])
+    assert torch.equal(both[:, 0], was[:, 0]) and torch.equal(both[:, 1], was[:, 0][:, at.flatten().long()])
+    tron.tron_beam_reorder(at, both[:, 1], both[:, 0])
+    assert torch.equal(both[:, 0], both[:, 1][:, at.flatten().long()])
+    with pytest.raises(tron.TronError):
+        tron.tron_beam_reorder(at, both[:, 1], both.view(3, 8, 5, 6)[:, 3:7])

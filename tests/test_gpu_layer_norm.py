@@ -168,6 +168,19 @@ def test_layer_norm_in_place_and_of_one_row_for_all():
     assert _same(again, y)
 
 
+@pytest.mark.parametrize("d", [1027, 1032, 1537, 8195, 20483])
+def test_layer_norm_with_its_sum_over_x_or_the_residual(d):
+    """Rows whose last chunk is another wavefront's than the one before it."""
+    torch = torch_mod()
+    x, r = torch.randn(700, d, device="cuda").bfloat16(), torch.randn(700, d, device="cuda").bfloat16()
+    y, total, again = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    tron.tron_layer_norm(x, y, residual=r, total=total)
+    for over in ("x", "residual"):
+        a, b = x.clone(), r.clone()
+        tron.tron_layer_norm(a, again, residual=b, total=a if over == "x" else b)
+        assert torch.equal(again, y) and torch.equal(a if over == "x" else b, total)
+
+
 # --------------------------------------------------------------------------- gradient
 def _plain_grad(total, mean, rstd, gain, dy, dtotal):
     s, dy, mean, rstd = total.double(), dy.double(), mean.double()[:, None], rstd.double()[:, None]
