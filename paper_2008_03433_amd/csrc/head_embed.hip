@@ -250,9 +250,15 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
         return;
     }
     const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
-    const int64_t count = *A.S.count, begin = t * A.tile, end = begin + A.tile < count ? begin + A.tile : count;
+    // All that does not wait for the number of places is read beside it: what lies behind the last place is nobody's token, but in the work space.  The
+    // places of the first 64, one a lane.
+    const int64_t begin = t * A.tile, last = A.m - 1;
+    auto clamped = [&](int64_t i) { return i < last ? i : last; };
+    int key = A.S.key[clamped(begin + lane)], from = A.S.from[clamped(begin + lane)];
+    const int key_before = A.S.key[begin > 0 ? begin - 1 : 0], key_end = A.S.key[clamped(begin + A.tile)], key_last = A.S.key[clamped(begin + A.tile - 1)];
+    const int64_t count = *A.S.count, end = begin + A.tile < count ? begin + A.tile : count;
     if (begin >= count) return;
-    const bool enters = begin > 0 && A.S.key[begin - 1] == A.S.key[begin], leaves = end < count && A.S.key[end] == A.S.key[end - 1];
+    const bool enters = begin > 0 && key_before == __builtin_amdgcn_readfirstlane(key), leaves = end < count && key_end == key_last;
     const bool there = j < A.d;
     const T *dy = static_cast<const T *>(A.dy);
     float sum[kVec];
@@ -261,11 +267,15 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
     bool first = enters;
     constexpr int kAhead = 8;
     for (int64_t c0 = begin; c0 < end; c0 += kWave) {
-        // tokens and rows of 64 places, one a lane; behind the tile's last place -1, and that place's row once more
-        const int here = (int)(end - c0 < kWave ? end - c0 : kWave);
-        const int at = lane < here ? lane : here - 1;
-        const int from = A.S.from[c0 + at], after = c0 + kWave < end ? A.S.key[c0 + kWave] : -1;
-        int key = A.S.key[c0 + at];
+        // behind the tile's last place the token is -1, and the row that place's
+        const int here = (int)(end - c0 < kWave ? end - c0 : kWave), at = lane < here ? lane : here - 1;
+        if (c0 > begin) {
+            key = A.S.key[c0 + at];
+            from = A.S.from[c0 + at];
+        } else {
+            from = lane < here ? from : __builtin_amdgcn_readlane(from, here - 1);
+        }
+        const int after = c0 + kWave < end ? A.S.key[c0 + kWave] : -1;
         if (lane >= here) key = -1;
         for (int i0 = 0; i0 < here; i0 += kAhead) {
             Raw8<T> raw[kAhead];
@@ -309,11 +319,13 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void k_embed_join(EmbedGradArgs 
     if (unit >= A.tile_units) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
-    const int64_t count = *A.S.count, begin = t * A.tile, end = begin + A.tile;
-    if (end >= count) return;
-    const int v = A.S.key[end - 1];
-    if (A.S.key[end] != v || A.S.start[v] < begin) return;
-    const int64_t last = (A.S.stop[v] - 1) / A.tile, each = (last - t + kJoinWaves - 1) / kJoinWaves;
+    const int64_t begin = t * A.tile, end = begin + A.tile;
+    if (end >= A.m) return;
+    const int v = A.S.key[end - 1], next = A.S.key[end];   // read beside the number of places, behind which there are no tokens
+    if (end >= *A.S.count || next != v) return;
+    const int64_t start = A.S.start[v], stop = A.S.stop[v];
+    if (start < begin) return;
+    const int64_t last = (stop - 1) / A.tile, each = (last - t + kJoinWaves - 1) / kJoinWaves;
     const int64_t from = t + 1 + wave * each, to = from + each < last + 1 ? from + each : last + 1;
     float sum[kVec];
 #pragma unroll
@@ -371,10 +383,10 @@ void embed_typed(const EmbedArgs &A, int out, hipStream_t st)
     else embed_launch<T, _Float16>(A, st);
 }
 
-// Places of a tile: tiles of 512 columns for some 16 wavefronts a compute unit, of 16 places at least and of 512 at most
+// Places of a tile: tiles of 512 columns for some 16 wavefronts a compute unit, of 8 places at least, one turn's loads, and of 512 at most
 int tile_of_places(int64_t m, int64_t d)
 {
-    int tile = 16;
+    int tile = 8;
     while (tile < 512 && ceil_div(m, tile) * ceil_div(d, kColumns) > 4096) tile *= 2;
     return tile;
 }
