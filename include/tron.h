@@ -396,10 +396,11 @@ TRON_API int tron_probe_copy_bandwidth(double *dst_dev, const double *src_dev, i
                                        void *hip_stream, double *ms_per_launch);
 
 /* ------------------------------------------------------------------------------------------
- * Operators of a multi-class softmax head: the norm that makes its features, the matrix product that makes its
+ * Operators of a multi-class softmax head: the norms that make its features, the matrix product that makes its
  * logits, and the loss against a teacher's top logits that it is trained by, with gradients and the
  * Hessian-vector product.  For many classes, and features that a network made, they are what z = X w, zhat and D
- * are for two.
+ * are for two.  At both ends of it, tokens: the embeddings that the features are made of, with their gradient, and the beam
+ * search over the logits.
  *
  * They have no handle: every array is a caller's device pointer on the current device, row-major, with a leading
  * dimension in elements, and every call enqueues on `hip_stream` and returns (nothing synchronises or allocates, so

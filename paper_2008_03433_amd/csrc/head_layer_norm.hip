@@ -7,6 +7,10 @@
 // of a workgroup.  The mean is taken first and the squares are those of differences to it, so that rows that lie far from 0 keep the
 // digits of their variance: with m the mean rounded to 32 bits and c = s - m,  mean s = m + mean c  and  variance = mean c^2 - (mean c)^2.  mean c is what
 // the rounding of m and the order of its sum left; it is subtracted from c once more.
+//
+// Measured: 16384 x 8192 bf16 with a residual and its sum 200 us (1.07 GB, 5.37 TB/s: outputs past the caches); one row of 4096 to e4m3 4.6 us of the device's time,
+// 9.3 us a call; gradient of 16384 x 4096 bf16 with all its inputs 115 us, of which 7 us the columns' sums (537 MB, 4.9 TB/s beside them), of 30011 x 1023 f16
+// 54 us, of which 9 us these sums (184 MB).  Rows at odd places cost nothing by themselves (30011 x 1024 f16 in rows of 1025: 3% more).
 #include "head_rows.h"
 
 namespace tron {
@@ -545,11 +549,13 @@ int layer_typed(const LayerArgs &A, int out_type, hipStream_t st)
     return past ? layer_launch<T, T, true>(A, st) : layer_launch<T, T, false>(A, st);
 }
 
-// Columns up to which a wavefront of the gradient holds its rows, and above which rows are read twice
+// Columns up to which lanes of one wavefront hold a row in the gradient, and above which rows are read twice.  30011 x 1024 f16 67 us by wavefronts with two chunks a lane,
+// 53 us by workgroups of 128 threads.
 constexpr int64_t kGradNarrow = 512;
 constexpr int64_t kGradWide = 16384;
 
-// workgroups of the gradient, each with a share of dgain and of dshift
+// Workgroups of the gradient, each with a share of dgain and of dshift: as many as are resident.  16384 x 4096 f16 97 us with 512, 108 us with 1024; 30011 x 1024 53 us with
+// 2048 of 128 threads, 69 us with 1024.
 int64_t layer_shares(int64_t m, int64_t d)
 {
     if (d <= kGradNarrow) return std::min<int64_t>(ceil_div(m, kTeamBlock / (d <= kSlim ? 16 : kWave)), 1024);

@@ -1,4 +1,4 @@
-"""The operators of a multi-class softmax head, as include/tron.h declares them, on torch CUDA tensors: argument marshalling only.
+"""The operators of a multi-class softmax head and of the tokens at both its ends, as include/tron.h declares them, on torch CUDA tensors: argument marshalling only.
 
 Matrices are 2-D tensors whose last dimension is contiguous (or 1-D ones: a single row); the rows' stride is free, and a tensor that is only
 read may be expanded over its rows.  Outputs are tensors of the caller's, as elsewhere in this package.  `stream` is a torch stream
