@@ -375,7 +375,9 @@ __global__ __launch_bounds__(1024) void k_column_sums(const float *shares, int64
     }
     if (!out) return;
     const int c = threadIdx.x % kColumns, group = threadIdx.x / kColumns;
-    const int64_t j = (int64_t)blockIdx.x * kColumns + c;
+    // Workgroups go to the eight XCDs in turn: of sixteen, two of one XCD take the two halves of a line
+    const unsigned block = blockIdx.x / 16 * 16 + 16 <= gridDim.x ? blockIdx.x / 16 * 16 + blockIdx.x % 8 * 2 + blockIdx.x / 8 % 2 : blockIdx.x;
+    const int64_t j = (int64_t)block * kColumns + c;
     float sum = 0.f;
     if (j < d) {
         int64_t i = group;
