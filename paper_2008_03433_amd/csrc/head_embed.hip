@@ -84,6 +84,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs A)
 // ------------------------------------------------------------------ sorted tokens
 constexpr int kSortWaves = 16;
 constexpr int kMostIds = 1024;    // of a workgroup: counts of each for every wavefront lie in LDS
+constexpr int kMostFound = 256;   // of a wavefront's own tokens that LDS keeps between the counting and the placing
 
 struct Sorted {
     int32_t *start, *stop; // [V]: first place of a token among the sorted ones, and the first behind it
@@ -100,6 +101,7 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids
     __shared__ int counts[kSortWaves][kMostIds];
     __shared__ int totals[2][kSortWaves];
     __shared__ uint8_t marks[kSortWaves][kMostIds];
+    __shared__ uint64_t found[kSortWaves][kMostFound];   // token's number of the workgroup's, row of dy
     const int64_t group = block_number(), below = (int64_t)1 << shift;
     if (group >= below) return;
     const int here = (int)((V - group + below - 1) >> shift);   // tokens; at most kMostIds
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids
     const uint32_t tokens = (uint32_t)V, mask = (uint32_t)below - 1, mine_of = (uint32_t)group;
     const int64_t share = (m + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave, begin = wave * share, end = begin + share < m ? begin + share : m;
     constexpr int kAhead = 8;
-    int before = 0;
+    int before = 0, own_here = 0;
     for (int64_t i0 = begin; i0 < end; i0 += kAhead * kWave) {
         uint32_t id[kAhead];
 #pragma unroll
@@ -133,6 +135,9 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids
             const uint64_t same = some & __ballot(k == token);
             if (lane == lead) atomicAdd(&counts[wave][token], __popcll(same));
             if ((some & ~same) >> lane & 1) atomicAdd(&counts[wave][k], 1);
+            const int at = own_here + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(some >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)some, 0));
+            if ((some >> lane & 1) && at < kMostFound) found[wave][at] = (uint64_t)k << 32 | (uint32_t)(i0 + u * kWave + lane);
+            own_here += __popcll(some);
         }
     }
     // places of the tokens: a thread a token
@@ -164,41 +169,51 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids
         }
     }
     __syncthreads();
+    // A wavefront of tokens, in the order of their rows
+    auto place_tokens = [&](bool own, int k, int from) {
+        uint64_t left = __ballot(own);
+        if (!left) return;
+        auto put = [&](int to) {
+            S.key[to] = (int32_t)((uint32_t)k << shift | mine_of);
+            S.from[to] = from;
+        };
+        // Every lane writes its number to its token's mark.  Whose number is not there has a token that is there twice: these go one token after the other,
+        // in the order of their lanes; the others all at once
+        volatile uint8_t *mark = marks[wave];
+        if (own) mark[k] = (uint8_t)lane;
+        uint64_t twice = __ballot(own && mark[k] != lane);
+        while (twice) {
+            const int token = __builtin_amdgcn_readlane(k, __builtin_ctzll(twice));
+            const uint64_t same = left & __ballot(k == token);
+            const int at = counts[wave][token];
+            if (same >> lane & 1) put(at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0)));
+            if (lane == 0) counts[wave][token] = at + __popcll(same);
+            left &= ~same;
+            twice &= ~same;
+        }
+        if (left >> lane & 1) {
+            const int at = counts[wave][k];
+            put(at);
+            counts[wave][k] = at + 1;
+        }
+    };
+    if (own_here <= kMostFound) {
+#pragma unroll 1
+        for (int i = 0; i < own_here; i += kWave) {
+            const bool own = i + lane < own_here;
+            const uint64_t one = own ? found[wave][i + lane] : 0;
+            place_tokens(own, (int)(one >> 32), (int)(uint32_t)one);
+        }
+        return;
+    }
+    // more than LDS keeps: they are read once more
+#pragma unroll 1
     for (int64_t i0 = begin; i0 < end; i0 += kAhead * kWave) {
         uint32_t id[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) id[u] = token_at(i0 + u * kWave + lane, end);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const bool own = id[u] < tokens && (id[u] & mask) == mine_of;
-            const int k = (int)(id[u] >> shift);
-            uint64_t left = __ballot(own);
-            if (!left) continue;
-            const int64_t from = i0 + u * kWave + lane;
-            auto put = [&](int to) {
-                S.key[to] = (int32_t)id[u];
-                S.from[to] = (int32_t)from;
-            };
-            // Every lane writes its number to its token's mark.  Whose number is not there has a token that is there twice: these go one token after the other,
-            // in the order of their lanes; the others all at once
-            volatile uint8_t *mark = marks[wave];
-            if (own) mark[k] = (uint8_t)lane;
-            uint64_t twice = __ballot(own && mark[k] != lane);
-            while (twice) {
-                const int token = __builtin_amdgcn_readlane(k, __builtin_ctzll(twice));
-                const uint64_t same = left & __ballot(k == token);
-                const int at = counts[wave][token];
-                if (same >> lane & 1) put(at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0)));
-                if (lane == 0) counts[wave][token] = at + __popcll(same);
-                left &= ~same;
-                twice &= ~same;
-            }
-            if (left >> lane & 1) {
-                const int at = counts[wave][k];
-                put(at);
-                counts[wave][k] = at + 1;
-            }
-        }
+        for (int u = 0; u < kAhead; ++u) place_tokens(id[u] < tokens && (id[u] & mask) == mine_of, (int)(id[u] >> shift), (int)(i0 + u * kWave + lane));
     }
 }
 
