@@ -25,8 +25,11 @@ constexpr int kMostBeams = 64;
 constexpr int kAhead = 4;            // chunks of eight columns of a lane under way
 constexpr int kTurn = kAhead * kWave * kVec;   // columns of a wavefront's turn
 constexpr int kSlack = 128;          // entries of a list beyond which it is cut to the K largest
-constexpr int kList = 2 * kSlack;
-constexpr int kLooked = 4;           // lanes whose columns of a turn are looked at more closely at once: two columns a lane of the wavefront
+// Lanes whose columns of a turn are looked at more closely at once.  Beside other wavefronts' first turns few pass in any; a wavefront alone has all of the K.
+template <int WAVES>
+constexpr int kLooked = WAVES == 1 ? 16 : 4;
+template <int WAVES>
+constexpr int kList = kSlack + kLooked<WAVES> * kAhead * kVec;   // behind kSlack entries, all that is looked at at once has its place
 constexpr int kMostParts = 64;       // of a row, one a lane
 constexpr int kMostOffers = kMostBeams * kMostPicks;   // of an item's rows' parts together
 
@@ -103,9 +106,10 @@ __device__ __forceinline__ key_t64 cut_to(key_t64 *list, int &count, int K, int 
 }
 
 // `count` is one of the wavefront's; the compiler keeps what it may not know to be such in a register of each lane, and branches by masks
+template <int LIST>
 __device__ __forceinline__ key_t64 cut(key_t64 *list, int &count, int K, int lane)
 {
-    const key_t64 bound = count <= kWave ? cut_to<1>(list, count, K, lane) : cut_to<kList / kWave>(list, count, K, lane);
+    const key_t64 bound = count <= kWave ? cut_to<1>(list, count, K, lane) : cut_to<LIST / kWave>(list, count, K, lane);
     count = __builtin_amdgcn_readfirstlane(count);
     return bound;
 }
@@ -174,8 +178,9 @@ struct Turn {
 template <typename T, int WAVES>
 __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
 {
-    __shared__ key_t64 lists[WAVES][kList];
-    __shared__ __align__(16) uint32_t looked[WAVES][kLooked][kAhead * 2 * sizeof(T)];
+    constexpr int kMine = kList<WAVES>;
+    __shared__ key_t64 lists[WAVES][kMine];
+    __shared__ __align__(16) uint32_t looked[WAVES][kLooked<WAVES>][kAhead * 2 * sizeof(T)];
     __shared__ uint32_t firsts[WAVES][kWave];   // the lanes' largest values of the first turns, in order
     __shared__ double sums[WAVES];
     __shared__ float tops[WAVES];
@@ -248,18 +253,20 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
         uint64_t some = __ballot(bound.passes(most));
         while (some) {
             if (count > kSlack) {
-                const uint32_t order = (uint32_t)(cut(list, count, K, lane) >> 32);
+                const uint32_t order = (uint32_t)(cut<kMine>(list, count, K, lane) >> 32);
                 bound.raise(order, false);   // lower columns of this turn may still come
                 if (WAVES > 1 && lane == 0) atomicMax(&common, order);
                 reached = reached > order ? reached : order;
             }
-            constexpr int kWords = kAhead * 2 * sizeof(T), kTwo = sizeof(T) / 2;   // 32-bit words of a lane, of two columns
+            // words of a lane's columns; lanes that read one lane's, and the columns that each of these takes
+            constexpr int kWords = kAhead * 2 * sizeof(T), kAcross = kWave / kLooked<WAVES>, kEach = kAhead * kVec / kAcross, kTaken = kWords / kAcross;
+            static_assert(kEach <= kVec && kVec % kEach == 0, "neighbouring columns");
             uint64_t rest = some;
             int from_lane = 0;
 #pragma unroll
-            for (int q = 0; q < kLooked; ++q) {
+            for (int q = 0; q < kLooked<WAVES>; ++q) {
                 const int l = rest ? __builtin_ctzll(rest) : 0;
-                if (lane / (kWave / kLooked) == q) from_lane = rest ? l : -1;
+                if (lane / kAcross == q) from_lane = rest ? l : -1;
                 if (rest && lane == l) {
 #pragma unroll
                     for (int u = 0; u < kAhead; ++u)
@@ -269,13 +276,13 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
                 rest &= rest - 1;
             }
             some = rest;
-            const int two = lane % (kWave / kLooked);   // of sixteen pairs, four a chunk
+            const int mine = lane % kAcross * kEach;   // first one of its columns
             Eight<T> w;
 #pragma unroll
-            for (int i = 0; i < kTwo; ++i) w.w[i] = looked[wave][lane / (kWave / kLooked)][two * kTwo + i];
-            const int64_t j = j0 + ((two / (kVec / 2)) * kWave + from_lane) * kVec + two % (kVec / 2) * 2;
+            for (int i = 0; i < kTaken; ++i) w.w[i] = looked[wave][lane / kAcross][lane % kAcross * kTaken + i];
+            const int64_t j = j0 + (mine / kVec * kWave + from_lane) * kVec + mine % kVec;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kEach; ++i) {
                 const float v = w.at(i);
                 const bool in = from_lane >= 0 && bound.passes(v) && j + i < to;
                 const uint64_t mask = __ballot(in);
@@ -293,7 +300,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
     double total = wave_sum((double)run.s * (double)exp_of(run.m - base_of(all_most)));
     if (WAVES > 1) {
         // one list of the wavefronts' keys that may be among the K, 64 of each at most
-        if (count > kWave) cut(list, count, K, lane);
+        if (count > kWave) cut<kMine>(list, count, K, lane);
         if (lane == 0) {
             tops[wave] = all_most;
             sums[wave] = total;
@@ -311,16 +318,16 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
         total = wave_sum(lane < WAVES ? sums[lane % WAVES] * exp((double)m - (double)base_of(all_most)) : 0.0);
         list = join;
         const int keys = __builtin_amdgcn_readfirstlane(joined);
-        count = keys < kList ? keys : kList;
-        for (int read = count; read < keys;) {   // kList of them at a time
-            cut(list, count, K, lane);
-            const int more = keys - read < kList - count ? keys - read : kList - count;
+        count = keys < kMine ? keys : kMine;
+        for (int read = count; read < keys;) {   // as many as a list holds at a time
+            cut<kMine>(list, count, K, lane);
+            const int more = keys - read < kMine - count ? keys - read : kMine - count;
             for (int i = lane; i < more; i += kWave) list[count + i] = join[read + i];
             count += more;
             read += more;
         }
     }
-    if (count > K) cut(list, count, K, lane);
+    if (count > K) cut<kMine>(list, count, K, lane);
     const int64_t at = row * A.parts + part;
     if (lane < K) A.part_key[at * K + lane] = lane < count ? list[lane] : 0;
     if (lane == 0) {
@@ -346,6 +353,36 @@ struct Offers {
     }
 };
 
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+
+// count += a > b, the last word first: the borrow of b - a.  (Comparisons make two of each word, and of 64 bits take four times as long: 144 offers were
+// ranked in 9 us of a launch.)
+__device__ __forceinline__ void count_larger(int &count, const words4 &a, const words4 &b)
+{
+    uint32_t difference;
+    asm("v_sub_co_u32_e32 %0, vcc, %2, %3\n\t"
+        "v_subb_co_u32_e32 %0, vcc, %4, %5, vcc\n\t"
+        "v_subb_co_u32_e32 %0, vcc, %6, %7, vcc\n\t"
+        "v_subb_co_u32_e32 %0, vcc, %8, %9, vcc\n\t"
+        "v_addc_co_u32_e32 %1, vcc, 0, %1, vcc"
+        : "=&v"(difference), "+v"(count)
+        : "v"(b[0]), "v"(a[0]), "v"(b[1]), "v"(a[1]), "v"(b[2]), "v"(a[2]), "v"(b[3]), "v"(a[3])
+        : "vcc");
+}
+
+// How many of `highs`, of one a thread, are larger and how many the same
+__device__ __forceinline__ void compare_high(const uint32_t *highs, uint32_t high, int &larger, int &same)
+{
+    for (int i = 0; i < kPickThreads; i += 8) {
+        const words4 a = *reinterpret_cast<const words4 *>(highs + i), b = *reinterpret_cast<const words4 *>(highs + i + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            larger += (a[k] > high) + (b[k] > high);
+            same += (a[k] == high) + (b[k] == high);
+        }
+    }
+}
+
 enum { LIVE = 0, OVER, DEAD };   // a beam whose logits make its offers, one that has ended, one of which nothing is possible
 
 // A workgroup an item
@@ -356,9 +393,10 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     __shared__ int kind[kMostBeams];
     __shared__ bool had_ended[kMostBeams];   // as next_ended may be ended
     __shared__ unsigned digits[256];
-    __shared__ int found[2], survivors, chosen[kRanked];
-    __shared__ key_t64 orders[kRanked + 32];   // 0 behind the last one
-    __shared__ uint64_t places[kRanked + 32];
+    __shared__ uint32_t bound;
+    __shared__ int found[2], survivors, left, chosen[kRanked];
+    __shared__ __align__(16) uint32_t highs[kPickThreads];   // of the scores' bits
+    __shared__ words4 keys[kRanked + 32];                    // score and place as one number of 128 bits, the higher the better; 0 behind the last one
     const int64_t item = block_number();
     if (item >= A.batch) return;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
@@ -387,7 +425,10 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
             had_ended[b] = A.ended && A.ended[row];
         }
     }
-    if (threadIdx.x == 0) survivors = 0;
+    if (threadIdx.x == 0) {
+        survivors = left = 0;
+        bound = 0;
+    }
     __syncthreads();
     const int64_t listed = A.V < K ? A.V : K;
     for (int e = threadIdx.x; e < count; e += kPickThreads) {
@@ -406,22 +447,43 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
         O.token[e] = token;
     }
     __syncthreads();
-    if (count > kRanked) {
-        // Digit by digit: who has a higher digit than the K-th best is chosen, who has the same is looked at further, until what is left fits
-        constexpr int kEach = kMostOffers / kPickThreads;
-        unsigned under = 0, taken = 0;   // one bit an offer of this thread
+    static_assert(kMostOffers <= 32 * kPickThreads, "one bit an offer of a thread");
+    const int each = (count + kPickThreads - 1) / kPickThreads;
+    unsigned taken = 0;
+    key_t64 top = 0;
 #pragma unroll 1
-        for (int i = 0; i < kEach; ++i) {
-            const int e = i * kPickThreads + threadIdx.x;
-            if (e < count && O.order[e]) under |= 1u << i;
-        }
+    for (int i = 0; i < each; ++i) {
+        const int e = i * kPickThreads + threadIdx.x;
+        const key_t64 order = e < count ? O.order[e] : 0;
+        taken |= (order != 0) << i;
+        top = order > top ? order : top;
+    }
+    if (count > kRanked) {
+        // Of the threads' best scores the K-th best is a bound that K offers reach; those that do are nearly always few enough
+        const uint32_t high = (uint32_t)(top >> 32);
+        highs[threadIdx.x] = high;
+        __syncthreads();
+        int better = 0, alike = 0;
+        compare_high(highs, high, better, alike);
+        if (high && better < K && better + alike >= K) bound = high;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i < each; ++i)
+            if (taken >> i & 1 && (uint32_t)(O.order[i * kPickThreads + threadIdx.x] >> 32) < bound) taken &= ~(1u << i);
+        if (taken) atomicAdd(&left, __popc(taken));
+        __syncthreads();
+    }
+    if (left > kRanked) {
+        // Digit by digit: who has a higher digit than the K-th best is chosen, who has the same is looked at further, until what is left fits
+        unsigned under = taken;
+        taken = 0;
         int need = K, have = 0;
 #pragma unroll 1
         for (int d = 0; d < 13; ++d) {
             digits[threadIdx.x] = 0;
             __syncthreads();
 #pragma unroll 1
-            for (int i = 0; i < kEach; ++i)
+            for (int i = 0; i < each; ++i)
                 if (under >> i & 1) atomicAdd(&digits[O.digit(i * kPickThreads + threadIdx.x, d)], 1u);
             __syncthreads();
             if (wave == 0) {
@@ -445,7 +507,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
             need -= found[1];
             have += found[1];
 #pragma unroll 1
-            for (int i = 0; i < kEach; ++i)
+            for (int i = 0; i < each; ++i)
                 if (under >> i & 1) {
                     const unsigned mine = O.digit(i * kPickThreads + threadIdx.x, d);
                     if (mine > at) taken |= 1u << i;
@@ -455,43 +517,45 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
             __syncthreads();
         }
         taken |= under;
-#pragma unroll 1
-        for (int i = 0; i < kEach; ++i)
-            if (taken >> i & 1) chosen[atomicAdd(&survivors, 1)] = i * kPickThreads + threadIdx.x;
-    } else if (threadIdx.x < count && O.order[threadIdx.x]) {
-        chosen[atomicAdd(&survivors, 1)] = threadIdx.x;
+    }
+    {
+        const int mine = __popc(taken), scanned = wave_scan_add(mine);
+        int at = 0;
+        if (lane == kWave - 1) at = atomicAdd(&survivors, scanned);
+        at = __builtin_amdgcn_readlane(at, kWave - 1) + scanned - mine;
+        for (unsigned rest = taken; rest; rest &= rest - 1) chosen[at++] = __builtin_ctz(rest) * kPickThreads + threadIdx.x;
     }
     __syncthreads();
     const int n = survivors;
     for (int i = threadIdx.x; i < kRanked + 32; i += kPickThreads) {
-        orders[i] = i < n ? O.order[chosen[i]] : 0;
-        places[i] = i < n ? O.place(chosen[i]) : 0;
+        words4 key = {0, 0, 0, 0};
+        if (i < n) {
+            const int e = chosen[i];
+            const key_t64 order = O.order[e];
+            key = words4{~O.token[e], ~(uint32_t)(e / of_beam), (uint32_t)order, (uint32_t)(order >> 32)};
+        }
+        keys[i] = key;
     }
     __syncthreads();
     // one, two or four threads an offer
     const int share = n <= kRanked / 4 ? 4 : n <= kRanked / 2 ? 2 : 1, mine = threadIdx.x / share;
+    const words4 own = keys[mine];
     int rank = 0;
     if (mine < n) {
-        const key_t64 order = orders[mine];
-        const uint64_t place = places[mine];
-        for (int i = threadIdx.x % share; i < n; i += 8 * share) {   // eight at a time are under way from LDS
-            key_t64 other[8];
-            uint64_t at[8];
+        const int some = ((n + share - 1) / share + 7) / 8 * 8, first = threadIdx.x % share * some;   // eights: share * some <= n + 32
+        for (int i = first; i < first + some; i += 8) {
+            words4 other[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                other[k] = orders[i + k * share];
-                at[k] = places[i + k * share];
-            }
+            for (int k = 0; k < 8; ++k) other[k] = keys[i + k];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) rank += other[k] > order || (other[k] == order && at[k] < place);
+            for (int k = 0; k < 8; ++k) count_larger(rank, other[k], own);
         }
     }
     if (share > 1) rank += __shfl_xor(rank, 1);
     if (share > 2) rank += __shfl_xor(rank, 2);
-    if (mine >= n || threadIdx.x % share) return;
+    if (mine >= n || threadIdx.x % share || rank >= K) return;
     const int e = chosen[mine];
-    const key_t64 order = orders[mine];
-    if (rank >= K) return;
+    const key_t64 order = (key_t64)own[3] << 32 | own[2];
     const int b = e / of_beam;
     const int64_t out = item * K + rank, row = item * A.beams + b;
     const uint32_t token = O.token[e];
