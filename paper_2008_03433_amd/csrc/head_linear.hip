@@ -280,8 +280,9 @@ __device__ __forceinline__ void put8(const Epilogue &E, const Columns &C, float 
     }
 }
 
-// Behind a product whose inner index was cut: eight sums a thread, four parts at a time, blockIdx.y and z the row.  More parts than
-// kJoinAlone are shared out over W wavefronts, whose sums meet in LDS in their order (64 parts of 16 x 4096: 13.8 us by one, 5 us by eight).
+// Behind a product whose inner index was cut: eight sums a thread, four parts at a time, the lanes of a wavefront on one row after the other
+// (9 parts of 3368 x 18: 18.6 us with a workgroup a row, 4.1 us so).  More parts than kJoinAlone are shared out over W wavefronts, whose sums
+// meet in LDS in their order (64 parts of 16 x 4096: 13.8 us by one, 5 us by eight).
 constexpr int kJoinAlone = 8, kJoinWaves = 8;
 
 // WHOLE: the parts hold whole numbers.
@@ -295,9 +296,8 @@ template <int W, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? kBlock : W * kWave) void k_linear_join(Epilogue E, int parts)
 {
     const int wave = W == 1 ? 0 : threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int64_t i = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, j = (W == 1 ? (int64_t)blockIdx.x * blockDim.x + threadIdx.x : (int64_t)blockIdx.x * kWave + lane) * kVec;
-    if (i >= E.m) return;
-    const int64_t n = E.n - j, each = E.m * E.n;
+    const int64_t chunks = (E.n + kVec - 1) / kVec, unit = W == 1 ? block_number() * blockDim.x + threadIdx.x : block_number() * kWave + lane;
+    const int64_t i = unit / chunks, j = (unit - i * chunks) * kVec, n = i < E.m ? E.n - j : 0, each = E.m * E.n;
     const float *p = E.part + i * E.n + j;
     float v[1][kVec];
 #pragma unroll
@@ -342,10 +342,11 @@ __global__ __launch_bounds__(W == 1 ? kBlock : W * kWave) void k_linear_join(Epi
 template <bool WHOLE = false>
 int join_parts(const Epilogue &E, int parts, hipStream_t st)
 {
-    const int64_t chunks = ceil_div(E.n, kVec), y = std::min<int64_t>(E.m, 32768);
+    const int64_t units = E.m * ceil_div(E.n, kVec);
     const bool alone = parts <= kJoinAlone;
-    const unsigned across = alone ? (unsigned)std::min<int64_t>(kBlock, ceil_div(chunks, kWave) * kWave) : kWave;
-    const dim3 grid((unsigned)ceil_div(chunks, across), (unsigned)y, (unsigned)ceil_div(E.m, y));
+    const unsigned across = alone ? (unsigned)std::min<int64_t>(kBlock, ceil_div(units, kWave) * kWave) : kWave;
+    const int64_t blocks = ceil_div(units, across), x = std::min<int64_t>(blocks, 1 << 20);
+    const dim3 grid((unsigned)x, (unsigned)ceil_div(blocks, x));
     if (alone) k_linear_join<1, WHOLE><<<grid, across, 0, st>>>(E, parts);
     else k_linear_join<kJoinWaves, WHOLE><<<grid, kJoinWaves * kWave, 0, st>>>(E, parts);
     TRON_HIP(hipGetLastError());

@@ -136,3 +136,19 @@ def test_an_output_over_its_residual():
         tron.tron_linear(x, w, y, residual=r, x_scale=s[:m], w_scale=s[100:])
         tron.tron_linear(x, w, r, residual=r, x_scale=s[:m], w_scale=s[100:])
         assert _same(r, y)
+
+
+@pytest.mark.parametrize("m,n,k", [(45, 1, 60000), (333, 9, 3001), (3368, 18, 1027), (700, 64, 2944), (34, 71, 100000)])
+def test_few_columns_whose_inner_index_is_cut(m, n, k):
+    """Rows of the parts that share wavefronts.  Scales are powers of two and sums stay below 2^24, so that the product is exact; the sum with the residual is rounded once."""
+    torch = torch_mod()
+    g = _gen(m + n + k)
+    x, w = torch.randint(-8, 9, (m, k), generator=g, dtype=torch.int8), torch.randint(-8, 9, (n, k), generator=g, dtype=torch.int8)   # 64 k < 2^24
+    xs, ws = 2.0 ** torch.randint(-3, 4, (m,), generator=g).float(), 2.0 ** torch.randint(-3, 4, (n,), generator=g).float()
+    residual = torch.randint(-9, 10, (m, n), generator=g).float()
+    assert tron.tron_linear_work(m, n, k, torch.int8) >= 2 * 4 * m * n   # it is cut
+    want = ((x.double() @ w.double().T) * xs.double()[:, None] * ws.double() + residual.double()).float()
+    y = torch.full((m + 1, n + 5), 7.0, device="cuda")
+    tron.tron_linear(x.cuda(), w.cuda(), y[:m, :n], x_scale=xs.cuda(), w_scale=ws.cuda(), residual=residual.cuda())
+    assert torch.equal(y[:m, :n].cpu(), want)
+    assert bool((y[m] == 7).all()) and bool((y[:, n:] == 7).all())
