@@ -13,8 +13,8 @@
 // The sum is the more exact the more rows are compared by it: exponents are products with log2(e) in two parts, lanes' sums are joined in 64 bits,
 // scores are compared in 64 bits.
 //
-// Measured: 64 items of 8 beams over 128000 bf16, 16 picks: 40 us the rows (118 MB that are read, 2.9 TB/s; the vector units are busy 68% of the cycles), 7 us
-// the joining; 2 layers of 129 x 128 bf16 states of 512 rows 9.5 us (50 MB, 5.3 TB/s).  One item of 4 beams over 32000 f32: 8 + 4 us.
+// Measured: 64 items of 8 beams over 128000 bf16, 16 picks: 41 us the rows (118 MB that are read, 2.9 TB/s; the vector units are busy 68% of the cycles), 6 us
+// the joining; 2 layers of 129 x 128 bf16 states of 512 rows 9.6 us (50 MB, 5.2 TB/s).  One item of 4 beams over 32000 f32: 8 + 4 us.
 #include "head_util.h"
 
 namespace tron {

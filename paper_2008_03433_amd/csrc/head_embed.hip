@@ -8,8 +8,8 @@
 // token is many tiles' work, and a wavefront sums a tile's rows over 512 columns and stores those tokens that lie in its tile alone
 // (k_embed_sums, whose further wavefronts fill the rows of tokens that are not there); the others' shares are joined (k_embed_join).
 //
-// Measured: 32768 tokens of 4096 bf16, a table of 128000 rows in f32: 24 us the sort, 427 us the sums and rows of zeros (2.35 GB, 5.4 TB/s), 9 us the joining,
-// 491 us a call; 9001 of 511 f16, 50021 rows: 10 + 17.5 + 5.5 us; lookup of 8 rows of 4096 i8 3.2 us.
+// Measured: 32768 tokens of 4096 bf16, a table of 128000 rows in f32: 15 us the sort, 427 us the sums and rows of zeros (2.35 GB, 5.4 TB/s), 9 us the joining,
+// 483 us a call; 9001 of 511 f16, 50021 rows: 7 + 17 + 5 us; lookup of 8 rows of 4096 i8 2.9 us.
 #include "head_util.h"
 
 namespace tron {
