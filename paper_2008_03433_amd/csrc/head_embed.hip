@@ -6,10 +6,10 @@
 // sums are those of the rows of equal tokens in the order of their places, whatever the tokens are, so that the same call gives the same bits.
 // Three launches: tokens are sorted (k_sort_tokens); the sorted places are cut into tiles of equal length, whatever tokens they hold, so that a frequent
 // token is many tiles' work, and a wavefront sums a tile's rows over 512 columns and stores those tokens that lie in its tile alone
-// (k_embed_sums, whose further wavefronts fill the rows of tokens that are not there); the others' shares are joined (k_embed_join).
+// (k_embed_sums, whose further workgroups fill the rows of tokens that are not there); the others' shares are joined (k_embed_join).
 //
-// Measured: 32768 tokens of 4096 bf16, a table of 128000 rows in f32: 15 us the sort, 427 us the sums and rows of zeros (2.35 GB, 5.4 TB/s), 9 us the joining,
-// 483 us a call; 9001 of 511 f16, 50021 rows: 7 + 17 + 5 us; lookup of 8 rows of 4096 i8 2.9 us.
+// Measured: 32768 tokens of 4096 bf16, a table of 128000 rows in f32: 15 us the sort, 405 us the sums and rows of zeros (2.35 GB, 5.8 TB/s), 9 us the joining,
+// 463 us a call; 9001 of 511 f16, 50021 rows: 7 + 16 + 5 us; lookup of 8 rows of 4096 i8 2.9 us.
 #include "head_util.h"
 
 namespace tron {
@@ -225,6 +225,7 @@ struct EmbedGradArgs {
     float *shares;     // [tiles][2][d]: sums of a tile's first token, where its places begin before the tile, and of its last one, where they go on behind it
     int64_t m, d, V, lddy, ldtable, across, tiles, tile_units;
     int tile;          // places of a tile
+    int rows_each;     // rows of the table that a workgroup looks at, 64 at most
     float scale;
     bool add;
 };
@@ -244,29 +245,38 @@ __device__ __forceinline__ void put_row(const EmbedGradArgs &A, int64_t v, int64
     store8_of<O, PAST>(row + j, out, A.d - j);
 }
 
-// The first wavefronts have a tile's 512 columns each, the others a row of the table each
+// The first wavefronts have a tile's 512 columns each, the workgroups behind them rows_each rows of the table, one for each wavefront, pair or four of them by
+// its length: some 16 KB, which lie side by side.  (A row a wavefront, which waits for its tokens' places first: rows of 69 f32 67 us for 256000, 36 us so; of
+// 4096 f32 399 us for 128000, 363 us so.)
 template <typename T, typename O, bool PAST>
 __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedGradArgs A)
 {
     const int64_t unit = block_number() * kWavesPerBlock + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int lane = threadIdx.x % kWave;
-    if (unit >= A.tile_units) {
-        const int64_t v = unit - A.tile_units;
-        if (v >= A.V || A.add || A.S.start[v] != A.S.stop[v]) return;
-        // sixteen bytes a lane, side by side: whole lines from one instruction
-        typedef int words __attribute__((ext_vector_type(4), aligned(2)));
+    const int64_t filler = block_number() - (A.tile_units + kWavesPerBlock - 1) / kWavesPerBlock;
+    if (filler >= 0) {
         constexpr int kEach = 16 / (int)sizeof(O);
-        O *row = static_cast<O *>(A.dtable) + v * A.ldtable;
-        for (int64_t j = lane * kEach; j < A.d; j += kWave * kEach) {
-            if (j + kEach <= A.d) {
-                if (PAST) __builtin_nontemporal_store(words{0, 0, 0, 0}, reinterpret_cast<words *>(row + j));
-                else *reinterpret_cast<words *>(row + j) = words{0, 0, 0, 0};
-            } else {
-                for (int64_t k = j; k < A.d; ++k) row[k] = static_cast<O>(0.f);
+        // wavefronts a row
+        const int team = A.d <= kWave * kEach ? 1 : A.d <= 2 * kWave * kEach ? 2 : 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int64_t v0 = filler * A.rows_each, v = v0 + lane, step = team * kWave * kEach;
+        const bool mine = lane % (kWavesPerBlock / team) == wave / team;
+        uint64_t none = __ballot(mine && lane < A.rows_each && v < A.V && A.S.start[v] == A.S.stop[v]);
+        for (; none; none &= none - 1) {
+            // sixteen bytes a lane, side by side: whole lines from one instruction
+            typedef int words __attribute__((ext_vector_type(4), aligned(2)));
+            O *row = static_cast<O *>(A.dtable) + (v0 + __builtin_ctzll(none)) * A.ldtable;
+            for (int64_t j = (wave % team * kWave + lane) * kEach; j < A.d; j += step) {
+                if (j + kEach <= A.d) {
+                    if (PAST) __builtin_nontemporal_store(words{0, 0, 0, 0}, reinterpret_cast<words *>(row + j));
+                    else *reinterpret_cast<words *>(row + j) = words{0, 0, 0, 0};
+                } else {
+                    for (int64_t k = j; k < A.d; ++k) row[k] = static_cast<O>(0.f);
+                }
             }
         }
         return;
     }
+    if (unit >= A.tile_units) return;
     const int64_t t = unit / A.across, j = (unit - t * A.across) * kColumns + lane * kVec;
     // All that does not wait for the number of places is read beside it: what lies behind the last place is nobody's token, but in the work space.  The
     // places of the first 64, one a lane.
@@ -434,8 +444,8 @@ EmbedSpace embed_space(int64_t m, int64_t d, int64_t V)
 template <typename T, typename O, bool PAST>
 int embed_grad_launch(const EmbedGradArgs &A, hipStream_t st)
 {
-    const int64_t units = A.tile_units + (A.add ? 0 : A.V);
-    if (units) k_embed_sums<T, O, PAST><<<block_grid(ceil_div(units, kWavesPerBlock)), kBlock, 0, st>>>(A);
+    const int64_t blocks = ceil_div(A.tile_units, kWavesPerBlock) + (A.add ? 0 : ceil_div(A.V, A.rows_each));
+    if (blocks) k_embed_sums<T, O, PAST><<<block_grid(blocks), kBlock, 0, st>>>(A);
     TRON_HIP(hipGetLastError());
     if (A.tiles > 1) k_embed_join<O, PAST><<<block_grid(A.tile_units), kJoinWaves * kWave, 0, st>>>(A);
     TRON_HIP(hipGetLastError());
@@ -526,7 +536,9 @@ int tron_embed_grad(int64_t m, int64_t d, int64_t V, const void *ids, int id_byt
     TRON_HIP(hipGetLastError());
     const int tile = tile_of_places(m, d);
     const int64_t across = ceil_div(d, kColumns), tiles = ceil_div(m, tile);
-    const EmbedGradArgs A{sorted, dy, dtable, reinterpret_cast<float *>(w + S.shares), m, d, V, lddy, ldtable, across, tiles, tiles * across, tile, (float)scale, add != 0};
+    const int64_t row_bytes = d * (out_type == TRON_TYPE_F32 ? 4 : 2);
+    const int rows_each = (int)std::min<int64_t>(std::max<int64_t>(16384 / row_bytes, 1), kWave);
+    const EmbedGradArgs A{sorted, dy, dtable, reinterpret_cast<float *>(w + S.shares), m, d, V, lddy, ldtable, across, tiles, tiles * across, tile, rows_each, (float)scale, add != 0};
     return type == TRON_TYPE_F32 ? embed_grad_typed<float>(A, out_type, st)
            : type == TRON_TYPE_BF16 ? embed_grad_typed<__bf16>(A, out_type, st) : embed_grad_typed<_Float16>(A, out_type, st);
 }
