@@ -235,3 +235,23 @@ def test_reorder_between_the_halves_of_each_layer():
     assert torch.equal(both[:, 0], both[:, 1][:, at.flatten().long()])
     with pytest.raises(tron.TronError):
         tron.tron_beam_reorder(at, both[:, 1], both.view(3, 8, 5, 6)[:, 3:7])
+
+
+@pytest.mark.parametrize("dtype,bits", [("bf16", 0x7F81), ("bf16", 0xFFFF - 0x10000), ("f16", 0x7C01), ("f32", 0x7F800001)])
+def test_rows_with_one_nan_of_any_kind(dtype, bits):
+    """Signalling ones too, beside the largest values and before them: the row offers nothing, the others all."""
+    torch = torch_mod()
+    batch, beams, V, picks = 6, 5, 9001, 8
+    g = _gen(bits & 0xFFFF)
+    z = (4 * torch.randn(batch * beams, V, generator=g)).to(_dt(dtype))
+    words = z.view(torch.int32 if dtype == "f32" else torch.int16)
+    for i, row in enumerate(range(0, batch * beams, 3)):
+        words[row, (0, 1, 7, 8, 511, 2048, 4099, V - 1)[i % 8]] = bits
+        z[row, (1, 0, 6, 9, 510, 2049, 4098, V - 2)[i % 8]] = 60.0
+    assert int(torch.isnan(z).any(1).sum()) == 10
+    _check(z, torch.randn(batch, beams, generator=g), picks)
+    one = z[:beams].clone()
+    words = one.view(torch.int32 if dtype == "f32" else torch.int16)
+    words[:, 5] = bits
+    out = _check(one, torch.zeros(1, beams), picks)   # no row is left
+    assert bool(torch.isinf(out[0]).all()) and out[2].cpu().tolist() == [list(range(picks))]
