@@ -71,11 +71,13 @@ struct Chunk {
         end = d < kVec ? d : kVec;
     }
     __device__ __forceinline__ bool counts(int i) const { return i >= skip && i < end; }
-    template <typename T>
+    // behind a row of fewer than eight columns: 0, or (AGAIN) its first element once more
+    template <bool AGAIN = false, typename T>
     __device__ __forceinline__ Eight<T> of(const T *row) const
     {
         Eight<T> e;
-        e.set(end == kVec ? load8(row + at) : load_first(row + at, end, static_cast<T>(0.f)));
+        if (end == kVec) e.set(load8(row + at));
+        else e.set(load_first(row + at, end, AGAIN ? row[0] : static_cast<T>(0.f)));
         return e;
     }
     __device__ __forceinline__ void factors(float *f, const float *p, float none) const
@@ -329,11 +331,14 @@ struct LayerGradArgs {
     float inv_d;
 };
 
-// What a thread holds of a row
+// What a thread holds of a row.  Where dy does not count it is 0, and h, by which it is multiplied, has to be finite: a row of one large number times its rstd
+// passes 32 bits, so that 0 in the place of s gives (0 - mean) rstd = -inf.  A chunk that is not there has h = (0 - 0) 0; what lies behind a row of fewer than
+// eight columns, and what a last chunk skips, is an element of the row.
 template <typename T, int CH>
 struct HeldRow {
     Eight<T> s[CH], dy[CH], dt[CH];
     float mean, rstd;
+    float mean_of[CH], rstd_of[CH];   // 0 for a chunk that is not there
     __device__ __forceinline__ void load(const LayerGradArgs &A, int64_t row, int me, int team)
     {
         const T *sp = static_cast<const T *>(A.total) + row * A.lds, *dyp = static_cast<const T *>(A.dy) + row * A.lddy;
@@ -344,8 +349,10 @@ struct HeldRow {
         for (int c = 0; c < CH; ++c) {
             const Chunk k(me + c * team, (int)A.d);
             s[c] = dy[c] = Eight<T>{};
+            mean_of[c] = k.there ? mean : 0.f;
+            rstd_of[c] = k.there ? rstd : 0.f;
             if (!k.there) continue;
-            s[c] = k.of(sp);
+            s[c] = k.of<true>(sp);
             dy[c] = k.of(dyp);
             if (A.dtotal) dt[c] = k.of(dtp);
         }
@@ -390,7 +397,7 @@ __global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm_grad(La
             for (int w = 0; w < kWords; ++w) own.w[w] = now.dy[c].w[w] & counted[c][w];
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const float u = own.at(i), h = (now.s[c].at(i) - now.mean) * now.rstd, uh = u * h;
+                const float u = own.at(i), h = (now.s[c].at(i) - now.mean_of[c]) * now.rstd_of[c], uh = u * h;
                 along = fmaf(uh, g[c][i], along);
                 level = fmaf(u, g[c][i], level);
                 dg[c][i] += uh;
@@ -474,9 +481,10 @@ __global__ __launch_bounds__(1024) void k_layer_norm_grad_wide(LayerGradArgs A)
     const Elements<T> sv{static_cast<const T *>(A.total) + row * A.lds, d}, dyv{static_cast<const T *>(A.dy) + row * A.lddy, d};
     const Elements<T> dtv{static_cast<const T *>(A.dtotal) + (A.dtotal ? row * A.lddt : 0), d};
     const float mean = A.mean[row], rstd = A.rstd[row];
+    const T behind = sv.p[0];   // of the row, so that h is finite where dy is 0
     float along = 0.f, level = 0.f;
     for (int64_t j = (int64_t)threadIdx.x * kVec; j < d; j += step) {
-        const Raw8<T> s = sv.at(j), dy = dyv.at(j);
+        const Raw8<T> s = load_row8(sv.p, j, d, behind), dy = dyv.at(j);
         float g[kVec];
         gain8(g, A.gain, j, d);
 #pragma unroll

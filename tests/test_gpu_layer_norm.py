@@ -271,3 +271,25 @@ def test_layer_norm_grad_of_broadcast_rows_and_of_no_rows():
     assert (dg == 0).all() and (db == 0).all()
     tron.tron_layer_norm_grad(total[:0], mean[:0], rstd[:0], dx2[:0], dx[:0], dshift=dg2)
     assert (dg2 == 0).all()
+
+
+@pytest.mark.parametrize("with_gain", [False, True])
+@pytest.mark.parametrize("kind,value", [("f32", "lowest"), ("bf16", "lowest"), ("f32", 1e37), ("bf16", 1e37), ("f16", "lowest")])
+@pytest.mark.parametrize("d", [1, 5, 8, 40, 43, 127, 700, 705, 1024, 1280, 5000, 9001, 16384, 17001, 17008])
+def test_layer_norm_grad_of_rows_of_one_large_number(d, kind, value, with_gain):
+    """mean * rstd passes 32 bits, and h is 0: dx = rstd (a - mean a).  Rows of many lengths, so that lanes and elements have no column."""
+    torch = torch_mod()
+    m, dt, g = 7, _dt(kind), _gen(d)
+    total, dy, dtotal = _randn(g, m, d).to(dt), _randn(g, m, d).to(dt), _randn(g, m, d).to(dt)
+    total[1:6] = torch.finfo(dt).min if value == "lowest" else value
+    gain = (1.0 + 0.2 * _randn(g, d)).float() if with_gain else None
+    mean = total.double().mean(1)
+    rstd = ((total.double() - mean[:, None]).pow(2).mean(1) + 1e-5).rsqrt()
+    mean, rstd = mean.float(), rstd.float()
+    mean[1:6], rstd[1:6] = total[1:6, 0].float(), 1e-5 ** -0.5   # without the roundings of sums of such numbers
+    dx, off, dgain, off_g, dshift, off_b = _plain_grad(total, mean, rstd, gain, dy, dtotal)
+    got, dg, db = torch.empty((m, d), dtype=dt, device="cuda"), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    tron.tron_layer_norm_grad(total.cuda(), mean.cuda(), rstd.cuda(), dy.cuda(), got, gain=_cuda(gain), dtotal=dtotal.cuda(), dgain=dg, dshift=db)
+    _within(got, dx, U[kind] * dx.abs() + (1 + U[kind]) * off + TINY[kind], "dx")
+    _within(dg, dgain, off_g + TINY["f32"], "dgain")
+    _within(db, dshift, off_b, "dshift")
