@@ -332,13 +332,12 @@ struct LayerGradArgs {
 };
 
 // What a thread holds of a row.  Where dy does not count it is 0, and h, by which it is multiplied, has to be finite: a row of one large number times its rstd
-// passes 32 bits, so that 0 in the place of s gives (0 - mean) rstd = -inf.  A chunk that is not there has h = (0 - 0) 0; what lies behind a row of fewer than
-// eight columns, and what a last chunk skips, is an element of the row.
+// passes 32 bits, so that 0 in the place of s gives (0 - mean) rstd = -inf.  A chunk that is not there has rstd 0; what lies behind a row of fewer than eight columns,
+// as what a last chunk skips, is an element of the row.
 template <typename T, int CH>
 struct HeldRow {
     Eight<T> s[CH], dy[CH], dt[CH];
     float mean, rstd;
-    float mean_of[CH], rstd_of[CH];   // 0 for a chunk that is not there
     __device__ __forceinline__ void load(const LayerGradArgs &A, int64_t row, int me, int team)
     {
         const T *sp = static_cast<const T *>(A.total) + row * A.lds, *dyp = static_cast<const T *>(A.dy) + row * A.lddy;
@@ -349,8 +348,6 @@ struct HeldRow {
         for (int c = 0; c < CH; ++c) {
             const Chunk k(me + c * team, (int)A.d);
             s[c] = dy[c] = Eight<T>{};
-            mean_of[c] = k.there ? mean : 0.f;
-            rstd_of[c] = k.there ? rstd : 0.f;
             if (!k.there) continue;
             s[c] = k.of<true>(sp);
             dy[c] = k.of(dyp);
@@ -392,12 +389,13 @@ __global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm_grad(La
         float along = 0.f, level = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
+            const float rstd = Chunk(me + c * team, d).there ? now.rstd : 0.f;
             Eight<T> own;
 #pragma unroll
             for (int w = 0; w < kWords; ++w) own.w[w] = now.dy[c].w[w] & counted[c][w];
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const float u = own.at(i), h = (now.s[c].at(i) - now.mean_of[c]) * now.rstd_of[c], uh = u * h;
+                const float u = own.at(i), h = (now.s[c].at(i) - now.mean) * rstd, uh = u * h;
                 along = fmaf(uh, g[c][i], along);
                 level = fmaf(u, g[c][i], level);
                 dg[c][i] += uh;
