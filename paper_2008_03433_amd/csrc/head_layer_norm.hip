@@ -6,7 +6,7 @@
 // Both are bound by memory: every matrix is read or written once, and a row stays in the registers of a wavefront (narrow rows: no barriers) or
 // of a workgroup.  The mean is taken first and the squares are those of differences to it, so that rows that lie far from 0 keep the
 // digits of their variance: with m the mean rounded to 32 bits and c = s - m,  mean s = m + mean c  and  variance = mean c^2 - (mean c)^2.  mean c is what
-// the rounding of m and the order of its sum left; it is subtracted from c once more.
+// the rounding of m and the order of its sum left; it is subtracted from c once more.  Where it is most of c, sums are of 64 bits and of differences to the row's first element.
 //
 // Measured: 16384 x 8192 bf16 with a residual and its sum 200 us (1.07 GB, 5.37 TB/s: outputs past the caches); one row of 4096 to e4m3 4.7 us of the device's time,
 // 9.5 us a call; gradient of 16384 x 4096 bf16 with all its inputs 116 us, of which 5 us the columns' sums (537 MB, 4.9 TB/s beside them), of 30011 x 1023 f16
@@ -117,6 +117,19 @@ __device__ __forceinline__ void for_each(const V (&s)[CH][kVec], int me, int tea
     }
 }
 
+// f(value) for those that count
+template <int CH, typename F>
+__device__ __forceinline__ void for_each_there(const float (&s)[CH][kVec], int me, int team, int d, F f)
+{
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const Chunk k(me + c * team, d);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (k.counts(i)) f(s[c][i]);
+    }
+}
+
 // CH chunks of eight elements a thread; TEAM lanes a row (16: heads of a few dozen columns, 47454 x 69 bf16 by wavefronts 31 us for its gradient), 0: a
 // workgroup
 template <typename T, typename O, int CH, int TEAM, bool PAST>
@@ -125,6 +138,7 @@ __global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm(LayerAr
     constexpr bool kEight = sizeof(O) == 1, kWhole = __is_same(O, whole8);
     __shared__ float room[5 * kMostWaves];
     __shared__ double wide_room[3 * kMostWaves];
+    __shared__ float first_room;
     constexpr int kTeam = TEAM ? TEAM : kWave;
     const int team = TEAM ? TEAM : (int)blockDim.x, me = TEAM ? (int)threadIdx.x % kTeam : (int)threadIdx.x;
     const int64_t row = TEAM ? block_number() * (kTeamBlock / kTeam) + threadIdx.x / kTeam : block_number();
@@ -187,19 +201,31 @@ __global__ __launch_bounds__(TEAM ? kTeamBlock : 1024) void k_layer_norm(LayerAr
     } else {
         block_sum_two(left, sum2, room + kMostWaves);
     }
-    if (sum2 >= kLeastSquares && sum2 <= kMostSquares) {
-        const float inv_d = (float)A.inv_d;
-        M.rest = left * inv_d;
-        M.rstd = 1.f / sqrtf(fmaxf((sum2 - left * M.rest) * inv_d, 0.f) + (float)A.eps);
-    } else {   // in 64 bits where 32 have lost the range
+    // The squares' sum less what the mean's rounding has of it.  Where it has more than half (rows whose numbers differ in their last places, or not at all: 55 times 1e9
+    // kept 2^-24 of it, a variance of 2e-4), and where 32 bits have lost the range, the sums are of 64 bits, of differences to one of the row's own: a row of one
+    // number has the variance 0.
+    M.rest = left * (float)A.inv_d;
+    const float kept = sum2 - left * M.rest;
+    if (sum2 >= kLeastSquares && sum2 <= kMostSquares && kept >= 0.5f * sum2) {
+        M.rstd = 1.f / sqrtf(kept * (float)A.inv_d + (float)A.eps);
+    } else {
+        float first = s[0][0];
+        if (TEAM) {
+            first = __shfl(first, 0, kTeam);
+        } else {
+            if (me == 0) first_room = first;
+            __syncthreads();
+            first = first_room;
+        }
         double l = 0.0, l2 = 0.0;
-        for_each<CH>(s, me, team, d, [&](float v) {
-            l += (double)v;
-            l2 = fma((double)v, (double)v, l2);
+        for_each_there<CH>(s, me, team, d, [&](float v) {
+            const double u = (double)v - (double)first;
+            l += u;
+            l2 = fma(u, u, l2);
         });
         l = TEAM ? team_sum<kTeam>(l) : block_sum_all(l, wide_room + kMostWaves);
         l2 = TEAM ? team_sum<kTeam>(l2) : block_sum_all(l2, wide_room + 2 * kMostWaves);
-        M.rest = (float)(l * A.inv_d);
+        M.rest = (float)((double)first + l * A.inv_d);
         const double variance = (l2 - l * (l * A.inv_d)) * A.inv_d;
         M.rstd = (float)(1.0 / sqrt((variance < 0.0 ? 0.0 : variance) + A.eps));   // NaN stays NaN
     }

@@ -293,3 +293,35 @@ def test_layer_norm_grad_of_rows_of_one_large_number(d, kind, value, with_gain):
     _within(got, dx, U[kind] * dx.abs() + (1 + U[kind]) * off + TINY[kind], "dx")
     _within(dg, dgain, off_g + TINY["f32"], "dgain")
     _within(db, dshift, off_b, "dshift")
+
+
+@pytest.mark.parametrize("value", [1e5, 3e8, 1e9, -3.3e12, 1e20, 1e26, 1e30, "lowest"])
+@pytest.mark.parametrize("d", [1, 5, 41, 47, 55, 61, 82, 83, 97, 115, 128, 249, 509, 700, 1019, 1033, 1311, 4093, 8189, 8201, 32003, 33001])
+def test_layer_norm_of_rows_of_one_number_or_nearly(d, value):
+    """A row of one number has no variance, whatever its size and however its sum is rounded, and one of few numbers a unit of the last place apart has theirs.
+
+    The squares' sum is taken in 32 bits only where at least half of it is the variance: a relative error of 2 LOST each of the two parts that are subtracted, 6 LOST of the
+    variance, 3 LOST of the root.  Its mean is mended by the mean of c, off by 1.5 LOST sigma there, and by three roundings of |c| and of the first mean's error, 66 E |s|."""
+    torch = torch_mod()
+    value = torch.finfo(torch.float32).min if value == "lowest" else value
+    x = torch.full((6, d), value, dtype=torch.float32)
+    if d > 1:   # towards 0, so that the lowest one stays finite
+        one = torch.nextafter(x[0, 0], torch.tensor(0.0))
+        x[1, d // 2] = one
+        x[2, 0] = one
+        x[3, ::2] = one
+        x[4, : d - d // 3] = one
+    x[5] = torch.randn(d, generator=_gen(d))
+    shift = torch.randn(d, generator=_gen(d + 1))
+    s = x.double()
+    mean = s.mean(1, keepdim=True)
+    sigma = (s - mean).pow(2).mean(1, keepdim=True).sqrt()
+    rstd = (sigma * sigma + 1e-5) ** -0.5
+    h = (s - mean) * rstd
+    off_h = rstd * (1.5 * LOST * sigma + 3 * E * ((s - mean).abs() + 2 * 66 * E * s.abs())) + 3 * LOST * h.abs()
+    y, ms, rs = torch.empty((6, d), device="cuda"), torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+    tron.tron_layer_norm(x.cuda(), y, shift=shift.cuda(), eps=1e-5, mean=ms, rstd=rs)
+    _within(rs, rstd[:, 0], (3 * LOST + 4 * E) * rstd[:, 0], "rstd")
+    _within(y, h + shift.double(), off_h + 4 * E * (h.abs() + shift.double().abs()), "y")
+    assert torch.equal(y[0].cpu(), shift) and float(ms[0]) == float(x[0, 0])
+    _within(ms, mean[:, 0], 2 * E * mean[:, 0].abs() + 2 * LOST * sigma[:, 0], "mean")
