@@ -538,9 +538,9 @@ TRON_API int tron_distill_hv(int64_t m, int64_t V, int type, const void *z, int6
  * A step of a beam search over the head's logits.  Row r = item * beams + beam of z (batch * beams rows of V columns, of `type`: f32, bf16, f16)
  * belongs to a beam whose log-probabilities so far sum to score[r] (batch * beams floats):
  *   c_rv = score_r + (z_rv - log sum_u exp z_ru);
- * of an item's beams * V candidates the `picks` largest are taken, in falling order, ties to the lowest beam, then the lowest column:
+ * of an item's beams * V candidates the `picks` largest are taken, in falling order, ties to the lowest beam, then, of one beam, the largest z, then the lowest column:
  *   next_score: their c;  parent: their rows r;  token: their columns v   (batch x picks each, contiguous).
- * Candidates are compared in 64 bits, before the rounding to next_score, and those of one beam by their z.
+ * Candidates are compared in 64 bits, before the rounding to next_score, and those of one beam by their z, whose differences a score of any size may take.
  * ended (batch * beams bytes, or NULL): a beam whose byte is not 0 has one candidate, column `end` once more at its score, whatever its row of z
  * holds.  next_ended (batch x picks bytes, or NULL): whether the beam that goes on has ended, its parent before or by the column `end` (-1: there is none).
  * A probability of 0 (z = -inf) has c = -inf, and is taken behind all others, in the same order of beams and columns.  So are all candidates of a beam whose score

@@ -2,7 +2,7 @@
 //
 // Row r = item * beams + beam holds z, score_r the beam's sum of log-probabilities so far:
 //   lse_r = log sum_v exp z_rv,   c_rv = score_r + (z_rv - lse_r),
-// and the K largest c of an item's beams * V are taken, ties to the lowest beam, then the lowest token.
+// and the K largest c of an item's beams * V are taken, ties to the lowest beam, then its largest z, then the lowest token.
 //
 // Bound by reading z, once.  Within a row c grows with z, so a row offers its K largest z whatever its lse will be.  A first launch
 // reads the rows (or parts of them): every wavefront keeps a running maximum and sum a lane, and a list in LDS of what may be among the K
@@ -357,33 +357,36 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
 constexpr int kPickThreads = 256;
 constexpr int kRanked = kPickThreads;   // offers that are ranked, one a thread
 
-// Offers of an item: score in 64 bits, in order (0: none), beam and token.  The better one of two has the higher score, then the lower beam and token.
+// Offers of an item: score in 64 bits, in order (0: none), beam, z, in order (0 where it does not count), and token.  The better one of two has the higher score, then
+// the lower beam, the higher z and the lower token: a score of large size takes the differences of its beam's z, and they still decide.
 struct Offers {
     key_t64 *order;
-    uint32_t *token;
+    uint32_t *z, *token;
     int of_beam;   // offers a beam
-    __device__ __forceinline__ uint64_t place(int e) const { return (uint64_t)(e / of_beam) << 32 | token[e]; }
-    // thirteen digits of eight bits, the first ones of the score, the others of the place, the higher the better
+    // digits of eight bits, the first ones of the score, the higher the better
+    static constexpr int kDigits = 17;
     __device__ __forceinline__ unsigned digit(int e, int d) const
     {
-        return d < 8 ? (unsigned)(order[e] >> (56 - 8 * d)) & 255u : (unsigned)(~place(e) >> (32 - 8 * (d - 8))) & 255u;
+        return (d < 8 ? (unsigned)(order[e] >> (56 - 8 * d)) : d == 8 ? ~(unsigned)(e / of_beam) : d < 13 ? z[e] >> (96 - 8 * d) : ~token[e] >> (128 - 8 * d)) & 255u;
     }
 };
+constexpr int kOfferBytes = 16;
 
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 
-// count += a > b, the last word first: the borrow of b - a.  (Comparisons make two of each word, and of 64 bits take four times as long: 144 offers were
-// ranked in 9 us of a launch.)
-__device__ __forceinline__ void count_larger(int &count, const words4 &a, const words4 &b)
+// count += a > b, the last word, of a number's lowest bits, first: the borrow of b - a.  (Comparisons make two of each word, and of 64 bits take four times as long: 144
+// offers were ranked in 9 us of a launch.)
+__device__ __forceinline__ void count_larger(int &count, const words4 &a, uint32_t a_last, const words4 &b, uint32_t b_last)
 {
     uint32_t difference;
     asm("v_sub_co_u32_e32 %0, vcc, %2, %3\n\t"
         "v_subb_co_u32_e32 %0, vcc, %4, %5, vcc\n\t"
         "v_subb_co_u32_e32 %0, vcc, %6, %7, vcc\n\t"
         "v_subb_co_u32_e32 %0, vcc, %8, %9, vcc\n\t"
+        "v_subb_co_u32_e32 %0, vcc, %10, %11, vcc\n\t"
         "v_addc_co_u32_e32 %1, vcc, 0, %1, vcc"
         : "=&v"(difference), "+v"(count)
-        : "v"(b[0]), "v"(a[0]), "v"(b[1]), "v"(a[1]), "v"(b[2]), "v"(a[2]), "v"(b[3]), "v"(a[3])
+        : "v"(b_last), "v"(a_last), "v"(b[0]), "v"(a[0]), "v"(b[1]), "v"(a[1]), "v"(b[2]), "v"(a[2]), "v"(b[3]), "v"(a[3])
         : "vcc");
 }
 
@@ -413,12 +416,13 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     __shared__ uint32_t bound;
     __shared__ int found[2], survivors, left, chosen[kRanked];
     __shared__ __align__(16) uint32_t highs[kPickThreads];   // of the scores' bits
-    __shared__ words4 keys[kRanked + 32];                    // score and place as one number of 128 bits, the higher the better; 0 behind the last one
+    __shared__ words4 keys[kRanked + 32];                    // score, beam and z as one number, the higher the better; 0 behind the last one
+    __shared__ __align__(16) uint32_t lasts[kRanked + 32];   // and its last word, of the token
     const int64_t item = block_number();
     if (item >= A.batch) return;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, K = A.picks;
     const int of_beam = A.parts * K, count = A.beams * of_beam;
-    const Offers O{room, reinterpret_cast<uint32_t *>(room + count), of_beam};
+    const Offers O{room, reinterpret_cast<uint32_t *>(room + count), reinterpret_cast<uint32_t *>(room + count) + count, of_beam};
     const int64_t row0 = item * A.beams;
     const key_t64 early = threadIdx.x < count ? A.part_key[row0 * of_beam + threadIdx.x] : 0;   // under way while the sums are joined
     // a beam's parts lie in neighbouring lanes, a power of two of them
@@ -461,6 +465,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
         const double score = A.score[row], logit = of_order((uint32_t)(key >> 32));
         const double c = live ? score + (logit - lse[b]) : over && i == 0 ? score : -INFINITY;
         O.order[e] = there ? in_order(c) : 0;
+        O.z[e] = live ? (uint32_t)(key >> 32) : 0;
         O.token[e] = token;
     }
     __syncthreads();
@@ -496,7 +501,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
         taken = 0;
         int need = K, have = 0;
 #pragma unroll 1
-        for (int d = 0; d < 13; ++d) {
+        for (int d = 0; d < Offers::kDigits; ++d) {
             digits[threadIdx.x] = 0;
             __syncthreads();
 #pragma unroll 1
@@ -546,26 +551,32 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
     const int n = survivors;
     for (int i = threadIdx.x; i < kRanked + 32; i += kPickThreads) {
         words4 key = {0, 0, 0, 0};
+        uint32_t last = 0;
         if (i < n) {
             const int e = chosen[i];
             const key_t64 order = O.order[e];
-            key = words4{~O.token[e], ~(uint32_t)(e / of_beam), (uint32_t)order, (uint32_t)(order >> 32)};
+            key = words4{O.z[e], ~(uint32_t)(e / of_beam), (uint32_t)order, (uint32_t)(order >> 32)};
+            last = ~O.token[e];
         }
         keys[i] = key;
+        lasts[i] = last;
     }
     __syncthreads();
     // one, two or four threads an offer
     const int share = n <= kRanked / 4 ? 4 : n <= kRanked / 2 ? 2 : 1, mine = threadIdx.x / share;
     const words4 own = keys[mine];
+    const uint32_t own_last = lasts[mine];
     int rank = 0;
     if (mine < n) {
         const int some = ((n + share - 1) / share + 7) / 8 * 8, first = threadIdx.x % share * some;   // eights: share * some <= n + 32
         for (int i = first; i < first + some; i += 8) {
-            words4 other[8];
+            words4 other[8], last[2];
 #pragma unroll
             for (int k = 0; k < 8; ++k) other[k] = keys[i + k];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) count_larger(rank, other[k], own);
+            for (int k = 0; k < 2; ++k) last[k] = *reinterpret_cast<const words4 *>(lasts + i + 4 * k);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) count_larger(rank, other[k], last[k / 4][k % 4], own, own_last);
         }
     }
     if (share > 1) rank += __shfl_xor(rank, 1);
@@ -714,7 +725,9 @@ int tron_beam_select(int64_t batch, int64_t beams, int64_t V, int type, const vo
     else if (type == TRON_TYPE_BF16) launch_offers<__bf16>(A, S.waves, st);
     else launch_offers<_Float16>(A, S.waves, st);
     TRON_HIP(hipGetLastError());
-    k_beam_pick<<<block_grid(batch), kPickThreads, beams * S.parts * picks * 12, st>>>(A);
+    const int lds = (int)(beams * S.parts * picks) * kOfferBytes;   // 64 KB at most, beside 12 KB
+    if (lds > 48 << 10) TRON_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_beam_pick), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    k_beam_pick<<<block_grid(batch), kPickThreads, lds, st>>>(A);
     TRON_HIP(hipGetLastError());
     return TRON_OK;
 }

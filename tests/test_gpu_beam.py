@@ -255,3 +255,43 @@ def test_rows_with_one_nan_of_any_kind(dtype, bits):
     words[:, 5] = bits
     out = _check(one, torch.zeros(1, beams), picks)   # no row is left
     assert bool(torch.isinf(out[0]).all()) and out[2].cpu().tolist() == [list(range(picks))]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V,picks", [(100, 8), (100, 64), (2500, 20), (40000, 33)])
+def test_scores_that_take_the_differences_of_a_beams_logits(V, picks, kind):
+    """Where all candidates of a beam have one score in 64 bits, they go by their z: those that are taken and their order."""
+    torch = torch_mod()
+    z = torch.randn(4, V, generator=_gen(V + picks)).to(_dt(kind))
+    for score in (-1e30, 3e38, -3.4e38):
+        _check(z[:1], torch.tensor([[score]]), picks)
+        _check(z[:2], torch.tensor([[score], [-score]]), picks)
+        _check(z[:2], torch.tensor([[score, score]]), picks)
+        # a beam that has ended before one of them, and behind it
+        _check(z[:2], torch.tensor([[-1.0, score]]), picks, torch.tensor([[True, False]]), 1)
+        _check(z[:3], torch.tensor([[score, -1.0, score]]), picks, torch.tensor([[False, True, False]]), 1)
+    # ordinary scores, and logits that differ by less than the last place of theirs
+    tiny = (torch.randn(4, V, generator=_gen(V + 1)) * 1e-20).to(_dt(kind))
+    if kind != "f16":   # which has no such numbers
+        _check(tiny[:1], torch.tensor([[-3.0]]), picks)
+        _check(tiny, torch.tensor([[-3.0, -3.0], [-1.0, -1e30]]), picks)
+    # equal z among them: the lower column
+    steps = (torch.randint(0, 5, (2, V), generator=_gen(V + 2)).float()).to(_dt(kind))
+    _check(steps, torch.tensor([[1e30, 1e30]]), picks)
+
+
+def test_many_offers_of_scores_that_take_the_differences():
+    """More than are ranked at once: beam, z and column decide, digit by digit."""
+    torch = torch_mod()
+    g = _gen(5)
+    for z in (torch.randn(64, 300, generator=g), torch.randint(0, 3, (64, 300), generator=g).float(), torch.randn(64, 300, generator=g).half()):
+        _check(z, torch.full((1, 64), -1e30), 64)
+        few = torch.full((1, 64), -1e30)
+        few[0, :63] = -math.inf
+        few[0, 3] = -2e30
+        _check(z, few, 64)
+    # 64 of several beams, the first of which have fewer than that
+    z = torch.randn(64, 300, generator=g)
+    z[:, 10:] = -math.inf
+    _check(z, torch.full((1, 64), 1e30), 64)
+    _check(z[:, :20].contiguous(), torch.full((1, 64), 1e30), 64)
