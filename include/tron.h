@@ -545,7 +545,8 @@ TRON_API int tron_distill_hv(int64_t m, int64_t V, int type, const void *z, int6
  * holds.  next_ended (batch x picks bytes, or NULL): whether the beam that goes on has ended, its parent before or by the column `end` (-1: there is none).
  * A probability of 0 (z = -inf) has c = -inf, and is taken behind all others, in the same order of beams and columns.  So are all candidates of a beam whose score
  * is not finite (the beams that a first step has not), or whose row holds NaN, +inf or nothing but -inf.
- * beams and picks up to 64, picks <= beams V, V < 2^31 - 64.  Where picks = beams, next_score may be score and next_ended ended.
+ * beams and picks up to 64, picks <= beams V, V < 2^31 - 64.  Where picks = beams, next_score may be score and next_ended ended; all other overlaps of outputs with
+ * score, ended, the work space or each other are refused.
  */
 TRON_API int64_t tron_beam_select_work(int64_t batch, int64_t beams, int64_t V, int64_t picks);
 TRON_API int tron_beam_select(int64_t batch, int64_t beams, int64_t V, int type, const void *z, int64_t ldz, const float *score,

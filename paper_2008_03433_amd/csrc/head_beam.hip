@@ -673,6 +673,15 @@ void launch_offers(const BeamArgs &A, int waves, hipStream_t st)
     else k_beam_offers<T, 8><<<grid, 8 * kWave, 0, st>>>(A);
 }
 
+struct Range {
+    const void *p;   // or NULL: nothing
+    int64_t bytes;
+};
+bool meet(const Range &a, const Range &b)
+{
+    return a.p && b.p && static_cast<const char *>(a.p) < static_cast<const char *>(b.p) + b.bytes && static_cast<const char *>(b.p) < static_cast<const char *>(a.p) + a.bytes;
+}
+
 // whether `layers` ranges of a_bytes that lie a_layer apart, and the same of b, have no byte in common: one behind the other, or side by side in each layer
 bool apart(int64_t layers, const char *a, int64_t a_layer, int64_t a_bytes, const char *b, int64_t b_layer, int64_t b_bytes)
 {
@@ -711,6 +720,20 @@ int tron_beam_select(int64_t batch, int64_t beams, int64_t V, int type, const vo
     if (batch > 0 && !work_ok(work, work_bytes, tron_beam_select_work(batch, beams, V, picks))) {
         set_error("tron_beam_select: needs a work space of tron_beam_select_work(batch, beams, V, picks) bytes at a multiple of 16");
         return TRON_EINVAL;
+    }
+    // A workgroup writes an item's picks while others read their items' scores and flags: only where it writes over its own, and has read them, may they be the same
+    const int64_t of = batch * beams, go_on = batch * picks;
+    const Range in[3] = {{score, of * 4}, {ended, of}, {work, tron_beam_select_work(batch, beams, V, picks)}};
+    const Range out[4] = {{next_score, go_on * 4}, {next_ended, go_on}, {parent, go_on * 4}, {token, go_on * 4}};
+    for (int o = 0; o < 4; ++o) {
+        bool over = false;
+        for (int i = 0; i < 3; ++i) over = over || (meet(out[o], in[i]) && !(o == i && picks == beams && out[o].p == in[i].p));
+        for (int p = 0; p < o; ++p) over = over || meet(out[o], out[p]);
+        if (over) {
+            set_error("tron_beam_select: next_score, parent, token and next_ended may overlap neither score, ended, the work space nor each other, but next_score may be score and "
+                      "next_ended ended where picks = beams");
+            return TRON_EINVAL;
+        }
     }
     TRON_TRY(check_device());
     if (batch == 0) return TRON_OK;

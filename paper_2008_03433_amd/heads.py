@@ -297,7 +297,8 @@ def tron_beam_select_work(batch, beams, V, picks) -> int:
 
 def tron_beam_select(z, score, next_score, parent, token, ended=None, end=-1, next_ended=None, work=None, stream=None) -> None:
     """The step of a beam search: z (batch * beams x V) are the logits of beams with score (batch x beams); next_score, parent (rows of z) and token,
-    batch x picks each, are the picks of largest log-probability.  ended and next_ended: bool or uint8."""
+    batch x picks each, are the picks of largest log-probability.  ended and next_ended: bool or uint8.  next_score may be score, and next_ended ended, of as many picks
+    as beams."""
     lib = _load()
     call = _Call("tron_beam_select", z, stream)
     zp, rows, V, ldz = call.matrix(z, "z")

@@ -84,3 +84,14 @@ def test_tensors_on_the_host_are_refused():
         with pytest.raises(tron.TronError) as e:
             call(*args)
         assert "no CPU fallback" in str(e.value)
+
+
+def test_outputs_of_beams_over_what_others_read():
+    """score lies at 4096 (48 bytes), ended at 8192 (12), outputs of 5 picks of 3 items at 12288 and more; no address is used."""
+    def call(picks=5, next_score=12288, parent=16384, token=20480, next_ended=24576, work=65536):
+        p = ctypes.c_void_p
+        return ("tron_beam_select", 3, 4, 8, 0, p(131072), 8, p(4096), p(8192), 1, picks, p(next_score), p(parent), p(token), p(next_ended), p(work), 1 << 16, None)
+    for wrong in (dict(next_score=4096), dict(next_score=4096 + 44), dict(next_score=4096 - 56), dict(parent=4096), dict(token=4100), dict(next_ended=8192), dict(next_ended=8203),
+                  dict(next_ended=8192 - 14), dict(next_ended=4096), dict(next_score=8192), dict(picks=4, next_score=4100), dict(picks=4, next_score=4092), dict(picks=4, next_ended=8193),
+                  dict(picks=4, parent=4096), dict(picks=4, token=8192), dict(parent=20480), dict(token=12288 + 56), dict(next_ended=16384), dict(next_score=65536), dict(token=65536 + 16)):
+        _refused(*call(**wrong), text="overlap")
