@@ -642,6 +642,10 @@ int tron_layer_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, 
         set_error("tron_layer_norm: bad argument (x, y and, for 8 bits, scale are needed; rows that are written may not overlap)");
         return TRON_EINVAL;
     }
+    if (m > 1 && total && ((total == x && ldt != ldx) || (total == residual && ldt != ldr))) {
+        set_error("tron_layer_norm: total may be x or residual with the same leading dimension");
+        return TRON_EINVAL;
+    }
     TRON_TRY(check_device());
     if (m == 0) return TRON_OK;
     const LayerArgs A{x, residual, gain, shift, total, y, scale, mean, rstd, m, d, ldx, ldr, ldt, ldy, eps, 1.0 / (double)d};
@@ -667,6 +671,10 @@ int tron_layer_norm_grad(int64_t m, int64_t d, int type, const void *total, int6
     if (m > 0 && (!total || !mean || !rstd || !dy || !dx || !rows_ok(m, d, lds, false) || !rows_ok(m, d, lddy, false) || (dtotal && !rows_ok(m, d, lddt, false)) ||
                   !rows_ok(m, d, lddx, true) || !extent_ok(m, lds, d) || !extent_ok(m, lddy, d) || !extent_ok(m, dtotal ? lddt : 0, d) || !extent_ok(m, lddx, d))) {
         set_error("tron_layer_norm_grad: bad argument (total, mean, rstd, dy and dx are needed; the rows of dx may not overlap)");
+        return TRON_EINVAL;
+    }
+    if (m > 1 && ((dx == dy && lddx != lddy) || (dx == dtotal && lddx != lddt))) {
+        set_error("tron_layer_norm_grad: dx may be dy or dtotal with the same leading dimension");
         return TRON_EINVAL;
     }
     if ((dgain || dshift) && !work_ok(work, work_bytes, tron_layer_norm_grad_work(m, d))) {

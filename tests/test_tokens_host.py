@@ -95,3 +95,18 @@ def test_outputs_of_beams_over_what_others_read():
                   dict(next_ended=8192 - 14), dict(next_ended=4096), dict(next_score=8192), dict(picks=4, next_score=4100), dict(picks=4, next_score=4092), dict(picks=4, next_ended=8193),
                   dict(picks=4, parent=4096), dict(picks=4, token=8192), dict(parent=20480), dict(token=12288 + 56), dict(next_ended=16384), dict(next_score=65536), dict(token=65536 + 16)):
         _refused(*call(**wrong), text="overlap")
+
+
+def test_layer_norms_over_rows_at_other_places():
+    """In place only where each row lies over itself: otherwise workgroups write what others still read."""
+    p = ctypes.c_void_p
+
+    def call(x=P, ldx=8, residual=None, ldr=0, total=p(65536), ldt=8):
+        return "tron_layer_norm", 4, 8, 0, x, ldx, residual, ldr, None, None, 1e-5, total, ldt, 0, p(131072), 8, None, None, None, None
+    for wrong in (dict(total=P, ldt=9), dict(total=P, ldx=0), dict(residual=p(65536), ldr=0), dict(residual=p(65536), ldr=16)):
+        _refused(*call(**wrong), text="leading dimension")
+
+    def grad(dy=P, lddy=8, dtotal=p(8192), lddt=8, dx=p(65536), lddx=8):
+        return "tron_layer_norm_grad", 4, 8, 0, p(131072), 8, P, P, None, dy, lddy, dtotal, lddt, dx, lddx, None, None, None, 0, None
+    for wrong in (dict(dx=P, lddx=10), dict(dx=P, lddy=0), dict(dx=p(8192), lddt=0), dict(dx=p(8192), lddx=9)):
+        _refused(*grad(**wrong), text="leading dimension")
