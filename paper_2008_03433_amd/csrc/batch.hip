@@ -307,13 +307,6 @@ __global__ __launch_bounds__(kBlock, 2) void k_batch_pass(int64_t n, int64_t d, 
 // know which kernel ran.  Sums are formed in a fixed order (the instruction's, then tiles in order, wavefronts 0..3).
 typedef double mfma4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ void wave_lds_fence()
-{
-    // LDS operations of one wavefront complete in the order issued; this keeps the compiler from reordering them
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // the 64-bit value of lane `src` (per-lane index)
 __device__ __forceinline__ uint64_t lane_value(uint64_t v, int src)
 {

@@ -5,6 +5,14 @@
 
 namespace tron {
 
+// Between accesses of LDS by which lanes of one wavefront exchange values.  Its LDS operations complete in the order issued; this keeps the compiler, which
+// may order a lane's own accesses to different places as it likes, from reordering them.  No instruction comes of it.
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Cross-lane moves through the DPP data path (a few cycles) instead of ds_bpermute (an LDS round trip):
 //   0xB1 = quad_perm [1,0,3,2] (lane ^ 1), 0x4E = quad_perm [2,3,0,1] (lane ^ 2),
 //   0x141 = row_half_mirror (lane i <-> 7-i inside each group of 8), 0x140 = row_mirror (i <-> 15-i inside 16).

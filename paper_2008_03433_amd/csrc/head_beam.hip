@@ -112,6 +112,7 @@ template <int N>
 __device__ __forceinline__ uint32_t cut_to(key_t64 *list, int &count, int K, int lane)
 {
     uint32_t high[N], low[N];
+    wave_lds_fence();   // other lanes put keys here
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const key_t64 key = i * kWave + lane < count ? list[i * kWave + lane] : 0;
@@ -129,6 +130,7 @@ __device__ __forceinline__ uint32_t cut_to(key_t64 *list, int &count, int K, int
         least = reached_by(low, K - above, 0, exactly, [&](int i) { return high[i] == bound; });
     }
     count = 0;
+    wave_lds_fence();   // all have read theirs
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const bool keep = high[i] && (high[i] > bound || (high[i] == bound && low[i] >= least));
@@ -136,6 +138,7 @@ __device__ __forceinline__ uint32_t cut_to(key_t64 *list, int &count, int K, int
         if (keep) list[count + lanes_before(mask)] = (key_t64)high[i] << 32 | low[i];
         count += __popcll(mask);
     }
+    wave_lds_fence();
     return bound;
 }
 
@@ -280,6 +283,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
             static_assert(kEach <= kVec && kVec % kEach == 0, "neighbouring columns");
             uint64_t rest = some;
             int from_lane = 0;
+            wave_lds_fence();   // the ones before have been read
 #pragma unroll
             for (int q = 0; q < kLooked<WAVES>; ++q) {
                 const int l = rest ? __builtin_ctzll(rest) : 0;
@@ -293,6 +297,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
                 rest &= rest - 1;
             }
             some = rest;
+            wave_lds_fence();
             const int mine = lane % kAcross * kEach;   // first one of its columns
             Eight<T> w;
 #pragma unroll
@@ -315,6 +320,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
     }
     float all_most = wave_maxf(run.m);
     double total = wave_sum((double)run.s * (double)exp_of(run.m - base_of(all_most)));
+    wave_lds_fence();   // the list is read from here on
     if (WAVES > 1) {
         // one list of the wavefronts' keys that may be among the K, 64 of each at most
         if (count > kWave) cut<kMine>(list, count, K, lane);
@@ -339,7 +345,11 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void k_beam_offers(BeamArgs A)
         for (int read = count; read < keys;) {   // as many as a list holds at a time
             cut<kMine>(list, count, K, lane);
             const int more = keys - read < kMine - count ? keys - read : kMine - count;
-            for (int i = lane; i < more; i += kWave) list[count + i] = join[read + i];
+            for (int i = lane; i < more; i += kWave) {   // from later places to earlier ones
+                const key_t64 key = join[read + i];
+                wave_lds_fence();
+                list[count + i] = key;
+            }
             count += more;
             read += more;
         }

@@ -181,13 +181,16 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids
         // in the order of their lanes; the others all at once
         volatile uint8_t *mark = marks[wave];
         if (own) mark[k] = (uint8_t)lane;
+        wave_lds_fence();
         uint64_t twice = __ballot(own && mark[k] != lane);
         while (twice) {
             const int token = __builtin_amdgcn_readlane(k, __builtin_ctzll(twice));
             const uint64_t same = left & __ballot(k == token);
             const int at = counts[wave][token];
             if (same >> lane & 1) put(at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0)));
+            wave_lds_fence();   // all have read it
             if (lane == 0) counts[wave][token] = at + __popcll(same);
+            wave_lds_fence();
             left &= ~same;
             twice &= ~same;
         }
@@ -196,6 +199,7 @@ __global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const Id *ids
             put(at);
             counts[wave][k] = at + 1;
         }
+        wave_lds_fence();
     };
     if (own_here <= kMostFound) {
 #pragma unroll 1
