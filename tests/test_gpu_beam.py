@@ -295,3 +295,11 @@ def test_many_offers_of_scores_that_take_the_differences():
     z[:, 10:] = -math.inf
     _check(z, torch.full((1, 64), 1e30), 64)
     _check(z[:, :20].contiguous(), torch.full((1, 64), 1e30), 64)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,V,picks", [(1, 3000001, 64), (2, 1200007, 32)])
+def test_selection_over_millions_of_columns(rows, V, picks, kind):
+    torch = torch_mod()
+    z = (3.0 * torch.randn(rows, V, generator=_gen(V))).to(_dt(kind))
+    _check(z, -torch.rand(1, rows, generator=_gen(1)), picks)

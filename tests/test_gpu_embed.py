@@ -141,3 +141,36 @@ def test_embed_grad_is_the_gradient():
     tron.tron_embed(ids, direction, y, scale=1.3)
     left, right = (dtable.double() * direction.double()).sum(), (y.double() * dy.double()).sum()
     assert abs(float(left - right)) <= (m + 8) * E * float((y.double() * dy.double()).abs().sum())
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("m,d,V,frequent", [(20000, 24, 70000, (5, 261, 517)), (20000, 24, 70000, (255, 69887, 511, 5)), (65536, 9, 100, ()), (65536, 9, 700, (3, 259, 515)),
+                                            (30000, 5, 1500000, (7, 4103, 1499999)), (300, 8, 262144, ()), (300, 8, 262143, (262142,))])
+def test_embed_grad_of_several_frequent_tokens_of_a_workgroup(m, d, V, frequent, wide):
+    """Tokens of which one workgroup of the sort has several (equal modulo the number of workgroups), more often in a wavefront's ids than LDS keeps, one among the
+    other; and vocabularies of more workgroups than 256."""
+    torch = torch_mod()
+    g = _gen(m + V + len(frequent))
+    ids = torch.randint(0, V, (m,), generator=g)
+    if frequent:
+        often = torch.rand(m, generator=g) < 0.7
+        ids[often] = torch.tensor(frequent)[torch.randint(0, len(frequent), (m,), generator=g)][often]
+    ids[torch.rand(m, generator=g) < 0.05] = -1
+    if not wide:
+        ids = ids.to(torch.int32)
+    dy = _randn(g, m, d).float()
+    there = ids >= 0
+    at = ids[there].long()
+    want = torch.zeros(V, d, dtype=torch.float64).index_add_(0, at, dy[there].double())
+    size = torch.zeros(V, d, dtype=torch.float64).index_add_(0, at, dy[there].double().abs())
+    number = torch.bincount(at, minlength=V).double()[:, None]
+    table, again = torch.full((V, d), math.nan, device="cuda"), torch.empty((V, d), device="cuda")
+    tron.tron_embed_grad(ids.cuda(), dy.cuda(), table)
+    _within(table, want, (number + 2) * E * size + TINY["f32"], "dtable")
+    tron.tron_embed_grad(ids.cuda(), dy.cuda(), again)
+    assert torch.equal(again, table)
+    # rows that hold their own place: sums of whole numbers, exact in any order, which a wrong place would change
+    whole = torch.stack([torch.arange(m) % 1021, torch.arange(m) // 1021], 1).float()
+    table = torch.empty((V, 2), device="cuda")
+    tron.tron_embed_grad(ids.cuda(), whole.cuda(), table)
+    assert torch.equal(table.cpu().double(), torch.zeros(V, 2, dtype=torch.float64).index_add_(0, at, whole[there].double()))

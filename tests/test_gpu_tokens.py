@@ -348,3 +348,34 @@ def test_refusals():
     refused(tron.tron_embed_grad, ids, f, torch.zeros(9, 8, dtype=torch.int8, device="cuda"))
     refused(tron.tron_embed_grad, ids, f, v8.expand(9, 8))
     refused(tron.tron_embed_grad, ids, f, torch.zeros(9, 8, device="cuda"), work=small)
+
+
+def test_softmax_head_over_layer_norms_is_the_problem_of_its_features():
+    """Function, gradient and Hessian-vector product from the formulas on the features and logits that are there, as of the head over RMS norms."""
+    torch = torch_mod()
+    g = _gen(13)
+    m, d, V, K, C, T = 90, 70, 33, 4, 2.0, 1.5
+    hidden, residual = (_randn(g, m, d) + _randn(g, m, 1)).bfloat16(), _randn(g, m, d).bfloat16()
+    gain, shift = (1 + 0.1 * _randn(g, d)).float(), (0.1 * _randn(g, d)).float()
+    ids, t, weight = torch.randint(0, V, (m, K), generator=g), _randn(g, m, K).float(), torch.rand(m, generator=g) + 0.5
+    W, D = (_randn(g, V, d) / 8).bfloat16().float(), (_randn(g, V, d) / 8).bfloat16().float()   # exact in the products' type
+    head = tron.SoftmaxHead(hidden.cuda(), ids.cuda(), t.cuda(), gain=gain.cuda(), residual=residual.cuda(), temperature=T, weight=weight.cuda(), eps=1e-5, norm="layer",
+                            shift=shift.cuda())
+    G, HD = torch.empty(V, d, device="cuda"), torch.empty(V, d, device="cuda")
+    f = head.fun_grad(C, W.cuda(), G)
+    X = head.X.double().cpu()
+    _, _, _, y, _, _, off = _layer_plain(hidden, residual, gain, shift, 1e-5)
+    _within(X, y, U["bf16"] * y.abs() + 1.01 * off + TINY["bf16"], "features")
+    z = head.z.cpu()
+    _within(z, X @ W.double().T, U["bf16"] * (X @ W.double().T).abs() * 1.01 + (d + 8) * 2 * E * (X.abs() @ W.double().abs().T), "logits")
+    loss, _, dz, p, _, w = _distill_plain(z, ids, t, T, weight)
+    want = 0.5 * float((W.double() ** 2).sum()) + C * float(loss.sum())
+    assert abs(f - want) <= 1e-5 * abs(want)
+    # dz is rounded to bf16 (and computed to 2^-16 of p)
+    _within(G, W.double() + C * dz.T @ X, C * ((U["bf16"] + 2.0 ** -10) * dz.abs() + 2.0 ** -15 * w * T * p).T @ X.abs() + 1e-6, "gradient")
+    head.hv(C, D.cuda(), HD)
+    u = X @ D.double().T
+    h = w * (p * u - p * (p * u).sum(1, keepdim=True))
+    # u is rounded to bf16 before, H u after
+    off = w * p * (u.abs() + (p * u.abs()).sum(1, keepdim=True)) * (U["bf16"] + 2.0 ** -10) + h.abs() * U["bf16"]
+    _within(HD, D.double() + C * h.T @ X, C * off.T @ X.abs() + 1e-6, "Hessian-vector product")
