@@ -303,3 +303,36 @@ def test_selection_over_millions_of_columns(rows, V, picks, kind):
     torch = torch_mod()
     z = (3.0 * torch.randn(rows, V, generator=_gen(V))).to(_dt(kind))
     _check(z, -torch.rand(1, rows, generator=_gen(1)), picks)
+
+
+def test_more_rows_than_a_dimension_of_a_launch():
+    torch = torch_mod()
+    rows, V = 70001, 100
+    z, score = torch.randn(rows, V, generator=_gen(9)).bfloat16(), -torch.rand(rows, 1, generator=_gen(10))
+    out = (torch.empty((rows, 2), device="cuda"), torch.empty((rows, 2), dtype=torch.int32, device="cuda"), torch.empty((rows, 2), dtype=torch.int32, device="cuda"))
+    tron.tron_beam_select(z.cuda(), score.cuda(), *out)
+    best, at = torch.sort(z.double(), dim=1, descending=True, stable=True)
+    assert torch.equal(out[1].cpu(), torch.arange(rows, dtype=torch.int32)[:, None].expand(rows, 2)) and torch.equal(out[2].cpu().long(), at[:, :2])
+    want = score.double() + best[:, :2] - torch.logsumexp(z.double(), 1)[:, None]
+    assert float(((out[0].double().cpu() - want).abs() - LSE - 1.01 * E * want.abs()).max()) <= 0
+
+
+def test_the_most_offers_in_a_graph():
+    """64 beams with 64 picks: the workgroups that join them have more LDS than others."""
+    torch = torch_mod()
+    z, score = torch.randn(2 * 64, 700, generator=_gen(11)).cuda(), -torch.rand(2, 64, generator=_gen(12)).cuda()
+    new = lambda dtype: torch.zeros((2, 64), dtype=dtype, device="cuda")  # noqa: E731
+    want, out = [(new(torch.float32), new(torch.int32), new(torch.int32)) for _ in range(2)]
+    tron.tron_beam_select(z, score, *want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tron.tron_beam_select(z, score, *out)
+    for _ in range(3):
+        for t in out:
+            t.zero_()
+        tron.tron_beam_select(z, score, *want)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out))
