@@ -411,8 +411,8 @@ TRON_API int tron_probe_copy_bandwidth(double *dst_dev, const double *src_dev, i
  * tron_..._work says its bytes; it lies at a multiple of 16, its contents are undefined before and after, and calls on
  * different streams need different ones.  Outputs may not overlap inputs except where it is said.
  * Sums, softmax statistics and activations are held in 32 bits or more (gelu and silu are off by a dozen units of their
- * last place at most, or by 2^-120); results are rounded once to the output's type, to nearest, ties to even.  No atomics:
- * the same call gives the same bits.
+ * last place at most, or by 2^-120); results are rounded once to the output's type, to nearest, ties to even.  No atomics
+ * decide an order or a sum: the same call gives the same bits.
  * ------------------------------------------------------------------------------------------ */
 enum {
     TRON_TYPE_F32 = 0,
@@ -452,7 +452,8 @@ TRON_API int tron_rms_norm_grad(int64_t m, int64_t d, int type, const void *tota
 /*
  * Layer norm with the residual's addition:
  *   s = x + residual;  mean = mean_j s_j;  rstd = (mean_j (s_j - mean)^2 + eps)^-1/2;  y = (s - mean) rstd gain + shift.
- * As tron_rms_norm; shift: d floats, or NULL for 0; mean: m floats or NULL.  Rows that lie far from 0 have the variance of their differences to the mean.
+ * As tron_rms_norm; shift: d floats, or NULL for 0; mean: m floats or NULL.  Rows that lie far from 0 have the variance of their differences to the mean,
+ * and a row of one number has none; the differences themselves have to lie in the range of 32 bits.
  */
 TRON_API int tron_layer_norm(int64_t m, int64_t d, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
                              const float *gain, const float *shift, double eps, void *total, int64_t ldt, int out_type, void *y,
@@ -544,7 +545,7 @@ TRON_API int tron_distill_hv(int64_t m, int64_t V, int type, const void *z, int6
  * ended (batch * beams bytes, or NULL): a beam whose byte is not 0 has one candidate, column `end` once more at its score, whatever its row of z
  * holds.  next_ended (batch x picks bytes, or NULL): whether the beam that goes on has ended, its parent before or by the column `end` (-1: there is none).
  * A probability of 0 (z = -inf) has c = -inf, and is taken behind all others, in the same order of beams and columns.  So are all candidates of a beam whose score
- * is not finite (the beams that a first step has not), or whose row holds NaN, +inf or nothing but -inf.
+ * is not finite, ended or not (the beams that a first step has not), or whose row holds NaN, +inf or nothing but -inf.
  * beams and picks up to 64, picks <= beams V, V < 2^31 - 64.  Where picks = beams, next_score may be score and next_ended ended; all other overlaps of outputs with
  * score, ended, the work space or each other are refused.
  */

@@ -13,7 +13,7 @@
 // The sum is the more exact the more rows are compared by it: exponents are products with log2(e) in two parts, lanes' sums are joined in 64 bits,
 // scores are compared in 64 bits.
 //
-// Measured: 64 items of 8 beams over 128000 bf16, 16 picks: 39 us the rows (118 MB that are read, 3.0 TB/s; the vector units are busy two thirds of the cycles), 6 us
+// Measured: 64 items of 8 beams over 128000 bf16, 16 picks: 39.5 us the rows (118 MB that are read, 3.0 TB/s; the vector units are busy two thirds of the cycles), 6.5 us
 // the joining; 2 layers of 129 x 128 bf16 states of 512 rows 9.6 us (50 MB, 5.2 TB/s).  One item of 4 beams over 32000 f32: 8 + 4 us.
 #include "head_util.h"
 
@@ -73,7 +73,7 @@ __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f 
 __device__ __forceinline__ float exp_of(float d) { return exp2_(fmaf(d, 1.44269502f, d * 1.925963e-8f)); }
 
 // The largest of three, one instruction: fmaxf first makes a quiet NaN of an argument that may be another one, as bits shifted to a float may (bf16: 46
-// instructions for 32 columns, 12 so; 512 rows of 128000 with 16 picks 46.6 -> 44.9 us).  A NaN may hide the others here: its row has no candidates.
+// instructions for 32 columns, 12 so; 512 rows of 128000 with 16 picks, both launches on fresh logits, 48.6 us by fmaxf, 47.5 us so).  A NaN may hide the others here: its row has no candidates.
 __device__ __forceinline__ float top3(float a, float b, float c)
 {
     float m;
@@ -466,7 +466,9 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs A)
         const int b = e / of_beam, i = e - b * of_beam;
         const int64_t row = item * A.beams + b;
         const bool live = kind[b] == LIVE, over = kind[b] == OVER;
-        // one condition after the other: of a choice of three in one, the compiler (ROCm 7.2) leaves the last one's token undefined
+        // One condition after the other.  Of a choice of three in one the compiler makes a switch, and of its default, which lanes of two branches reach (kinds below and
+        // above the ones named), ROCm 7.2 sets the token in one branch alone: the optimized intermediate code has the value for all, the machine code not for
+        // kind 2, also where this loop is compiled by itself.  There is no switch in this file's intermediate code.
         key_t64 key = 1;
         if (live) key = e == (int)threadIdx.x ? early : A.part_key[row * of_beam + i];
         const uint32_t other = over ? i == 0 ? (uint32_t)A.end : (uint32_t)(i - (i <= A.end)) : (uint32_t)i;   // columns in order, behind `end` where it is first
@@ -655,7 +657,12 @@ struct Split {
 };
 
 // Wavefronts a workgroup by the row's length, so that each has two turns or more where it can; parts of a row where there are fewer rows than 512, which are
-// resident at once.  512 rows of 128000 bf16 41 us so, 57 us by four wavefronts, 45 and 54 us in two and four parts.
+// resident at once.  us of both launches, 8 beams, 16 picks, fresh logits.
+//   By eight, four and one wavefronts: 512 rows of 128000 bf16 47, 62, 197; 64 rows 26, 26, 62; 512 of 32000 f32 28.5, 30, 77; 2048 of 32000 bf16 65, 52, 96; 2048 of 6000
+//   49, 29, 34.  Long rows of few items want eight; many shorter rows would do better by four.
+//   Whole rows, and in parts by the rule (or, from 512 rows on, in two): 128000 bf16 64 rows 32, 26; 256 rows 35, 37; 304 rows 42, 46; 400 rows 44, 54; 512 rows 47, 56; 520 rows 58,
+//   61; 768 rows 68, 74; 1024 rows 77, 92; 2048 rows 133, 161.  32000 f32 64 rows 18.6, 20; 256 rows 22, 26; 400 rows 27, 34; 512 rows 28.5, 36; 768 rows 40, 47.  Parts gain where
+//   rows are long and few; from 256 to 511 rows, and of 32000 columns, whole rows would be faster by 5 to 25%.
 Split split_of(int64_t rows, int64_t beams, int64_t V, int64_t picks)
 {
     const int64_t turns = ceil_div(V, kTurn);

@@ -3,13 +3,15 @@
 //   y_i = scale row_scale[id_i] table[id_i];      dtable_v = scale sum_{i: id_i = v} dy_i  (+ dtable_v)
 //
 // The lookup is bound by reading the rows of the tokens and writing y.  The gradient is bound by reading dy once and writing the table; its
-// sums are those of the rows of equal tokens in the order of their places, whatever the tokens are, so that the same call gives the same bits.
+// sums are those of the rows of equal tokens in the order of their places, so that the same call gives the same bits.  Where a token's sum is cut depends on all ids: other
+// tokens' number moves its places over the tiles' borders.
 // Three launches: tokens are sorted (k_sort_tokens); the sorted places are cut into tiles of equal length, whatever tokens they hold, so that a frequent
 // token is many tiles' work, and a wavefront sums a tile's rows over 512 columns and stores those tokens that lie in its tile alone
 // (k_embed_sums, whose further workgroups fill the rows of tokens that are not there); the others' shares are joined (k_embed_join).
 //
-// Measured: 32768 tokens of 4096 bf16, a table of 128000 rows in f32: 15 us the sort, 405 us the sums and rows of zeros (2.35 GB, 5.8 TB/s), 9 us the joining,
-// 463 us a call; 9001 of 511 f16, 50021 rows: 7 + 16 + 5 us; lookup of 8 rows of 4096 i8 2.9 us.
+// Measured: 32768 tokens of 4096 bf16, a table of 128000 rows in f32: 15 us the sort, 402 us the sums and rows of zeros (2.35 GB, 5.8 TB/s), 10 us the joining,
+// 461 us a call; 9001 of 511 f16, 50021 rows: 8 + 16 + 5 us; lookup of 8 rows of 4096 i8 3 us, of 32768 rows of 4096 bf16 94 us (4.7 TB/s).  Every workgroup of the sort reads all
+// ids, so that many take it long: 32768, 262144 and 1000000 tokens of 1024 bf16 15 + 117 + 9, 170 + 238 + 14 and 701 + 557 + 16 us.
 #include "head_util.h"
 
 namespace tron {

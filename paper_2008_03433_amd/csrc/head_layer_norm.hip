@@ -8,9 +8,9 @@
 // digits of their variance: with m the mean rounded to 32 bits and c = s - m,  mean s = m + mean c  and  variance = mean c^2 - (mean c)^2.  mean c is what
 // the rounding of m and the order of its sum left; it is subtracted from c once more.  Where it is most of c, sums are of 64 bits and of differences to the row's first element.
 //
-// Measured: 16384 x 8192 bf16 with a residual and its sum 200 us (1.07 GB, 5.37 TB/s: outputs past the caches); one row of 4096 to e4m3 4.7 us of the device's time,
-// 9.5 us a call; gradient of 16384 x 4096 bf16 with all its inputs 116 us, of which 5 us the columns' sums (537 MB, 4.9 TB/s beside them), of 30011 x 1023 f16
-// 52 us, of which 7 us these sums (184 MB).  Rows at odd places cost nothing by themselves (30011 x 1024 f16 in rows of 1025: 3% more).
+// Measured: 16384 x 8192 bf16 with a residual and its sum 190 us (1.07 GB, 5.6 TB/s: outputs past the caches), to e4m3 203 us, to whole numbers 194 us; one row of 4096 to e4m3
+// 4.6 us of the device's time, 9.2 us a call; gradient of 16384 x 4096 bf16 with all its inputs 116 us, of which 5 us the columns' sums (537 MB, 4.8 TB/s beside them), of
+// 30011 x 1023 f16 52 us, of which 7 us these sums (184 MB).  Rows at odd places cost nothing by themselves (30011 x 1024 f16 in rows of 1025: 3% more).
 #include "head_rows.h"
 
 namespace tron {

@@ -14,8 +14,8 @@
 // Many rows are bound by the matrix units and what feeds them: 8192 x 32000 x 4096 bf16 1.70 ms, 1262 TFLOP/s; the units are busy 57% of the cycles of a
 // clock that falls to 2.0 GHz under them.  Without the fetches the same loop runs at 1500 to 1600 TFLOP/s.  Few rows are bound by reading w: one
 // row of 32000 x 4096 bf16 55 us, 4.8 TB/s.  In between the way to memory and the launch count: 777 x 1001 x 2049 f16 23 us.
-// Whole numbers of 8 bits take the same bytes a step and twice the inner index: 8192 x 8192 x 4096 with silu 287 us, 1915 TOP/s; eight rows of
-// 32000 x 4096 33 us, 4.0 TB/s; 515 x 1003 x 2051 20 us.
+// Whole numbers of 8 bits take the same bytes a step and twice the inner index: 8192 x 8192 x 4096 with silu 292 us, 1880 TOP/s; eight rows of
+// 32000 x 4096 32.5 us, 4.0 TB/s; 515 x 1003 x 2051 20 us.
 #include <type_traits>
 
 #include "head_util.h"
